@@ -464,6 +464,85 @@ AFLEX_API aflex_status aflex_rope_append(aflex_ctx* ctx, const aflex_attn_desc* 
                                          const aflex_kv* kv, int batch, const void* w_q_norm, const void* w_k_norm,
                                          float rms_eps, float rope_theta, void* q_out, void* stream);
 
+/* ---- Page-sparse decode attention ----------------------------------------------------------
+ *
+ * Decode attention is bound by reading the whole KV cache for every token (the paper's Sections 1-2); on long contexts most
+ * of that weight goes to few tokens.  These operators let a decode step read a chosen part: every cache page keeps bounds
+ * of its keys, a page is scored by how large a product with the row's queries the bounds allow, and attention reads the
+ * best pages only (no counterpart in the paper; the operators' definitions are below).  A step is
+ *     aflex_rope_append_bounds  ->  aflex_page_select  ->  aflex_attn_decode_pages
+ * in the place of aflex_rope_append -> aflex_attn_decode; with top_pages >= the pages of every sequence the two agree.
+ *
+ * Rows.  With q_offsets == NULL there is one row per sequence, the token being decoded at position seq_lens[b] - 1
+ * (rows == batch).  With q_offsets (DEVICE i32 [batch + 1], starting at 0, not decreasing) row q_offsets[b] + i is token i
+ * of the last m = q_offsets[b+1] - q_offsets[b] tokens of sequence b, at position seq_lens[b] - m + i: drafted tokens to
+ * verify, or a prompt chunk.  m = 0 is allowed.  `rows` is the number of rows the tensors have; rows from q_offsets[batch] on
+ * are padding and neither read nor written.  seq_lens counts all of the call's tokens.  A sequence whose length is outside
+ * [1, 16 * max_pages_per_seq] or shorter than m raises AFLEX_ERR_BOUNDS in the status word.
+ *
+ * Key bounds of page P and KV head g, over the tokens stored in the page so far (NaN ignored; a channel without any number
+ * counts as 0):  hi_d = max_j K_j[d],  lo_d = min_j K_j[d];  per block c of 32 channels, with a the largest magnitude among
+ * the block's hi and lo, e_c is the smallest integer with a <= 127 * 2^e_c, clamped to [-60, 50] (-60 for a = 0), and
+ *     HI_d = ceil(hi_d / 2^e_c),  LO_d = floor(lo_d / 2^e_c),  both clamped to [-127, 127]
+ *   codes  i8 [num_pages][Hkv][D / 8][2][8]   for channels 8 i .. 8 i + 7: the eight HI, then the eight LO
+ *   scales u8 [num_pages][Hkv][D / 32]        e_c + 127
+ * (2 D + D / 32 bytes beside the page's 64 D bytes of K and V).  They depend on the stored keys alone, not on how many calls
+ * stored them.  Bounds of pages that no call has made yet must not be selected from.
+ */
+typedef struct { int8_t* codes; uint8_t* scales; } aflex_key_bounds;
+
+/* Which pages a row reads: all of them while it sees at most top_pages; otherwise the first sink_pages, the last
+ * window_pages (the row's own page among them) and the best-scored others, top_pages in all.
+ * sink_pages >= 0, window_pages >= 1, sink_pages + window_pages <= top_pages. */
+typedef struct { int top_pages, sink_pages, window_pages; } aflex_page_policy;
+
+/*
+ * The q / k / v step of the decoder layer on qkv bf16 [rows][(Hq + 2 Hkv) * D] (as aflex_rope_append: optional head norms,
+ * rotary embedding, q_out bf16 [rows][Hq][D], K/V cache slots of the rows' tokens written), and the key bounds of every page
+ * that received a token.  Keys are formed in fp64 and rounded to fp32, then bf16; queries in fp32.  No page may receive tokens of two
+ * sequences.  A bad page id raises AFLEX_ERR_BOUNDS and skips that page's writes.
+ */
+AFLEX_API aflex_status aflex_rope_append_bounds(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* qkv, const aflex_kv* kv,
+                                                const aflex_key_bounds* bounds, int batch, const int32_t* q_offsets, int rows,
+                                                const void* w_q_norm, const void* w_k_norm, float rms_eps, float rope_theta,
+                                                void* q_out, void* stream);
+
+/*
+ * The key bounds of pages that another call filled (aflex_prefill_layers, aflex_rope_append, a copied cache): every page of
+ * every sequence that holds a token at position first_token[b] or later (first_token: DEVICE i32 [batch], NULL = all pages).
+ * v_cache is not read (any non-null pointer).  Sequences may share full pages; a sequence of length 0 has none.
+ */
+AFLEX_API aflex_status aflex_page_bounds(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_kv* kv,
+                                         const aflex_key_bounds* bounds, int batch, const int32_t* first_token, void* stream);
+
+/*
+ * Page selection per (row, KV head).  q bf16 [rows][Hq][D] (rotated).  Score of a page for query head h, per block c of 32
+ * channels: f_c from the block's largest |q_d| by the rule of e_c above, Q_d = q_d / 2^f_c rounded to the nearest integer
+ * (halves to even; NaN counts as 0; within [-127, 127]), i_c = sum_d Q_d (HI_d if Q_d > 0, else LO_d), v_c = i_c 2^e_c 2^f_c, and
+ * s_h = ((v_0 + v_1) + v_2) + v_3 in fp32 (D = 64: v_0 + v_1).  A page's score is the largest s_h of the group's heads; of
+ * equal scores the lower page goes first.  Every step but the fp32 additions is exact, so the result is the same bit for bit
+ * on every run and for every way the work is split.
+ *   page_list  i32 [rows][Hkv][top_pages]  page indices within the sequence, ascending; -1 behind the last
+ *   page_count i32 [rows][Hkv]             number of pages listed
+ * A row without a valid length gets count 0.  max_pages_per_seq up to 393216 (6.3 M tokens); otherwise UNSUPPORTED.
+ */
+AFLEX_API aflex_status aflex_page_select(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,
+                                         const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch,
+                                         const int32_t* q_offsets, int rows, int32_t* page_list, int32_t* page_count, void* stream);
+
+/*
+ * Attention of every row over the tokens, up to its own, of the pages listed for it and its KV head (the first
+ * page_count entries of its list, from aflex_page_select or the caller's own, in any order):
+ *     s_j = sm_scale * <q, K_j>,  out = sum_j softmax(s)_j V_j -> bf16,  lse = ln sum_j exp(s_j)
+ * A page that is listed twice counts twice.  An entry outside the pages the row sees, or with a bad page id, is left out
+ * and raises AFLEX_ERR_BOUNDS.  With nothing to attend to out is 0 and lse -infinity.  fp32 scores and sums; P enters the
+ * second product as the sum of two bf16 values.  out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  No workspace.
+ * Deterministic run to run.
+ */
+AFLEX_API aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,
+                                               const int32_t* page_list, const int32_t* page_count, int top_pages, int batch,
+                                               const int32_t* q_offsets, int rows, void* out, float* lse, void* stream);
+
 /* ---- Host-side decisions of the data plane and the DVFS controller ------------------------
  *
  * Pure host computation on HOST pointers: nothing is launched and no GPU setting is read or

@@ -27,6 +27,7 @@ EXPORTS = (
     "aflex_trace_read", "aflex_attn_decode_static", "aflex_attn_decode_static_status", "aflex_decoder_layers", "aflex_decoder_workspace_bytes",
     "aflex_add_rmsnorm", "aflex_rope_append", "aflex_attn_prefill", "aflex_af_decoder_layers", "aflex_af_workspace_bytes",
     "aflex_prefill_layers", "aflex_prefill_workspace_bytes",
+    "aflex_rope_append_bounds", "aflex_page_bounds", "aflex_page_select", "aflex_attn_decode_pages",
     "aflex_eq2_layer_time", "aflex_curve_eval",
     "aflex_pipeline_makespan", "aflex_plan_microbatches", "aflex_dvfs_window", "aflex_dvfs_decode_step",
     "aflex_dvfs_prefill_pair",
@@ -42,6 +43,14 @@ class KV(ctypes.Structure):
     _fields_ = [("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
                 ("page_table", ctypes.c_void_p), ("max_pages_per_seq", ctypes.c_int),
                 ("seq_lens", ctypes.c_void_p), ("seq_lens_host", ctypes.c_void_p)]
+
+
+class KeyBounds(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class PagePolicy(ctypes.Structure):
+    _fields_ = [("top_pages", ctypes.c_int), ("sink_pages", ctypes.c_int), ("window_pages", ctypes.c_int)]
 
 
 class LayerDesc(ctypes.Structure):
@@ -160,6 +169,16 @@ def load_library() -> ctypes.CDLL:
     lib.aflex_rope_append.restype = ci
     lib.aflex_rope_append.argtypes = [vp, ctypes.POINTER(AttnDesc), vp, ctypes.POINTER(KV), ci, vp, vp,
                                       ctypes.c_float, ctypes.c_float, vp, vp]
+    lib.aflex_rope_append_bounds.restype = ci
+    lib.aflex_rope_append_bounds.argtypes = [vp, ctypes.POINTER(AttnDesc), vp, ctypes.POINTER(KV), ctypes.POINTER(KeyBounds), ci, vp,
+                                             ci, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp]
+    lib.aflex_page_bounds.restype = ci
+    lib.aflex_page_bounds.argtypes = [vp, ctypes.POINTER(AttnDesc), ctypes.POINTER(KV), ctypes.POINTER(KeyBounds), ci, vp, vp]
+    lib.aflex_page_select.restype = ci
+    lib.aflex_page_select.argtypes = [vp, ctypes.POINTER(AttnDesc), vp, ctypes.POINTER(KV), ctypes.POINTER(KeyBounds),
+                                      ctypes.POINTER(PagePolicy), ci, vp, ci, vp, vp, vp]
+    lib.aflex_attn_decode_pages.restype = ci
+    lib.aflex_attn_decode_pages.argtypes = [vp, ctypes.POINTER(AttnDesc), vp, ctypes.POINTER(KV), vp, vp, ci, ci, vp, ci, vp, vp, vp]
     cd, dp, ip = ctypes.c_double, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)
     lib.aflex_eq2_layer_time.restype = cd
     lib.aflex_eq2_layer_time.argtypes = [cd, cd, cd, ci]
@@ -196,6 +215,11 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
+def _stream_of(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
+    """The given stream, or the current one of the tensor's device."""
+    return (stream or torch.cuda.current_stream(t.device)).cuda_stream
+
+
 def attn_desc(num_q_heads: int, num_kv_heads: int, head_dim: int, sm_scale: float = 0.0) -> AttnDesc:
     return AttnDesc(num_q_heads, num_kv_heads, head_dim, 16, sm_scale)
 
@@ -213,6 +237,21 @@ def make_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tens
         kv.seq_lens_host = _ptr(seq_lens_host)
     kv._keep = (k_cache, v_cache, page_table, seq_lens, seq_lens_host)
     return kv
+
+
+def empty_page_bounds(num_pages: int, num_kv_heads: int, head_dim: int, device="cuda"):
+    """(codes, scales) for a cache of that shape, zeroed: i8 [num_pages,Hkv,D/8,2,8] and u8 [num_pages,Hkv,D/32]."""
+    return (torch.zeros(num_pages, num_kv_heads, head_dim // 8, 2, 8, dtype=torch.int8, device=device),
+            torch.zeros(num_pages, num_kv_heads, head_dim // 32, dtype=torch.uint8, device=device))
+
+
+def make_page_bounds(codes: torch.Tensor, scales: torch.Tensor) -> KeyBounds:
+    """The key bounds of a cache's pages (see the header for the layout).  The struct borrows the tensors: keep them alive."""
+    assert codes.dtype == torch.int8 and scales.dtype == torch.uint8
+    assert codes.dim() == 5 and codes.shape[3:] == (2, 8) and tuple(scales.shape) == (codes.shape[0], codes.shape[1], codes.shape[2] // 4)
+    b = KeyBounds(_ptr(codes), _ptr(scales))
+    b._keep = (codes, scales)
+    return b
 
 
 def layer_desc(attn: AttnDesc, hidden: int, inter: int, w_o, w_gate, w_up, w_down, num_experts: int = 0,
@@ -527,3 +566,60 @@ class Context:
         self._check(self._lib.aflex_rope_append(self._h, ctypes.byref(desc), _ptr(qkv), ctypes.byref(kv),
                                                 qkv.shape[0], _ptr(w_q_norm), _ptr(w_k_norm), rms_eps, rope_theta,
                                                 _ptr(q_out), _stream(stream)))
+
+    # ---- page-sparse decode attention.  q_offsets: None for one row per sequence, else i32 CUDA [B+1] (see the header).
+    @staticmethod
+    def _rows(rows: int, q_offsets):
+        if q_offsets is None:
+            return rows, None
+        assert q_offsets.dtype == torch.int32 and q_offsets.dim() == 1
+        return q_offsets.shape[0] - 1, _ptr(q_offsets)
+
+    def _match(self, desc: AttnDesc, kv: KV, batch: int, bounds: Optional[KeyBounds] = None) -> None:
+        """The descriptors against the tensors they borrow, where the binding holds them."""
+        keep = getattr(kv, "_keep", None)
+        if keep is not None:
+            assert tuple(keep[0].shape[1:]) == (desc.num_kv_heads, desc.page_size, desc.head_dim), "cache shape does not fit the descriptor"
+            assert batch <= keep[2].shape[0] and batch <= keep[3].shape[0], "more sequences than page table rows or lengths"
+        if bounds is not None and getattr(bounds, "_keep", None) is not None:
+            assert tuple(bounds._keep[0].shape[1:3]) == (desc.num_kv_heads, desc.head_dim // 8), "key bounds do not fit the descriptor"
+            assert bounds._keep[0].shape[0] >= kv.num_pages, "key bounds of fewer pages than the cache has"
+
+    def rope_append_bounds(self, desc: AttnDesc, qkv, kv: KV, bounds: KeyBounds, q_out, w_q_norm, w_k_norm, rms_eps: float,
+                           rope_theta: float, q_offsets=None, stream=None) -> None:
+        """rope_append for one token or a chunk per sequence that also makes the key bounds of every page it touches."""
+        batch, offs = self._rows(qkv.shape[0], q_offsets)
+        self._match(desc, kv, batch, bounds)
+        self._check(self._lib.aflex_rope_append_bounds(self._h, ctypes.byref(desc), _ptr(qkv), ctypes.byref(kv), ctypes.byref(bounds),
+                                                       batch, offs, qkv.shape[0], _ptr(w_q_norm), _ptr(w_k_norm), rms_eps,
+                                                       rope_theta, _ptr(q_out), _stream_of(qkv, stream)))
+
+    def page_bounds(self, desc: AttnDesc, kv: KV, bounds: KeyBounds, batch: int, first_token=None, stream=None) -> None:
+        """Key bounds of the pages of sequences 0 .. batch - 1 that hold a token at first_token[b] (i32 CUDA [B]; None: 0) or later."""
+        assert first_token is None or first_token.dtype == torch.int32
+        self._match(desc, kv, batch, bounds)
+        st = stream.cuda_stream if stream is not None else torch.cuda.current_stream(self.device).cuda_stream
+        self._check(self._lib.aflex_page_bounds(self._h, ctypes.byref(desc), ctypes.byref(kv), ctypes.byref(bounds), batch,
+                                                _ptr(first_token), st))
+
+    def page_select(self, desc: AttnDesc, q, kv: KV, bounds: KeyBounds, top_pages: int, page_list, page_count,
+                    sink_pages: int = 1, window_pages: int = 2, q_offsets=None, stream=None) -> None:
+        """The pages each row's queries should read: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
+        assert page_list.dtype == torch.int32 and page_count.dtype == torch.int32
+        assert tuple(page_list.shape) == (q.shape[0], desc.num_kv_heads, top_pages) and page_count.numel() == q.shape[0] * desc.num_kv_heads
+        batch, offs = self._rows(q.shape[0], q_offsets)
+        self._match(desc, kv, batch, bounds)
+        pol = PagePolicy(top_pages, sink_pages, window_pages)
+        self._check(self._lib.aflex_page_select(self._h, ctypes.byref(desc), _ptr(q), ctypes.byref(kv), ctypes.byref(bounds),
+                                                ctypes.byref(pol), batch, offs, q.shape[0], _ptr(page_list), _ptr(page_count),
+                                                _stream_of(q, stream)))
+
+    def attn_decode_pages(self, desc: AttnDesc, q, kv: KV, page_list, page_count, out, lse=None, q_offsets=None, stream=None) -> None:
+        """Attention of every row over the pages listed for it: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
+        assert page_list.dtype == torch.int32 and page_count.dtype == torch.int32
+        assert tuple(page_list.shape[:2]) == (q.shape[0], desc.num_kv_heads) and page_count.numel() == q.shape[0] * desc.num_kv_heads
+        batch, offs = self._rows(q.shape[0], q_offsets)
+        self._match(desc, kv, batch)
+        self._check(self._lib.aflex_attn_decode_pages(self._h, ctypes.byref(desc), _ptr(q), ctypes.byref(kv), _ptr(page_list),
+                                                      _ptr(page_count), page_list.shape[2], batch, offs, q.shape[0], _ptr(out),
+                                                      _ptr(lse), _stream_of(q, stream)))

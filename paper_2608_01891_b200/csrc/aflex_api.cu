@@ -397,7 +397,8 @@ aflex_status aflex_get_device_status(aflex_ctx* ctx, void* stream) {
 static const char* kKernelNames[kKKindCount] = {
     "attn_decode", "linear_gemm", "down_gemm", "gateup_gemm", "router_logits",
     "moe_route", "moe_gather", "moe_gateup_gemm", "moe_down_gemm", "moe_combine",
-    "add_rmsnorm", "qkv_gemm", "rope_append", "attn_prefill", "gemm_chain"};
+    "add_rmsnorm", "qkv_gemm", "rope_append", "attn_prefill", "gemm_chain", "append_bounds", "page_bounds",
+    "page_select", "attn_pages"};
 
 int aflex_num_kernel_kinds(void) { return kKKindCount; }
 
@@ -767,6 +768,87 @@ aflex_status aflex_rope_append(aflex_ctx* ctx, const aflex_attn_desc* desc, cons
     if (!(rope_theta > 0.f)) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "rope_append: rope_theta must be > 0");
     return rope_append_launch(ctx, desc, qkv, kv, batch, w_q_norm, w_k_norm, rms_eps, rope_theta, q_out,
                               reinterpret_cast<cudaStream_t>(stream));
+}
+
+// ---- page-sparse decode attention ------------------------------------------------------------
+namespace {
+// The calls may be made with another device current than the ctx's: launches go to the ctx's device, the caller's comes back.
+struct CtxDevice {
+    int saved = -1;
+    explicit CtxDevice(const aflex_ctx* ctx) {
+        int dev = -1;
+        if (cudaGetDevice(&dev) == cudaSuccess && dev != ctx->device) { saved = dev; cudaSetDevice(ctx->device); }
+    }
+    ~CtxDevice() { if (saved >= 0) cudaSetDevice(saved); }
+};
+// Rows of a call: one per sequence, or `rows` rows laid out by q_offsets.
+aflex_status validate_rows(aflex_ctx* ctx, const char* what, int batch, const int32_t* q_offsets, int rows) {
+    if (rows < 1 || (!q_offsets && rows != batch))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: rows = %d (batch %d; without q_offsets one row per sequence)", what, rows, batch);
+    return AFLEX_OK;
+}
+aflex_status validate_bounds(aflex_ctx* ctx, const char* what, const aflex_key_bounds* bounds) {
+    if (!bounds || !bounds->codes || !bounds->scales) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: null key bounds", what);
+    if (!aligned16(bounds->codes) || !aligned16(bounds->scales))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", what);
+    return AFLEX_OK;
+}
+}  // namespace
+
+aflex_status aflex_rope_append_bounds(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* qkv, const aflex_kv* kv,
+                                      const aflex_key_bounds* bounds, int batch, const int32_t* q_offsets, int rows,
+                                      const void* w_q_norm, const void* w_k_norm, float rms_eps, float rope_theta, void* q_out,
+                                      void* stream) {
+    aflex_status s = validate_attn(ctx, desc, qkv, kv, batch, q_out);
+    if (s == AFLEX_OK) s = validate_bounds(ctx, "rope_append_bounds", bounds);
+    if (s == AFLEX_OK) s = validate_rows(ctx, "rope_append_bounds", batch, q_offsets, rows);
+    if (s != AFLEX_OK) return s;
+    if (!(rope_theta > 0.f) || !(rms_eps >= 0.f))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "rope_append_bounds: rope_theta must be > 0 and rms_eps >= 0");
+    CtxDevice dev(ctx);
+    return rope_append_bounds_launch(ctx, desc, qkv, kv, bounds, batch, q_offsets, rows, w_q_norm, w_k_norm, rms_eps, rope_theta,
+                                     q_out, reinterpret_cast<cudaStream_t>(stream));
+}
+
+aflex_status aflex_page_bounds(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_kv* kv, const aflex_key_bounds* bounds,
+                               int batch, const int32_t* first_token, void* stream) {
+    aflex_status s = validate_bounds(ctx, "page_bounds", bounds);
+    if (s == AFLEX_OK) s = validate_attn(ctx, desc, bounds->codes, kv, batch, bounds->codes);
+    if (s != AFLEX_OK) return s;
+    if ((long long)kv->max_pages_per_seq * desc->num_kv_heads >= (1LL << 31) - 8)
+        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page_bounds: max_pages_per_seq * Hkv does not fit 31 bits");
+    CtxDevice dev(ctx);
+    return page_bounds_launch(ctx, desc, kv, bounds, batch, first_token, reinterpret_cast<cudaStream_t>(stream));
+}
+
+aflex_status aflex_page_select(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,
+                               const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch, const int32_t* q_offsets,
+                               int rows, int32_t* page_list, int32_t* page_count, void* stream) {
+    aflex_status s = validate_attn(ctx, desc, q, kv, batch, page_list);
+    if (s == AFLEX_OK) s = validate_bounds(ctx, "page_select", bounds);
+    if (s == AFLEX_OK) s = validate_rows(ctx, "page_select", batch, q_offsets, rows);
+    if (s != AFLEX_OK) return s;
+    if (!policy || !page_count) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "page_select: null argument");
+    if (policy->sink_pages < 0 || policy->window_pages < 1 || policy->top_pages < 1 ||
+        (long long)policy->sink_pages + policy->window_pages > policy->top_pages)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "page_select: sink_pages %d >= 0, window_pages %d >= 1 and their sum <= top_pages %d are required",
+                         policy->sink_pages, policy->window_pages, policy->top_pages);
+    CtxDevice dev(ctx);
+    return page_select_launch(ctx, desc, q, kv, bounds, policy, batch, q_offsets, rows, page_list, page_count,
+                              reinterpret_cast<cudaStream_t>(stream));
+}
+
+aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,
+                                     const int32_t* page_list, const int32_t* page_count, int top_pages, int batch,
+                                     const int32_t* q_offsets, int rows, void* out, float* lse, void* stream) {
+    aflex_status s = validate_attn(ctx, desc, q, kv, batch, out);
+    if (s == AFLEX_OK) s = validate_rows(ctx, "attention over pages", batch, q_offsets, rows);
+    if (s != AFLEX_OK) return s;
+    if (!page_list || !page_count || top_pages < 1)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "attention over pages: null page_list / page_count or top_pages < 1");
+    CtxDevice dev(ctx);
+    return attn_decode_pages_launch(ctx, desc, q, kv, page_list, page_count, top_pages, batch, q_offsets, rows, out, lse,
+                                    reinterpret_cast<cudaStream_t>(stream));
 }
 
 namespace {

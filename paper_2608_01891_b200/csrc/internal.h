@@ -26,7 +26,8 @@ namespace aflex {
 enum KernelKind {
     kKAttnDecode = 0, kKLinearGemm, kKDownGemm, kKGateUpGemm, kKRouterLogits,
     kKMoeRoute, kKMoeGather, kKMoeGateUpGemm, kKMoeDownGemm, kKMoeCombine,
-    kKAddRmsNorm, kKQkvGemm, kKRopeAppend, kKAttnPrefill, kKGemmChain, kKKindCount
+    kKAddRmsNorm, kKQkvGemm, kKRopeAppend, kKAttnPrefill, kKGemmChain, kKAppendBounds, kKPageBounds,
+    kKPageSelect, kKAttnPages, kKKindCount
 };
 constexpr int kProfMaxSlots = 8192;
 struct ProfSlot { cudaEvent_t start, stop; int kind; };
@@ -58,6 +59,7 @@ struct aflex_ctx {
     bool chain_attr_set = false;
     bool attn_attr_set[2] = {false, false};
     bool prefill_attr_set[2] = {false, false};   // shared-memory limit raised for attn_prefill_kernel<64 / 128> on this device
+    bool select_attr_set[2] = {false, false};    // ... for page_select_kernel<64 / 128>
     char err[512] = {0};
     // launch counters (always on) and event-pair timing of every launch (when profiling is enabled)
     long long launches[aflex::kKKindCount] = {};
@@ -202,5 +204,19 @@ aflex_status add_rmsnorm_launch(aflex_ctx* ctx, const void* res, const void* add
 aflex_status rope_append_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* qkv, const aflex_kv* kv, int batch,
                                 const void* w_qn, const void* w_kn, float eps, float theta, void* q_out, cudaStream_t st,
                                 const int32_t* q_offsets = nullptr, int rows = 0);
+
+// ---- page-sparse decode attention: key bounds (page_bounds.cu), selection and attention (attn_pages.cu).  q_offsets == nullptr:
+// one row per sequence (rows == batch).
+aflex_status page_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const aflex_kv* kv, const aflex_key_bounds* bounds,
+                                int batch, const int32_t* first_token, cudaStream_t st);
+aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* qkv, const aflex_kv* kv,
+                                       const aflex_key_bounds* bounds, int batch, const int32_t* q_offsets, int rows,
+                                       const void* w_qn, const void* w_kn, float eps, float theta, void* q_out, cudaStream_t st);
+aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
+                                const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch, const int32_t* q_offsets,
+                                int rows, int32_t* page_list, int32_t* page_count, cudaStream_t st);
+aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
+                                      const int32_t* page_list, const int32_t* page_count, int top_pages, int batch,
+                                      const int32_t* q_offsets, int rows, void* out, float* lse, cudaStream_t st);
 
 }  // namespace aflex
