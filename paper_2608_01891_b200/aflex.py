@@ -215,9 +215,36 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
+def _stream_on(device: int, stream: Optional[torch.cuda.Stream]) -> int:
+    """The given stream, or the current one of that device (without building a Stream object: these calls last microseconds)."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
 def _stream_of(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
-    """The given stream, or the current one of the tensor's device."""
-    return (stream or torch.cuda.current_stream(t.device)).cuda_stream
+    return _stream_on(t.get_device(), stream)
+
+
+def _row_args(rows: int, q_offsets: Optional[torch.Tensor]):
+    """(batch, q_offsets pointer) of a call on `rows` rows."""
+    if q_offsets is None:
+        return rows, None
+    assert q_offsets.dtype == torch.int32 and q_offsets.dim() == 1
+    return q_offsets.shape[0] - 1, _ptr(q_offsets)
+
+
+def _match(desc: "AttnDesc", kv: "KV", batch: int, bounds: "Optional[KeyBounds]" = None) -> None:
+    """The descriptors against the shapes of the tensors they were made from (structs made by hand are not checked)."""
+    shape = kv.__dict__.get("_shape")
+    if shape is not None:
+        heads, tokens, dim, most = shape
+        assert heads == desc.num_kv_heads and tokens == desc.page_size and dim == desc.head_dim, "cache shape does not fit the descriptor"
+        assert batch <= most, "more sequences than page table rows or lengths"
+    if bounds is not None:
+        shape = bounds.__dict__.get("_shape")
+        if shape is not None:
+            pages, heads, chunks = shape
+            assert heads == desc.num_kv_heads and chunks * 8 == desc.head_dim, "key bounds do not fit the descriptor"
+            assert pages >= kv.num_pages, "key bounds of fewer pages than the cache has"
 
 
 def attn_desc(num_q_heads: int, num_kv_heads: int, head_dim: int, sm_scale: float = 0.0) -> AttnDesc:
@@ -236,6 +263,7 @@ def make_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tens
         assert seq_lens_host.dtype == torch.int32 and seq_lens_host.device.type == "cpu"
         kv.seq_lens_host = _ptr(seq_lens_host)
     kv._keep = (k_cache, v_cache, page_table, seq_lens, seq_lens_host)
+    kv._shape = (*k_cache.shape[1:], min(page_table.shape[0], seq_lens.shape[0]))
     return kv
 
 
@@ -251,6 +279,7 @@ def make_page_bounds(codes: torch.Tensor, scales: torch.Tensor) -> KeyBounds:
     assert codes.dim() == 5 and codes.shape[3:] == (2, 8) and tuple(scales.shape) == (codes.shape[0], codes.shape[1], codes.shape[2] // 4)
     b = KeyBounds(_ptr(codes), _ptr(scales))
     b._keep = (codes, scales)
+    b._shape = tuple(codes.shape[:3])
     return b
 
 
@@ -568,58 +597,39 @@ class Context:
                                                 _ptr(q_out), _stream(stream)))
 
     # ---- page-sparse decode attention.  q_offsets: None for one row per sequence, else i32 CUDA [B+1] (see the header).
-    @staticmethod
-    def _rows(rows: int, q_offsets):
-        if q_offsets is None:
-            return rows, None
-        assert q_offsets.dtype == torch.int32 and q_offsets.dim() == 1
-        return q_offsets.shape[0] - 1, _ptr(q_offsets)
-
-    def _match(self, desc: AttnDesc, kv: KV, batch: int, bounds: Optional[KeyBounds] = None) -> None:
-        """The descriptors against the tensors they borrow, where the binding holds them."""
-        keep = getattr(kv, "_keep", None)
-        if keep is not None:
-            assert tuple(keep[0].shape[1:]) == (desc.num_kv_heads, desc.page_size, desc.head_dim), "cache shape does not fit the descriptor"
-            assert batch <= keep[2].shape[0] and batch <= keep[3].shape[0], "more sequences than page table rows or lengths"
-        if bounds is not None and getattr(bounds, "_keep", None) is not None:
-            assert tuple(bounds._keep[0].shape[1:3]) == (desc.num_kv_heads, desc.head_dim // 8), "key bounds do not fit the descriptor"
-            assert bounds._keep[0].shape[0] >= kv.num_pages, "key bounds of fewer pages than the cache has"
-
     def rope_append_bounds(self, desc: AttnDesc, qkv, kv: KV, bounds: KeyBounds, q_out, w_q_norm, w_k_norm, rms_eps: float,
                            rope_theta: float, q_offsets=None, stream=None) -> None:
         """rope_append for one token or a chunk per sequence that also makes the key bounds of every page it touches."""
-        batch, offs = self._rows(qkv.shape[0], q_offsets)
-        self._match(desc, kv, batch, bounds)
-        self._check(self._lib.aflex_rope_append_bounds(self._h, ctypes.byref(desc), _ptr(qkv), ctypes.byref(kv), ctypes.byref(bounds),
-                                                       batch, offs, qkv.shape[0], _ptr(w_q_norm), _ptr(w_k_norm), rms_eps,
-                                                       rope_theta, _ptr(q_out), _stream_of(qkv, stream)))
+        rows = qkv.shape[0]
+        batch, offs = _row_args(rows, q_offsets)
+        _match(desc, kv, batch, bounds)
+        assert q_out.shape[0] == rows, "q_out has another number of rows than qkv"
+        self._check(self._lib.aflex_rope_append_bounds(self._h, desc, _ptr(qkv), kv, bounds, batch, offs, rows, _ptr(w_q_norm),
+                                                       _ptr(w_k_norm), rms_eps, rope_theta, _ptr(q_out), _stream_of(qkv, stream)))
 
     def page_bounds(self, desc: AttnDesc, kv: KV, bounds: KeyBounds, batch: int, first_token=None, stream=None) -> None:
         """Key bounds of the pages of sequences 0 .. batch - 1 that hold a token at first_token[b] (i32 CUDA [B]; None: 0) or later."""
         assert first_token is None or first_token.dtype == torch.int32
-        self._match(desc, kv, batch, bounds)
-        st = stream.cuda_stream if stream is not None else torch.cuda.current_stream(self.device).cuda_stream
-        self._check(self._lib.aflex_page_bounds(self._h, ctypes.byref(desc), ctypes.byref(kv), ctypes.byref(bounds), batch,
-                                                _ptr(first_token), st))
+        _match(desc, kv, batch, bounds)
+        self._check(self._lib.aflex_page_bounds(self._h, desc, kv, bounds, batch, _ptr(first_token), _stream_on(self.device, stream)))
 
     def page_select(self, desc: AttnDesc, q, kv: KV, bounds: KeyBounds, top_pages: int, page_list, page_count,
                     sink_pages: int = 1, window_pages: int = 2, q_offsets=None, stream=None) -> None:
         """The pages each row's queries should read: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
+        rows = q.shape[0]
         assert page_list.dtype == torch.int32 and page_count.dtype == torch.int32
-        assert tuple(page_list.shape) == (q.shape[0], desc.num_kv_heads, top_pages) and page_count.numel() == q.shape[0] * desc.num_kv_heads
-        batch, offs = self._rows(q.shape[0], q_offsets)
-        self._match(desc, kv, batch, bounds)
-        pol = PagePolicy(top_pages, sink_pages, window_pages)
-        self._check(self._lib.aflex_page_select(self._h, ctypes.byref(desc), _ptr(q), ctypes.byref(kv), ctypes.byref(bounds),
-                                                ctypes.byref(pol), batch, offs, q.shape[0], _ptr(page_list), _ptr(page_count),
-                                                _stream_of(q, stream)))
+        assert page_list.shape == (rows, desc.num_kv_heads, top_pages) and page_count.shape == page_list.shape[:2]
+        batch, offs = _row_args(rows, q_offsets)
+        _match(desc, kv, batch, bounds)
+        self._check(self._lib.aflex_page_select(self._h, desc, _ptr(q), kv, bounds, PagePolicy(top_pages, sink_pages, window_pages),
+                                                batch, offs, rows, _ptr(page_list), _ptr(page_count), _stream_of(q, stream)))
 
     def attn_decode_pages(self, desc: AttnDesc, q, kv: KV, page_list, page_count, out, lse=None, q_offsets=None, stream=None) -> None:
         """Attention of every row over the pages listed for it: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
+        rows, heads, top = page_list.shape
         assert page_list.dtype == torch.int32 and page_count.dtype == torch.int32
-        assert tuple(page_list.shape[:2]) == (q.shape[0], desc.num_kv_heads) and page_count.numel() == q.shape[0] * desc.num_kv_heads
-        batch, offs = self._rows(q.shape[0], q_offsets)
-        self._match(desc, kv, batch)
-        self._check(self._lib.aflex_attn_decode_pages(self._h, ctypes.byref(desc), _ptr(q), ctypes.byref(kv), _ptr(page_list),
-                                                      _ptr(page_count), page_list.shape[2], batch, offs, q.shape[0], _ptr(out),
-                                                      _ptr(lse), _stream_of(q, stream)))
+        assert heads == desc.num_kv_heads and rows == q.shape[0] and rows == out.shape[0] and page_count.shape == (rows, heads)
+        batch, offs = _row_args(rows, q_offsets)
+        _match(desc, kv, batch)
+        self._check(self._lib.aflex_attn_decode_pages(self._h, desc, _ptr(q), kv, _ptr(page_list), _ptr(page_count), top, batch, offs,
+                                                      rows, _ptr(out), _ptr(lse), _stream_of(q, stream)))

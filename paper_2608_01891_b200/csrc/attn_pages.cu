@@ -15,26 +15,32 @@ namespace {
 constexpr int kPageTokens = 16;
 constexpr float kNegBig = -1.0e30f;
 
-// Sequence and position of a row.  Returns false (and reports it) where the inputs give none; rows behind the last
-// sequence's are not theirs to report: `padding`.
-struct RowAt { int b, pos; bool padding; };
-__device__ __forceinline__ bool locate_row(int row, const int32_t* q_offsets, const int32_t* seq_lens, int batch, int max_pages,
-                                           RowAt& at) {
+// Sequence and position of a row; every lane of a warp takes part.  `ok` is false where the inputs give none.  Rows behind the
+// last sequence's are padding: nothing is to be read, written or reported for them.
+struct RowAt { int b, pos; bool ok, padding; };
+__device__ __forceinline__ RowAt locate_row(int row, const int32_t* q_offsets, const int32_t* seq_lens, int batch, int max_pages) {
+    RowAt at;
     int back = 0;
     at.b = row; at.padding = false;
     if (q_offsets != nullptr) {
-        if (row >= q_offsets[batch]) { at.padding = true; return false; }
-        int lo = 0, hi = batch;                    // largest b with q_offsets[b] <= row
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (q_offsets[mid] <= row) lo = mid; else hi = mid;
+        // largest b with q_offsets[b] <= row: the lanes look at 32 sequences at a time (one load's latency for up to 32)
+        const int lane = threadIdx.x & 31, end = __ldg(q_offsets + batch);
+        int lo = 0, span = batch;
+        while (span > 1) {
+            const int step = (span + 31) / 32, i = lane * step;
+            const unsigned le = __ballot_sync(0xffffffffu, i < span && __ldg(q_offsets + lo + (i < span ? i : 0)) <= row);
+            const int at_step = max(__popc(le) - 1, 0) * step;
+            lo += at_step;
+            span = min(step, span - at_step);
         }
         at.b = lo;
-        back = q_offsets[lo + 1] - 1 - row;
+        at.padding = row >= end;
+        back = __ldg(q_offsets + lo + 1) - 1 - row;
     }
-    const int len = seq_lens[at.b];
+    const int len = __ldg(seq_lens + at.b);
     at.pos = len - 1 - back;
-    return back >= 0 && at.pos >= 0 && len <= max_pages * kPageTokens;
+    at.ok = !at.padding && back >= 0 && at.pos >= 0 && len <= max_pages * kPageTokens;
+    return at;
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -50,6 +56,11 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
 __device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
     float v;
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
 }
 
@@ -123,10 +134,9 @@ __global__ void __launch_bounds__(kSelThreads) page_select_kernel(const SelectPa
     if (S > 1) cluster_arrive();                                  // the cluster's CTAs have started: waited for below
     pdl_launch_dependents();
     pdl_wait();
-    RowAt at;
-    const bool ok = locate_row(row, p.q_offsets, p.seq_lens, p.batch, p.max_pages, at);
-    const int n = ok ? at.pos / kPageTokens + 1 : 0;
-    if (!ok && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    const RowAt at = locate_row(row, p.q_offsets, p.seq_lens, p.batch, p.max_pages);
+    const int n = at.ok ? at.pos / kPageTokens + 1 : 0;
+    if (!at.ok && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
     int32_t* list = p.list + item * p.top;
     const int keep = p.top - p.sink - p.window;                   // scored pages to keep
     const int cand = n - p.sink - p.window;                       // scored pages
@@ -335,16 +345,19 @@ __global__ void __launch_bounds__(kSelThreads) page_select_kernel(const SelectPa
 //   s_j = sm_scale <q, K_j>,  out = sum_j softmax(s)_j V_j,  lse = ln sum_j exp(s_j)
 //
 // Bound: the K and V bytes of the listed pages.  Every page is 4 KB of K and 4 KB of V (D = 128) somewhere in HBM, read once
-// by one warp straight into registers: with the channels of a row permuted alike for q and K (a sum does not mind), sixteen
-// contiguous bytes per lane are MMA fragments as they are, S = Q K^T leaves P in the layout of the second product's A operand,
-// and V's fragments are two rows' words interleaved.  No shared memory, no barrier, no copy engine in the loop: the next
-// page's K is loaded as soon as the current one has been multiplied, the next V likewise.
+// by one warp through a ring of pages of its own (asynchronous 16-byte copies, so what is in flight does not cost registers).
+// Warps share nothing until the end: no barrier in the loop, only the warp's own copy groups.
+// With the channels of a row permuted alike for q and K (a sum does not mind), sixteen contiguous bytes per lane are MMA
+// fragments as they are, S = Q K^T leaves P in the layout of the second product's A operand, and V's fragments are two rows'
+// words interleaved.  The copies swizzle the 16-byte chunks of a row so that both reads are free of bank conflicts.
 // The MMA has 16 rows and a group at most 8 heads: the other 8 rows carry the low half of P (P = P_hi + P_lo, both bf16), so
 // the second product loses nothing to the rounding of P.
 // Lists are short (tens to a few hundred pages), so the work is split by (row, KV head) and, where those are few, the list is
-// cut over a cluster's CTAs; warps and CTAs keep their own running maximum and sum and are joined through shared memory.
+// dealt out page by page over a cluster's CTAs and warps (which page is whose does not depend on the count, so the list entry
+// is loaded along with it); each keeps its own running maximum and sum, joined at the end through shared memory.
 constexpr int kPagesWarps = 4;
 constexpr int kPagesThreads = kPagesWarps * 32;
+constexpr int kPagesMaxCluster = 8;
 
 struct PagesParams {
     const __nv_bfloat16* q;
@@ -363,22 +376,42 @@ struct PagesParams {
     int* status;
 };
 
-template <int D> struct PagesShared {
-    float o[kPagesWarps][8][D];
-    float m[kPagesWarps][8], l[kPagesWarps][8];
+template <int D> struct PagesRing {
+    static constexpr int kStages = D == 128 ? 3 : 4;
+    static constexpr int kPageBytes = kPageTokens * D * 2;            // of K; as many of V
+    static constexpr int kWarpBytes = kStages * 2 * kPageBytes;       // holds the warp's state (8 heads x D floats) at the end
+    static constexpr int kBytes = kPagesWarps * kWarpBytes;
+    static constexpr int kResident = D == 128 ? 2 : 3;                // CTAs per SM
 };
 
-__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+struct PagesShared {
+    float m[kPagesWarps][8], l[kPagesWarps][8];
+    float cm[8], cl[8];            // the CTA's own, joined
+    int valid[kPagesWarps][4];     // tokens of the page in each stage of the ring
+};
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {      // fewer than 16 bytes: the rest is zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
     return v;
 }
+// Place of a row's 16-byte chunk: K is read as (8 rows) x (4 neighbouring chunks) per instruction, V as (rows 0, 2, 4, 6 or
+// 1, 3, 5, 7) x (8 chunks); either way the eight lanes of a bank cycle then touch eight different 16-byte banks.
+__device__ __forceinline__ int swizzle(int row) { return (((row >> 1) & 3) << 1) ^ ((row & 1) << 2); }
 
 template <int D>
-__global__ void __launch_bounds__(kPagesThreads, 3) attn_decode_pages_kernel(const PagesParams p) {
-    constexpr int kSteps = D / 32;                 // 16-byte loads per lane and K row
-    constexpr int kHalves = D / 64;                // 16-byte loads per lane and V row
-    __shared__ __align__(16) PagesShared<D> sh;
+__global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const PagesParams p) {
+    typedef PagesRing<D> R;
+    constexpr int kSteps = D / 32;                 // 16-byte reads per lane and K row
+    constexpr int kHalves = D / 64;                // 16-byte reads per lane and V row
+    constexpr int kChunks = D / 8;                 // 16-byte chunks of a row
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ PagesShared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int hl = lane >> 2, l4 = lane & 3;
     const int S = p.cluster, rank = (int)(blockIdx.x % S);
@@ -386,174 +419,208 @@ __global__ void __launch_bounds__(kPagesThreads, 3) attn_decode_pages_kernel(con
     const int row = (int)(item / p.Hkv), g = (int)(item % p.Hkv);
     pdl_launch_dependents();
     pdl_wait();
-    RowAt at;
-    const bool ok = locate_row(row, p.q_offsets, p.seq_lens, p.batch, p.max_pages, at);
-    if (at.padding) return;                        // (the same for the whole cluster)
-    int total = 0;
-    if (ok) total = max(0, min(p.top, p.count[item]));
-    else if (tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
-    const int lo = (int)((long long)total * rank / S), hi = (int)((long long)total * (rank + 1) / S);
+    // This warp's pages are list entries first, first + stride, ...; lane i holds the i-th of the next 32.
+    const int first = rank * kPagesWarps + warp, stride = S * kPagesWarps;
     const int32_t* list = p.list + item * p.top;
-    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
-
+    auto entry = [&](int i0) -> int {
+        const long long i = first + (long long)(i0 + lane) * stride;
+        return i < p.top ? __ldg(list + i) : -1;
+    };
+    int next = entry(0);
+    const int total = max(0, min(p.top, __ldg(p.count + item)));
     uint4 qf[kSteps];                              // head lane / 4, channels 32 step + 8 (lane % 4) .. + 7
     {
         const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + (hl < p.G ? hl : 0)) * D);
 #pragma unroll
-        for (int c = 0; c < kSteps; ++c) {
-            qf[c] = src[c * 4 + l4];
-            if (hl >= p.G) qf[c] = make_uint4(0, 0, 0, 0);
-        }
+        for (int c = 0; c < kSteps; ++c) qf[c] = __ldg(src + c * 4 + l4);
     }
+    const RowAt at = locate_row(row, p.q_offsets, p.seq_lens, p.batch, p.max_pages);
+    if (at.padding) return;                        // (the same for the whole cluster)
+    if (!at.ok && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    const int n = at.ok ? max(0, (total - first + stride - 1) / stride) : 0;           // this warp's pages
+    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
+    if (hl >= p.G) {
+#pragma unroll
+        for (int c = 0; c < kSteps; ++c) qf[c] = make_uint4(0, 0, 0, 0);
+    }
+    const uint32_t base = smem_u32(ring) + (uint32_t)(warp * R::kWarpBytes);
+    int phys = 0, valid = 0;
+    // starts the copies of page i of this warp's into stage i % kStages
+    auto issue = [&](int i) {
+        if ((i & 31) == 0) {                       // look up the next 32 entries, and load the 32 after them
+            phys = 0; valid = 0;
+            if (i + lane < n) {
+                if (next >= 0 && next <= at.pos / kPageTokens) {
+                    phys = __ldg(table + next);
+                    valid = min(kPageTokens, at.pos - next * kPageTokens + 1);
+                }
+                if (valid == 0 || phys < 0 || phys >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); phys = 0; valid = 0; }
+            }
+            next = entry(i + 32);
+        }
+        const int nv = __shfl_sync(0xffffffffu, valid, i & 31);
+        const size_t slab = ((size_t)__shfl_sync(0xffffffffu, phys, i & 31) * p.Hkv + g) * kPageTokens * D;
+        const int stage = i % R::kStages;
+        if (lane == 0) sh.valid[warp][stage] = nv;
+        const uint32_t dst = base + (uint32_t)(stage * 2 * R::kPageBytes);
+#pragma unroll
+        for (int k = 0; k < kPageTokens * kChunks / 32; ++k) {
+            const int c = k * 32 + lane, r = c / kChunks, ch = c % kChunks;
+            const uint32_t to = dst + (uint32_t)(r * (D * 2) + ((ch ^ swizzle(r)) << 4));
+            // slots past the end may hold anything: K's scores are masked, V has to be zero
+            copy16(to, p.k_cache + slab + c * 8, 16);
+            copy16(to + R::kPageBytes, p.v_cache + slab + c * 8, r < nv ? 16 : 0);
+        }
+    };
     float o[kHalves][8][4];                        // [half][channel of the lane's chunk][rows 0-7: P_hi, rows 8-15: P_lo]
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
         for (int c = 0; c < 8; ++c) o[h][c][0] = o[h][c][1] = o[h][c][2] = o[h][c][3] = 0.f;
     float m = kNegBig, l = 0.f;
-
-    for (int i0 = lo + warp; i0 < hi; i0 += 32 * kPagesWarps) {
-        // this warp's next 32 list entries, one per lane: physical page and valid tokens
-        int phys = 0, valid = 0;
-        const int ie = i0 + lane * kPagesWarps;
-        if (ie < hi) {
-            const int e = list[ie];
-            if (e >= 0 && e <= at.pos / kPageTokens) {
-                phys = table[e];
-                valid = min(kPageTokens, at.pos - e * kPageTokens + 1);
-            }
-            if (valid == 0 || phys < 0 || phys >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); phys = 0; valid = 0; }
-        }
-        const int nb = min(32, (hi - i0 + kPagesWarps - 1) / kPagesWarps);
-        uint4 kx[2][kSteps], vx[4][kHalves];
-        auto load_k = [&](int j) {
-            const size_t slab = (size_t)__shfl_sync(0xffffffffu, phys, j) * p.Hkv + g;
-            const uint4* src = reinterpret_cast<const uint4*>(p.k_cache + slab * kPageTokens * D) + hl * (D / 8) + l4;
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int c = 0; c < kSteps; ++c) kx[r][c] = ld_stream(src + r * D + c * 4);        // 8 rows are D sixteen-byte words
-        };
-        auto load_v = [&](int j) {
-            const size_t slab = (size_t)__shfl_sync(0xffffffffu, phys, j) * p.Hkv + g;
-            const int nv = __shfl_sync(0xffffffffu, valid, j);
-            const uint4* src = reinterpret_cast<const uint4*>(p.v_cache + slab * kPageTokens * D) + hl;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = 2 * l4 + (r & 1) + (r >> 1) * 8;
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h) {
-                    vx[r][h] = make_uint4(0, 0, 0, 0);                                             // slots past the end may hold NaN
-                    if (t < nv) vx[r][h] = ld_stream(src + t * (D / 8) + h * 8);
-                }
-            }
-        };
-        load_k(0);
-        load_v(0);
-        for (int j = 0; j < nb; ++j) {
-            const int nv = __shfl_sync(0xffffffffu, valid, j);
+    for (int i = 0; i < R::kStages - 1; ++i) {
+        if (i < n) issue(i);
+        copy_commit();
+    }
+    for (int i = 0; i < n; ++i) {
+        if (i + R::kStages - 1 < n) issue(i + R::kStages - 1);
+        copy_commit();
+        copy_wait<R::kStages - 1>();
+        __syncwarp();
+        const int stage = i % R::kStages;
+        const int nv = sh.valid[warp][stage];
+        const uint32_t kp = base + (uint32_t)(stage * 2 * R::kPageBytes), vp = kp + R::kPageBytes;
+        if (nv > 0) {
             float s[2][4];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
+                const int t = hl + 8 * r;
 #pragma unroll
                 for (int c = 0; c < kSteps; ++c) {
-                    mma_bf16_16816(s[r], qf[c].x, 0u, qf[c].y, 0u, kx[r][c].x, kx[r][c].y);
-                    mma_bf16_16816(s[r], qf[c].z, 0u, qf[c].w, 0u, kx[r][c].z, kx[r][c].w);
+                    const uint4 x = lds128(kp + (uint32_t)(t * (D * 2) + (((c * 4 + l4) ^ swizzle(t)) << 4)));
+                    mma_bf16_16816(s[r], qf[c].x, 0u, qf[c].y, 0u, x.x, x.y);
+                    mma_bf16_16816(s[r], qf[c].z, 0u, qf[c].w, 0u, x.z, x.w);
                 }
             }
-            if (j + 1 < nb) load_k(j + 1);
-            if (nv > 0) {
-                // tokens 2 l4, 2 l4 + 1 and those + 8 of head lane / 4
-                float x0 = 2 * l4 < nv ? s[0][0] * p.scale_log2 : -INFINITY;
-                float x1 = 2 * l4 + 1 < nv ? s[0][1] * p.scale_log2 : -INFINITY;
-                float x2 = 2 * l4 + 8 < nv ? s[1][0] * p.scale_log2 : -INFINITY;
-                float x3 = 2 * l4 + 9 < nv ? s[1][1] * p.scale_log2 : -INFINITY;
-                float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                if (__any_sync(0xffffffffu, mx > m)) {
-                    const float mn = fmaxf(m, mx), corr = fast_exp2(m - mn);
-                    m = mn;
-                    l *= corr;
+            // tokens 2 l4, 2 l4 + 1 and those + 8 of head lane / 4
+            float x0 = 2 * l4 < nv ? s[0][0] * p.scale_log2 : -INFINITY;
+            float x1 = 2 * l4 + 1 < nv ? s[0][1] * p.scale_log2 : -INFINITY;
+            float x2 = 2 * l4 + 8 < nv ? s[1][0] * p.scale_log2 : -INFINITY;
+            float x3 = 2 * l4 + 9 < nv ? s[1][1] * p.scale_log2 : -INFINITY;
+            float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+            if (__any_sync(0xffffffffu, mx > m)) {
+                const float mn = fmaxf(m, mx), corr = fast_exp2(m - mn);
+                m = mn;
+                l *= corr;
 #pragma unroll
-                    for (int h = 0; h < kHalves; ++h)
+                for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) { o[h][c][0] *= corr; o[h][c][1] *= corr; o[h][c][2] *= corr; o[h][c][3] *= corr; }
+                    for (int c = 0; c < 8; ++c) { o[h][c][0] *= corr; o[h][c][1] *= corr; o[h][c][2] *= corr; o[h][c][3] *= corr; }
+            }
+            x0 = fast_exp2(x0 - m); x1 = fast_exp2(x1 - m); x2 = fast_exp2(x2 - m); x3 = fast_exp2(x3 - m);
+            l += (x0 + x1) + (x2 + x3);
+            const uint32_t a0 = pack_bf16x2(x0, x1), a2 = pack_bf16x2(x2, x3);
+            const uint32_t a1 = pack_bf16x2(x0 - __uint_as_float(a0 << 16), x1 - __uint_as_float(a0 & 0xffff0000u));
+            const uint32_t a3 = pack_bf16x2(x2 - __uint_as_float(a2 << 16), x3 - __uint_as_float(a2 & 0xffff0000u));
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+                uint4 v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int t = 2 * l4 + (r & 1) + (r >> 1) * 8;
+                    v[r] = lds128(vp + (uint32_t)(t * (D * 2) + (((h * 8 + hl) ^ swizzle(t)) << 4)));
                 }
-                x0 = fast_exp2(x0 - m); x1 = fast_exp2(x1 - m); x2 = fast_exp2(x2 - m); x3 = fast_exp2(x3 - m);
-                l += (x0 + x1) + (x2 + x3);
-                const uint32_t a0 = pack_bf16x2(x0, x1), a2 = pack_bf16x2(x2, x3);
-                const uint32_t a1 = pack_bf16x2(x0 - __uint_as_float(a0 << 16), x1 - __uint_as_float(a0 & 0xffff0000u));
-                const uint32_t a3 = pack_bf16x2(x2 - __uint_as_float(a2 << 16), x3 - __uint_as_float(a2 & 0xffff0000u));
+                const uint32_t* r0 = reinterpret_cast<const uint32_t*>(&v[0]);
+                const uint32_t* r1 = reinterpret_cast<const uint32_t*>(&v[1]);
+                const uint32_t* r2 = reinterpret_cast<const uint32_t*>(&v[2]);
+                const uint32_t* r3 = reinterpret_cast<const uint32_t*>(&v[3]);
 #pragma unroll
-                for (int h = 0; h < kHalves; ++h) {
-                    const uint32_t* r0 = reinterpret_cast<const uint32_t*>(&vx[0][h]);
-                    const uint32_t* r1 = reinterpret_cast<const uint32_t*>(&vx[1][h]);
-                    const uint32_t* r2 = reinterpret_cast<const uint32_t*>(&vx[2][h]);
-                    const uint32_t* r3 = reinterpret_cast<const uint32_t*>(&vx[3][h]);
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        mma_bf16_16816(o[h][2 * w], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x5410), __byte_perm(r2[w], r3[w], 0x5410));
-                        mma_bf16_16816(o[h][2 * w + 1], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x7632), __byte_perm(r2[w], r3[w], 0x7632));
-                    }
+                for (int w = 0; w < 4; ++w) {
+                    mma_bf16_16816(o[h][2 * w], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x5410), __byte_perm(r2[w], r3[w], 0x5410));
+                    mma_bf16_16816(o[h][2 * w + 1], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x7632), __byte_perm(r2[w], r3[w], 0x7632));
                 }
             }
-            if (j + 1 < nb) load_v(j + 1);
         }
+        __syncwarp();                              // everybody has read the stage that the next copies overwrite
     }
     // ---- join the warps, then the cluster's CTAs.  Lane: head lane / 4, channels 64 h + 16 l4 + 8 x + c at o[h][c][x].
+    // The copies that this warp started have all landed (a group is waited for before its page is used), so its ring is free.
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
+    auto state = [&](int w) { return reinterpret_cast<float*>(ring + w * R::kWarpBytes); };       // [8][D]
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-            float* dst = &sh.o[warp][hl][64 * h + 16 * l4 + 8 * x];
+            float* dst = state(warp) + hl * D + 64 * h + 16 * l4 + 8 * x;
             *reinterpret_cast<float4*>(dst) = make_float4(o[h][0][x] + o[h][0][x + 2], o[h][1][x] + o[h][1][x + 2],
                                                           o[h][2][x] + o[h][2][x + 2], o[h][3][x] + o[h][3][x + 2]);
             *reinterpret_cast<float4*>(dst + 4) = make_float4(o[h][4][x] + o[h][4][x + 2], o[h][5][x] + o[h][5][x + 2],
                                                               o[h][6][x] + o[h][6][x + 2], o[h][7][x] + o[h][7][x + 2]);
         }
     if (l4 == 0) { sh.m[warp][hl] = m; sh.l[warp][hl] = l; }
-    if (S > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
-    // The G * D outputs in runs of eight channels; CTA `rank` of the cluster makes its share of the runs
-    for (int i = rank * kPagesThreads + tid; i < p.G * (D / 8); i += S * kPagesThreads) {
-        const int h = i / (D / 8), c0 = (i % (D / 8)) * 8;
-        float M = kNegBig, L = 0.f, acc[8];
+    __syncthreads();
+    constexpr int kRuns = D / 4;                   // a head's outputs in runs of four channels
+    auto store = [&](int h, int c, float M, float L, const float4& acc) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;            // a row with nothing to attend to: zeros
+        const size_t hq = (size_t)row * p.Hq + (size_t)g * p.G + h;
+        reinterpret_cast<uint2*>(p.out + hq * D)[c] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (p.lse != nullptr && c == 0) p.lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    };
+    for (int i = tid; i < p.G * kRuns; i += kPagesThreads) {
+        const int h = i / kRuns, c = i % kRuns;
+        float M = kNegBig, L = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int c = 0; c < 8; ++c) acc[c] = 0.f;
-        for (int s = 0; s < S; ++s) {
+        for (int w = 0; w < kPagesWarps; ++w) M = fmaxf(M, sh.m[w][h]);
 #pragma unroll
-            for (int w = 0; w < kPagesWarps; ++w) {
-                float pm, pl, v[8];
-                if (S == 1) {
-                    pm = sh.m[w][h]; pl = sh.l[w][h];
+        for (int w = 0; w < kPagesWarps; ++w) {
+            const float f = fast_exp2(sh.m[w][h] - M);
+            const float4 v = *reinterpret_cast<const float4*>(state(w) + h * D + 4 * c);
+            L = fmaf(sh.l[w][h], f, L);
+            acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y); acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
+        }
+        if (S == 1) store(h, c, M, L, acc);
+        else {
+            *reinterpret_cast<float4*>(state(0) + h * D + 4 * c) = acc;        // read by nobody else in this loop
+            if (c == 0) { sh.cm[h] = M; sh.cl[h] = L; }
+        }
+    }
+    if (S == 1) return;
+    // the cluster's CTAs: each makes its share of the runs, all pieces loaded before the first is used
+    cluster_arrive();
+    cluster_wait();
+    for (int i = rank + S * tid; i < p.G * kRuns; i += S * kPagesThreads) {
+        const int h = i / kRuns, c = i % kRuns;
+        float pm[kPagesMaxCluster], pl[kPagesMaxCluster];
+        float4 v[kPagesMaxCluster];
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) v[c] = sh.o[w][h][c0 + c];
-                } else {
-                    pm = ld_cluster_f32(cluster_map_shared(smem_u32(&sh.m[w][h]), (uint32_t)s));
-                    pl = ld_cluster_f32(cluster_map_shared(smem_u32(&sh.l[w][h]), (uint32_t)s));
-                    const uint32_t base = cluster_map_shared(smem_u32(&sh.o[w][h][c0]), (uint32_t)s);
+        for (int s = 0; s < kPagesMaxCluster; ++s) {
+            const uint32_t from = (uint32_t)(s < S ? s : 0);
+            pm[s] = ld_cluster_f32(cluster_map_shared(smem_u32(&sh.cm[h]), from));
+            pl[s] = ld_cluster_f32(cluster_map_shared(smem_u32(&sh.cl[h]), from));
+            v[s] = ld_cluster_f32x4(cluster_map_shared(smem_u32(state(0) + h * D + 4 * c), from));
+        }
+        float M = kNegBig, L = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) v[c] = ld_cluster_f32(base + 4 * c);
-                }
-                const float mn = fmaxf(M, pm), ca = fast_exp2(M - mn), cb = fast_exp2(pm - mn);
-                M = mn;
-                L = L * ca + pl * cb;
+        for (int s = 0; s < kPagesMaxCluster; ++s) if (s < S) M = fmaxf(M, pm[s]);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) acc[c] = acc[c] * ca + v[c] * cb;
+        for (int s = 0; s < kPagesMaxCluster; ++s) {
+            if (s < S) {
+                const float f = fast_exp2(pm[s] - M);
+                L = fmaf(pl[s], f, L);
+                acc.x = fmaf(v[s].x, f, acc.x); acc.y = fmaf(v[s].y, f, acc.y); acc.z = fmaf(v[s].z, f, acc.z); acc.w = fmaf(v[s].w, f, acc.w);
             }
         }
-        const float inv = L == 0.f ? 0.f : 1.f / L;           // a row with nothing to attend to: zeros
-        uint4 y;
-        y.x = pack_bf16x2(acc[0] * inv, acc[1] * inv); y.y = pack_bf16x2(acc[2] * inv, acc[3] * inv);
-        y.z = pack_bf16x2(acc[4] * inv, acc[5] * inv); y.w = pack_bf16x2(acc[6] * inv, acc[7] * inv);
-        const size_t hq = (size_t)row * p.Hq + (size_t)g * p.G + h;
-        reinterpret_cast<uint4*>(p.out + hq * D)[c0 / 8] = y;
-        if (p.lse != nullptr && c0 == 0) p.lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        store(h, c, M, L, acc);
     }
-    if (S > 1) { cluster_arrive(); cluster_wait(); }          // the others' shared memory stays until everybody has read it
+    cluster_arrive();
+    cluster_wait();                                // the others' shared memory stays until everybody has read it
 }
 
 template <typename P>
@@ -622,13 +689,25 @@ aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, 
     p.scale_log2 = scale * 1.4426950408889634f;
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
-    int S = 1;
-    while (S < 8 && items * S < 6LL * ctx->num_sms && top_pages > S * kPagesWarps) S *= 2;
+    // CTAs per (row, KV head): what fits the GPU at once, down to one page per warp.  A CTA costs about 5 us beside its pages
+    // (three dependent loads before the first page, the join), so a second wave costs more than an even split gains: 8 items of
+    // 128 pages 23.8 / 15.1 / 9.9 / 7.2 us with 1 / 2 / 4 / 8 CTAs each, 256 items of up to 64 pages 26 / 32 / 43 / 61 us.
+    const long long slots = (long long)ctx->num_sms * (d->head_dim == 128 ? PagesRing<128>::kResident : PagesRing<64>::kResident);
+    const int most = (top_pages + kPagesWarps - 1) / kPagesWarps;
+    int S = (int)(slots / items < kPagesMaxCluster ? slots / items : kPagesMaxCluster);
+    if (S > most) S = most;
+    if (S < 1) S = 1;
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "attention over pages: rows * Hkv = %lld", items);
     p.cluster = S;
     void (*kernel)(const PagesParams) = d->head_dim == 128 ? attn_decode_pages_kernel<128> : attn_decode_pages_kernel<64>;
+    const int smem = d->head_dim == 128 ? PagesRing<128>::kBytes : PagesRing<64>::kBytes;
+    if (!ctx->pages_attr_set[d->head_dim == 128]) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(attention over pages)");
+        ctx->pages_attr_set[d->head_dim == 128] = true;
+    }
     KernelScope scope(ctx, kKAttnPages, st);
-    return check_cuda(ctx, launch_cluster(kernel, items * S, kPagesThreads, 0, S, st, p), "attn_decode_pages_kernel launch");
+    return check_cuda(ctx, launch_cluster(kernel, items * S, kPagesThreads, smem, S, st, p), "attn_decode_pages_kernel launch");
 }
 
 }  // namespace aflex

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kBoundsThreads) rope_append_bounds_kernel(cons
     typedef Lanes<D> L;
     constexpr int kHalf = D / 2;
     __shared__ int s_warp[kBoundsWarps];
-    __shared__ int s_b, s_page, s_total;
+    __shared__ int s_b, s_page;
     __shared__ float2 s_rot[kPageTokens][kHalf];                    // (cos, sin), queries
     __shared__ double2 s_rotd[kPageTokens][kHalf];                  // keys
     pdl_wait();
