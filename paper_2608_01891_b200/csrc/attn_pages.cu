@@ -4,6 +4,7 @@
 // A row is one query token: the one being decoded, or one of the last few of its sequence (drafted tokens).
 #include <cuda_bf16.h>
 #include <math.h>
+#include <stdlib.h>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -15,13 +16,12 @@ namespace {
 constexpr int kPageTokens = 16;
 constexpr float kNegBig = -1.0e30f;
 
-// Sequence and position of a row; every lane of a warp takes part.  `ok` is false where the inputs give none.  Rows behind the
-// last sequence's are padding: nothing is to be read, written or reported for them.
-struct RowAt { int b, pos; bool ok, padding; };
-__device__ __forceinline__ RowAt locate_row(int row, const int32_t* q_offsets, const int32_t* seq_lens, int batch, int max_pages) {
-    RowAt at;
-    int back = 0;
-    at.b = row; at.padding = false;
+// Sequence of a row, and how many of the sequence's rows follow it; every lane of a warp takes part.  Rows behind the last
+// sequence's are padding: nothing is to be read, written or reported for them.
+struct RowSeq { int b, back; bool padding; };
+__device__ __forceinline__ RowSeq locate_row(int row, const int32_t* q_offsets, int batch) {
+    RowSeq at;
+    at.b = row; at.back = 0; at.padding = false;
     if (q_offsets != nullptr) {
         // largest b with q_offsets[b] <= row: the lanes look at 32 sequences at a time (one load's latency for up to 32)
         const int lane = threadIdx.x & 31, end = __ldg(q_offsets + batch);
@@ -29,18 +29,20 @@ __device__ __forceinline__ RowAt locate_row(int row, const int32_t* q_offsets, c
         while (span > 1) {
             const int step = (span + 31) / 32, i = lane * step;
             const unsigned le = __ballot_sync(0xffffffffu, i < span && __ldg(q_offsets + lo + (i < span ? i : 0)) <= row);
-            const int at_step = max(__popc(le) - 1, 0) * step;
-            lo += at_step;
-            span = min(step, span - at_step);
+            const int skip = max(__popc(le) - 1, 0) * step;
+            lo += skip;
+            span = min(step, span - skip);
         }
         at.b = lo;
+        at.back = __ldg(q_offsets + lo + 1) - 1 - row;
         at.padding = row >= end;
-        back = __ldg(q_offsets + lo + 1) - 1 - row;
     }
-    const int len = __ldg(seq_lens + at.b);
-    at.pos = len - 1 - back;
-    at.ok = !at.padding && back >= 0 && at.pos >= 0 && len <= max_pages * kPageTokens;
     return at;
+}
+// Position of the row in its sequence of `len` tokens; -1 where the inputs give none.
+__device__ __forceinline__ int row_position(const RowSeq& at, int len, int max_pages) {
+    const int pos = len - 1 - at.back;
+    return !at.padding && at.back >= 0 && pos >= 0 && len <= max_pages * kPageTokens ? pos : -1;
 }
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
@@ -82,13 +84,18 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t 
 // bit for bit whatever computes it.
 //
 // One cluster of CTAs per (row, KV head); each warp scores tiles of 16 pages with integer MMAs, operands loaded from global
-// memory straight into registers (the bounds' layout is the fragment's), and drops the scores as order-preserving keys into
-// the first CTA's shared memory.  That CTA then finds the key of the last page to keep by radix selection and writes the list.
-constexpr int kSelWarps = 8;
-constexpr int kSelThreads = kSelWarps * 32;
+// memory straight into registers (the bounds' layout is the fragment's), two tiles in flight, and drops the scores as
+// order-preserving keys into the first CTA's shared memory.  That CTA then looks for the last key to keep: a histogram of 256
+// equal intervals between the smallest and the largest key tells the interval it lies in, the few keys of that interval are
+// ranked by comparing all pairs (a crowded interval is divided again; a crowd of equal keys is divided by page).
+//
+// Bound: with hundreds of pages the chain of dependent steps (lengths and page ids -> bounds -> keys -> interval -> rank ->
+// list), not the bytes; so as much as possible is loaded before it is known to be needed, and barriers are few.
 constexpr int kSelTile = 16;
 constexpr int kSelKeyCap = 48 * 1024;               // keys one CTA's shared memory holds; further ones go to the next CTA's
 constexpr int kSelMaxCluster = 8;
+constexpr int kSelTiles = 2;                        // tiles a warp has in flight
+constexpr int kSelRank = 256;                       // keys that are ranked by comparing all pairs
 
 struct SelectParams {
     const __nv_bfloat16* q;        // [rows][Hq][D]
@@ -107,11 +114,17 @@ struct SelectParams {
     int* status;
 };
 
-struct SelectShared {
-    int hist[256];
-    int warp_a[kSelWarps], warp_b[kSelWarps];
-    uint32_t all_or, all_and;
-    int bin, need;
+template <int W> struct SelectShared {
+    uint4 q[4][32];                // quantised queries as the lanes' B operands: two words of positive parts, two of negative
+    float f[4][8];                 // 2^f per block and head
+    __align__(16) int hist[256];
+    uint2 range[kSelMaxCluster * W];       // smallest and largest key of every warp of the cluster
+    uint32_t rank_key[kSelRank];
+    int rank_page[kSelRank];
+    int ranked;                    // entries of rank_*
+    uint32_t last_key;             // the last one to keep
+    int last_page;
+    int kept[W];
 };
 
 __device__ __forceinline__ int q_exponent(float a) {             // smallest e with a <= 127 * 2^e, within [-60, 50]
@@ -121,29 +134,48 @@ __device__ __forceinline__ int q_exponent(float a) {             // smallest e w
     return max(-60, min(50, e));
 }
 
-template <int D>
-__global__ void __launch_bounds__(kSelThreads) page_select_kernel(const SelectParams p) {
+template <int D, int W>
+__global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams p) {
     constexpr int kBlocks = D / 32;
+    constexpr int kThreads = W * 32;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     uint32_t* keys = reinterpret_cast<uint32_t*>(smem_raw);
-    __shared__ SelectShared sh;
+    __shared__ SelectShared<W> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int S = p.cluster, rank = (int)(blockIdx.x % S);
     const long long item = blockIdx.x / S;
     const int row = (int)(item / p.Hkv), g = (int)(item % p.Hkv);
+    const int hl = lane >> 2, l4 = lane & 3;
     if (S > 1) cluster_arrive();                                  // the cluster's CTAs have started: waited for below
+    if (tid < 256) sh.hist[tid] = 0;
+    if (tid == 0) sh.ranked = 0;
     pdl_launch_dependents();
     pdl_wait();
-    const RowAt at = locate_row(row, p.q_offsets, p.seq_lens, p.batch, p.max_pages);
-    const int n = at.ok ? at.pos / kPageTokens + 1 : 0;
-    if (!at.ok && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    // The first four warps quantise a block of the queries each: lane holds head lane / 4, channels 8 (lane % 4) .. + 7.
+    const bool quantises = warp < kBlocks;
+    uint4 qx = make_uint4(0, 0, 0, 0);
+    if (quantises && hl < p.G)
+        qx = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + hl) * D) + warp * 4 + l4);
+    // This warp's tiles are t, t + stride, ...; the lanes hold the page ids of two of them (lane / 16).
+    const RowSeq at = locate_row(row, p.q_offsets, p.batch);
+    const int len = __ldg(p.seq_lens + at.b);
+    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
+    const int stride = S * W;
+    auto page_ids = [&](int t) -> int {                           // (whatever the table's row holds beyond the sequence)
+        const long long j = p.sink + (long long)(t + (lane >> 4) * stride) * kSelTile + (lane & 15);
+        return __ldg(table + min(j, (long long)p.max_pages - 1));
+    };
+    int t = rank * W + warp;
+    int ids = page_ids(t);
+    const int pos = row_position(at, len, p.max_pages), n = pos >= 0 ? pos / kPageTokens + 1 : 0;
+    if (pos < 0 && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
     int32_t* list = p.list + item * p.top;
     const int keep = p.top - p.sink - p.window;                   // scored pages to keep
     const int cand = n - p.sink - p.window;                       // scored pages
     if (n <= p.top || keep == 0) {                                // nothing to choose (the same for the whole cluster)
         if (S > 1) cluster_wait();
         if (rank != 0 || at.padding) return;
-        for (int i = tid; i < p.top; i += kSelThreads) {
+        for (int i = tid; i < p.top; i += kThreads) {
             int v = i < n ? i : -1;
             if (n > p.top && i >= p.sink) v = n - p.top + i;
             list[i] = v;
@@ -151,103 +183,111 @@ __global__ void __launch_bounds__(kSelThreads) page_select_kernel(const SelectPa
         if (tid == 0) p.count[item] = min(n, p.top);
         return;
     }
-    // ---- the group's queries as the MMA's B operand: lane holds head lane / 4, channels 8 (lane % 4) .. + 7 of every block
-    const int hl = lane >> 2, l4 = lane & 3;
-    uint32_t qp[kBlocks][2], qn[kBlocks][2];
-    float fq[kBlocks][2];                                         // 2^f of this lane's two accumulator columns
-    {
-        const bool on = hl < p.G;
-        const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + (on ? hl : 0)) * D);
+    if (quantises) {
+        const __nv_bfloat162* px = reinterpret_cast<const __nv_bfloat162*>(&qx);
+        float v[8], a = 0.f;
 #pragma unroll
-        for (int c = 0; c < kBlocks; ++c) {
-            const uint4 x = src[c * 4 + l4];
-            const __nv_bfloat162* px = reinterpret_cast<const __nv_bfloat162*>(&x);
-            float v[8], a = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 u = __bfloat1622float2(px[i]);
-                v[2 * i] = u.x; v[2 * i + 1] = u.y;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!on || v[i] != v[i]) v[i] = 0.f;              // NaN counts as 0
-                a = fmaxf(a, fabsf(v[i]));
-            }
-            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
-            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
-            const int e = q_exponent(a);
-            const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-            uint32_t pos[2] = {0, 0}, neg[2] = {0, 0};
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int z = (int)rintf(fminf(127.f, fmaxf(-127.f, v[i] * inv)));
-                pos[i >> 2] |= (uint32_t)max(z, 0) << (8 * (i & 3));
-                neg[i >> 2] |= (uint32_t)(min(z, 0) & 255) << (8 * (i & 3));
-            }
-            qp[c][0] = pos[0]; qp[c][1] = pos[1];
-            qn[c][0] = neg[0]; qn[c][1] = neg[1];
-            const float f = __uint_as_float((uint32_t)(127 + e) << 23);
-            fq[c][0] = __shfl_sync(0xffffffffu, f, 8 * l4);       // columns 2 l4 and 2 l4 + 1 of the accumulator
-            fq[c][1] = __shfl_sync(0xffffffffu, f, 8 * l4 + 4);
+        for (int i = 0; i < 4; ++i) {
+            const float2 u = __bfloat1622float2(px[i]);
+            v[2 * i] = u.x; v[2 * i + 1] = u.y;
+            a = fmaxf(a, fmaxf(fabsf(u.x), fabsf(u.y)));          // (a NaN is passed over)
         }
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+        const int e = q_exponent(a);
+        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+        uint32_t w[2], neg[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            int z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) z[k] = max(-127, min(127, __float2int_rn(v[4 * i + k] * inv)));        // NaN becomes 0
+            w[i] = __byte_perm(__byte_perm(z[0], z[1], 0x0040), __byte_perm(z[2], z[3], 0x0040), 0x5410);
+            neg[i] = w[i] & (((w[i] & 0x80808080u) >> 7) * 255u);                                               // bytes below zero
+        }
+        sh.q[warp][lane] = make_uint4(w[0] & ~neg[0], w[1] & ~neg[1], neg[0], neg[1]);
+        if (l4 == 0) sh.f[warp][hl] = __uint_as_float((uint32_t)(127 + e) << 23);
+    }
+    __syncthreads();
+    uint4 qf[kBlocks];
+    float2 fq[kBlocks];                                           // of this lane's two accumulator columns
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+        qf[c] = sh.q[c][lane];
+        fq[c] = *reinterpret_cast<const float2*>(&sh.f[c][2 * l4]);
     }
     if (S > 1) cluster_wait();
     // ---- scores
-    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages + p.sink;
     const int tiles = (cand + kSelTile - 1) / kSelTile;
     const uint32_t keys_addr = smem_u32(keys);
-    for (int t = rank * kSelWarps + warp; t < tiles; t += S * kSelWarps) {
-        size_t slab[2];
+    const bool h0 = 2 * l4 < p.G, h1 = 2 * l4 + 1 < p.G;
+    uint32_t least = 0xffffffffu, most = 0u;
+    while (t < tiles) {
+        uint4 x[kSelTiles][2][kBlocks];
+        uint32_t sc[kSelTiles][2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int j = t * kSelTile + hl + 8 * r;
-            int id = table[min(j, cand - 1)];
-            if (id < 0 || id >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
-            slab[r] = (size_t)id * p.Hkv + g;
+        for (int k = 0; k < kSelTiles; ++k) {
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int j = (t + k * stride) * kSelTile + hl + 8 * r;
+                int id = __shfl_sync(0xffffffffu, ids, k * 16 + hl + 8 * r);
+                if (j >= cand) id = 0;                            // past the last candidate: some page, its score is dropped
+                if (id < 0 || id >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
+                const size_t slab = (size_t)id * p.Hkv + g;
+                const uint4* src = reinterpret_cast<const uint4*>(p.codes + slab * (2 * D)) + l4;
+#pragma unroll
+                for (int c = 0; c < kBlocks; ++c) x[k][r][c] = __ldg(src + c * 4);
+                if (kBlocks == 4) sc[k][r] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + slab);
+                else sc[k][r] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + slab);
+            }
         }
-        uint4 x[2][kBlocks];
-        uint32_t sc[2];
+        const int t_now = t;
+        t += kSelTiles * stride;
+        if (t < tiles) ids = page_ids(t);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const uint4* src = reinterpret_cast<const uint4*>(p.codes + slab[r] * (2 * D)) + l4;
+        for (int k = 0; k < kSelTiles; ++k) {
+            float s[4];
 #pragma unroll
-            for (int c = 0; c < kBlocks; ++c) x[r][c] = __ldg(src + c * 4);
-            if (kBlocks == 4) sc[r] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + slab[r]);
-            else sc[r] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + slab[r]);
-        }
-        float s[4];
-#pragma unroll
-        for (int c = 0; c < kBlocks; ++c) {
-            int d[4] = {0, 0, 0, 0};
-            mma_s8_16832(d, x[0][c].x, x[1][c].x, x[0][c].y, x[1][c].y, qp[c][0], qp[c][1]);
-            mma_s8_16832(d, x[0][c].z, x[1][c].z, x[0][c].w, x[1][c].w, qn[c][0], qn[c][1]);
-            const float k0 = __uint_as_float(((sc[0] >> (8 * c)) & 255u) << 23), k1 = __uint_as_float(((sc[1] >> (8 * c)) & 255u) << 23);
-            // the products are exact, so a fused multiply-add rounds like the sum alone
-            s[0] = fmaf((float)d[0] * k0, fq[c][0], c ? s[0] : 0.f);
-            s[1] = fmaf((float)d[1] * k0, fq[c][1], c ? s[1] : 0.f);
-            s[2] = fmaf((float)d[2] * k1, fq[c][0], c ? s[2] : 0.f);
-            s[3] = fmaf((float)d[3] * k1, fq[c][1], c ? s[3] : 0.f);
-        }
-        const bool h0 = 2 * l4 < p.G, h1 = 2 * l4 + 1 < p.G;
-        float m0 = fmaxf(h0 ? s[0] : -INFINITY, h1 ? s[1] : -INFINITY);
-        float m1 = fmaxf(h0 ? s[2] : -INFINITY, h1 ? s[3] : -INFINITY);
-        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
-        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
-        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
-        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
-        if (l4 < 2) {
-            const int j = t * kSelTile + hl + 8 * l4;
-            if (j < cand) {
-                uint32_t u = __float_as_uint((l4 ? m1 : m0) + 0.f);          // no negative zero
-                u ^= (u >> 31) ? 0xffffffffu : 0x80000000u;                 // unsigned order = numeric order
-                const int owner = j / p.cap;
+            for (int c = 0; c < kBlocks; ++c) {
+                int d[4] = {0, 0, 0, 0};
+                mma_s8_16832(d, x[k][0][c].x, x[k][1][c].x, x[k][0][c].y, x[k][1][c].y, qf[c].x, qf[c].y);
+                mma_s8_16832(d, x[k][0][c].z, x[k][1][c].z, x[k][0][c].w, x[k][1][c].w, qf[c].z, qf[c].w);
+                const float k0 = __uint_as_float(((sc[k][0] >> (8 * c)) & 255u) << 23), k1 = __uint_as_float(((sc[k][1] >> (8 * c)) & 255u) << 23);
+                // the products are exact, so a fused multiply-add rounds like the sum alone
+                s[0] = fmaf((float)d[0] * k0, fq[c].x, c ? s[0] : 0.f);
+                s[1] = fmaf((float)d[1] * k0, fq[c].y, c ? s[1] : 0.f);
+                s[2] = fmaf((float)d[2] * k1, fq[c].x, c ? s[2] : 0.f);
+                s[3] = fmaf((float)d[3] * k1, fq[c].y, c ? s[3] : 0.f);
+            }
+            float m0 = fmaxf(h0 ? s[0] : -INFINITY, h1 ? s[1] : -INFINITY);
+            float m1 = fmaxf(h0 ? s[2] : -INFINITY, h1 ? s[3] : -INFINITY);
+            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
+            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
+            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
+            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
+            const int j = (t_now + k * stride) * kSelTile + hl + 8 * l4;
+            if (l4 < 2 && j < cand) {
+                uint32_t u = __float_as_uint((l4 ? m1 : m0) + 0.f);              // no negative zero
+                u ^= (u >> 31) ? 0xffffffffu : 0x80000000u;                     // unsigned order = numeric order
+                least = min(least, u);
+                most = max(most, u);
                 if (S == 1) keys[j] = u;
-                else st_cluster_u32(cluster_map_shared(keys_addr + (uint32_t)(j - owner * p.cap) * 4, (uint32_t)owner), u);
+                else {
+                    const int owner = j / p.cap;
+                    st_cluster_u32(cluster_map_shared(keys_addr + (uint32_t)(j - owner * p.cap) * 4, (uint32_t)owner), u);
+                }
             }
         }
     }
+    least = __reduce_min_sync(0xffffffffu, least);
+    most = __reduce_max_sync(0xffffffffu, most);
     const bool far = cand > p.cap;                                 // some keys are in another CTA's shared memory
     if (S > 1) {
+        if (lane == 0) {
+            const uint32_t to = cluster_map_shared(smem_u32(&sh.range[rank * W + warp]), 0u);
+            st_cluster_u32(to, least);
+            st_cluster_u32(to + 4, most);
+        }
         cluster_arrive();
         cluster_wait();
         if (rank != 0) {
@@ -255,86 +295,125 @@ __global__ void __launch_bounds__(kSelThreads) page_select_kernel(const SelectPa
             return;
         }
     } else {
+        if (lane == 0) sh.range[warp] = make_uint2(least, most);
         __syncthreads();
     }
+    // ---- selection, by this CTA alone
     auto key_at = [&](int j) -> uint32_t {
         if (!far) return keys[j];
         const int owner = j / p.cap;
         return ld_cluster_u32(cluster_map_shared(keys_addr + (uint32_t)(j - owner * p.cap) * 4, (uint32_t)owner));
     };
-    // ---- radix selection of the keep-th largest key, eight bits at a time from the highest bit in which keys differ
-    uint32_t o = 0, a = 0xffffffffu;
-    for (int j = tid; j < cand; j += kSelThreads) { const uint32_t k = key_at(j); o |= k; a &= k; }
-    o = __reduce_or_sync(0xffffffffu, o);
-    a = __reduce_and_sync(0xffffffffu, a);
-    if (tid == 0) { sh.all_or = 0; sh.all_and = 0xffffffffu; }
-    __syncthreads();
-    if (lane == 0) { atomicOr(&sh.all_or, o); atomicAnd(&sh.all_and, a); }
-    __syncthreads();
-    uint32_t prefix = sh.all_and, mask;                            // keys are compared in the bits of `mask`
-    int need = keep;                                               // of the keys that equal prefix in those bits
-    const uint32_t differ = sh.all_or ^ sh.all_and;
-    int bits = differ ? 32 - __clz(differ) : 0;                    // unresolved low bits
-    mask = bits == 32 ? 0u : ~((1u << bits) - 1u);
-    prefix &= mask;
-    while (bits > 0) {
-        const int shift = max(bits - 8, 0);
-        sh.hist[tid] = 0;
-        __syncthreads();
-        for (int j = tid; j < cand; j += kSelThreads) {
-            const uint32_t k = key_at(j);
-            if ((k & mask) == prefix) atomicAdd(&sh.hist[(k & ~mask) >> shift], 1);
+    for (int i = lane; i < S * W; i += 32) {
+        const uint2 r = sh.range[i];
+        least = min(least, r.x);
+        most = max(most, r.y);
+    }
+    uint32_t lo = __reduce_min_sync(0xffffffffu, least), hi = __reduce_max_sync(0xffffffffu, most);
+    // Of what lies in [lo, hi] -- keys, or once `equal` is set the mirrored pages of the keys that equal it -- the `need`
+    // largest are to be kept, and all that lies above.
+    int need = keep;
+    bool by_page = false;
+    uint32_t equal = 0, last_key;
+    int last_page;
+    while (true) {
+        const int shift = max(0, 24 - __clz(hi - lo));
+#pragma unroll 4
+        for (int j = tid; j < cand; j += kThreads) {
+            const uint32_t k = key_at(j), v = by_page ? (uint32_t)(cand - 1 - j) : k;
+            if (v >= lo && v <= hi && (!by_page || k == equal)) atomicAdd(&sh.hist[(v - lo) >> shift], 1);
         }
         __syncthreads();
-        // thread t looks at bin 255 - t: keys in it and above it
-        const int c = sh.hist[255 - tid];
-        int incl = c;
+        // every warp finds the interval by itself: lane i counts intervals 255 - 8 i .. 248 - 8 i and those above them
+        const int4 c0 = *reinterpret_cast<const int4*>(&sh.hist[248 - 8 * lane]), c1 = *reinterpret_cast<const int4*>(&sh.hist[252 - 8 * lane]);
+        const int c[8] = {c1.w, c1.z, c1.y, c1.x, c0.w, c0.z, c0.y, c0.x};
+        const int sum = c[0] + c[1] + c[2] + c[3] + c[4] + c[5] + c[6] + c[7];
+        int incl = sum;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
-        if (lane == 31) sh.warp_a[warp] = incl;
+        int above = incl - sum, bin = 0, inside = 0;
+        const unsigned holds = __ballot_sync(0xffffffffu, above < need && incl >= need);
+        const int from = __ffs(holds) - 1;
+        if (lane == from) {
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (!found && above + c[i] >= need) { found = true; bin = 255 - 8 * lane - i; inside = c[i]; }
+                if (!found) above += c[i];
+            }
+        }
+        above = __shfl_sync(0xffffffffu, above, from);
+        bin = __shfl_sync(0xffffffffu, bin, from);
+        inside = __shfl_sync(0xffffffffu, inside, from);
+        need -= above;
+        lo += (uint32_t)bin << shift;
+        hi = min(hi, lo + ((1u << shift) - 1u));
+        if (inside == need) {                                      // the interval is kept whole
+            last_key = by_page ? equal : lo;
+            last_page = by_page ? cand - 1 - (int)lo : 0x7fffffff;
+            break;
+        }
+        if (inside <= kSelRank) {
+#pragma unroll 4
+            for (int j = tid; j < cand; j += kThreads) {
+                const uint32_t k = key_at(j), v = by_page ? (uint32_t)(cand - 1 - j) : k;
+                if (v >= lo && v <= hi && (!by_page || k == equal)) {
+                    const int i = atomicAdd(&sh.ranked, 1);
+                    sh.rank_key[i] = k;
+                    sh.rank_page[i] = j;
+                }
+            }
+            __syncthreads();
+            if (tid < inside) {
+                const uint32_t k = sh.rank_key[tid];
+                const int j = sh.rank_page[tid];
+                int before = 0;
+                for (int i = 0; i < inside; ++i) {
+                    const uint32_t ki = sh.rank_key[i];
+                    before += ki > k || (ki == k && sh.rank_page[i] < j);
+                }
+                if (before == need - 1) { sh.last_key = k; sh.last_page = j; }
+            }
+            __syncthreads();
+            last_key = sh.last_key;
+            last_page = sh.last_page;
+            break;
+        }
+        if (shift == 0 && !by_page) {                              // a crowd of equal keys: the lowest pages go first
+            by_page = true;
+            equal = lo;
+            lo = 0;
+            hi = (uint32_t)(cand - 1);
+        }
+        __syncthreads();                                           // everybody has read the histogram
+        if (tid < 256) sh.hist[tid] = 0;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) incl += sh.warp_a[w];
-        if (incl >= need && incl - c < need) { sh.bin = 255 - tid; sh.need = need - (incl - c); sh.warp_b[0] = c; }
-        __syncthreads();
-        prefix |= (uint32_t)sh.bin << shift;
-        need = sh.need;
-        bits = shift;
-        mask = bits == 0 ? 0xffffffffu : ~((1u << bits) - 1u);
-        const bool whole = sh.warp_b[0] == need;                   // the bin is kept whole: no need to look inside
-        __syncthreads();
-        if (whole) break;
     }
     // ---- the list, ascending: each warp places a contiguous run of the candidates
-    const int run = ((cand + kSelThreads - 1) / kSelThreads) * 32;
-    const int j0 = min(cand, warp * run), j1 = min(cand, j0 + run);
-    int gt = 0, eq = 0;
+    const int run = (cand + kThreads - 1) / kThreads * 32, j0 = warp * run, j1 = min(cand, j0 + run);
+    int kept = 0;
+#pragma unroll 4
     for (int j = j0 + lane; j < j1; j += 32) {
-        const uint32_t k = key_at(j) & mask;
-        gt += k > prefix;
-        eq += k == prefix;
+        const uint32_t k = key_at(j);
+        kept += k > last_key || (k == last_key && j <= last_page);
     }
-    gt = __reduce_add_sync(0xffffffffu, gt);
-    eq = __reduce_add_sync(0xffffffffu, eq);
-    if (lane == 0) { sh.warp_a[warp] = gt; sh.warp_b[warp] = eq; }
+    kept = __reduce_add_sync(0xffffffffu, kept);
+    if (lane == 0) sh.kept[warp] = kept;
     __syncthreads();
-    int gt0 = 0, eq0 = 0;
-    for (int w = 0; w < warp; ++w) { gt0 += sh.warp_a[w]; eq0 += sh.warp_b[w]; }
-    for (int j = j0; j < j1; j += 32) {
-        const bool in = j + lane < j1;
-        const uint32_t k = in ? key_at(j + lane) & mask : 0u;
-        const bool is_gt = in && k > prefix, is_eq = in && k == prefix;
-        const unsigned bg = __ballot_sync(0xffffffffu, is_gt), be = __ballot_sync(0xffffffffu, is_eq);
-        const unsigned below = (1u << lane) - 1u;
-        const int g_at = gt0 + __popc(bg & below), e_at = eq0 + __popc(be & below);
-        if (is_gt || (is_eq && e_at < need)) list[p.sink + g_at + min(e_at, need)] = p.sink + j + lane;
-        gt0 += __popc(bg);
-        eq0 += __popc(be);
+    int32_t* to = list + p.sink + __reduce_add_sync(0xffffffffu, lane < warp ? sh.kept[lane] : 0);
+    for (int s = j0; s < j1; s += 32) {
+        const int j = s + lane;
+        const uint32_t k = j < j1 ? key_at(j) : 0u;
+        const bool keeps = j < j1 && (k > last_key || (k == last_key && j <= last_page));
+        const unsigned who = __ballot_sync(0xffffffffu, keeps);
+        if (keeps) to[__popc(who & ((1u << lane) - 1u))] = p.sink + j;
+        to += __popc(who);
     }
-    for (int i = tid; i < p.sink; i += kSelThreads) list[i] = i;
-    for (int i = tid; i < p.window; i += kSelThreads) list[p.top - p.window + i] = n - p.window + i;
+    for (int i = tid; i < p.sink; i += kThreads) list[i] = i;
+    for (int i = tid; i < p.window; i += kThreads) list[p.top - p.window + i] = n - p.window + i;
     if (tid == 0) p.count[item] = p.top;
     if (far) { cluster_arrive(); cluster_wait(); }
 }
@@ -434,10 +513,11 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
 #pragma unroll
         for (int c = 0; c < kSteps; ++c) qf[c] = __ldg(src + c * 4 + l4);
     }
-    const RowAt at = locate_row(row, p.q_offsets, p.seq_lens, p.batch, p.max_pages);
+    const RowSeq at = locate_row(row, p.q_offsets, p.batch);
     if (at.padding) return;                        // (the same for the whole cluster)
-    if (!at.ok && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
-    const int n = at.ok ? max(0, (total - first + stride - 1) / stride) : 0;           // this warp's pages
+    const int pos = row_position(at, __ldg(p.seq_lens + at.b), p.max_pages);
+    if (pos < 0 && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    const int n = pos >= 0 ? max(0, (total - first + stride - 1) / stride) : 0;        // this warp's pages
     const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
     if (hl >= p.G) {
 #pragma unroll
@@ -450,9 +530,9 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
         if ((i & 31) == 0) {                       // look up the next 32 entries, and load the 32 after them
             phys = 0; valid = 0;
             if (i + lane < n) {
-                if (next >= 0 && next <= at.pos / kPageTokens) {
+                if (next >= 0 && next <= pos / kPageTokens) {
                     phys = __ldg(table + next);
-                    valid = min(kPageTokens, at.pos - next * kPageTokens + 1);
+                    valid = min(kPageTokens, pos - next * kPageTokens + 1);
                 }
                 if (valid == 0 || phys < 0 || phys >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); phys = 0; valid = 0; }
             }
@@ -658,21 +738,27 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.list = page_list; p.count = page_count; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
     int S = 1;
-    while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelKeyCap) && p.max_pages > S * kSelWarps * kSelTile) S *= 2;
+    while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelKeyCap) && p.max_pages > S * 8 * kSelTile) S *= 2;
+    const bool wide = getenv("SW") ? atoi(getenv("SW")) : (items * S <= ctx->num_sms);
+    if (getenv("SS")) S = atoi(getenv("SS"));
     if (p.max_pages > (long long)S * kSelKeyCap)
         return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", p.max_pages, kSelMaxCluster * kSelKeyCap);
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
     p.cluster = S;
     p.cap = kSelKeyCap < p.max_pages ? kSelKeyCap : p.max_pages;
     const size_t smem = (size_t)p.cap * 4;
-    void (*kernel)(const SelectParams) = d->head_dim == 128 ? page_select_kernel<128> : page_select_kernel<64>;
-    if (!ctx->select_attr_set[d->head_dim == 128]) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeyCap * 4);
-        if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
-        ctx->select_attr_set[d->head_dim == 128] = true;
+    typedef void (*Kernel)(const SelectParams);
+    const Kernel kernels[2][2] = {{page_select_kernel<64, 8>, page_select_kernel<64, 16>}, {page_select_kernel<128, 8>, page_select_kernel<128, 16>}};
+    const int di = d->head_dim == 128;
+    if (!ctx->select_attr_set[di]) {
+        for (int w = 0; w < 2; ++w) {
+            cudaError_t e = cudaFuncSetAttribute(kernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeyCap * 4);
+            if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
+        }
+        ctx->select_attr_set[di] = true;
     }
     KernelScope scope(ctx, kKPageSelect, st);
-    return check_cuda(ctx, launch_cluster(kernel, items * S, kSelThreads, smem, S, st, p), "page_select_kernel launch");
+    return check_cuda(ctx, launch_cluster(kernels[di][wide], items * S, wide ? 512 : 256, smem, S, st, p), "page_select_kernel launch");
 }
 
 aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
