@@ -4,7 +4,6 @@
 // A row is one query token: the one being decoded, or one of the last few of its sequence (drafted tokens).
 #include <cuda_bf16.h>
 #include <math.h>
-#include <stdlib.h>
 
 #include "internal.h"
 #include "ptx.cuh"
@@ -50,6 +49,9 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
+__device__ __forceinline__ void st_cluster_v2(uint32_t addr, uint32_t x, uint32_t y) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
+}
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
     uint32_t v;
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
@@ -83,19 +85,20 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t 
 // group's heads.  i_c is an integer below 2^19 and v_c exact in fp32, so the score, and with it the selection, is the same
 // bit for bit whatever computes it.
 //
-// One cluster of CTAs per (row, KV head); each warp scores tiles of 16 pages with integer MMAs, operands loaded from global
-// memory straight into registers (the bounds' layout is the fragment's), two tiles in flight, and drops the scores as
-// order-preserving keys into the first CTA's shared memory.  That CTA then looks for the last key to keep: a histogram of 256
-// equal intervals between the smallest and the largest key tells the interval it lies in, the few keys of that interval are
-// ranked by comparing all pairs (a crowded interval is divided again; a crowd of equal keys is divided by page).
+// One cluster of CTAs per (row, KV head), a contiguous share of the candidate pages each; a warp scores tiles of 16 pages with
+// integer MMAs, operands loaded from global memory straight into registers (the bounds' layout is the fragment's), and leaves
+// the scores in shared memory.  A histogram of 256 equal intervals between the lowest and the highest score, summed over the
+// cluster, tells the interval that holds the last page to keep, and the few pages of that interval are ranked by comparing all
+// pairs (a crowded interval is divided again, by the scores' bits; a crowd of equal scores by page).  Every CTA draws the same
+// conclusions and writes its share of the list.
 //
-// Bound: with hundreds of pages the chain of dependent steps (lengths and page ids -> bounds -> keys -> interval -> rank ->
-// list), not the bytes; so as much as possible is loaded before it is known to be needed, and barriers are few.
+// Bound: with hundreds of pages the chain of dependent steps (lengths and page ids -> bounds -> scores -> interval -> rank ->
+// list), not the bytes; so as much as possible is loaded before it is known to be needed, and barriers are few.  A score
+// takes some 60 instructions on its way through the selection, which is why a long row's selection is spread over the cluster.
 constexpr int kSelTile = 16;
-constexpr int kSelKeyCap = 48 * 1024;               // keys one CTA's shared memory holds; further ones go to the next CTA's
+constexpr int kSelCap = 48 * 1024;                  // scores one CTA's shared memory holds
 constexpr int kSelMaxCluster = 8;
-constexpr int kSelTiles = 2;                        // tiles a warp has in flight
-constexpr int kSelRank = 256;                       // keys that are ranked by comparing all pairs
+constexpr int kSelRank = 64;                        // members of an interval that are ranked by comparing all pairs
 
 struct SelectParams {
     const __nv_bfloat16* q;        // [rows][Hq][D]
@@ -108,7 +111,6 @@ struct SelectParams {
     long long num_pages;
     int top, sink, window;
     int cluster;                   // CTAs per (row, KV head)
-    int cap;                       // keys per CTA
     int32_t* list;                 // [rows][Hkv][top]
     int32_t* count;                // [rows][Hkv]
     int* status;
@@ -117,14 +119,18 @@ struct SelectParams {
 template <int W> struct SelectShared {
     uint4 q[4][32];                // quantised queries as the lanes' B operands: two words of positive parts, two of negative
     float f[4][8];                 // 2^f per block and head
-    __align__(16) int hist[256];
-    uint2 range[kSelMaxCluster * W];       // smallest and largest key of every warp of the cluster
-    uint32_t rank_key[kSelRank];
-    int rank_page[kSelRank];
-    int ranked;                    // entries of rank_*
-    uint32_t last_key;             // the last one to keep
+    __align__(16) int hist[256];   // this CTA's
+    __align__(16) int sum[256];    // the cluster's
+    uint2 range[W];                // lowest and highest score of every warp, as ordered bits
+    uint2 all_range[kSelMaxCluster];
+    int members;                   // of the interval that is ranked, in this CTA
+    int all_members[kSelMaxCluster];
+    uint2 member[kSelMaxCluster][kSelRank];        // (score, page) of every CTA's
+    uint2 rank[kSelRank];          // all of them in one piece
+    float last_score;              // the last one to keep
     int last_page;
-    int kept[W];
+    int kept[W];                   // of every warp's run
+    int all_kept[kSelMaxCluster];  // of every CTA
 };
 
 __device__ __forceinline__ int q_exponent(float a) {             // smallest e with a <= 127 * 2^e, within [-60, 50]
@@ -134,12 +140,13 @@ __device__ __forceinline__ int q_exponent(float a) {             // smallest e w
     return max(-60, min(50, e));
 }
 
-template <int D, int W>
-__global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams p) {
+// W warps, T tiles per warp in flight.
+template <int D, int W, int T>
+__global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_select_kernel(const SelectParams p) {
     constexpr int kBlocks = D / 32;
     constexpr int kThreads = W * 32;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    uint32_t* keys = reinterpret_cast<uint32_t*>(smem_raw);
+    float* scores = reinterpret_cast<float*>(smem_raw);            // of this CTA's candidates
     __shared__ SelectShared<W> sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int S = p.cluster, rank = (int)(blockIdx.x % S);
@@ -148,7 +155,7 @@ __global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams 
     const int hl = lane >> 2, l4 = lane & 3;
     if (S > 1) cluster_arrive();                                  // the cluster's CTAs have started: waited for below
     if (tid < 256) sh.hist[tid] = 0;
-    if (tid == 0) sh.ranked = 0;
+    if (tid == 0) sh.members = 0;
     pdl_launch_dependents();
     pdl_wait();
     // The first four warps quantise a block of the queries each: lane holds head lane / 4, channels 8 (lane % 4) .. + 7.
@@ -156,17 +163,16 @@ __global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams 
     uint4 qx = make_uint4(0, 0, 0, 0);
     if (quantises && hl < p.G)
         qx = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + hl) * D) + warp * 4 + l4);
-    // This warp's tiles are t, t + stride, ...; the lanes hold the page ids of two of them (lane / 16).
     const RowSeq at = locate_row(row, p.q_offsets, p.batch);
     const int len = __ldg(p.seq_lens + at.b);
     const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
-    const int stride = S * W;
-    auto page_ids = [&](int t) -> int {                           // (whatever the table's row holds beyond the sequence)
-        const long long j = p.sink + (long long)(t + (lane >> 4) * stride) * kSelTile + (lane & 15);
+    // The lanes hold the page ids of two of the warp's tiles (lane / 16).  With one CTA the warp's tiles do not depend on the
+    // length, so the first ids are loaded along with it (whatever the table's row holds beyond the sequence).
+    auto page_ids = [&](int t) -> int {
+        const long long j = p.sink + (long long)(t + (lane >> 4) * W) * kSelTile + (lane & 15);
         return __ldg(table + min(j, (long long)p.max_pages - 1));
     };
-    int t = rank * W + warp;
-    int ids = page_ids(t);
+    int t = warp, ids = S == 1 ? page_ids(t) : 0;
     const int pos = row_position(at, len, p.max_pages), n = pos >= 0 ? pos / kPageTokens + 1 : 0;
     if (pos < 0 && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
     int32_t* list = p.list + item * p.top;
@@ -208,6 +214,11 @@ __global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams 
         sh.q[warp][lane] = make_uint4(w[0] & ~neg[0], w[1] & ~neg[1], neg[0], neg[1]);
         if (l4 == 0) sh.f[warp][hl] = __uint_as_float((uint32_t)(127 + e) << 23);
     }
+    if (rank == 0 && warp == W - 1) {                             // meanwhile: the pages that are listed in any case
+        for (int i = lane; i < p.sink; i += 32) list[i] = i;
+        for (int i = lane; i < p.window; i += 32) list[p.top - p.window + i] = n - p.window + i;
+        if (lane == 0) p.count[item] = p.top;
+    }
     __syncthreads();
     uint4 qf[kBlocks];
     float2 fq[kBlocks];                                           // of this lane's two accumulator columns
@@ -217,21 +228,26 @@ __global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams 
         fq[c] = *reinterpret_cast<const float2*>(&sh.f[c][2 * l4]);
     }
     if (S > 1) cluster_wait();
-    // ---- scores
-    const int tiles = (cand + kSelTile - 1) / kSelTile;
-    const uint32_t keys_addr = smem_u32(keys);
+    // ---- scores of this CTA's candidates [c0, c1)
+    const int tiles = (cand + kSelTile - 1) / kSelTile, share = (tiles + S - 1) / S;
+    const int c0 = min(cand, rank * share * kSelTile), c1 = min(cand, c0 + share * kSelTile);
+    const int t_end = min(tiles, (rank + 1) * share);
     const bool h0 = 2 * l4 < p.G, h1 = 2 * l4 + 1 < p.G;
-    uint32_t least = 0xffffffffu, most = 0u;
-    while (t < tiles) {
-        uint4 x[kSelTiles][2][kBlocks];
-        uint32_t sc[kSelTiles][2];
+    float low = INFINITY, high = -INFINITY;
+    if (S > 1) {
+        t += rank * share;
+        ids = page_ids(t);
+    }
+    while (t < t_end) {
+        uint4 x[T][2][kBlocks];
+        uint32_t sc[T][2];
 #pragma unroll
-        for (int k = 0; k < kSelTiles; ++k) {
+        for (int k = 0; k < T; ++k) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const int j = (t + k * stride) * kSelTile + hl + 8 * r;
+                const int j = (t + k * W) * kSelTile + hl + 8 * r;
                 int id = __shfl_sync(0xffffffffu, ids, k * 16 + hl + 8 * r);
-                if (j >= cand) id = 0;                            // past the last candidate: some page, its score is dropped
+                if (j >= c1) id = 0;                              // past the last candidate: some page, its score is dropped
                 if (id < 0 || id >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
                 const size_t slab = (size_t)id * p.Hkv + g;
                 const uint4* src = reinterpret_cast<const uint4*>(p.codes + slab * (2 * D)) + l4;
@@ -242,10 +258,10 @@ __global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams 
             }
         }
         const int t_now = t;
-        t += kSelTiles * stride;
-        if (t < tiles) ids = page_ids(t);
+        t += T * W;
+        if (t < t_end) ids = page_ids(t);
 #pragma unroll
-        for (int k = 0; k < kSelTiles; ++k) {
+        for (int k = 0; k < T; ++k) {
             float s[4];
 #pragma unroll
             for (int c = 0; c < kBlocks; ++c) {
@@ -265,157 +281,187 @@ __global__ void __launch_bounds__(W * 32) page_select_kernel(const SelectParams 
             m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
             m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
             m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
-            const int j = (t_now + k * stride) * kSelTile + hl + 8 * l4;
-            if (l4 < 2 && j < cand) {
-                uint32_t u = __float_as_uint((l4 ? m1 : m0) + 0.f);              // no negative zero
-                u ^= (u >> 31) ? 0xffffffffu : 0x80000000u;                     // unsigned order = numeric order
-                least = min(least, u);
-                most = max(most, u);
-                if (S == 1) keys[j] = u;
-                else {
-                    const int owner = j / p.cap;
-                    st_cluster_u32(cluster_map_shared(keys_addr + (uint32_t)(j - owner * p.cap) * 4, (uint32_t)owner), u);
-                }
+            const int j = (t_now + k * W) * kSelTile + hl + 8 * l4;
+            if (l4 < 2 && j < c1) {
+                const float v = l4 ? m1 : m0;
+                low = fminf(low, v);
+                high = fmaxf(high, v);
+                scores[j - c0] = v;
             }
         }
     }
-    least = __reduce_min_sync(0xffffffffu, least);
-    most = __reduce_max_sync(0xffffffffu, most);
-    const bool far = cand > p.cap;                                 // some keys are in another CTA's shared memory
-    if (S > 1) {
-        if (lane == 0) {
-            const uint32_t to = cluster_map_shared(smem_u32(&sh.range[rank * W + warp]), 0u);
-            st_cluster_u32(to, least);
-            st_cluster_u32(to + 4, most);
-        }
-        cluster_arrive();
-        cluster_wait();
-        if (rank != 0) {
-            if (far) { cluster_arrive(); cluster_wait(); }
-            return;
-        }
-    } else {
-        if (lane == 0) sh.range[warp] = make_uint2(least, most);
-        __syncthreads();
-    }
-    // ---- selection, by this CTA alone
-    auto key_at = [&](int j) -> uint32_t {
-        if (!far) return keys[j];
-        const int owner = j / p.cap;
-        return ld_cluster_u32(cluster_map_shared(keys_addr + (uint32_t)(j - owner * p.cap) * 4, (uint32_t)owner));
+    const unsigned below = (1u << lane) - 1u;
+    // ---- division.  What the CTAs tell one another goes through shared memory that is written before a barrier and read after.
+    auto sync_all = [&]() {
+        if (S > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
     };
-    for (int i = lane; i < S * W; i += 32) {
-        const uint2 r = sh.range[i];
-        least = min(least, r.x);
-        most = max(most, r.y);
+    auto bits_of = [](float s) -> uint32_t { const uint32_t u = __float_as_uint(s + 0.f); return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u); };
+    auto score_of = [](uint32_t u) -> float { return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu)); };
+    uint32_t lo = __reduce_min_sync(0xffffffffu, bits_of(low)), hi = __reduce_max_sync(0xffffffffu, bits_of(high));
+    if (lane == 0) sh.range[warp] = make_uint2(lo, hi);
+    __syncthreads();
+    uint2 r = sh.range[lane % W];
+    lo = __reduce_min_sync(0xffffffffu, r.x); hi = __reduce_max_sync(0xffffffffu, r.y);
+    if (S > 1) {
+        if (warp == 0 && lane < S) st_cluster_v2(cluster_map_shared(smem_u32(&sh.all_range[rank]), (uint32_t)lane), lo, hi);
+        sync_all();
+        r = sh.all_range[lane % S];
+        lo = __reduce_min_sync(0xffffffffu, r.x); hi = __reduce_max_sync(0xffffffffu, r.y);
     }
-    uint32_t lo = __reduce_min_sync(0xffffffffu, least), hi = __reduce_max_sync(0xffffffffu, most);
-    // Of what lies in [lo, hi] -- keys, or once `equal` is set the mirrored pages of the keys that equal it -- the `need`
-    // largest are to be kept, and all that lies above.
-    int need = keep;
-    bool by_page = false;
-    uint32_t equal = 0, last_key;
-    int last_page;
-    while (true) {
-        const int shift = max(0, 24 - __clz(hi - lo));
-#pragma unroll 4
-        for (int j = tid; j < cand; j += kThreads) {
-            const uint32_t k = key_at(j), v = by_page ? (uint32_t)(cand - 1 - j) : k;
-            if (v >= lo && v <= hi && (!by_page || k == equal)) atomicAdd(&sh.hist[(v - lo) >> shift], 1);
+    low = score_of(lo); high = score_of(hi);
+    // 256 intervals of equal width.  (One fused operation rounds monotonically: a higher score is never in a lower interval.)
+    const float per = 256.f / fmaxf(high - low, 1e-30f), shift_by = -low * per;
+    auto interval = [&](float s) -> int { return max(0, min(255, (int)fmaf(s, per, shift_by))); };
+    // f(candidate, its score, whether there is one) over the warp's run of the CTA's candidates, all lanes together
+    const int steps = (share * kSelTile + kThreads - 1) / kThreads;
+    const int j0 = c0 + warp * steps * 32 + lane, j1 = min(c1, c0 + (warp + 1) * steps * 32);
+    auto each = [&](auto f) {
+#pragma unroll 2
+        for (int s = 0; s < steps; ++s) {
+            const int j = j0 + 32 * s;
+            f(j, j < j1 ? scores[j - c0] : 0.f, j < j1);
         }
-        __syncthreads();
-        // every warp finds the interval by itself: lane i counts intervals 255 - 8 i .. 248 - 8 i and those above them
-        const int4 c0 = *reinterpret_cast<const int4*>(&sh.hist[248 - 8 * lane]), c1 = *reinterpret_cast<const int4*>(&sh.hist[252 - 8 * lane]);
-        const int c[8] = {c1.w, c1.z, c1.y, c1.x, c0.w, c0.z, c0.y, c0.x};
-        const int sum = c[0] + c[1] + c[2] + c[3] + c[4] + c[5] + c[6] + c[7];
+    };
+    // Sums the CTAs' histograms and counts from the top: the interval in which the need-th highest lies, what lies above it
+    // (taken off need) and in it.  Every warp counts by itself: lane i has intervals 255 - 8 i .. 248 - 8 i.
+    int need = keep, bin = 0, inside = 0;
+    auto divide = [&]() {
+        sync_all();                                                // the histograms are complete
+        if (S > 1) {
+            if (tid < 256) {
+                uint32_t v[kSelMaxCluster], sum = 0;
+#pragma unroll
+                for (int s = 0; s < kSelMaxCluster; ++s) v[s] = ld_cluster_u32(cluster_map_shared(smem_u32(&sh.hist[tid]), (uint32_t)(s < S ? s : 0)));
+#pragma unroll
+                for (int s = 0; s < kSelMaxCluster; ++s) sum += s < S ? v[s] : 0u;
+                sh.sum[tid] = (int)sum;
+            }
+            __syncthreads();
+        }
+        const int* h = S > 1 ? sh.sum : sh.hist;
+        const int4 a = *reinterpret_cast<const int4*>(h + 248 - 8 * lane), b = *reinterpret_cast<const int4*>(h + 252 - 8 * lane);
+        const int sum = a.x + a.y + a.z + a.w + b.x + b.y + b.z + b.w;
         int incl = sum;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
-        int above = incl - sum, bin = 0, inside = 0;
-        const unsigned holds = __ballot_sync(0xffffffffu, above < need && incl >= need);
-        const int from = __ffs(holds) - 1;
-        if (lane == from) {
-            bool found = false;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!found && above + c[i] >= need) { found = true; bin = 255 - 8 * lane - i; inside = c[i]; }
-                if (!found) above += c[i];
-            }
+        const int from = __ffs(__ballot_sync(0xffffffffu, incl - sum < need && incl >= need)) - 1;
+        need -= __shfl_sync(0xffffffffu, incl - sum, from);
+        bin = 255 - 8 * from;
+        while (true) {
+            inside = h[bin];
+            if (inside >= need) break;
+            need -= inside;
+            --bin;
         }
-        above = __shfl_sync(0xffffffffu, above, from);
-        bin = __shfl_sync(0xffffffffu, bin, from);
-        inside = __shfl_sync(0xffffffffu, inside, from);
-        need -= above;
+    };
+    each([&](int, float s, bool in) { if (in) atomicAdd(&sh.hist[interval(s)], 1); });
+    divide();
+    const int first_bin = bin;
+    // A crowded interval is divided by the scores' bits (in numeric order) and, where a crowd of equal ones is left, by page.
+    // Of the members in [lo, hi] -- bits, or once `by_page` is set mirrored pages -- the `need` largest are to be kept.
+    uint32_t equal = 0;
+    bool by_page = false;
+    auto value = [&](int j, float s) -> uint32_t { return by_page ? (uint32_t)(cand - 1 - j) : bits_of(s); };
+    auto member = [&](int j, float s) -> bool {
+        if (interval(s) != first_bin) return false;
+        const uint32_t v = value(j, s);
+        return v >= lo && v <= hi && (!by_page || bits_of(s) == equal);
+    };
+    while (inside > kSelRank && inside > need) {
+        sync_all();                                                // everybody has read the histograms
+        if (tid < 256) sh.hist[tid] = 0;
+        __syncthreads();
+        const int shift = max(0, 24 - __clz(hi - lo));
+        each([&](int j, float s, bool in) { if (in && member(j, s)) atomicAdd(&sh.hist[(value(j, s) - lo) >> shift], 1); });
+        divide();
         lo += (uint32_t)bin << shift;
         hi = min(hi, lo + ((1u << shift) - 1u));
-        if (inside == need) {                                      // the interval is kept whole
-            last_key = by_page ? equal : lo;
-            last_page = by_page ? cand - 1 - (int)lo : 0x7fffffff;
-            break;
-        }
-        if (inside <= kSelRank) {
-#pragma unroll 4
-            for (int j = tid; j < cand; j += kThreads) {
-                const uint32_t k = key_at(j), v = by_page ? (uint32_t)(cand - 1 - j) : k;
-                if (v >= lo && v <= hi && (!by_page || k == equal)) {
-                    const int i = atomicAdd(&sh.ranked, 1);
-                    sh.rank_key[i] = k;
-                    sh.rank_page[i] = j;
-                }
-            }
-            __syncthreads();
-            if (tid < inside) {
-                const uint32_t k = sh.rank_key[tid];
-                const int j = sh.rank_page[tid];
-                int before = 0;
-                for (int i = 0; i < inside; ++i) {
-                    const uint32_t ki = sh.rank_key[i];
-                    before += ki > k || (ki == k && sh.rank_page[i] < j);
-                }
-                if (before == need - 1) { sh.last_key = k; sh.last_page = j; }
-            }
-            __syncthreads();
-            last_key = sh.last_key;
-            last_page = sh.last_page;
-            break;
-        }
-        if (shift == 0 && !by_page) {                              // a crowd of equal keys: the lowest pages go first
-            by_page = true;
+        if (shift == 0 && !by_page && inside > kSelRank && inside > need) {
+            by_page = true;                                        // equal scores: the lowest pages go first
             equal = lo;
             lo = 0;
             hi = (uint32_t)(cand - 1);
         }
-        __syncthreads();                                           // everybody has read the histogram
-        if (tid < 256) sh.hist[tid] = 0;
+    }
+    // Kept are the candidates above the interval, and of its members those before (last bits, last page) in the order.
+    uint32_t last;
+    int last_page;
+    if (inside > kSelRank) {                                       // (all members are kept)
+        last = by_page ? equal : lo;
+        last_page = by_page ? cand - 1 - (int)lo : 0x7fffffff;
+    } else {
+        // every member goes to every CTA's copy of its CTA's list
+        each([&](int j, float s, bool in) {
+            if (in && member(j, s)) {
+                const int i = atomicAdd(&sh.members, 1);
+                for (int c = 0; c < S; ++c)
+                    st_cluster_v2(cluster_map_shared(smem_u32(&sh.member[rank][i]), (uint32_t)c), __float_as_uint(s), (uint32_t)j);
+            }
+        });
         __syncthreads();
-    }
-    // ---- the list, ascending: each warp places a contiguous run of the candidates
-    const int run = (cand + kThreads - 1) / kThreads * 32, j0 = warp * run, j1 = min(cand, j0 + run);
-    int kept = 0;
+        if (S > 1) {
+            if (tid < S) st_cluster_u32(cluster_map_shared(smem_u32(&sh.all_members[rank]), (uint32_t)tid), (uint32_t)sh.members);
+            sync_all();
+            const int m = lane < S ? sh.all_members[lane] : 0;
+            int end = m;
+#pragma unroll
+            for (int off = 1; off < kSelMaxCluster; off <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, end, off);
+                if (lane >= off) end += v;
+            }
+            // warp w packs the lists of CTAs w, w + W, ...
+            for (int c = warp; c < S; c += W) {
+                const int mc = __shfl_sync(0xffffffffu, m, c), to = __shfl_sync(0xffffffffu, end, c) - mc;
+                for (int i = lane; i < mc; i += 32) sh.rank[to + i] = sh.member[c][i];
+            }
+            __syncthreads();
+        }
+        const uint2* members = S > 1 ? sh.rank : sh.member[0];
+        if (tid < inside) {
+            const float s = __uint_as_float(members[tid].x);
+            const uint32_t j = members[tid].y;
+            int before = 0;
 #pragma unroll 4
-    for (int j = j0 + lane; j < j1; j += 32) {
-        const uint32_t k = key_at(j);
-        kept += k > last_key || (k == last_key && j <= last_page);
+            for (int i = 0; i < inside; ++i) {
+                const uint2 o = members[i];
+                before += __uint_as_float(o.x) > s || (__uint_as_float(o.x) == s && o.y < j);
+            }
+            if (before == need - 1) { sh.last_score = s; sh.last_page = (int)j; }
+        }
+        __syncthreads();
+        last = bits_of(sh.last_score);
+        last_page = sh.last_page;
     }
+    auto keeps = [&](int j, float s) -> bool {
+        const int i = interval(s);
+        if (i != first_bin) return i > first_bin;
+        const uint32_t u = bits_of(s);
+        return u > last || (u == last && j <= last_page);
+    };
+    // ---- the list, ascending: each warp places its run's
+    int kept = 0;
+    each([&](int j, float s, bool in) { kept += in && keeps(j, s); });
     kept = __reduce_add_sync(0xffffffffu, kept);
     if (lane == 0) sh.kept[warp] = kept;
     __syncthreads();
-    int32_t* to = list + p.sink + __reduce_add_sync(0xffffffffu, lane < warp ? sh.kept[lane] : 0);
-    for (int s = j0; s < j1; s += 32) {
-        const int j = s + lane;
-        const uint32_t k = j < j1 ? key_at(j) : 0u;
-        const bool keeps = j < j1 && (k > last_key || (k == last_key && j <= last_page));
-        const unsigned who = __ballot_sync(0xffffffffu, keeps);
-        if (keeps) to[__popc(who & ((1u << lane) - 1u))] = p.sink + j;
-        to += __popc(who);
+    const int k = lane < W ? sh.kept[lane] : 0;
+    int base = __reduce_add_sync(0xffffffffu, lane < warp ? k : 0);
+    if (S > 1) {
+        const uint32_t all = (uint32_t)__reduce_add_sync(0xffffffffu, k);
+        if (tid < S) st_cluster_u32(cluster_map_shared(smem_u32(&sh.all_kept[rank]), (uint32_t)tid), all);
+        sync_all();                                                // behind it nobody reads another CTA's shared memory
+        base += __reduce_add_sync(0xffffffffu, lane < rank ? sh.all_kept[lane] : 0);
     }
-    for (int i = tid; i < p.sink; i += kThreads) list[i] = i;
-    for (int i = tid; i < p.window; i += kThreads) list[p.top - p.window + i] = n - p.window + i;
-    if (tid == 0) p.count[item] = p.top;
-    if (far) { cluster_arrive(); cluster_wait(); }
+    int32_t* to = list + p.sink + base;
+    each([&](int j, float s, bool in) {
+        const bool mine = in && keeps(j, s);
+        const unsigned who = __ballot_sync(0xffffffffu, mine);
+        if (mine) to[__popc(who & below)] = p.sink + j;
+        to += __popc(who);
+    });
 }
 
 // ------------------------------------------------------------------------------------------ attention over listed pages
@@ -737,28 +783,33 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.top = policy->top_pages; p.sink = policy->sink_pages; p.window = policy->window_pages;
     p.list = page_list; p.count = page_count; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
+    // A cluster per (row, KV head) where those are fewer than the SMs (and where the scores need the room), each CTA at least
+    // eight tiles; 16 warps per CTA while an SM has no second one, else 8 warps with two tiles or (more CTAs than fit that way)
+    // one tile in flight.  8 x 8192 pages: 34.0 / 22.6 / 11.9 us with 1 / 2 / 8 CTAs of 16 warps, 13.4 with 8 of 8 warps; 256 x up
+    // to 256 pages: 11.1 us with 16 warps, 6.2 and 8.9 with 8 and two or one tile; 640 x up to 512: 27.5, 19.0 and 15.6.
     int S = 1;
-    while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelKeyCap) && p.max_pages > S * 8 * kSelTile) S *= 2;
-    const bool wide = getenv("SW") ? atoi(getenv("SW")) : (items * S <= ctx->num_sms);
-    if (getenv("SS")) S = atoi(getenv("SS"));
-    if (p.max_pages > (long long)S * kSelKeyCap)
-        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", p.max_pages, kSelMaxCluster * kSelKeyCap);
+    while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelCap) && p.max_pages > S * 8 * kSelTile) S *= 2;
+    const int form = items * S <= ctx->num_sms ? 2 : items * S <= 2 * ctx->num_sms ? 1 : 0;
+    const int share = ((p.max_pages + kSelTile - 1) / kSelTile + S - 1) / S * kSelTile;       // candidates per CTA at most
+    if (share > kSelCap)
+        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", p.max_pages, kSelMaxCluster * kSelCap);
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
     p.cluster = S;
-    p.cap = kSelKeyCap < p.max_pages ? kSelKeyCap : p.max_pages;
-    const size_t smem = (size_t)p.cap * 4;
+    const size_t smem = (size_t)(share + 4) * sizeof(float);
     typedef void (*Kernel)(const SelectParams);
-    const Kernel kernels[2][2] = {{page_select_kernel<64, 8>, page_select_kernel<64, 16>}, {page_select_kernel<128, 8>, page_select_kernel<128, 16>}};
+    static const Kernel kernels[2][3] = {
+        {page_select_kernel<64, 8, 1>, page_select_kernel<64, 8, 2>, page_select_kernel<64, 16, 2>},
+        {page_select_kernel<128, 8, 1>, page_select_kernel<128, 8, 2>, page_select_kernel<128, 16, 2>}};
     const int di = d->head_dim == 128;
     if (!ctx->select_attr_set[di]) {
-        for (int w = 0; w < 2; ++w) {
-            cudaError_t e = cudaFuncSetAttribute(kernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, kSelKeyCap * 4);
+        for (int w = 0; w < 3; ++w) {
+            cudaError_t e = cudaFuncSetAttribute(kernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (kSelCap + 4) * (int)sizeof(float));
             if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
         }
         ctx->select_attr_set[di] = true;
     }
     KernelScope scope(ctx, kKPageSelect, st);
-    return check_cuda(ctx, launch_cluster(kernels[di][wide], items * S, wide ? 512 : 256, smem, S, st, p), "page_select_kernel launch");
+    return check_cuda(ctx, launch_cluster(kernels[di][form], items * S, form == 2 ? 512 : 256, smem, S, st, p), "page_select_kernel launch");
 }
 
 aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,

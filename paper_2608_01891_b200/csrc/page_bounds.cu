@@ -123,23 +123,24 @@ struct BoundsParams {
     const int32_t* page_table;
     const int32_t* seq_lens;
     const int32_t* first_token;    // [batch] or null
-    int max_pages, Hkv;
+    int max_pages, Hkv, heads_per_warp;
     long long num_pages;
     int* status;
 };
 
-// One warp per (sequence, page, KV head): 16 keys, 8 sixteen-byte loads per lane in flight at once (D = 128).
-// Bound: the read of the keys.  No state is carried between pages, so plain CTAs suffice: the resident 64 warps of an SM keep
-// 256 KB of loads in flight.
+// One warp per (sequence, page) and run of KV heads: a head's 16 keys are 8 sixteen-byte loads per lane (D = 128), and the next
+// head's are in flight while one is reduced.  Bound: the read of the keys.
 template <int D>
 __global__ void __launch_bounds__(kBoundsThreads) page_bounds_kernel(const BoundsParams p) {
     pdl_launch_dependents();
     pdl_wait();
     typedef Lanes<D> L;
     const int lane = threadIdx.x & 31;
+    const int runs = (p.Hkv + p.heads_per_warp - 1) / p.heads_per_warp;
     const int item = blockIdx.x * kBoundsWarps + (threadIdx.x >> 5);
-    const int page_i = item / p.Hkv, g = item % p.Hkv, b = blockIdx.y;
+    const int page_i = item / runs, b = blockIdx.y;
     if (page_i >= p.max_pages) return;
+    const int page = p.page_table[(size_t)b * p.max_pages + page_i];
     const int raw = p.seq_lens[b];
     if (raw < 0 || raw > p.max_pages * kPageTokens) {
         if (item == 0 && lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
@@ -147,27 +148,33 @@ __global__ void __launch_bounds__(kBoundsThreads) page_bounds_kernel(const Bound
     const int len = max(0, min(raw, p.max_pages * kPageTokens));
     if (page_i * kPageTokens >= len) return;
     if (p.first_token && (page_i + 1) * kPageTokens <= p.first_token[b]) return;     // a page without a new token
-    const int page = p.page_table[(size_t)b * p.max_pages + page_i];
     if (page < 0 || page >= p.num_pages) {
         if (lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
         return;
     }
     const int valid = min(kPageTokens, len - page_i * kPageTokens);
-    const size_t slab = (size_t)page * p.Hkv + g;
-    const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + slab * kPageTokens * D);
+    const int g0 = (item % runs) * p.heads_per_warp, g1 = min(p.Hkv, g0 + p.heads_per_warp);
     const int sub = lane / L::kPer, l = lane % L::kPer;
     uint4 a[L::kIter], c[L::kIter];
+    auto load = [&](int g) {
+        const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + ((size_t)page * p.Hkv + g) * kPageTokens * D);
 #pragma unroll
-    for (int it = 0; it < L::kIter; ++it) {
-        const int t = min(it * L::kTok + sub, valid - 1);           // a slot past the end repeats the last valid key
-        a[it] = __ldg(k + t * (D / 8) + l);
-        c[it] = __ldg(k + t * (D / 8) + D / 16 + l);
+        for (int it = 0; it < L::kIter; ++it) {
+            const int t = min(it * L::kTok + sub, valid - 1);       // a slot past the end repeats the last valid key
+            a[it] = __ldg(k + t * (D / 8) + l);
+            c[it] = __ldg(k + t * (D / 8) + D / 16 + l);
+        }
+    };
+    load(g0);
+    for (int g = g0; g < g1; ++g) {
+        Range16 r;
+        r.reset();
+#pragma unroll
+        for (int it = 0; it < L::kIter; ++it) r.add(a[it], c[it]);
+        if (g + 1 < g1) load(g + 1);
+        const size_t slab = (size_t)page * p.Hkv + g;
+        store_bounds<D>(r, lane, p.codes + slab * 2 * D, p.scales + slab * (D / 32));
     }
-    Range16 r;
-    r.reset();
-#pragma unroll
-    for (int it = 0; it < L::kIter; ++it) r.add(a[it], c[it]);
-    store_bounds<D>(r, lane, p.codes + slab * 2 * D, p.scales + slab * (D / 32));
 }
 
 struct AppendParams {
@@ -198,15 +205,16 @@ struct AppendParams {
 // Queries are rotated in fp32.  Keys (one head in ten on the shapes served here) are normalised and rotated in double and
 // rounded to fp32 and then to bf16: the stored key no longer depends on the order in which sums were formed (but for values
 // within 1e-11 of a rounding border), and the bounds, which are integers made from it, come out the same everywhere.
-template <int D>
-__global__ void __launch_bounds__(kBoundsThreads) rope_append_bounds_kernel(const AppendParams p) {
+// U: how many times kTok query heads a warp has in flight.
+template <int D, int U>
+__global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(const AppendParams p) {
     // No early release of the dependents: the dense attention kernel reads the cache without waiting for the grid
     // dependency, which is sound only if the kernel that writes the cache has finished before anything later starts.
     typedef Lanes<D> L;
     constexpr int kHalf = D / 2;
     __shared__ int s_warp[kBoundsWarps];
     __shared__ int s_b, s_page;
-    __shared__ float2 s_rot[kPageTokens][kHalf];                    // (cos, sin), queries
+    __shared__ __align__(16) float2 s_rot[kPageTokens][kHalf];      // (cos, sin), queries
     __shared__ double2 s_rotd[kPageTokens][kHalf];                  // keys
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -295,10 +303,12 @@ __global__ void __launch_bounds__(kBoundsThreads) rope_append_bounds_kernel(cons
     __syncthreads();
     const int sub = lane / L::kPer, l = lane % L::kPer;
     if (!kv_part) {
-        // ---- query heads: (row, head) pairs, kTok of them per warp at a time
-        const int h0 = ((int)blockIdx.y - p.kv_ctas) * p.q_heads_per_cta;
-        const int nh = min(p.q_heads_per_cta, p.Hq - h0);
+        // ---- query heads.  A warp takes a row and U * kTok of its heads at a time: one rotation in registers, all loads first.
+        const int h_lo = ((int)blockIdx.y - p.kv_ctas) * p.q_heads_per_cta, h_hi = min(p.Hq, h_lo + p.q_heads_per_cta);
+        const int groups = (h_hi - h_lo + U * L::kTok - 1) / (U * L::kTok);
         float gn[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) gn[i] = 1.f;
         if (p.w_qn) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -306,43 +316,52 @@ __global__ void __launch_bounds__(kBoundsThreads) rope_append_bounds_kernel(cons
                 gn[8 + i] = __bfloat162float(p.w_qn[kHalf + 8 * l + i]);
             }
         }
-        for (int i0 = warp * L::kTok; i0 < nrows * nh; i0 += kBoundsWarps * L::kTok) {
-            const int i = i0 + sub;
-            const bool on = i < nrows * nh;
-            const int r = on ? i / nh : 0, h = h0 + (on ? i % nh : 0);
-            const uint4* src = reinterpret_cast<const uint4*>(p.qkv + ((size_t)(row0 + r) * heads + h) * D);
-            const uint4 xa = src[l], xb = src[D / 16 + l];
-            float a[8], c[8];
-            const __nv_bfloat162* pa = reinterpret_cast<const __nv_bfloat162*>(&xa);
-            const __nv_bfloat162* pb = reinterpret_cast<const __nv_bfloat162*>(&xb);
+        for (int task = warp; task < nrows * groups; task += kBoundsWarps) {
+            const int r = task / groups, h0 = h_lo + (task % groups) * (U * L::kTok) + sub;
+            const uint4* src = reinterpret_cast<const uint4*>(p.qkv + (size_t)(row0 + r) * heads * D) + l;
+            uint4 xa[U], xb[U];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 u = __bfloat1622float2(pa[k]), v = __bfloat1622float2(pb[k]);
-                a[2 * k] = u.x; a[2 * k + 1] = u.y; c[2 * k] = v.x; c[2 * k + 1] = v.y;
+            for (int u = 0; u < U; ++u) {
+                const int h = min(h0 + u * L::kTok, h_hi - 1);
+                xa[u] = __ldg(src + h * (D / 8));
+                xb[u] = __ldg(src + h * (D / 8) + D / 16);
             }
-            if (p.w_qn) {
-                float ss = 0.f;
+            float4 cs[4];                                           // (cos, sin) of this lane's eight pairs
 #pragma unroll
-                for (int k = 0; k < 8; ++k) ss = fmaf(a[k], a[k], fmaf(c[k], c[k], ss));
+            for (int k = 0; k < 4; ++k) cs[k] = *reinterpret_cast<const float4*>(&s_rot[r][8 * l + 2 * k]);
 #pragma unroll
-                for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                const float rinv = rsqrtf(ss / (float)D + p.eps);
+            for (int u = 0; u < U; ++u) {
+                const __nv_bfloat162* pa = reinterpret_cast<const __nv_bfloat162*>(&xa[u]);
+                const __nv_bfloat162* pb = reinterpret_cast<const __nv_bfloat162*>(&xb[u]);
+                float a[8], c[8], ss = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) { a[k] *= rinv * gn[k]; c[k] *= rinv * gn[8 + k]; }
-            }
-            uint4 oa, ob;
-            __nv_bfloat162* qa = reinterpret_cast<__nv_bfloat162*>(&oa);
-            __nv_bfloat162* qb = reinterpret_cast<__nv_bfloat162*>(&ob);
+                for (int k = 0; k < 4; ++k) {
+                    const float2 x = __bfloat1622float2(pa[k]), y = __bfloat1622float2(pb[k]);
+                    a[2 * k] = x.x; a[2 * k + 1] = x.y; c[2 * k] = y.x; c[2 * k + 1] = y.y;
+                }
+                if (p.w_qn) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float2 r0 = s_rot[r][8 * l + 2 * k], r1 = s_rot[r][8 * l + 2 * k + 1];
-                qa[k] = __floats2bfloat162_rn(a[2 * k] * r0.x - c[2 * k] * r0.y, a[2 * k + 1] * r1.x - c[2 * k + 1] * r1.y);
-                qb[k] = __floats2bfloat162_rn(c[2 * k] * r0.x + a[2 * k] * r0.y, c[2 * k + 1] * r1.x + a[2 * k + 1] * r1.y);
-            }
-            if (on) {
-                uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)(row0 + r) * p.Hq + h) * D);
-                dst[l] = oa;
-                dst[D / 16 + l] = ob;
+                    for (int k = 0; k < 8; ++k) ss = fmaf(a[k], a[k], fmaf(c[k], c[k], ss));
+#pragma unroll
+                    for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                    const float rinv = rsqrtf(ss / (float)D + p.eps);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) { a[k] *= rinv * gn[k]; c[k] *= rinv * gn[8 + k]; }
+                }
+                uint4 oa, ob;
+                __nv_bfloat162* qa = reinterpret_cast<__nv_bfloat162*>(&oa);
+                __nv_bfloat162* qb = reinterpret_cast<__nv_bfloat162*>(&ob);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    qa[k] = __floats2bfloat162_rn(a[2 * k] * cs[k].x - c[2 * k] * cs[k].y, a[2 * k + 1] * cs[k].z - c[2 * k + 1] * cs[k].w);
+                    qb[k] = __floats2bfloat162_rn(c[2 * k] * cs[k].x + a[2 * k] * cs[k].y, c[2 * k + 1] * cs[k].z + a[2 * k + 1] * cs[k].w);
+                }
+                const int h = h0 + u * L::kTok;
+                if (h < h_hi) {
+                    uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)(row0 + r) * p.Hq + h) * D);
+                    dst[l] = oa;
+                    dst[D / 16 + l] = ob;
+                }
             }
         }
         return;
@@ -353,11 +372,18 @@ __global__ void __launch_bounds__(kBoundsThreads) rope_append_bounds_kernel(cons
         const int g = i < p.Hkv ? i : i - p.Hkv;
         const size_t slab = (size_t)page * p.Hkv + g;
         if (i >= p.Hkv) {
-            const __nv_bfloat16* src = p.qkv + ((size_t)row0 * heads + p.Hq + p.Hkv + g) * D;
+            const uint4* src = reinterpret_cast<const uint4*>(p.qkv + ((size_t)row0 * heads + p.Hq + p.Hkv + g) * D);
             uint4* dst = reinterpret_cast<uint4*>(p.v_cache + (slab * kPageTokens + slot0) * D);
-            for (int j = lane; j < nrows * (D / 8); j += 32) {
-                const int r = j / (D / 8), c = j % (D / 8);
-                dst[r * (D / 8) + c] = reinterpret_cast<const uint4*>(src + (size_t)r * heads * D)[c];
+            uint4 v[kPageTokens * D / 256];
+#pragma unroll
+            for (int k = 0; k < kPageTokens * D / 256; ++k) {
+                const int j = k * 32 + lane, r = j / (D / 8);
+                if (r < nrows) v[k] = __ldg(src + (size_t)r * heads * (D / 8) + j % (D / 8));
+            }
+#pragma unroll
+            for (int k = 0; k < kPageTokens * D / 256; ++k) {
+                const int j = k * 32 + lane;
+                if (j / (D / 8) < nrows) dst[j] = v[k];
             }
             continue;
         }
@@ -381,35 +407,33 @@ __global__ void __launch_bounds__(kBoundsThreads) rope_append_bounds_kernel(cons
             const int t = min(t0 + sub, end - 1);
             if (t0 + L::kTok > slot0) {                             // some of these tokens are new (the same for the whole warp)
                 const int r = max(0, t - slot0);
-                double a[8], c[8];
-                const __nv_bfloat162* pa = reinterpret_cast<const __nv_bfloat162*>(&xa[it]);
-                const __nv_bfloat162* pb = reinterpret_cast<const __nv_bfloat162*>(&xb[it]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 u = __bfloat1622float2(pa[k]), v = __bfloat1622float2(pb[k]);
-                    a[2 * k] = u.x; a[2 * k + 1] = u.y; c[2 * k] = v.x; c[2 * k + 1] = v.y;
-                }
+                const __nv_bfloat16* pa = reinterpret_cast<const __nv_bfloat16*>(&xa[it]);
+                const __nv_bfloat16* pb = reinterpret_cast<const __nv_bfloat16*>(&xb[it]);
+                double rinv = 1.0;
                 if (p.w_kn) {
                     double ss = 0.0;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) ss = fma(a[k], a[k], fma(c[k], c[k], ss));
+                    for (int k = 0; k < 8; ++k) {
+                        const double a = __bfloat162float(pa[k]), c = __bfloat162float(pb[k]);
+                        ss = fma(a, a, fma(c, c, ss));
+                    }
 #pragma unroll
                     for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                    const double rinv = 1.0 / sqrt(ss / (double)D + (double)p.eps);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        a[k] *= rinv * (double)__bfloat162float(p.w_kn[8 * l + k]);
-                        c[k] *= rinv * (double)__bfloat162float(p.w_kn[kHalf + 8 * l + k]);
-                    }
+                    rinv = 1.0 / sqrt(ss / (double)D + (double)p.eps);
                 }
                 uint4 oa, ob;
                 __nv_bfloat16* qa = reinterpret_cast<__nv_bfloat16*>(&oa);
                 __nv_bfloat16* qb = reinterpret_cast<__nv_bfloat16*>(&ob);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
+                    double a = __bfloat162float(pa[k]), c = __bfloat162float(pb[k]);
+                    if (p.w_kn) {
+                        a *= rinv * (double)__bfloat162float(p.w_kn[8 * l + k]);
+                        c *= rinv * (double)__bfloat162float(p.w_kn[kHalf + 8 * l + k]);
+                    }
                     const double2 rot = s_rotd[r][8 * l + k];
-                    qa[k] = __float2bfloat16_rn((float)(a[k] * rot.x - c[k] * rot.y));
-                    qb[k] = __float2bfloat16_rn((float)(c[k] * rot.x + a[k] * rot.y));
+                    qa[k] = __float2bfloat16_rn((float)(a * rot.x - c * rot.y));
+                    qb[k] = __float2bfloat16_rn((float)(c * rot.x + a * rot.y));
                 }
                 if (t >= slot0) {
                     xa[it] = oa;
@@ -437,7 +461,11 @@ aflex_status page_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.page_table = kv->page_table; p.seq_lens = kv->seq_lens; p.first_token = first_token;
     p.max_pages = kv->max_pages_per_seq; p.Hkv = d->num_kv_heads; p.num_pages = kv->num_pages;
     p.status = ctx->dev_status;
-    const long long items = (long long)p.max_pages * p.Hkv;
+    // all heads of a page on one warp where that still leaves 16 warps per SM, fewer of them where there are few pages
+    const long long pages = (long long)batch * p.max_pages;
+    p.heads_per_warp = 1;
+    while (p.heads_per_warp < p.Hkv && pages * p.Hkv >= 2LL * p.heads_per_warp * 16 * ctx->num_sms) p.heads_per_warp *= 2;
+    const long long items = (long long)p.max_pages * ((p.Hkv + p.heads_per_warp - 1) / p.heads_per_warp);
     const dim3 grid((unsigned)((items + kBoundsWarps - 1) / kBoundsWarps), (unsigned)batch);
     KernelScope scope(ctx, kKPageBounds, st);
     return check_cuda(ctx, launch_pdl(d->head_dim == 128 ? page_bounds_kernel<128> : page_bounds_kernel<64>, grid, dim3(kBoundsThreads), 0, st, p),
@@ -460,14 +488,19 @@ aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d,
     p.eps = eps;
     for (int i = 0; i < 64; ++i) p.inv_freq[i] = i < d->head_dim / 2 ? pow((double)theta, -2.0 * i / (double)d->head_dim) : 0.0;
     p.status = ctx->dev_status;
-    // a page's K and V heads on one CTA per eight of them; its query heads in groups of 16
+    // A page's K and V heads on one CTA per eight of them.  One row per sequence: 16 query heads per CTA, every warp a few of
+    // them; chunks: 32 query heads per CTA, so that a warp keeps a row's rotation for several loads.
     p.kv_ctas = (2 * p.Hkv + kBoundsWarps - 1) / kBoundsWarps;
-    p.q_heads_per_cta = p.Hq < 16 ? p.Hq : 16;
+    const int per_cta = q_offsets ? 32 : 16;
+    p.q_heads_per_cta = p.Hq < per_cta ? p.Hq : per_cta;
     const int q_ctas = (p.Hq + p.q_heads_per_cta - 1) / p.q_heads_per_cta;
     // m new tokens of a sequence touch at most (m + 14) / 16 + 1 pages
     const long long tasks = q_offsets ? ((long long)rows + 14LL * batch) / 16 + batch : batch;
     KernelScope scope(ctx, kKAppendBounds, st);
-    return check_cuda(ctx, launch_pdl(d->head_dim == 128 ? rope_append_bounds_kernel<128> : rope_append_bounds_kernel<64>,
+    typedef void (*Kernel)(const AppendParams);
+    static const Kernel kernels[2][2] = {{rope_append_bounds_kernel<64, 1>, rope_append_bounds_kernel<64, 2>},
+                                         {rope_append_bounds_kernel<128, 1>, rope_append_bounds_kernel<128, 4>}};
+    return check_cuda(ctx, launch_pdl(kernels[d->head_dim == 128][q_offsets != nullptr],
                                       dim3((unsigned)tasks, (unsigned)(p.kv_ctas + q_ctas)), dim3(kBoundsThreads), 0, st, p),
                       "rope_append_bounds_kernel launch");
 }
