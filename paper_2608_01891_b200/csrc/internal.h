@@ -60,6 +60,7 @@ struct aflex_ctx {
     bool attn_attr_set[2] = {false, false};
     bool prefill_attr_set[2] = {false, false};   // shared-memory limit raised for attn_prefill_kernel<64 / 128> on this device
     bool select_attr_set[2] = {false, false};    // ... for page_select_kernel<64 / 128>
+    bool bounds_attr_set[2] = {false, false};    // ... for page_bounds_kernel<64 / 128>
     bool pages_attr_set[2] = {false, false};     // ... for attn_decode_pages_kernel<64 / 128>
     char err[512] = {0};
     // launch counters (always on) and event-pair timing of every launch (when profiling is enabled)

@@ -35,26 +35,49 @@ template <int D> struct Lanes {
     static constexpr int kIter = kPageTokens / kTok;
 };
 
+// Larger / smaller of two bf16 pairs; the other operand where one is NaN.
+__device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t min_pair(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("min.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
 struct Range16 {                                  // running extremes of this lane's 16 channels, bf16 pairs
-    __nv_bfloat162 hi[8], lo[8];
+    uint32_t hi[8], lo[8];
     __device__ __forceinline__ void reset() {
-        const __nv_bfloat162 ninf = __halves2bfloat162(__ushort_as_bfloat16(0xff80), __ushort_as_bfloat16(0xff80));
-        const __nv_bfloat162 pinf = __halves2bfloat162(__ushort_as_bfloat16(0x7f80), __ushort_as_bfloat16(0x7f80));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { hi[i] = ninf; lo[i] = pinf; }
+        for (int i = 0; i < 8; ++i) { hi[i] = 0xff80ff80u; lo[i] = 0x7f807f80u; }      // -inf, +inf
     }
     __device__ __forceinline__ void add(const uint4& a, const uint4& b) {      // a: first half's channels, b: second half's
-        const __nv_bfloat162* pa = reinterpret_cast<const __nv_bfloat162*>(&a);
-        const __nv_bfloat162* pb = reinterpret_cast<const __nv_bfloat162*>(&b);
+        const uint32_t v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            hi[i] = __hmax2(hi[i], pa[i]);         // the other operand where one is NaN
-            lo[i] = __hmin2(lo[i], pa[i]);
-            hi[4 + i] = __hmax2(hi[4 + i], pb[i]);
-            lo[4 + i] = __hmin2(lo[4 + i], pb[i]);
-        }
+        for (int i = 0; i < 8; ++i) { hi[i] = max_pair(hi[i], v[i]); lo[i] = min_pair(lo[i], v[i]); }
     }
 };
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack_f32x2(float x, float y) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+    return d;
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t widen_bf16x2(uint32_t v) { return pack_f32x2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 
 // Smallest e with a <= 127 * 2^e, within [-60, 50]; -60 for a == 0.
 __device__ __forceinline__ int block_exponent(float a) {
@@ -69,50 +92,62 @@ __device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
     return (uint32_t)(a & 255) | ((uint32_t)(b & 255) << 8) | ((uint32_t)(c & 255) << 16) | ((uint32_t)d << 24);
 }
 
-// Joins the lanes' ranges of one (page, KV head) and writes its bounds.  All 32 lanes take part.
+// Joins the lanes' ranges of one (page, KV head) and writes its bounds.  All 32 lanes take part.  Each joining step hands half
+// of a lane's channels to its partner, so that in the end every channel is quantised by one lane: lane bit 4 tells which half
+// of the head, bits 3 (and 2, D = 64) which of the chunk's channels, the others the chunk.
+template <int K>                                    // of 2 K pairs keep K, the first or (upper lanes) the last
+__device__ __forceinline__ void join(Range16& r, int lane, int off) {
+    const bool upper = (lane & off) != 0;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const uint32_t h0 = r.hi[i], h1 = r.hi[i + K], l0 = r.lo[i], l1 = r.lo[i + K];
+        r.hi[i] = max_pair(upper ? h1 : h0, __shfl_xor_sync(0xffffffffu, upper ? h0 : h1, off));
+        r.lo[i] = min_pair(upper ? l1 : l0, __shfl_xor_sync(0xffffffffu, upper ? l0 : l1, off));
+    }
+}
 template <int D>
 __device__ __forceinline__ void store_bounds(Range16& r, int lane, int8_t* codes, uint8_t* scales) {
     constexpr int kPer = Lanes<D>::kPer;
+    constexpr int kPairs = D == 128 ? 2 : 1;       // channel pairs a lane ends up with
+    join<4>(r, lane, 16);
+    join<2>(r, lane, 8);
+    if (D == 64) join<1>(r, lane, 4);
+    float hi[2 * kPairs], lo[2 * kPairs], a = 0.f;
 #pragma unroll
-    for (int off = kPer; off < 32; off <<= 1) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            r.hi[i] = __hmax2(r.hi[i], __shfl_xor_sync(0xffffffffu, r.hi[i], off));
-            r.lo[i] = __hmin2(r.lo[i], __shfl_xor_sync(0xffffffffu, r.lo[i], off));
-        }
+    for (int i = 0; i < kPairs; ++i) {
+        hi[2 * i] = __uint_as_float(r.hi[i] << 16); hi[2 * i + 1] = __uint_as_float(r.hi[i] & 0xffff0000u);
+        lo[2 * i] = __uint_as_float(r.lo[i] << 16); lo[2 * i + 1] = __uint_as_float(r.lo[i] & 0xffff0000u);
     }
-    const int l = lane % kPer;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        float hi[8], lo[8], a = 0.f;
+    for (int i = 0; i < 2 * kPairs; ++i) {
+        if (hi[i] < lo[i]) hi[i] = lo[i] = 0.f;               // no key was a number
+        a = fmaxf(a, fmaxf(fabsf(hi[i]), fabsf(lo[i])));
+    }
+    // the lanes of a 32-channel block: four chunks, and the lanes that share a chunk
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
+    if (D == 64) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 4));
+    const int e = block_exponent(a);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    int ih[2 * kPairs], il[2 * kPairs];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 h = __bfloat1622float2(r.hi[half * 4 + i]), w = __bfloat1622float2(r.lo[half * 4 + i]);
-            hi[2 * i] = h.x; hi[2 * i + 1] = h.y;
-            lo[2 * i] = w.x; lo[2 * i + 1] = w.y;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (hi[i] < lo[i]) hi[i] = lo[i] = 0.f;           // no key was a number
-            a = fmaxf(a, fmaxf(fabsf(hi[i]), fabsf(lo[i])));
-        }
-        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));      // the four lanes of a 32-channel block
-        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
-        const int e = block_exponent(a);
-        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-        int ih[8], il[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            ih[i] = (int)fminf(127.f, fmaxf(-127.f, ceilf(hi[i] * inv)));
-            il[i] = (int)fminf(127.f, fmaxf(-127.f, floorf(lo[i] * inv)));
-        }
-        if (lane < kPer) {
-            uint4 o;
-            o.x = pack4(ih[0], ih[1], ih[2], ih[3]); o.y = pack4(ih[4], ih[5], ih[6], ih[7]);
-            o.z = pack4(il[0], il[1], il[2], il[3]); o.w = pack4(il[4], il[5], il[6], il[7]);
-            reinterpret_cast<uint4*>(codes)[half * kPer + l] = o;
-            if ((l & 3) == 0) scales[half * (D / 64) + l / 4] = (uint8_t)(e + 127);
-        }
+    for (int i = 0; i < 2 * kPairs; ++i) {                     // (conversions saturate, so infinity ends at the border)
+        ih[i] = max(-127, min(127, __float2int_ru(hi[i] * inv)));
+        il[i] = max(-127, min(127, __float2int_rd(lo[i] * inv)));
+    }
+    const int half = lane >> 4, l = lane & (kPer - 1);
+    int8_t* chunk = codes + (half * kPer + l) * 16;
+    if (D == 128) {
+        const int q = (lane >> 3) & 1;
+        reinterpret_cast<uint32_t*>(chunk)[q] = pack4(ih[0], ih[1], ih[2 * kPairs - 2], ih[2 * kPairs - 1]);
+        reinterpret_cast<uint32_t*>(chunk)[2 + q] = pack4(il[0], il[1], il[2 * kPairs - 2], il[2 * kPairs - 1]);
+        if ((lane & 11) == 0) scales[half * 2 + (l >> 2)] = (uint8_t)(e + 127);
+    } else {
+        const int q = ((lane >> 3) & 1) * 2 + ((lane >> 2) & 1);
+        reinterpret_cast<uint16_t*>(chunk)[q] = (uint16_t)((ih[0] & 255) | (ih[1] << 8));
+        reinterpret_cast<uint16_t*>(chunk)[4 + q] = (uint16_t)((il[0] & 255) | (il[1] << 8));
+        if ((lane & 15) == 0) scales[half] = (uint8_t)(e + 127);
     }
 }
 
@@ -123,57 +158,73 @@ struct BoundsParams {
     const int32_t* page_table;
     const int32_t* seq_lens;
     const int32_t* first_token;    // [batch] or null
-    int max_pages, Hkv, heads_per_warp;
+    int max_pages, Hkv, pages_per_cta;
     long long num_pages;
     int* status;
 };
 
-// One warp per (sequence, page) and run of KV heads: a head's 16 keys are 8 sixteen-byte loads per lane (D = 128), and the next
-// head's are in flight while one is reduced.  Bound: the read of the keys.
+// A CTA takes a run of pages of one sequence (their ids are looked up once), a warp every eighth (page, KV head) of it.  A head's
+// 16 keys go through a ring in shared memory by asynchronous copies, the next head's in flight while one is reduced; a lane copies
+// exactly the 16-byte words that it will read, so nothing but its own copies has to be waited for.  Bound: the read of the keys.
+constexpr int kBoundsStages = 2;
 template <int D>
 __global__ void __launch_bounds__(kBoundsThreads) page_bounds_kernel(const BoundsParams p) {
+    typedef Lanes<D> L;
+    constexpr int kWords = 2 * L::kIter;                            // 16-byte words of a head per lane
+    extern __shared__ __align__(16) uint4 ring[];                   // [warp][stage][word][lane]
     pdl_launch_dependents();
     pdl_wait();
-    typedef Lanes<D> L;
-    const int lane = threadIdx.x & 31;
-    const int runs = (p.Hkv + p.heads_per_warp - 1) / p.heads_per_warp;
-    const int item = blockIdx.x * kBoundsWarps + (threadIdx.x >> 5);
-    const int page_i = item / runs, b = blockIdx.y;
-    if (page_i >= p.max_pages) return;
-    const int page = p.page_table[(size_t)b * p.max_pages + page_i];
-    const int raw = p.seq_lens[b];
-    if (raw < 0 || raw > p.max_pages * kPageTokens) {
-        if (item == 0 && lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
-    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
+    const int first_page = blockIdx.x * p.pages_per_cta, my_page = first_page + lane;     // lane i holds the run's i-th page
+    const int raw = __ldg(p.seq_lens + b);
+    const int from = p.first_token ? __ldg(p.first_token + b) : 0;
+    int id = lane < p.pages_per_cta && my_page < p.max_pages ? __ldg(p.page_table + (size_t)b * p.max_pages + my_page) : 0;
+    if ((raw < 0 || raw > p.max_pages * kPageTokens) && blockIdx.x == 0 && threadIdx.x == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
     const int len = max(0, min(raw, p.max_pages * kPageTokens));
-    if (page_i * kPageTokens >= len) return;
-    if (p.first_token && (page_i + 1) * kPageTokens <= p.first_token[b]) return;     // a page without a new token
-    if (page < 0 || page >= p.num_pages) {
-        if (lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
-        return;
-    }
-    const int valid = min(kPageTokens, len - page_i * kPageTokens);
-    const int g0 = (item % runs) * p.heads_per_warp, g1 = min(p.Hkv, g0 + p.heads_per_warp);
+    const int pages = min(p.pages_per_cta, (len + kPageTokens - 1) / kPageTokens - first_page);
+    if (pages <= 0) return;
+    // Valid tokens of this lane's page; 0: nothing to do (a page before the first new token, or a bad id)
+    int valid = lane < pages && (my_page + 1) * kPageTokens > from ? min(kPageTokens, len - my_page * kPageTokens) : 0;
+    if (valid > 0 && (id < 0 || id >= p.num_pages)) { atomicExch(p.status, AFLEX_ERR_BOUNDS); valid = 0; }
     const int sub = lane / L::kPer, l = lane % L::kPer;
-    uint4 a[L::kIter], c[L::kIter];
-    auto load = [&](int g) {
-        const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + ((size_t)page * p.Hkv + g) * kPageTokens * D);
+    uint4* mine = ring + (size_t)warp * kBoundsStages * kWords * 32 + lane;
+    const int items = pages * p.Hkv;
+    auto issue = [&](int i, int stage) {
+        const int v = __shfl_sync(0xffffffffu, valid, i / p.Hkv);
+        if (v > 0) {
+            const size_t slab = (size_t)__shfl_sync(0xffffffffu, id, i / p.Hkv) * p.Hkv + i % p.Hkv;
+            const uint4* k = reinterpret_cast<const uint4*>(p.k_cache + slab * kPageTokens * D) + l;
+            const uint32_t to = smem_u32(mine + stage * kWords * 32);
 #pragma unroll
-        for (int it = 0; it < L::kIter; ++it) {
-            const int t = min(it * L::kTok + sub, valid - 1);       // a slot past the end repeats the last valid key
-            a[it] = __ldg(k + t * (D / 8) + l);
-            c[it] = __ldg(k + t * (D / 8) + D / 16 + l);
+            for (int w = 0; w < kWords; ++w) {
+                const int t = (w >> 1) * L::kTok + sub;             // a slot past the end repeats the last valid key
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                             ::"r"(to + w * 512), "l"(k + (v == kPageTokens ? t : min(t, v - 1)) * (D / 8) + (w & 1) * (D / 16)) : "memory");
+            }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    load(g0);
-    for (int g = g0; g < g1; ++g) {
-        Range16 r;
-        r.reset();
+    int ahead = warp;                                               // next item to copy
 #pragma unroll
-        for (int it = 0; it < L::kIter; ++it) r.add(a[it], c[it]);
-        if (g + 1 < g1) load(g + 1);
-        const size_t slab = (size_t)page * p.Hkv + g;
-        store_bounds<D>(r, lane, p.codes + slab * 2 * D, p.scales + slab * (D / 32));
+    for (int s = 0; s < kBoundsStages - 1; ++s) {
+        if (ahead < items) issue(ahead, s); else asm volatile("cp.async.commit_group;" ::: "memory");
+        ahead += kBoundsWarps;
+    }
+    int stage = 0;
+    for (int i = warp; i < items; i += kBoundsWarps) {
+        const int to = stage == 0 ? kBoundsStages - 1 : stage - 1;  // the stage that was read last
+        if (ahead < items) issue(ahead, to); else asm volatile("cp.async.commit_group;" ::: "memory");
+        ahead += kBoundsWarps;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kBoundsStages - 1) : "memory");
+        if (__shfl_sync(0xffffffffu, valid, i / p.Hkv) > 0) {
+            Range16 r;
+            r.reset();
+#pragma unroll
+            for (int it = 0; it < L::kIter; ++it) r.add(mine[(stage * kWords + 2 * it) * 32], mine[(stage * kWords + 2 * it + 1) * 32]);
+            const size_t slab = (size_t)__shfl_sync(0xffffffffu, id, i / p.Hkv) * p.Hkv + i % p.Hkv;
+            store_bounds<D>(r, lane, p.codes + slab * 2 * D, p.scales + slab * (D / 32));
+        }
+        stage = stage + 1 == kBoundsStages ? 0 : stage + 1;
     }
 }
 
@@ -191,22 +242,23 @@ struct AppendParams {
     __nv_bfloat16* v_cache;
     int8_t* codes;
     uint8_t* scales;
-    int q_heads_per_cta, kv_ctas;  // blockIdx.y < kv_ctas: K and V heads, a share each; else query heads
+    int q_heads_per_cta, kv_ctas, groups;  // head groups of a page: kv_ctas for its K and V heads, the others for its query heads
     float eps;
     double inv_freq[64];           // theta^(-2 i / D), formed in double on the host
+    double step_cos[64], step_sin[64];             // ... and the cosine and sine of that angle: one position's rotation
     int* status;
 };
 
 // A CTA handles the rows of ONE page of one sequence (1 to 16 rows), so that whoever rotates the page's keys holds all of
-// them when the bounds are formed.  blockIdx.x: the page among the pages touched by the call (located by a scan over the
-// sequences), blockIdx.y: a group of heads.
+// them when the bounds are formed: a page among the pages touched by the call (located by a scan over the sequences) and a
+// group of heads.  In chunks a page's groups are neighbours, so that key CTAs (arithmetic in double) run next to query and
+// value CTAs (bytes): 64 against 70 us for 7420 rows of 64 + 2 x 8 heads.  One row per page: all key CTAs, the longest, first.
 //
 // Bound: qkv read and q, K, V written once.  Two rotary halves of eight channels per lane make every access 16 bytes.
 // Queries are rotated in fp32.  Keys (one head in ten on the shapes served here) are normalised and rotated in double and
 // rounded to fp32 and then to bf16: the stored key no longer depends on the order in which sums were formed (but for values
 // within 1e-11 of a rounding border), and the bounds, which are integers made from it, come out the same everywhere.
-// U: how many times kTok query heads a warp has in flight.
-template <int D, int U>
+template <int D>
 __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(const AppendParams p) {
     // No early release of the dependents: the dense attention kernel reads the cache without waiting for the grid
     // dependency, which is sound only if the kernel that writes the cache has finished before anything later starts.
@@ -214,13 +266,19 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
     constexpr int kHalf = D / 2;
     __shared__ int s_warp[kBoundsWarps];
     __shared__ int s_b, s_page;
-    __shared__ __align__(16) float2 s_rot[kPageTokens][kHalf];      // (cos, sin), queries
-    __shared__ double2 s_rotd[kPageTokens][kHalf];                  // keys
+    // A row's rotation per pair, the gains of the head norms multiplied in: x' = x A - y B, y' = y C + x E.  Stored so that
+    // the lanes of a token read neighbouring words; queries' in pairs, for the packed arithmetic.
+    __shared__ __align__(16) union Rotation {
+        float4 q[kPageTokens][4][2][L::kPer];      // pairs 8 l + 2 k, + 1: (A, A', -B, -B'), (C, C', E, E') at [slot][k][0, 1][l]
+        double2 k[kPageTokens][8][2][L::kPer];     // (A, B), (C, E)
+    } rot;
+    const int task = (int)(p.q_offsets ? blockIdx.x / p.groups : blockIdx.x % p.batch);
+    const int group = (int)(p.q_offsets ? blockIdx.x % p.groups : blockIdx.x / p.batch);
     pdl_wait();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int b, page_i, row0, nrows, slot0;                              // rows row0 .. of the call go to slots slot0 .. of the page
     if (p.q_offsets == nullptr) {
-        b = blockIdx.x;
+        b = task;
         const int len = p.seq_lens[b];
         if (len < 1 || len > p.max_pages * kPageTokens) {
             if (tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
@@ -244,7 +302,7 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
         int local = 0, first;
         for (int i = lo; i < hi; ++i) {
             const int c = touched(i, first);
-            if (c < 0) { if (blockIdx.x == 0 && blockIdx.y == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS); }
+            if (c < 0) { if (blockIdx.x == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS); }
             else local += c;
         }
         int incl = local;
@@ -258,7 +316,7 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
         __syncthreads();
         int before = incl - local;
         for (int w = 0; w < warp; ++w) before += s_warp[w];
-        const int want = (int)blockIdx.x;
+        const int want = task;
         if (want >= before && want < before + local) {
             int at = before;
             for (int i = lo; i < hi; ++i) {
@@ -278,89 +336,101 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
         nrows = end - begin;
     }
     const int heads = p.Hq + 2 * p.Hkv;
-    const bool kv_part = (int)blockIdx.y < p.kv_ctas;
+    const bool kv_part = group < p.kv_ctas;
     const int page = p.page_table[(size_t)b * p.max_pages + page_i];
     if (kv_part && (page < 0 || page >= p.num_pages)) {
         if (tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
         return;
     }
-    // the rows' rotations: angle and its reduction to [-pi, pi] in double (two-term 2 pi)
-    for (int i = tid; i < nrows * kHalf; i += kBoundsThreads) {
-        const int r = i / kHalf, c = i % kHalf;
-        const double ang = (double)(page_i * kPageTokens + slot0 + r) * p.inv_freq[c];
-        const double turns = rint(ang * 0.15915494309189535);
-        const double red = fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
-        if (kv_part) {
-            double sn, cs;
-            sincos(red, &sn, &cs);
-            s_rotd[r][c] = make_double2(cs, sn);
-        } else {
-            float sn, cs;
-            sincosf((float)red, &sn, &cs);
-            s_rot[r][c] = make_float2(cs, sn);
-        }
-    }
-    __syncthreads();
     const int sub = lane / L::kPer, l = lane % L::kPer;
+    // Rotations, by slot of the page: angle and its reduction to [-pi, pi] in double (two-term 2 pi).  A thread makes the sine
+    // and cosine of one pair at every fourth slot and steps to the next three by the pair's rotation of one position; the
+    // steps start at fixed slots, so a position's rotation does not depend on which rows came with it.
+    const int slot1 = slot0 + nrows, c_rot = tid % kHalf, s_rot = 4 * (tid / kHalf);
+    const bool rotates = s_rot < slot1 && s_rot + 4 > slot0;
+    auto reduced = [&](int slot, int c) -> double {
+        const double ang = (double)(page_i * kPageTokens + slot) * p.inv_freq[c];
+        const double turns = rint(ang * 0.15915494309189535);
+        return fma(-turns, 2.4492935982947064e-16, fma(-turns, 6.283185307179586, ang));
+    };
     if (!kv_part) {
-        // ---- query heads.  A warp takes a row and U * kTok of its heads at a time: one rotation in registers, all loads first.
-        const int h_lo = ((int)blockIdx.y - p.kv_ctas) * p.q_heads_per_cta, h_hi = min(p.Hq, h_lo + p.q_heads_per_cta);
-        const int groups = (h_hi - h_lo + U * L::kTok - 1) / (U * L::kTok);
-        float gn[16];
+        // ---- query heads.  The warps are dealt out over rows and heads, two times kTok heads of a row at once; the next ones
+        // are loaded while these are rotated (the first ones while the rotations are made).
+        const int h_lo = (group - p.kv_ctas) * p.q_heads_per_cta, h_hi = min(p.Hq, h_lo + p.q_heads_per_cta);
+        const int along = nrows >= 8 ? 1 : nrows >= 4 ? 2 : nrows >= 2 ? 4 : 8;              // warps along the heads of a row
+        const int h_first = h_lo + (warp & (along - 1)) * 2 * L::kTok + sub, h_step = along * 2 * L::kTok;
+        const int r_first = warp / along, r_step = kBoundsWarps / along;
+        uint4 xa[2], xb[2];
+        auto load = [&](int r, int h) {
+            const uint4* src = reinterpret_cast<const uint4*>(p.qkv + (size_t)(row0 + r) * heads * D) + l;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) gn[i] = 1.f;
-        if (p.w_qn) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                gn[i] = __bfloat162float(p.w_qn[8 * l + i]);
-                gn[8 + i] = __bfloat162float(p.w_qn[kHalf + 8 * l + i]);
+            for (int u = 0; u < 2; ++u) {
+                const uint4* s = src + min(h + u * L::kTok, h_hi - 1) * (D / 8);
+                xa[u] = __ldg(s);
+                xb[u] = __ldg(s + D / 16);
+            }
+        };
+        if (r_first < nrows) load(r_first, h_first);
+        if (rotates) {
+            const int c = c_rot;
+            const float ga = p.w_qn ? __bfloat162float(p.w_qn[c]) : 1.f, gc = p.w_qn ? __bfloat162float(p.w_qn[kHalf + c]) : 1.f;
+            const float step_cs = (float)p.step_cos[c], step_sn = (float)p.step_sin[c];
+            float sn, cs;
+            sincosf((float)reduced(s_rot, c), &sn, &cs);
+            for (int s = s_rot; s < min(slot1, s_rot + 4); ++s) {
+                float* z = reinterpret_cast<float*>(&rot.q[s][(c & 7) >> 1][0][c >> 3]) + (c & 1);
+                z[0] = ga * cs; z[2] = -gc * sn;
+                z += 4 * L::kPer;
+                z[0] = gc * cs; z[2] = ga * sn;
+                const float next = cs * step_cs - sn * step_sn;
+                sn = sn * step_cs + cs * step_sn;
+                cs = next;
             }
         }
-        for (int task = warp; task < nrows * groups; task += kBoundsWarps) {
-            const int r = task / groups, h0 = h_lo + (task % groups) * (U * L::kTok) + sub;
-            const uint4* src = reinterpret_cast<const uint4*>(p.qkv + (size_t)(row0 + r) * heads * D) + l;
-            uint4 xa[U], xb[U];
+        __syncthreads();
+        for (int r = r_first; r < nrows; r += r_step) {
+            // (h_first - sub is the same for the whole warp)
+            for (int h = h_first; h - sub < h_hi; h += h_step) {
+                uint4 ya[2], yb[2];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = min(h0 + u * L::kTok, h_hi - 1);
-                xa[u] = __ldg(src + h * (D / 8));
-                xb[u] = __ldg(src + h * (D / 8) + D / 16);
-            }
-            float4 cs[4];                                           // (cos, sin) of this lane's eight pairs
+                for (int u = 0; u < 2; ++u) { ya[u] = xa[u]; yb[u] = xb[u]; }
+                if (h - sub + h_step < h_hi) load(r, h + h_step);
+                else if (r + r_step < nrows) load(r + r_step, h_first);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) cs[k] = *reinterpret_cast<const float4*>(&s_rot[r][8 * l + 2 * k]);
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t va[4] = {ya[u].x, ya[u].y, ya[u].z, ya[u].w}, vc[4] = {yb[u].x, yb[u].y, yb[u].z, yb[u].w};
+                    uint64_t a[4], c[4], rinv = pack_f32x2(1.f, 1.f);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const __nv_bfloat162* pa = reinterpret_cast<const __nv_bfloat162*>(&xa[u]);
-                const __nv_bfloat162* pb = reinterpret_cast<const __nv_bfloat162*>(&xb[u]);
-                float a[8], c[8], ss = 0.f;
+                    for (int k = 0; k < 4; ++k) { a[k] = widen_bf16x2(va[k]); c[k] = widen_bf16x2(vc[k]); }
+                    if (p.w_qn) {
+                        uint64_t s2 = 0;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 x = __bfloat1622float2(pa[k]), y = __bfloat1622float2(pb[k]);
-                    a[2 * k] = x.x; a[2 * k + 1] = x.y; c[2 * k] = y.x; c[2 * k + 1] = y.y;
-                }
-                if (p.w_qn) {
+                        for (int k = 0; k < 4; ++k) s2 = fma_f32x2(a[k], a[k], fma_f32x2(c[k], c[k], s2));
+                        float s0, s1;
+                        unpack_f32x2(s2, s0, s1);
+                        float ss = s0 + s1;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) ss = fmaf(a[k], a[k], fmaf(c[k], c[k], ss));
+                        for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
+                        const float ri = rsqrtf(ss / (float)D + p.eps);
+                        rinv = pack_f32x2(ri, ri);
+                    }
+                    uint32_t qa[4], qb[4];
 #pragma unroll
-                    for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                    const float rinv = rsqrtf(ss / (float)D + p.eps);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) { a[k] *= rinv * gn[k]; c[k] *= rinv * gn[8 + k]; }
-                }
-                uint4 oa, ob;
-                __nv_bfloat162* qa = reinterpret_cast<__nv_bfloat162*>(&oa);
-                __nv_bfloat162* qb = reinterpret_cast<__nv_bfloat162*>(&ob);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    qa[k] = __floats2bfloat162_rn(a[2 * k] * cs[k].x - c[2 * k] * cs[k].y, a[2 * k + 1] * cs[k].z - c[2 * k + 1] * cs[k].w);
-                    qb[k] = __floats2bfloat162_rn(c[2 * k] * cs[k].x + a[2 * k] * cs[k].y, c[2 * k + 1] * cs[k].z + a[2 * k + 1] * cs[k].w);
-                }
-                const int h = h0 + u * L::kTok;
-                if (h < h_hi) {
-                    uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)(row0 + r) * p.Hq + h) * D);
-                    dst[l] = oa;
-                    dst[D / 16 + l] = ob;
+                    for (int k = 0; k < 4; ++k) {
+                        const ulonglong2 z0 = *reinterpret_cast<const ulonglong2*>(&rot.q[slot0 + r][k][0][l]);
+                        const ulonglong2 z1 = *reinterpret_cast<const ulonglong2*>(&rot.q[slot0 + r][k][1][l]);
+                        float x0, x1, y0, y1;
+                        unpack_f32x2(mul_f32x2(fma_f32x2(a[k], z0.x, mul_f32x2(c[k], z0.y)), rinv), x0, x1);
+                        unpack_f32x2(mul_f32x2(fma_f32x2(c[k], z1.x, mul_f32x2(a[k], z1.y)), rinv), y0, y1);
+                        qa[k] = pack_bf16x2(x0, x1);
+                        qb[k] = pack_bf16x2(y0, y1);
+                    }
+                    const uint4 oa = make_uint4(qa[0], qa[1], qa[2], qa[3]), ob = make_uint4(qb[0], qb[1], qb[2], qb[3]);
+                    if (h + u * L::kTok < h_hi) {
+                        uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)(row0 + r) * p.Hq + h + u * L::kTok) * D);
+                        dst[l] = oa;
+                        dst[D / 16 + l] = ob;
+                    }
                 }
             }
         }
@@ -368,7 +438,23 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
     }
     // ---- value heads: copied as they are; key heads: a warp each
     const int step = p.kv_ctas * kBoundsWarps;
-    for (int i = (int)blockIdx.y * kBoundsWarps + warp; i < 2 * p.Hkv; i += step) {
+    if (group * kBoundsWarps < p.Hkv) {                   // (not where this CTA has values only)
+        if (rotates) {
+            const int c = c_rot;
+            const double ga = p.w_kn ? __bfloat162float(p.w_kn[c]) : 1.f, gc = p.w_kn ? __bfloat162float(p.w_kn[kHalf + c]) : 1.f;
+            double sn, cs;
+            sincos(reduced(s_rot, c), &sn, &cs);
+            for (int s = s_rot; s < min(slot1, s_rot + 4); ++s) {
+                rot.k[s][c & 7][0][c >> 3] = make_double2(ga * cs, gc * sn);
+                rot.k[s][c & 7][1][c >> 3] = make_double2(gc * cs, ga * sn);
+                const double next = cs * p.step_cos[c] - sn * p.step_sin[c];
+                sn = sn * p.step_cos[c] + cs * p.step_sin[c];
+                cs = next;
+            }
+        }
+        __syncthreads();
+    }
+    for (int i = group * kBoundsWarps + warp; i < 2 * p.Hkv; i += step) {
         const int g = i < p.Hkv ? i : i - p.Hkv;
         const size_t slab = (size_t)page * p.Hkv + g;
         if (i >= p.Hkv) {
@@ -406,7 +492,7 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
             if (t0 >= end) break;
             const int t = min(t0 + sub, end - 1);
             if (t0 + L::kTok > slot0) {                             // some of these tokens are new (the same for the whole warp)
-                const int r = max(0, t - slot0);
+                const int s = max(slot0, t);
                 const __nv_bfloat16* pa = reinterpret_cast<const __nv_bfloat16*>(&xa[it]);
                 const __nv_bfloat16* pb = reinterpret_cast<const __nv_bfloat16*>(&xb[it]);
                 double rinv = 1.0;
@@ -426,14 +512,10 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
                 __nv_bfloat16* qb = reinterpret_cast<__nv_bfloat16*>(&ob);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    double a = __bfloat162float(pa[k]), c = __bfloat162float(pb[k]);
-                    if (p.w_kn) {
-                        a *= rinv * (double)__bfloat162float(p.w_kn[8 * l + k]);
-                        c *= rinv * (double)__bfloat162float(p.w_kn[kHalf + 8 * l + k]);
-                    }
-                    const double2 rot = s_rotd[r][8 * l + k];
-                    qa[k] = __float2bfloat16_rn((float)(a * rot.x - c * rot.y));
-                    qb[k] = __float2bfloat16_rn((float)(c * rot.x + a * rot.y));
+                    const double a = __bfloat162float(pa[k]), c = __bfloat162float(pb[k]);
+                    const double2 z0 = rot.k[s][k][0][l], z1 = rot.k[s][k][1][l];
+                    qa[k] = __float2bfloat16_rn((float)((a * z0.x - c * z0.y) * rinv));
+                    qb[k] = __float2bfloat16_rn((float)((c * z1.x + a * z1.y) * rinv));
                 }
                 if (t >= slot0) {
                     xa[it] = oa;
@@ -461,14 +543,23 @@ aflex_status page_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.page_table = kv->page_table; p.seq_lens = kv->seq_lens; p.first_token = first_token;
     p.max_pages = kv->max_pages_per_seq; p.Hkv = d->num_kv_heads; p.num_pages = kv->num_pages;
     p.status = ctx->dev_status;
-    // all heads of a page on one warp where that still leaves 16 warps per SM, fewer of them where there are few pages
-    const long long pages = (long long)batch * p.max_pages;
-    p.heads_per_warp = 1;
-    while (p.heads_per_warp < p.Hkv && pages * p.Hkv >= 2LL * p.heads_per_warp * 16 * ctx->num_sms) p.heads_per_warp *= 2;
-    const long long items = (long long)p.max_pages * ((p.Hkv + p.heads_per_warp - 1) / p.heads_per_warp);
-    const dim3 grid((unsigned)((items + kBoundsWarps - 1) / kBoundsWarps), (unsigned)batch);
+    // Pages per CTA: one (page, head) per warp at least; twice and four times that where four CTAs per SM are still left.
+    // 32 sequences of up to 256 pages x 8 heads: 37.2 / 29.2 / 28.8 / 32.5 us with 1 / 2 / 4 / 8 heads per warp (a ring of
+    // three: 48.4 / 34.7 / 29.9 / 31.7; every warp's 16 keys in registers: 35.3).
+    const int least = (kBoundsWarps + p.Hkv - 1) / p.Hkv;
+    p.pages_per_cta = least;
+    while (p.pages_per_cta < 4 * least && p.pages_per_cta <= 16 && (long long)batch * p.max_pages >= 2LL * p.pages_per_cta * 4 * ctx->num_sms)
+        p.pages_per_cta *= 2;
+    const dim3 grid((unsigned)((p.max_pages + p.pages_per_cta - 1) / p.pages_per_cta), (unsigned)batch);
+    const size_t smem = (size_t)kBoundsWarps * kBoundsStages * kPageTokens * d->head_dim * 2;
+    const bool wide = d->head_dim == 128;
+    if (!ctx->bounds_attr_set[wide]) {
+        cudaError_t e = cudaFuncSetAttribute(wide ? page_bounds_kernel<128> : page_bounds_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(page bounds)");
+        ctx->bounds_attr_set[wide] = true;
+    }
     KernelScope scope(ctx, kKPageBounds, st);
-    return check_cuda(ctx, launch_pdl(d->head_dim == 128 ? page_bounds_kernel<128> : page_bounds_kernel<64>, grid, dim3(kBoundsThreads), 0, st, p),
+    return check_cuda(ctx, launch_pdl(wide ? page_bounds_kernel<128> : page_bounds_kernel<64>, grid, dim3(kBoundsThreads), smem, st, p),
                       "page_bounds_kernel launch");
 }
 
@@ -487,21 +578,20 @@ aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d,
     p.codes = bounds->codes; p.scales = bounds->scales;
     p.eps = eps;
     for (int i = 0; i < 64; ++i) p.inv_freq[i] = i < d->head_dim / 2 ? pow((double)theta, -2.0 * i / (double)d->head_dim) : 0.0;
+    for (int i = 0; i < 64; ++i) { p.step_cos[i] = cos(p.inv_freq[i]); p.step_sin[i] = sin(p.inv_freq[i]); }
     p.status = ctx->dev_status;
-    // A page's K and V heads on one CTA per eight of them.  One row per sequence: 16 query heads per CTA, every warp a few of
-    // them; chunks: 32 query heads per CTA, so that a warp keeps a row's rotation for several loads.
-    p.kv_ctas = (2 * p.Hkv + kBoundsWarps - 1) / kBoundsWarps;
+    // A page's K and V heads on one CTA per eight of them; its query heads 32 per CTA, 16 where a page has one new row.
+    // m new tokens of a sequence touch at most (m + 14) / 16 + 1 pages.
+    const long long tasks = q_offsets ? ((long long)rows + 14LL * batch) / 16 + batch : batch;
     const int per_cta = q_offsets ? 32 : 16;
+    p.kv_ctas = (2 * p.Hkv + kBoundsWarps - 1) / kBoundsWarps;
     p.q_heads_per_cta = p.Hq < per_cta ? p.Hq : per_cta;
     const int q_ctas = (p.Hq + p.q_heads_per_cta - 1) / p.q_heads_per_cta;
-    // m new tokens of a sequence touch at most (m + 14) / 16 + 1 pages
-    const long long tasks = q_offsets ? ((long long)rows + 14LL * batch) / 16 + batch : batch;
+    p.groups = p.kv_ctas + q_ctas;
+    if (tasks * p.groups > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "rope_append_bounds: rows = %d", rows);
     KernelScope scope(ctx, kKAppendBounds, st);
-    typedef void (*Kernel)(const AppendParams);
-    static const Kernel kernels[2][2] = {{rope_append_bounds_kernel<64, 1>, rope_append_bounds_kernel<64, 2>},
-                                         {rope_append_bounds_kernel<128, 1>, rope_append_bounds_kernel<128, 4>}};
-    return check_cuda(ctx, launch_pdl(kernels[d->head_dim == 128][q_offsets != nullptr],
-                                      dim3((unsigned)tasks, (unsigned)(p.kv_ctas + q_ctas)), dim3(kBoundsThreads), 0, st, p),
+    return check_cuda(ctx, launch_pdl(d->head_dim == 128 ? rope_append_bounds_kernel<128> : rope_append_bounds_kernel<64>,
+                                      dim3((unsigned)(tasks * p.groups)), dim3(kBoundsThreads), 0, st, p),
                       "rope_append_bounds_kernel launch");
 }
 
