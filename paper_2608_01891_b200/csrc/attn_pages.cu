@@ -107,10 +107,10 @@ struct SelectParams {
     const int32_t* page_table;
     const int32_t* seq_lens;
     const int32_t* q_offsets;
-    int batch, max_pages, Hq, Hkv, G;
+    int batch, rows, max_pages, Hq, Hkv, G;
     long long num_pages;
     int top, sink, window;
-    int cluster;                   // CTAs per (row, KV head)
+    int cluster;                   // CTAs per (row, KV head); rows per group
     int32_t* list;                 // [rows][Hkv][top]
     int32_t* count;                // [rows][Hkv]
     int* status;
@@ -140,156 +140,104 @@ __device__ __forceinline__ int q_exponent(float a) {             // smallest e w
     return max(-60, min(50, e));
 }
 
-// W warps, T tiles per warp in flight.
-template <int D, int W, int T>
-__global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_select_kernel(const SelectParams p) {
-    constexpr int kBlocks = D / 32;
-    constexpr int kThreads = W * 32;
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    float* scores = reinterpret_cast<float*>(smem_raw);            // of this CTA's candidates
-    __shared__ SelectShared<W> sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int S = p.cluster, rank = (int)(blockIdx.x % S);
-    const long long item = blockIdx.x / S;
-    const int row = (int)(item / p.Hkv), g = (int)(item % p.Hkv);
-    const int hl = lane >> 2, l4 = lane & 3;
-    if (S > 1) cluster_arrive();                                  // the cluster's CTAs have started: waited for below
-    if (tid < 256) sh.hist[tid] = 0;
-    if (tid == 0) sh.members = 0;
-    pdl_launch_dependents();
-    pdl_wait();
-    // The first four warps quantise a block of the queries each: lane holds head lane / 4, channels 8 (lane % 4) .. + 7.
-    const bool quantises = warp < kBlocks;
-    uint4 qx = make_uint4(0, 0, 0, 0);
-    if (quantises && hl < p.G)
-        qx = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + hl) * D) + warp * 4 + l4);
-    const RowSeq at = locate_row(row, p.q_offsets, p.batch);
-    const int len = __ldg(p.seq_lens + at.b);
-    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
-    // The lanes hold the page ids of two of the warp's tiles (lane / 16).  With one CTA the warp's tiles do not depend on the
-    // length, so the first ids are loaded along with it (whatever the table's row holds beyond the sequence).
-    auto page_ids = [&](int t) -> int {
-        const long long j = p.sink + (long long)(t + (lane >> 4) * W) * kSelTile + (lane & 15);
-        return __ldg(table + min(j, (long long)p.max_pages - 1));
-    };
-    int t = warp, ids = S == 1 ? page_ids(t) : 0;
-    const int pos = row_position(at, len, p.max_pages), n = pos >= 0 ? pos / kPageTokens + 1 : 0;
-    if (pos < 0 && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+// Quantises a 32-channel block of a group's queries: lane holds head lane / 4, channels 8 (lane % 4) .. + 7 in x.
+__device__ __forceinline__ void quantise_block(uint4 x, int lane, uint4& out, float& f) {
+    const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+    float v[8], a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(in[i] << 16); v[2 * i + 1] = __uint_as_float(in[i] & 0xffff0000u);
+        a = fmaxf(a, fmaxf(fabsf(v[2 * i]), fabsf(v[2 * i + 1])));      // (a NaN is passed over)
+    }
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    const int e = q_exponent(a);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    uint32_t w[2], neg[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int z[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] = max(-127, min(127, __float2int_rn(v[4 * i + k] * inv)));        // NaN becomes 0
+        w[i] = __byte_perm(__byte_perm(z[0], z[1], 0x0040), __byte_perm(z[2], z[3], 0x0040), 0x5410);
+        neg[i] = w[i] & (((w[i] & 0x80808080u) >> 7) * 255u);                                               // bytes below zero
+    }
+    out = make_uint4(w[0] & ~neg[0], w[1] & ~neg[1], neg[0], neg[1]);
+    f = __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+// The bounds of a tile's 16 pages as this lane's A operands: rows lane / 4 and + 8.  `ids`: page ids by lane, the tile's from
+// lane `from` on; j: the candidate of row 0, of which those below `end` exist (of the others some page is loaded).
+template <int D> struct Tile { uint4 x[2][D / 32]; uint32_t scale[2]; };
+template <int D>
+__device__ __forceinline__ void load_tile(Tile<D>& tile, const SelectParams& p, int g, int ids, int from, int j, int end) {
+    const int lane = threadIdx.x & 31, hl = lane >> 2, l4 = lane & 3;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        int id = __shfl_sync(0xffffffffu, ids, from + hl + 8 * r);
+        if (j + hl + 8 * r >= end) id = 0;
+        if (id < 0 || id >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
+        const size_t slab = (size_t)id * p.Hkv + g;
+        const uint4* src = reinterpret_cast<const uint4*>(p.codes + slab * (2 * D)) + l4;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) tile.x[r][c] = __ldg(src + c * 4);
+        if (D == 128) tile.scale[r] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + slab);
+        else tile.scale[r] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + slab);
+    }
+}
+// Scores of a tile's pages; lanes 4 i and 4 i + 1 return those of rows i and i + 8.
+template <int D>
+__device__ __forceinline__ float score_tile(const Tile<D>& tile, const uint4 (&qf)[D / 32], const float2 (&fq)[D / 32], int G) {
+    const int l4 = threadIdx.x & 3;
+    float s[4];
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        int d[4] = {0, 0, 0, 0};
+        mma_s8_16832(d, tile.x[0][c].x, tile.x[1][c].x, tile.x[0][c].y, tile.x[1][c].y, qf[c].x, qf[c].y);
+        mma_s8_16832(d, tile.x[0][c].z, tile.x[1][c].z, tile.x[0][c].w, tile.x[1][c].w, qf[c].z, qf[c].w);
+        const float k0 = __uint_as_float(((tile.scale[0] >> (8 * c)) & 255u) << 23), k1 = __uint_as_float(((tile.scale[1] >> (8 * c)) & 255u) << 23);
+        // the products are exact, so a fused multiply-add rounds like the sum alone
+        s[0] = fmaf((float)d[0] * k0, fq[c].x, c ? s[0] : 0.f);
+        s[1] = fmaf((float)d[1] * k0, fq[c].y, c ? s[1] : 0.f);
+        s[2] = fmaf((float)d[2] * k1, fq[c].x, c ? s[2] : 0.f);
+        s[3] = fmaf((float)d[3] * k1, fq[c].y, c ? s[3] : 0.f);
+    }
+    const bool h0 = 2 * l4 < G, h1 = 2 * l4 + 1 < G;
+    float m0 = fmaxf(h0 ? s[0] : -INFINITY, h1 ? s[1] : -INFINITY);
+    float m1 = fmaxf(h0 ? s[2] : -INFINITY, h1 ? s[3] : -INFINITY);
+    m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
+    m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
+    m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
+    m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
+    return l4 ? m1 : m0;
+}
+// The list of a row that sees n pages of which nothing has to be chosen: all of them, or the first and the last ones.
+__device__ __forceinline__ void list_without_choice(const SelectParams& p, long long item, int n, int threads) {
     int32_t* list = p.list + item * p.top;
-    const int keep = p.top - p.sink - p.window;                   // scored pages to keep
-    const int cand = n - p.sink - p.window;                       // scored pages
-    if (n <= p.top || keep == 0) {                                // nothing to choose (the same for the whole cluster)
-        if (S > 1) cluster_wait();
-        if (rank != 0 || at.padding) return;
-        for (int i = tid; i < p.top; i += kThreads) {
-            int v = i < n ? i : -1;
-            if (n > p.top && i >= p.sink) v = n - p.top + i;
-            list[i] = v;
-        }
-        if (tid == 0) p.count[item] = min(n, p.top);
-        return;
+    for (int i = threadIdx.x; i < p.top; i += threads) {
+        int v = i < n ? i : -1;
+        if (n > p.top && i >= p.sink) v = n - p.top + i;
+        list[i] = v;
     }
-    if (quantises) {
-        const __nv_bfloat162* px = reinterpret_cast<const __nv_bfloat162*>(&qx);
-        float v[8], a = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 u = __bfloat1622float2(px[i]);
-            v[2 * i] = u.x; v[2 * i + 1] = u.y;
-            a = fmaxf(a, fmaxf(fabsf(u.x), fabsf(u.y)));          // (a NaN is passed over)
-        }
-        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
-        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
-        const int e = q_exponent(a);
-        const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-        uint32_t w[2], neg[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            int z[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) z[k] = max(-127, min(127, __float2int_rn(v[4 * i + k] * inv)));        // NaN becomes 0
-            w[i] = __byte_perm(__byte_perm(z[0], z[1], 0x0040), __byte_perm(z[2], z[3], 0x0040), 0x5410);
-            neg[i] = w[i] & (((w[i] & 0x80808080u) >> 7) * 255u);                                               // bytes below zero
-        }
-        sh.q[warp][lane] = make_uint4(w[0] & ~neg[0], w[1] & ~neg[1], neg[0], neg[1]);
-        if (l4 == 0) sh.f[warp][hl] = __uint_as_float((uint32_t)(127 + e) << 23);
-    }
-    if (rank == 0 && warp == W - 1) {                             // meanwhile: the pages that are listed in any case
-        for (int i = lane; i < p.sink; i += 32) list[i] = i;
-        for (int i = lane; i < p.window; i += 32) list[p.top - p.window + i] = n - p.window + i;
-        if (lane == 0) p.count[item] = p.top;
-    }
-    __syncthreads();
-    uint4 qf[kBlocks];
-    float2 fq[kBlocks];                                           // of this lane's two accumulator columns
-#pragma unroll
-    for (int c = 0; c < kBlocks; ++c) {
-        qf[c] = sh.q[c][lane];
-        fq[c] = *reinterpret_cast<const float2*>(&sh.f[c][2 * l4]);
-    }
-    if (S > 1) cluster_wait();
-    // ---- scores of this CTA's candidates [c0, c1)
-    const int tiles = (cand + kSelTile - 1) / kSelTile, share = (tiles + S - 1) / S;
-    const int c0 = min(cand, rank * share * kSelTile), c1 = min(cand, c0 + share * kSelTile);
-    const int t_end = min(tiles, (rank + 1) * share);
-    const bool h0 = 2 * l4 < p.G, h1 = 2 * l4 + 1 < p.G;
-    float low = INFINITY, high = -INFINITY;
-    if (S > 1) {
-        t += rank * share;
-        ids = page_ids(t);
-    }
-    while (t < t_end) {
-        uint4 x[T][2][kBlocks];
-        uint32_t sc[T][2];
-#pragma unroll
-        for (int k = 0; k < T; ++k) {
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int j = (t + k * W) * kSelTile + hl + 8 * r;
-                int id = __shfl_sync(0xffffffffu, ids, k * 16 + hl + 8 * r);
-                if (j >= c1) id = 0;                              // past the last candidate: some page, its score is dropped
-                if (id < 0 || id >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
-                const size_t slab = (size_t)id * p.Hkv + g;
-                const uint4* src = reinterpret_cast<const uint4*>(p.codes + slab * (2 * D)) + l4;
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) x[k][r][c] = __ldg(src + c * 4);
-                if (kBlocks == 4) sc[k][r] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + slab);
-                else sc[k][r] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + slab);
-            }
-        }
-        const int t_now = t;
-        t += T * W;
-        if (t < t_end) ids = page_ids(t);
-#pragma unroll
-        for (int k = 0; k < T; ++k) {
-            float s[4];
-#pragma unroll
-            for (int c = 0; c < kBlocks; ++c) {
-                int d[4] = {0, 0, 0, 0};
-                mma_s8_16832(d, x[k][0][c].x, x[k][1][c].x, x[k][0][c].y, x[k][1][c].y, qf[c].x, qf[c].y);
-                mma_s8_16832(d, x[k][0][c].z, x[k][1][c].z, x[k][0][c].w, x[k][1][c].w, qf[c].z, qf[c].w);
-                const float k0 = __uint_as_float(((sc[k][0] >> (8 * c)) & 255u) << 23), k1 = __uint_as_float(((sc[k][1] >> (8 * c)) & 255u) << 23);
-                // the products are exact, so a fused multiply-add rounds like the sum alone
-                s[0] = fmaf((float)d[0] * k0, fq[c].x, c ? s[0] : 0.f);
-                s[1] = fmaf((float)d[1] * k0, fq[c].y, c ? s[1] : 0.f);
-                s[2] = fmaf((float)d[2] * k1, fq[c].x, c ? s[2] : 0.f);
-                s[3] = fmaf((float)d[3] * k1, fq[c].y, c ? s[3] : 0.f);
-            }
-            float m0 = fmaxf(h0 ? s[0] : -INFINITY, h1 ? s[1] : -INFINITY);
-            float m1 = fmaxf(h0 ? s[2] : -INFINITY, h1 ? s[3] : -INFINITY);
-            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
-            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
-            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
-            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
-            const int j = (t_now + k * W) * kSelTile + hl + 8 * l4;
-            if (l4 < 2 && j < c1) {
-                const float v = l4 ? m1 : m0;
-                low = fminf(low, v);
-                high = fmaxf(high, v);
-                scores[j - c0] = v;
-            }
-        }
-    }
+    if (threadIdx.x == 0) p.count[item] = min(n, p.top);
+}
+// What is listed in any case of a row that sees n > top pages, by one warp.
+__device__ __forceinline__ void list_forced(const SelectParams& p, long long item, int n) {
+    const int lane = threadIdx.x & 31;
+    int32_t* list = p.list + item * p.top;
+    for (int i = lane; i < p.sink; i += 32) list[i] = i;
+    for (int i = lane; i < p.window; i += 32) list[p.top - p.window + i] = n - p.window + i;
+    if (lane == 0) p.count[item] = p.top;
+}
+
+// Keeps the `keep` best of a row's `cand` candidates and writes them to list[sink ..], ascending.  This CTA (of S in the
+// cluster) holds the scores of [c0, c1); low and high are the extremes of what the thread has seen of them.  `share`: the most
+// tiles that a CTA holds.  The histogram and the member count are zero on entry.
+template <int W>
+__device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* scores, int S, int rank, int cand, int c0, int c1, int share,
+                                             float low, float high, int keep, int sink, int32_t* list) {
+    constexpr int kThreads = W * 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned below = (1u << lane) - 1u;
     // ---- division.  What the CTAs tell one another goes through shared memory that is written before a barrier and read after.
     auto sync_all = [&]() {
@@ -397,7 +345,8 @@ __global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_sele
         each([&](int j, float s, bool in) {
             if (in && member(j, s)) {
                 const int i = atomicAdd(&sh.members, 1);
-                for (int c = 0; c < S; ++c)
+                if (S == 1) sh.member[0][i] = make_uint2(__float_as_uint(s), (uint32_t)j);       // (cluster or not: this CTA's)
+                else for (int c = 0; c < S; ++c)
                     st_cluster_v2(cluster_map_shared(smem_u32(&sh.member[rank][i]), (uint32_t)c), __float_as_uint(s), (uint32_t)j);
             }
         });
@@ -455,13 +404,204 @@ __global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_sele
         sync_all();                                                // behind it nobody reads another CTA's shared memory
         base += __reduce_add_sync(0xffffffffu, lane < rank ? sh.all_kept[lane] : 0);
     }
-    int32_t* to = list + p.sink + base;
+    int32_t* to = list + sink + base;
     each([&](int j, float s, bool in) {
         const bool mine = in && keeps(j, s);
         const unsigned who = __ballot_sync(0xffffffffu, mine);
-        if (mine) to[__popc(who & below)] = p.sink + j;
+        if (mine) to[__popc(who & below)] = sink + j;
         to += __popc(who);
     });
+}
+
+// W warps, T tiles per warp in flight.
+template <int D, int W, int T>
+__global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_select_kernel(const SelectParams p) {
+    constexpr int kBlocks = D / 32;
+    constexpr int kThreads = W * 32;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    float* scores = reinterpret_cast<float*>(smem_raw);            // of this CTA's candidates
+    __shared__ SelectShared<W> sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int S = p.cluster, rank = (int)(blockIdx.x % S);
+    const long long item = blockIdx.x / S;
+    const int row = (int)(item / p.Hkv), g = (int)(item % p.Hkv);
+    const int hl = lane >> 2, l4 = lane & 3;
+    if (S > 1) cluster_arrive();                                  // the cluster's CTAs have started: waited for below
+    if (tid < 256) sh.hist[tid] = 0;
+    if (tid == 0) sh.members = 0;
+    pdl_launch_dependents();
+    pdl_wait();
+    // The first four warps quantise a block of the queries each: lane holds head lane / 4, channels 8 (lane % 4) .. + 7.
+    const bool quantises = warp < kBlocks;
+    uint4 qx = make_uint4(0, 0, 0, 0);
+    if (quantises && hl < p.G)
+        qx = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + hl) * D) + warp * 4 + l4);
+    const RowSeq at = locate_row(row, p.q_offsets, p.batch);
+    const int len = __ldg(p.seq_lens + at.b);
+    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
+    // The lanes hold the page ids of two of the warp's tiles (lane / 16).  With one CTA the warp's tiles do not depend on the
+    // length, so the first ids are loaded along with it (whatever the table's row holds beyond the sequence).
+    auto page_ids = [&](int t) -> int {
+        const long long j = p.sink + (long long)(t + (lane >> 4) * W) * kSelTile + (lane & 15);
+        return __ldg(table + min(j, (long long)p.max_pages - 1));
+    };
+    int t = warp, ids = S == 1 ? page_ids(t) : 0;
+    const int pos = row_position(at, len, p.max_pages), n = pos >= 0 ? pos / kPageTokens + 1 : 0;
+    if (pos < 0 && !at.padding && tid == 0 && rank == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    int32_t* list = p.list + item * p.top;
+    const int keep = p.top - p.sink - p.window;                   // scored pages to keep
+    const int cand = n - p.sink - p.window;                       // scored pages
+    if (n <= p.top || keep == 0) {                                // nothing to choose (the same for the whole cluster)
+        if (S > 1) cluster_wait();
+        if (rank == 0 && !at.padding) list_without_choice(p, item, n, kThreads);
+        return;
+    }
+    if (quantises) {
+        float f;
+        quantise_block(qx, lane, sh.q[warp][lane], f);
+        if (l4 == 0) sh.f[warp][hl] = f;
+    }
+    if (rank == 0 && warp == W - 1) list_forced(p, item, n);
+    __syncthreads();
+    uint4 qf[kBlocks];
+    float2 fq[kBlocks];                                           // of this lane's two accumulator columns
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+        qf[c] = sh.q[c][lane];
+        fq[c] = *reinterpret_cast<const float2*>(&sh.f[c][2 * l4]);
+    }
+    if (S > 1) cluster_wait();
+    // ---- scores of this CTA's candidates [c0, c1)
+    const int tiles = (cand + kSelTile - 1) / kSelTile, share = (tiles + S - 1) / S;
+    const int c0 = min(cand, rank * share * kSelTile), c1 = min(cand, c0 + share * kSelTile);
+    const int t_end = min(tiles, (rank + 1) * share);
+    float low = INFINITY, high = -INFINITY;
+    if (S > 1) {
+        t += rank * share;
+        ids = page_ids(t);
+    }
+    while (t < t_end) {
+        Tile<D> tile[T];
+#pragma unroll
+        for (int k = 0; k < T; ++k) load_tile<D>(tile[k], p, g, ids, k * 16, (t + k * W) * kSelTile, c1);
+        const int t_now = t;
+        t += T * W;
+        if (t < t_end) ids = page_ids(t);
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+            const float v = score_tile<D>(tile[k], qf, fq, p.G);
+            const int j = (t_now + k * W) * kSelTile + hl + 8 * l4;
+            if (l4 < 2 && j < c1) {
+                low = fminf(low, v);
+                high = fmaxf(high, v);
+                scores[j - c0] = v;
+            }
+        }
+    }
+    select_pages<W>(sh, scores, S, rank, cand, c0, c1, share, low, high, keep, p.sink, list);
+}
+
+// The same for several rows of one sequence (drafted tokens, a prompt chunk): a cluster of `group` CTAs per `group` neighbouring
+// rows and KV head.  Each CTA scores a share of the pages for all of the rows, so that a page's bounds are read once for them
+// -- read once per row they are what bounds the kernel above when rows are many: an SM takes some 32 bytes a cycle out of L2 --
+// and sends the scores to the CTA of the row, which then selects for its row alone.  Rows of different sequences in one group
+// (the host can only guess where sequences end) are scored by their own CTAs.
+constexpr int kRowsWarps = 8;
+template <int D>
+__global__ void __launch_bounds__(kRowsWarps * 32, 3) page_select_rows_kernel(const SelectParams p) {
+    constexpr int kBlocks = D / 32, W = kRowsWarps, kThreads = W * 32;
+    extern __shared__ __align__(16) uint8_t smem_raw[];
+    const int R = p.cluster;
+    uint4* queries = reinterpret_cast<uint4*>(smem_raw);                          // [R][kBlocks][32]
+    float* factors = reinterpret_cast<float*>(queries + R * kBlocks * 32);        // [R][kBlocks][8]
+    float* scores = factors + R * kBlocks * 8;                                    // of this CTA's row
+    __shared__ SelectShared<W> sh;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int hl = lane >> 2, l4 = lane & 3;
+    const int rank = (int)(blockIdx.x % R), g = (int)(blockIdx.x / R % p.Hkv), row0 = (int)(blockIdx.x / R / p.Hkv) * R;
+    const int nrows = min(R, p.rows - row0), row = row0 + rank;
+    cluster_arrive();
+    if (tid < 256) sh.hist[tid] = 0;
+    if (tid == 0) sh.members = 0;
+    pdl_launch_dependents();
+    pdl_wait();
+    // A warp quantises up to four (row, block) pairs of the group's queries; they are loaded before it is known which are needed.
+    constexpr int kPairs = kSelMaxCluster * kBlocks / W;
+    uint4 qx[kPairs];
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+        const int i = warp + k * W, r = i / kBlocks;
+        qx[k] = make_uint4(0, 0, 0, 0);
+        if (r < nrows && hl < p.G)
+            qx[k] = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)(row0 + r) * p.Hq + (size_t)g * p.G + hl) * D) + (i % kBlocks) * 4 + l4);
+    }
+    const RowSeq first = locate_row(row0, p.q_offsets, p.batch);
+    const bool shared = !first.padding && first.back >= nrows - 1;                // all rows of the group in one sequence
+    RowSeq at = first, last = first;
+    last.back -= nrows - 1;
+    if (shared) at.back = first.back - rank;
+    else if (rank < nrows) at = locate_row(row, p.q_offsets, p.batch);
+    const int len = __ldg(p.seq_lens + at.b);
+    const bool mine = rank < nrows && !at.padding;                                // this CTA has a row
+    const int pos = mine ? row_position(at, len, p.max_pages) : -1, n = pos >= 0 ? pos / kPageTokens + 1 : 0;
+    if (mine && pos < 0 && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    const int keep = p.top - p.sink - p.window, forced = p.sink + p.window;
+    // pages to score: of the group, as its last row sees them, or of this CTA's row
+    const int n_all = shared ? max(0, row_position(last, len, p.max_pages)) / kPageTokens + 1 : n;
+    const int cand = n_all > p.top && keep > 0 ? n_all - forced : 0;
+    const int ra = shared ? 0 : rank, rb = shared ? nrows : rank + 1;
+    const int t0 = shared ? rank * W + warp : warp, stride = shared ? R * W : W;
+    const int tiles = (cand + kSelTile - 1) / kSelTile;
+    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
+    auto page_ids = [&](int t) -> int {
+        const long long j = p.sink + (long long)t * kSelTile + (lane & 15);
+        return __ldg(table + min(j, (long long)p.max_pages - 1));
+    };
+    int ids = page_ids(t0);
+    if (cand > 0) {
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+            const int i = warp + k * W;
+            if (i < R * kBlocks) {
+                float f;
+                quantise_block(qx[k], lane, queries[i * 32 + lane], f);
+                if (l4 == 0) factors[i * 8 + hl] = f;
+            }
+        }
+    }
+    __syncthreads();
+    cluster_wait();                                                               // the group's CTAs have started
+    const uint32_t scores_addr = smem_u32(scores);
+    for (int t = t0; t < tiles; t += stride) {
+        Tile<D> tile;
+        load_tile<D>(tile, p, g, ids, 0, t * kSelTile, cand);
+        if (t + stride < tiles) ids = page_ids(t + stride);
+        const int j = t * kSelTile + hl + 8 * l4;
+        for (int r = ra; r < rb; ++r) {
+            uint4 qf[kBlocks];
+            float2 fq[kBlocks];
+#pragma unroll
+            for (int c = 0; c < kBlocks; ++c) {
+                qf[c] = queries[(r * kBlocks + c) * 32 + lane];
+                fq[c] = *reinterpret_cast<const float2*>(factors + (r * kBlocks + c) * 8 + 2 * l4);
+            }
+            const float v = score_tile<D>(tile, qf, fq, p.G);
+            if (l4 < 2 && j < cand) st_cluster_u32(cluster_map_shared(scores_addr + (uint32_t)j * 4, (uint32_t)r), __float_as_uint(v));
+        }
+    }
+    cluster_arrive();
+    cluster_wait();                                                               // behind it nobody writes another CTA's shared memory
+    if (!mine) return;
+    const long long item = (long long)row * p.Hkv + g;
+    if (n <= p.top || keep == 0) {
+        list_without_choice(p, item, n, kThreads);
+        return;
+    }
+    if (warp == W - 1) list_forced(p, item, n);
+    const int own = n - forced;                                                   // (an earlier row may see a page less)
+    float low = INFINITY, high = -INFINITY;
+    for (int j = tid; j < own; j += kThreads) { low = fminf(low, scores[j]); high = fmaxf(high, scores[j]); }
+    select_pages<W>(sh, scores, 1, 0, own, 0, own, (own + kSelTile - 1) / kSelTile, low, high, keep, p.sink, p.list + item * p.top);
 }
 
 // ------------------------------------------------------------------------------------------ attention over listed pages
@@ -771,6 +911,23 @@ cudaError_t launch_cluster(void (*kernel)(const P), long long ctas, int threads,
 }  // namespace
 
 // ------------------------------------------------------------------------------------------ host
+typedef void (*SelectKernel)(const SelectParams);
+static const SelectKernel kSelectKernels[2][3] = {
+    {page_select_kernel<64, 8, 1>, page_select_kernel<64, 8, 2>, page_select_kernel<64, 16, 2>},
+    {page_select_kernel<128, 8, 1>, page_select_kernel<128, 8, 2>, page_select_kernel<128, 16, 2>}};
+
+// Raises the kernels' shared-memory limits on the current device.
+static aflex_status select_attributes(aflex_ctx* ctx, int di) {
+    cudaError_t e = cudaSuccess;
+    for (int w = 0; w < 3 && e == cudaSuccess; ++w)
+        e = cudaFuncSetAttribute(kSelectKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (kSelCap + 4) * (int)sizeof(float));
+    // (group's queries and scores: 8 * 4 * (512 + 32) bytes and 4 per page)
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(di ? page_select_rows_kernel<128> : page_select_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 8 * 4 * 544 + kSelCap * (int)sizeof(float));
+    return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
+}
+
 aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
                                 const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch, const int32_t* q_offsets,
                                 int rows, int32_t* page_list, int32_t* page_count, cudaStream_t st) {
@@ -778,11 +935,33 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.q = (const __nv_bfloat16*)q;
     p.codes = bounds->codes; p.scales = bounds->scales;
     p.page_table = kv->page_table; p.seq_lens = kv->seq_lens; p.q_offsets = q_offsets;
-    p.batch = batch; p.max_pages = kv->max_pages_per_seq;
+    p.batch = batch; p.rows = rows; p.max_pages = kv->max_pages_per_seq;
     p.Hq = d->num_q_heads; p.Hkv = d->num_kv_heads; p.G = p.Hq / p.Hkv; p.num_pages = kv->num_pages;
     p.top = policy->top_pages; p.sink = policy->sink_pages; p.window = policy->window_pages;
     p.list = page_list; p.count = page_count; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
+    const int di = d->head_dim == 128;
+    if (!ctx->select_attr_set[di]) {
+        aflex_status s = select_attributes(ctx, di);
+        if (s != AFLEX_OK) return s;
+        ctx->select_attr_set[di] = true;
+    }
+    // Rows that share their sequence go in groups, if there are enough of them to fill the GPU one CTA each: as many as a
+    // sequence has (up to 8, a divisor of more), four where the sequences' numbers of rows differ.  Ungrouped against grouped,
+    // 32 query on 8 KV heads: 16 x 5 rows of 128 / 512 / 1024 / 2048 pages 12.8 / 25.5 / 48.8 / 88.4 against 16.0 / 18.5 / 28.0 /
+    // 43.9 us, 40 x 3 rows 14.9 / 34.4 / 59.2 / 107 against 20.6 / 31.9 / 41.7 / 66.5, 10 x 2 rows never better.
+    if (q_offsets != nullptr && rows >= 3LL * batch && items > ctx->num_sms && p.max_pages > 512 && p.max_pages <= kSelCap) {
+        const int each = rows % batch == 0 ? rows / batch : 4;
+        int R = each <= 8 ? each : 4;
+        for (int r = 8; r >= 2 && each > 8; --r) if (each % r == 0) { R = r; break; }
+        const long long ctas = ((long long)rows + R - 1) / R * p.Hkv * R;
+        if (ctas > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
+        p.cluster = R;
+        const size_t smem = (size_t)R * (d->head_dim / 32) * (32 * sizeof(uint4) + 8 * sizeof(float)) + (size_t)p.max_pages * sizeof(float);
+        KernelScope scope(ctx, kKPageSelect, st);
+        return check_cuda(ctx, launch_cluster(di ? page_select_rows_kernel<128> : page_select_rows_kernel<64>, ctas, kRowsWarps * 32, smem, R, st, p),
+                          "page_select_rows_kernel launch");
+    }
     // A cluster per (row, KV head) where those are fewer than the SMs (and where the scores need the room), each CTA at least
     // eight tiles; 16 warps per CTA while an SM has no second one, else 8 warps with two tiles or (more CTAs than fit that way)
     // one tile in flight.  8 x 8192 pages: 34.0 / 22.6 / 11.9 us with 1 / 2 / 8 CTAs of 16 warps, 13.4 with 8 of 8 warps; 256 x up
@@ -796,20 +975,8 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
     p.cluster = S;
     const size_t smem = (size_t)(share + 4) * sizeof(float);
-    typedef void (*Kernel)(const SelectParams);
-    static const Kernel kernels[2][3] = {
-        {page_select_kernel<64, 8, 1>, page_select_kernel<64, 8, 2>, page_select_kernel<64, 16, 2>},
-        {page_select_kernel<128, 8, 1>, page_select_kernel<128, 8, 2>, page_select_kernel<128, 16, 2>}};
-    const int di = d->head_dim == 128;
-    if (!ctx->select_attr_set[di]) {
-        for (int w = 0; w < 3; ++w) {
-            cudaError_t e = cudaFuncSetAttribute(kernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (kSelCap + 4) * (int)sizeof(float));
-            if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
-        }
-        ctx->select_attr_set[di] = true;
-    }
     KernelScope scope(ctx, kKPageSelect, st);
-    return check_cuda(ctx, launch_cluster(kernels[di][form], items * S, form == 2 ? 512 : 256, smem, S, st, p), "page_select_kernel launch");
+    return check_cuda(ctx, launch_cluster(kSelectKernels[di][form], items * S, form == 2 ? 512 : 256, smem, S, st, p), "page_select_kernel launch");
 }
 
 aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,

@@ -62,6 +62,9 @@ struct aflex_ctx {
     bool select_attr_set[2] = {false, false};    // ... for page_select_kernel<64 / 128>
     bool bounds_attr_set[2] = {false, false};    // ... for page_bounds_kernel<64 / 128>
     bool pages_attr_set[2] = {false, false};     // ... for attn_decode_pages_kernel<64 / 128>
+    float rope_theta = 0.f;       // what rope_freq and rope_step (cosine, sine of one position's angle) were made for
+    int rope_dim = 0;
+    double rope_freq[64] = {}, rope_step[2][64] = {};
     char err[512] = {0};
     // launch counters (always on) and event-pair timing of every launch (when profiling is enabled)
     long long launches[aflex::kKKindCount] = {};

@@ -577,15 +577,24 @@ aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d,
     p.v_cache = (__nv_bfloat16*)const_cast<void*>(kv->v_cache);
     p.codes = bounds->codes; p.scales = bounds->scales;
     p.eps = eps;
-    for (int i = 0; i < 64; ++i) p.inv_freq[i] = i < d->head_dim / 2 ? pow((double)theta, -2.0 * i / (double)d->head_dim) : 0.0;
-    for (int i = 0; i < 64; ++i) { p.step_cos[i] = cos(p.inv_freq[i]); p.step_sin[i] = sin(p.inv_freq[i]); }
+    // the frequencies of the last theta and head size (a few microseconds of host time for a launch of as many)
+    if (ctx->rope_theta != theta || ctx->rope_dim != d->head_dim) {
+        for (int i = 0; i < d->head_dim / 2; ++i) {
+            ctx->rope_freq[i] = pow((double)theta, -2.0 * i / (double)d->head_dim);
+            ctx->rope_step[0][i] = cos(ctx->rope_freq[i]);
+            ctx->rope_step[1][i] = sin(ctx->rope_freq[i]);
+        }
+        ctx->rope_theta = theta;
+        ctx->rope_dim = d->head_dim;
+    }
+    for (int i = 0; i < 64; ++i) { p.inv_freq[i] = ctx->rope_freq[i]; p.step_cos[i] = ctx->rope_step[0][i]; p.step_sin[i] = ctx->rope_step[1][i]; }
     p.status = ctx->dev_status;
-    // A page's K and V heads on one CTA per eight of them; its query heads 32 per CTA, 16 where a page has one new row.
+    // A page's K and V heads on one CTA per eight of them; its query heads 32 per CTA (7420 rows: 87 / 71 / 64.6 / 65.7 us with
+    // 8 / 16 / 32 / 64; 256 single rows: 10.5 / 7.6 / 6.9 / 6.9: every CTA locates its page and makes its rotations).
     // m new tokens of a sequence touch at most (m + 14) / 16 + 1 pages.
     const long long tasks = q_offsets ? ((long long)rows + 14LL * batch) / 16 + batch : batch;
-    const int per_cta = q_offsets ? 32 : 16;
     p.kv_ctas = (2 * p.Hkv + kBoundsWarps - 1) / kBoundsWarps;
-    p.q_heads_per_cta = p.Hq < per_cta ? p.Hq : per_cta;
+    p.q_heads_per_cta = p.Hq < 32 ? p.Hq : 32;
     const int q_ctas = (p.Hq + p.q_heads_per_cta - 1) / p.q_heads_per_cta;
     p.groups = p.kv_ctas + q_ctas;
     if (tasks * p.groups > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "rope_append_bounds: rows = %d", rows);

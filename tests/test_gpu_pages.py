@@ -282,6 +282,40 @@ def test_selection_is_the_definition_bit_for_bit(ctx, Hq, Hkv, D, lens, top, sin
     np.testing.assert_array_equal(got[0], want[0])
 
 
+GROUPS = [  # Hq, Hkv, D, lens, top, sink, window, new, padding rows
+    (16, 8, 64, [500, 333, 700, 64, 1200], 9, 1, 2, [4, 4, 4, 4, 4], 0),
+    (8, 8, 128, [900, 400], 12, 0, 1, [16, 16], 0),             # groups of eight, one page more for the later rows
+    (8, 8, 128, [400, 300, 257], 16, 2, 2, [11, 11, 11], 0),    # a prime number of rows per sequence
+    (8, 4, 64, [600, 90, 17, 450, 800, 33], 5, 1, 1, [9, 1, 0, 20, 7, 13], 5),      # groups across sequences and padding
+    (8, 8, 64, [40, 500, 35], 4, 1, 1, [9, 9, 9], 0),           # rows that see everything beside rows that choose
+    (8, 8, 64, [300, 200, 250], 3, 1, 2, [8, 8, 8], 0),         # nothing but the forced pages
+]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens,top,sink,window,new,pad", GROUPS)
+def test_selection_of_neighbouring_rows(ctx, Hq, Hkv, D, lens, top, sink, window, new, pad):
+    """Enough (row, head) pairs that rows of a sequence are scored together."""
+    c = Cache(lens, Hkv, D, seed=top + D, max_pages=600)
+    ctx.page_bounds(AF.attn_desc(Hq, Hkv, D), c.kv, c.bounds, len(lens))
+    offs = np.concatenate([[0], np.cumsum(new)])
+    rows = int(offs[-1]) + pad
+    assert rows * Hkv > 148 and rows >= 3 * len(lens)
+    q = torch.randn(rows, Hq, D, generator=torch.Generator().manual_seed(9)).to(torch.bfloat16)
+    got = run_select(ctx, c, q, Hq, top, sink, window, offs)
+    assert ctx.device_status() == AF.OK
+    want = PO.page_select(f64(q), c.codes.cpu().numpy(), c.scales.cpu().numpy(), c.table, lens, top, sink, window, offs)
+    np.testing.assert_array_equal(got[1], want[1])
+    np.testing.assert_array_equal(got[0], want[0])
+    # a sequence shorter than its rows is reported; the others are as they were
+    c.ld[1] = new[1] - 1
+    if new[1] > 1:
+        bad = run_select(ctx, c, q, Hq, top, sink, window, offs)
+        assert ctx.device_status() == AF.ERR_BOUNDS
+        others = np.r_[0:offs[1], offs[2]:rows]
+        np.testing.assert_array_equal(bad[0][others], want[0][others])
+        assert (bad[1][offs[1]] == 0).all() and (bad[0][offs[1]] == -1).all()
+
+
 def test_selection_ties_and_odd_queries(ctx):
     lens = [50 * 16 - 3] * 6
     c = Cache(lens, 2, 128, seed=1)
