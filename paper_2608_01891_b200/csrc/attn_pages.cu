@@ -633,7 +633,7 @@ struct PagesParams {
     const int32_t* q_offsets;
     const int32_t* list;           // [rows][Hkv][top]
     const int32_t* count;          // [rows][Hkv]
-    int batch, max_pages, Hq, Hkv, G, top, cluster;
+    int batch, rows, max_pages, Hq, Hkv, G, top, cluster;
     long long num_pages;
     float scale_log2;
     __nv_bfloat16* out;
@@ -646,7 +646,6 @@ template <int D> struct PagesRing {
     static constexpr int kPageBytes = kPageTokens * D * 2;            // of K; as many of V
     static constexpr int kWarpBytes = kStages * 2 * kPageBytes;       // holds the warp's state (8 heads x D floats) at the end
     static constexpr int kBytes = kPagesWarps * kWarpBytes;
-    static constexpr int kResident = D == 128 ? 2 : 3;                // CTAs per SM
 };
 
 struct PagesShared {
@@ -669,12 +668,138 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 // 1, 3, 5, 7) x (8 chunks); either way the eight lanes of a bank cycle then touch eight different 16-byte banks.
 __device__ __forceinline__ int swizzle(int row) { return (((row >> 1) & 3) << 1) ^ ((row & 1) << 2); }
 
+// One page for one warp: K at shared address kp, V at vp (swizzled rows), the first nv > 0 tokens of it.
+template <int D> struct PageState {
+    float o[D / 64][8][4];                         // [half][channel of the lane's chunk][rows 0-7: P_hi, rows 8-15: P_lo]
+    float m, l;
+    __device__ __forceinline__ void reset() {
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[h][c][0] = o[h][c][1] = o[h][c][2] = o[h][c][3] = 0.f;
+        m = kNegBig;
+        l = 0.f;
+    }
+};
+template <int D>
+__device__ __forceinline__ void attend_page(PageState<D>& st, uint32_t kp, uint32_t vp, int nv, const uint4 (&qf)[D / 32], float scale_log2) {
+    constexpr int kSteps = D / 32;                 // 16-byte reads per lane and K row
+    constexpr int kHalves = D / 64;                // 16-byte reads per lane and V row
+    const int lane = threadIdx.x & 31, hl = lane >> 2, l4 = lane & 3;
+    auto& o = st.o;
+    float& m = st.m;
+    float& l = st.l;
+                float s[2][4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
+                    const int t = hl + 8 * r;
+#pragma unroll
+                    for (int c = 0; c < kSteps; ++c) {
+                        const uint4 x = lds128(kp + (uint32_t)(t * (D * 2) + (((c * 4 + l4) ^ swizzle(t)) << 4)));
+                        mma_bf16_16816(s[r], qf[c].x, 0u, qf[c].y, 0u, x.x, x.y);
+                        mma_bf16_16816(s[r], qf[c].z, 0u, qf[c].w, 0u, x.z, x.w);
+                    }
+                }
+                // tokens 2 l4, 2 l4 + 1 and those + 8 of head lane / 4
+                float x0 = 2 * l4 < nv ? s[0][0] * scale_log2 : -INFINITY;
+                float x1 = 2 * l4 + 1 < nv ? s[0][1] * scale_log2 : -INFINITY;
+                float x2 = 2 * l4 + 8 < nv ? s[1][0] * scale_log2 : -INFINITY;
+                float x3 = 2 * l4 + 9 < nv ? s[1][1] * scale_log2 : -INFINITY;
+                float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                if (__any_sync(0xffffffffu, mx > m)) {
+                    const float mn = fmaxf(m, mx), corr = fast_exp2(m - mn);
+                    m = mn;
+                    l *= corr;
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) { o[h][c][0] *= corr; o[h][c][1] *= corr; o[h][c][2] *= corr; o[h][c][3] *= corr; }
+                }
+                x0 = fast_exp2(x0 - m); x1 = fast_exp2(x1 - m); x2 = fast_exp2(x2 - m); x3 = fast_exp2(x3 - m);
+                l += (x0 + x1) + (x2 + x3);
+                const uint32_t a0 = pack_bf16x2(x0, x1), a2 = pack_bf16x2(x2, x3);
+                const uint32_t a1 = pack_bf16x2(x0 - __uint_as_float(a0 << 16), x1 - __uint_as_float(a0 & 0xffff0000u));
+                const uint32_t a3 = pack_bf16x2(x2 - __uint_as_float(a2 << 16), x3 - __uint_as_float(a2 & 0xffff0000u));
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) {
+                    uint4 v[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int t = 2 * l4 + (r & 1) + (r >> 1) * 8;
+                        v[r] = lds128(vp + (uint32_t)(t * (D * 2) + (((h * 8 + hl) ^ swizzle(t)) << 4)));
+                    }
+                    const uint32_t* r0 = reinterpret_cast<const uint32_t*>(&v[0]);
+                    const uint32_t* r1 = reinterpret_cast<const uint32_t*>(&v[1]);
+                    const uint32_t* r2 = reinterpret_cast<const uint32_t*>(&v[2]);
+                    const uint32_t* r3 = reinterpret_cast<const uint32_t*>(&v[3]);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        mma_bf16_16816(o[h][2 * w], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x5410), __byte_perm(r2[w], r3[w], 0x5410));
+                        mma_bf16_16816(o[h][2 * w + 1], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x7632), __byte_perm(r2[w], r3[w], 0x7632));
+                    }
+                }
+}
+// Leaves a warp's state in shared memory: [8 heads][D] unnormalised sums at `to`, maximum and sum at m_to / l_to [8].
+// Lane: head lane / 4, channels 64 h + 16 l4 + 8 x + c at o[h][c][x].
+template <int D>
+__device__ __forceinline__ void park_state(const PageState<D>& st, float* to, float* m_to, float* l_to) {
+    const int lane = threadIdx.x & 31, hl = lane >> 2, l4 = lane & 3;
+    float l = st.l;
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    const auto& o = st.o;
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            float* dst = to + hl * D + 64 * h + 16 * l4 + 8 * x;
+            *reinterpret_cast<float4*>(dst) = make_float4(o[h][0][x] + o[h][0][x + 2], o[h][1][x] + o[h][1][x + 2],
+                                                          o[h][2][x] + o[h][2][x + 2], o[h][3][x] + o[h][3][x + 2]);
+            *reinterpret_cast<float4*>(dst + 4) = make_float4(o[h][4][x] + o[h][4][x + 2], o[h][5][x] + o[h][5][x + 2],
+                                                              o[h][6][x] + o[h][6][x + 2], o[h][7][x] + o[h][7][x + 2]);
+        }
+    if (l4 == 0) { m_to[hl] = st.m; l_to[hl] = l; }
+}
+// Joins pieces of one output run of four channels.
+struct RunSum {
+    float M, L;
+    float4 acc;
+};
+__device__ __forceinline__ void add_piece(RunSum& s, float m, float l, const float4& v) {
+    const float f = fast_exp2(m - s.M);            // (s.M: the largest m of all pieces)
+    s.L = fmaf(l, f, s.L);
+    s.acc.x = fmaf(v.x, f, s.acc.x); s.acc.y = fmaf(v.y, f, s.acc.y); s.acc.z = fmaf(v.z, f, s.acc.z); s.acc.w = fmaf(v.w, f, s.acc.w);
+}
+template <int D>
+__device__ __forceinline__ void store_run(const PagesParams& p, int row, int g, int h, int c, const RunSum& s) {
+    const float inv = s.L == 0.f ? 0.f : 1.f / s.L;            // a row with nothing to attend to: zeros
+    const size_t hq = (size_t)row * p.Hq + (size_t)g * p.G + h;
+    reinterpret_cast<uint2*>(p.out + hq * D)[c] = make_uint2(pack_bf16x2(s.acc.x * inv, s.acc.y * inv), pack_bf16x2(s.acc.z * inv, s.acc.w * inv));
+    if (p.lse != nullptr && c == 0) p.lse[hq] = s.L == 0.f ? -INFINITY : (s.M + log2f(s.L)) * 0.6931471805599453f;
+}
+
+// Starts the copies of a page (slab: its K or V block's first element) to shared address dst, V behind K.
+template <int D>
+__device__ __forceinline__ void copy_page(const PagesParams& p, size_t slab, int nv, uint32_t dst) {
+    constexpr int kChunks = D / 8;                 // 16-byte chunks of a row
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < kPageTokens * kChunks / 32; ++k) {
+        const int c = k * 32 + lane, r = c / kChunks, ch = c % kChunks;
+        const uint32_t to = dst + (uint32_t)(r * (D * 2) + ((ch ^ swizzle(r)) << 4));
+        // slots past the end may hold anything: K's scores are masked, V has to be zero
+        copy16(to, p.k_cache + slab + c * 8, 16);
+        copy16(to + PagesRing<D>::kPageBytes, p.v_cache + slab + c * 8, r < nv ? 16 : 0);
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const PagesParams p) {
     typedef PagesRing<D> R;
     constexpr int kSteps = D / 32;                 // 16-byte reads per lane and K row
-    constexpr int kHalves = D / 64;                // 16-byte reads per lane and V row
-    constexpr int kChunks = D / 8;                 // 16-byte chunks of a row
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ PagesShared sh;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -728,22 +853,10 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
         const size_t slab = ((size_t)__shfl_sync(0xffffffffu, phys, i & 31) * p.Hkv + g) * kPageTokens * D;
         const int stage = i % R::kStages;
         if (lane == 0) sh.valid[warp][stage] = nv;
-        const uint32_t dst = base + (uint32_t)(stage * 2 * R::kPageBytes);
-#pragma unroll
-        for (int k = 0; k < kPageTokens * kChunks / 32; ++k) {
-            const int c = k * 32 + lane, r = c / kChunks, ch = c % kChunks;
-            const uint32_t to = dst + (uint32_t)(r * (D * 2) + ((ch ^ swizzle(r)) << 4));
-            // slots past the end may hold anything: K's scores are masked, V has to be zero
-            copy16(to, p.k_cache + slab + c * 8, 16);
-            copy16(to + R::kPageBytes, p.v_cache + slab + c * 8, r < nv ? 16 : 0);
-        }
+        copy_page<D>(p, slab, nv, base + (uint32_t)(stage * 2 * R::kPageBytes));
     };
-    float o[kHalves][8][4];                        // [half][channel of the lane's chunk][rows 0-7: P_hi, rows 8-15: P_lo]
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) o[h][c][0] = o[h][c][1] = o[h][c][2] = o[h][c][3] = 0.f;
-    float m = kNegBig, l = 0.f;
+    PageState<D> st;
+    st.reset();
 #pragma unroll
     for (int i = 0; i < R::kStages - 1; ++i) {
         if (i < n) issue(i);
@@ -757,103 +870,26 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
         const int stage = i % R::kStages;
         const int nv = sh.valid[warp][stage];
         const uint32_t kp = base + (uint32_t)(stage * 2 * R::kPageBytes), vp = kp + R::kPageBytes;
-        if (nv > 0) {
-            float s[2][4];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                s[r][0] = s[r][1] = s[r][2] = s[r][3] = 0.f;
-                const int t = hl + 8 * r;
-#pragma unroll
-                for (int c = 0; c < kSteps; ++c) {
-                    const uint4 x = lds128(kp + (uint32_t)(t * (D * 2) + (((c * 4 + l4) ^ swizzle(t)) << 4)));
-                    mma_bf16_16816(s[r], qf[c].x, 0u, qf[c].y, 0u, x.x, x.y);
-                    mma_bf16_16816(s[r], qf[c].z, 0u, qf[c].w, 0u, x.z, x.w);
-                }
-            }
-            // tokens 2 l4, 2 l4 + 1 and those + 8 of head lane / 4
-            float x0 = 2 * l4 < nv ? s[0][0] * p.scale_log2 : -INFINITY;
-            float x1 = 2 * l4 + 1 < nv ? s[0][1] * p.scale_log2 : -INFINITY;
-            float x2 = 2 * l4 + 8 < nv ? s[1][0] * p.scale_log2 : -INFINITY;
-            float x3 = 2 * l4 + 9 < nv ? s[1][1] * p.scale_log2 : -INFINITY;
-            float mx = fmaxf(fmaxf(x0, x1), fmaxf(x2, x3));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-            if (__any_sync(0xffffffffu, mx > m)) {
-                const float mn = fmaxf(m, mx), corr = fast_exp2(m - mn);
-                m = mn;
-                l *= corr;
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) { o[h][c][0] *= corr; o[h][c][1] *= corr; o[h][c][2] *= corr; o[h][c][3] *= corr; }
-            }
-            x0 = fast_exp2(x0 - m); x1 = fast_exp2(x1 - m); x2 = fast_exp2(x2 - m); x3 = fast_exp2(x3 - m);
-            l += (x0 + x1) + (x2 + x3);
-            const uint32_t a0 = pack_bf16x2(x0, x1), a2 = pack_bf16x2(x2, x3);
-            const uint32_t a1 = pack_bf16x2(x0 - __uint_as_float(a0 << 16), x1 - __uint_as_float(a0 & 0xffff0000u));
-            const uint32_t a3 = pack_bf16x2(x2 - __uint_as_float(a2 << 16), x3 - __uint_as_float(a2 & 0xffff0000u));
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                uint4 v[4];
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int t = 2 * l4 + (r & 1) + (r >> 1) * 8;
-                    v[r] = lds128(vp + (uint32_t)(t * (D * 2) + (((h * 8 + hl) ^ swizzle(t)) << 4)));
-                }
-                const uint32_t* r0 = reinterpret_cast<const uint32_t*>(&v[0]);
-                const uint32_t* r1 = reinterpret_cast<const uint32_t*>(&v[1]);
-                const uint32_t* r2 = reinterpret_cast<const uint32_t*>(&v[2]);
-                const uint32_t* r3 = reinterpret_cast<const uint32_t*>(&v[3]);
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    mma_bf16_16816(o[h][2 * w], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x5410), __byte_perm(r2[w], r3[w], 0x5410));
-                    mma_bf16_16816(o[h][2 * w + 1], a0, a1, a2, a3, __byte_perm(r0[w], r1[w], 0x7632), __byte_perm(r2[w], r3[w], 0x7632));
-                }
-            }
-        }
+        if (nv > 0) attend_page<D>(st, kp, vp, nv, qf, p.scale_log2);
         __syncwarp();                              // everybody has read the stage that the next copies overwrite
     }
     // ---- join the warps, then the cluster's CTAs.  Lane: head lane / 4, channels 64 h + 16 l4 + 8 x + c at o[h][c][x].
     // The copies that this warp started have all landed (a group is waited for before its page is used), so its ring is free.
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
     auto state = [&](int w) { return reinterpret_cast<float*>(ring + w * R::kWarpBytes); };       // [8][D]
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-            float* dst = state(warp) + hl * D + 64 * h + 16 * l4 + 8 * x;
-            *reinterpret_cast<float4*>(dst) = make_float4(o[h][0][x] + o[h][0][x + 2], o[h][1][x] + o[h][1][x + 2],
-                                                          o[h][2][x] + o[h][2][x + 2], o[h][3][x] + o[h][3][x + 2]);
-            *reinterpret_cast<float4*>(dst + 4) = make_float4(o[h][4][x] + o[h][4][x + 2], o[h][5][x] + o[h][5][x + 2],
-                                                              o[h][6][x] + o[h][6][x + 2], o[h][7][x] + o[h][7][x + 2]);
-        }
-    if (l4 == 0) { sh.m[warp][hl] = m; sh.l[warp][hl] = l; }
+    park_state<D>(st, state(warp), sh.m[warp], sh.l[warp]);
     __syncthreads();
     constexpr int kRuns = D / 4;                   // a head's outputs in runs of four channels
-    auto store = [&](int h, int c, float M, float L, const float4& acc) {
-        const float inv = L == 0.f ? 0.f : 1.f / L;            // a row with nothing to attend to: zeros
-        const size_t hq = (size_t)row * p.Hq + (size_t)g * p.G + h;
-        reinterpret_cast<uint2*>(p.out + hq * D)[c] = make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-        if (p.lse != nullptr && c == 0) p.lse[hq] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-    };
     for (int i = tid; i < p.G * kRuns; i += kPagesThreads) {
         const int h = i / kRuns, c = i % kRuns;
-        float M = kNegBig, L = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        RunSum s = {kNegBig, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
-        for (int w = 0; w < kPagesWarps; ++w) M = fmaxf(M, sh.m[w][h]);
+        for (int w = 0; w < kPagesWarps; ++w) s.M = fmaxf(s.M, sh.m[w][h]);
 #pragma unroll
-        for (int w = 0; w < kPagesWarps; ++w) {
-            const float f = fast_exp2(sh.m[w][h] - M);
-            const float4 v = *reinterpret_cast<const float4*>(state(w) + h * D + 4 * c);
-            L = fmaf(sh.l[w][h], f, L);
-            acc.x = fmaf(v.x, f, acc.x); acc.y = fmaf(v.y, f, acc.y); acc.z = fmaf(v.z, f, acc.z); acc.w = fmaf(v.w, f, acc.w);
-        }
-        if (S == 1) store(h, c, M, L, acc);
+        for (int w = 0; w < kPagesWarps; ++w) add_piece(s, sh.m[w][h], sh.l[w][h], *reinterpret_cast<const float4*>(state(w) + h * D + 4 * c));
+        if (S == 1) store_run<D>(p, row, g, h, c, s);
         else {
-            *reinterpret_cast<float4*>(state(0) + h * D + 4 * c) = acc;        // read by nobody else in this loop
-            if (c == 0) { sh.cm[h] = M; sh.cl[h] = L; }
+            *reinterpret_cast<float4*>(state(0) + h * D + 4 * c) = s.acc;      // read by nobody else in this loop
+            if (c == 0) { sh.cm[h] = s.M; sh.cl[h] = s.L; }
         }
     }
     if (S == 1) return;
@@ -871,19 +907,12 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
             pl[s] = ld_cluster_f32(cluster_map_shared(smem_u32(&sh.cl[h]), from));
             v[s] = ld_cluster_f32x4(cluster_map_shared(smem_u32(state(0) + h * D + 4 * c), from));
         }
-        float M = kNegBig, L = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        RunSum sum = {kNegBig, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
-        for (int s = 0; s < kPagesMaxCluster; ++s) if (s < S) M = fmaxf(M, pm[s]);
+        for (int s = 0; s < kPagesMaxCluster; ++s) if (s < S) sum.M = fmaxf(sum.M, pm[s]);
 #pragma unroll
-        for (int s = 0; s < kPagesMaxCluster; ++s) {
-            if (s < S) {
-                const float f = fast_exp2(pm[s] - M);
-                L = fmaf(pl[s], f, L);
-                acc.x = fmaf(v[s].x, f, acc.x); acc.y = fmaf(v[s].y, f, acc.y); acc.z = fmaf(v[s].z, f, acc.z); acc.w = fmaf(v[s].w, f, acc.w);
-            }
-        }
-        store(h, c, M, L, acc);
+        for (int s = 0; s < kPagesMaxCluster; ++s) if (s < S) add_piece(sum, pm[s], pl[s], v[s]);
+        store_run<D>(p, row, g, h, c, sum);
     }
     cluster_arrive();
     cluster_wait();                                // the others' shared memory stays until everybody has read it
@@ -987,29 +1016,47 @@ aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, 
     p.k_cache = (const __nv_bfloat16*)kv->k_cache; p.v_cache = (const __nv_bfloat16*)kv->v_cache;
     p.page_table = kv->page_table; p.seq_lens = kv->seq_lens; p.q_offsets = q_offsets;
     p.list = page_list; p.count = page_count;
-    p.batch = batch; p.max_pages = kv->max_pages_per_seq;
+    p.batch = batch; p.rows = rows; p.max_pages = kv->max_pages_per_seq;
     p.Hq = d->num_q_heads; p.Hkv = d->num_kv_heads; p.G = p.Hq / p.Hkv; p.top = top_pages; p.num_pages = kv->num_pages;
     const float scale = d->sm_scale != 0.f ? d->sm_scale : 1.0f / sqrtf((float)d->head_dim);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
-    // CTAs per (row, KV head): what fits the GPU at once, down to one page per warp.  A CTA costs about 5 us beside its pages
-    // (three dependent loads before the first page, the join), so a second wave costs more than an even split gains: 8 items of
-    // 128 pages 23.8 / 15.1 / 9.9 / 7.2 us with 1 / 2 / 4 / 8 CTAs each, 256 items of up to 64 pages 26 / 32 / 43 / 61 us.
-    const long long slots = (long long)ctx->num_sms * (d->head_dim == 128 ? PagesRing<128>::kResident : PagesRing<64>::kResident);
+    const bool wide = d->head_dim == 128;
+    void (*kernel)(const PagesParams) = wide ? attn_decode_pages_kernel<128> : attn_decode_pages_kernel<64>;
+    const int smem = wide ? PagesRing<128>::kBytes : PagesRing<64>::kBytes;
+    int* fit = ctx->pages_clusters[wide];          // clusters of 2, 3 .. 8 CTAs that the GPU holds at once
+    if (!ctx->pages_attr_set[wide]) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        for (int s = 2; s <= kPagesMaxCluster && e == cudaSuccess; ++s) {
+            cudaLaunchConfig_t lc = {};
+            lc.gridDim = dim3((unsigned)s);
+            lc.blockDim = dim3(kPagesThreads);
+            lc.dynamicSmemBytes = smem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = (unsigned)s;
+            attr[0].val.clusterDim.y = 1;
+            attr[0].val.clusterDim.z = 1;
+            lc.attrs = attr;
+            lc.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&fit[s], kernel, &lc);
+        }
+        if (e != cudaSuccess) return check_cuda(ctx, e, "attention over pages: kernel attributes");
+        ctx->pages_attr_set[wide] = true;
+    }
+    // CTAs per (row, KV head): as many as the GPU holds at once as clusters (fewer than the places that its SMs have, since a
+    // cluster stays inside one group of them), down to one page per warp.  A CTA costs about 5 us beside its pages (three
+    // dependent loads before the first page, the join), so a second wave costs more than an even split gains: 8 pairs of 128
+    // pages 23.8 / 15.1 / 9.9 / 7.2 us with 1 / 2 / 4 / 8 CTAs each; 80 pairs 29.4 / 19.9 / 19.6 / 26.9 with 1 / 2 / 3 / 4; 256 of
+    // up to 64 pages 26 / 32 / 43 with 1 / 2 / 4.  (Equal shares of all pairs' pages, cut anywhere and joined through global
+    // memory: 60 against 70 us at 304 pairs of 128, where one CTA each leaves a second wave of 8, but 52 against 47 at 256 and
+    // 93 against 84 at 512.)
     const int most = (top_pages + kPagesWarps - 1) / kPagesWarps;
-    int S = (int)(slots / items < kPagesMaxCluster ? slots / items : kPagesMaxCluster);
-    if (S > most) S = most;
-    if (S < 1) S = 1;
+    int S = 1;
+    for (int s = 2; s <= kPagesMaxCluster && s <= most; ++s) if (items <= fit[s]) S = s;
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "attention over pages: rows * Hkv = %lld", items);
     p.cluster = S;
-    void (*kernel)(const PagesParams) = d->head_dim == 128 ? attn_decode_pages_kernel<128> : attn_decode_pages_kernel<64>;
-    const int smem = d->head_dim == 128 ? PagesRing<128>::kBytes : PagesRing<64>::kBytes;
-    if (!ctx->pages_attr_set[d->head_dim == 128]) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return check_cuda(ctx, e, "cudaFuncSetAttribute(attention over pages)");
-        ctx->pages_attr_set[d->head_dim == 128] = true;
-    }
     KernelScope scope(ctx, kKAttnPages, st);
     return check_cuda(ctx, launch_cluster(kernel, items * S, kPagesThreads, smem, S, st, p), "attn_decode_pages_kernel launch");
 }

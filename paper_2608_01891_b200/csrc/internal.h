@@ -62,6 +62,7 @@ struct aflex_ctx {
     bool select_attr_set[2] = {false, false};    // ... for page_select_kernel<64 / 128>
     bool bounds_attr_set[2] = {false, false};    // ... for page_bounds_kernel<64 / 128>
     bool pages_attr_set[2] = {false, false};     // ... for attn_decode_pages_kernel<64 / 128>
+    int pages_clusters[2][9] = {};               // its clusters of 2 .. 8 CTAs that fit this device at once
     float rope_theta = 0.f;       // what rope_freq and rope_step (cosine, sine of one position's angle) were made for
     int rope_dim = 0;
     double rope_freq[64] = {}, rope_step[2][64] = {};
