@@ -86,6 +86,7 @@ class DvfsState(ctypes.Structure):
 
 
 DVFS_ESCALATED, DVFS_INFEASIBLE = 1, 2
+_BF16 = torch.bfloat16
 
 
 class AflexError(RuntimeError):
@@ -213,15 +214,6 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return (stream or torch.cuda.current_stream()).cuda_stream
-
-
-def _stream_on(device: int, stream: Optional[torch.cuda.Stream]) -> int:
-    """The given stream, or the current one of that device (without building a Stream object: these calls last microseconds)."""
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-
-
-def _stream_of(t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
-    return _stream_on(t.get_device(), stream)
 
 
 def _row_args(rows: int, q_offsets: Optional[torch.Tensor]):
@@ -601,35 +593,50 @@ class Context:
                            rope_theta: float, q_offsets=None, stream=None) -> None:
         """rope_append for one token or a chunk per sequence that also makes the key bounds of every page it touches."""
         rows = qkv.shape[0]
+        hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
+        assert qkv.dtype == _BF16 and qkv.numel() == rows * (hq + 2 * hkv) * d, "qkv is not bf16 [rows][(Hq + 2 Hkv) * D]"
+        assert q_out.dtype == _BF16 and q_out.numel() == rows * hq * d, "q_out is not bf16 [rows][Hq][D]"
+        for w in (w_q_norm, w_k_norm):
+            assert w is None or (w.dtype == _BF16 and w.numel() == d), "a head norm is not bf16 [D]"
         batch, offs = _row_args(rows, q_offsets)
         _match(desc, kv, batch, bounds)
-        assert q_out.shape[0] == rows, "q_out has another number of rows than qkv"
         self._check(self._lib.aflex_rope_append_bounds(self._h, desc, _ptr(qkv), kv, bounds, batch, offs, rows, _ptr(w_q_norm),
-                                                       _ptr(w_k_norm), rms_eps, rope_theta, _ptr(q_out), _stream_of(qkv, stream)))
+                                                       _ptr(w_k_norm), rms_eps, rope_theta, _ptr(q_out), self._stream_of(qkv, stream)))
 
     def page_bounds(self, desc: AttnDesc, kv: KV, bounds: KeyBounds, batch: int, first_token=None, stream=None) -> None:
         """Key bounds of the pages of sequences 0 .. batch - 1 that hold a token at first_token[b] (i32 CUDA [B]; None: 0) or later."""
-        assert first_token is None or first_token.dtype == torch.int32
+        assert first_token is None or (first_token.dtype == torch.int32 and first_token.numel() >= batch)
         _match(desc, kv, batch, bounds)
-        self._check(self._lib.aflex_page_bounds(self._h, desc, kv, bounds, batch, _ptr(first_token), _stream_on(self.device, stream)))
+        st = torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+        self._check(self._lib.aflex_page_bounds(self._h, desc, kv, bounds, batch, _ptr(first_token), st))
 
     def page_select(self, desc: AttnDesc, q, kv: KV, bounds: KeyBounds, top_pages: int, page_list, page_count,
                     sink_pages: int = 1, window_pages: int = 2, q_offsets=None, stream=None) -> None:
         """The pages each row's queries should read: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
-        rows = q.shape[0]
-        assert page_list.dtype == torch.int32 and page_count.dtype == torch.int32
-        assert page_list.shape == (rows, desc.num_kv_heads, top_pages) and page_count.shape == page_list.shape[:2]
+        rows, hkv = q.shape[0], desc.num_kv_heads
+        assert q.dtype == _BF16 and q.numel() == rows * desc.num_q_heads * desc.head_dim, "q is not bf16 [rows][Hq][D]"
+        assert page_list.dtype == torch.int32 and page_list.shape == (rows, hkv, top_pages), "page_list is not i32 [rows][Hkv][top_pages]"
+        assert page_count.dtype == torch.int32 and page_count.shape == (rows, hkv), "page_count is not i32 [rows][Hkv]"
         batch, offs = _row_args(rows, q_offsets)
         _match(desc, kv, batch, bounds)
         self._check(self._lib.aflex_page_select(self._h, desc, _ptr(q), kv, bounds, PagePolicy(top_pages, sink_pages, window_pages),
-                                                batch, offs, rows, _ptr(page_list), _ptr(page_count), _stream_of(q, stream)))
+                                                batch, offs, rows, _ptr(page_list), _ptr(page_count), self._stream_of(q, stream)))
 
     def attn_decode_pages(self, desc: AttnDesc, q, kv: KV, page_list, page_count, out, lse=None, q_offsets=None, stream=None) -> None:
         """Attention of every row over the pages listed for it: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
         rows, heads, top = page_list.shape
-        assert page_list.dtype == torch.int32 and page_count.dtype == torch.int32
-        assert heads == desc.num_kv_heads and rows == q.shape[0] and rows == out.shape[0] and page_count.shape == (rows, heads)
+        n = rows * desc.num_q_heads
+        assert page_list.dtype == torch.int32 and heads == desc.num_kv_heads, "page_list is not i32 [rows][Hkv][top_pages]"
+        assert page_count.dtype == torch.int32 and page_count.shape == (rows, heads), "page_count is not i32 [rows][Hkv]"
+        assert q.dtype == _BF16 and q.numel() == n * desc.head_dim, "q is not bf16 [rows][Hq][D]"
+        assert out.dtype == _BF16 and out.numel() == n * desc.head_dim, "out is not bf16 [rows][Hq][D]"
+        assert lse is None or (lse.dtype == torch.float32 and lse.numel() == n), "lse is not fp32 [rows][Hq]"
         batch, offs = _row_args(rows, q_offsets)
         _match(desc, kv, batch)
         self._check(self._lib.aflex_attn_decode_pages(self._h, desc, _ptr(q), kv, _ptr(page_list), _ptr(page_count), top, batch, offs,
-                                                      rows, _ptr(out), _ptr(lse), _stream_of(q, stream)))
+                                                      rows, _ptr(out), _ptr(lse), self._stream_of(q, stream)))
+
+    def _stream_of(self, t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
+        """The given stream, or the current one of the ctx's device (without building a Stream object: these calls last microseconds)."""
+        assert t.get_device() == self.device, "the tensors are not on the context's device"
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream

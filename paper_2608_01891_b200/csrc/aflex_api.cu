@@ -781,8 +781,16 @@ struct CtxDevice {
     }
     ~CtxDevice() { if (saved >= 0) cudaSetDevice(saved); }
 };
+// Positions are 32-bit.
+aflex_status validate_pages(aflex_ctx* ctx, const char* what, const aflex_kv* kv) {
+    if (kv->max_pages_per_seq > (1 << 26))
+        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "%s: max_pages_per_seq %d (supported: up to 2^26)", what, kv->max_pages_per_seq);
+    return AFLEX_OK;
+}
 // Rows of a call: one per sequence, or `rows` rows laid out by q_offsets.
-aflex_status validate_rows(aflex_ctx* ctx, const char* what, int batch, const int32_t* q_offsets, int rows) {
+aflex_status validate_rows(aflex_ctx* ctx, const char* what, const aflex_kv* kv, int batch, const int32_t* q_offsets, int rows) {
+    aflex_status s = validate_pages(ctx, what, kv);
+    if (s != AFLEX_OK) return s;
     if (rows < 1 || (!q_offsets && rows != batch))
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: rows = %d (batch %d; without q_offsets one row per sequence)", what, rows, batch);
     return AFLEX_OK;
@@ -801,7 +809,7 @@ aflex_status aflex_rope_append_bounds(aflex_ctx* ctx, const aflex_attn_desc* des
                                       void* stream) {
     aflex_status s = validate_attn(ctx, desc, qkv, kv, batch, q_out);
     if (s == AFLEX_OK) s = validate_bounds(ctx, "rope_append_bounds", bounds);
-    if (s == AFLEX_OK) s = validate_rows(ctx, "rope_append_bounds", batch, q_offsets, rows);
+    if (s == AFLEX_OK) s = validate_rows(ctx, "rope_append_bounds", kv, batch, q_offsets, rows);
     if (s != AFLEX_OK) return s;
     if (!(rope_theta > 0.f) || !(rms_eps >= 0.f))
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "rope_append_bounds: rope_theta must be > 0 and rms_eps >= 0");
@@ -814,9 +822,8 @@ aflex_status aflex_page_bounds(aflex_ctx* ctx, const aflex_attn_desc* desc, cons
                                int batch, const int32_t* first_token, void* stream) {
     aflex_status s = validate_bounds(ctx, "page_bounds", bounds);
     if (s == AFLEX_OK) s = validate_attn(ctx, desc, bounds->codes, kv, batch, bounds->codes);
+    if (s == AFLEX_OK) s = validate_pages(ctx, "page_bounds", kv);
     if (s != AFLEX_OK) return s;
-    if ((long long)kv->max_pages_per_seq * desc->num_kv_heads >= (1LL << 31) - 8)
-        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page_bounds: max_pages_per_seq * Hkv does not fit 31 bits");
     CtxDevice dev(ctx);
     return page_bounds_launch(ctx, desc, kv, bounds, batch, first_token, reinterpret_cast<cudaStream_t>(stream));
 }
@@ -826,7 +833,7 @@ aflex_status aflex_page_select(aflex_ctx* ctx, const aflex_attn_desc* desc, cons
                                int rows, int32_t* page_list, int32_t* page_count, void* stream) {
     aflex_status s = validate_attn(ctx, desc, q, kv, batch, page_list);
     if (s == AFLEX_OK) s = validate_bounds(ctx, "page_select", bounds);
-    if (s == AFLEX_OK) s = validate_rows(ctx, "page_select", batch, q_offsets, rows);
+    if (s == AFLEX_OK) s = validate_rows(ctx, "page_select", kv, batch, q_offsets, rows);
     if (s != AFLEX_OK) return s;
     if (!policy || !page_count) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "page_select: null argument");
     if (policy->sink_pages < 0 || policy->window_pages < 1 || policy->top_pages < 1 ||
@@ -842,7 +849,7 @@ aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc
                                      const int32_t* page_list, const int32_t* page_count, int top_pages, int batch,
                                      const int32_t* q_offsets, int rows, void* out, float* lse, void* stream) {
     aflex_status s = validate_attn(ctx, desc, q, kv, batch, out);
-    if (s == AFLEX_OK) s = validate_rows(ctx, "attention over pages", batch, q_offsets, rows);
+    if (s == AFLEX_OK) s = validate_rows(ctx, "attention over pages", kv, batch, q_offsets, rows);
     if (s != AFLEX_OK) return s;
     if (!page_list || !page_count || top_pages < 1)
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "attention over pages: null page_list / page_count or top_pages < 1");

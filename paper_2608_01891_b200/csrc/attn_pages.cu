@@ -969,6 +969,8 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.top = policy->top_pages; p.sink = policy->sink_pages; p.window = policy->window_pages;
     p.list = page_list; p.count = page_count; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
+    if (p.max_pages > kSelMaxCluster * kSelCap)
+        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", p.max_pages, kSelMaxCluster * kSelCap);
     const int di = d->head_dim == 128;
     if (!ctx->select_attr_set[di]) {
         aflex_status s = select_attributes(ctx, di);
@@ -999,8 +1001,6 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelCap) && p.max_pages > S * 8 * kSelTile) S *= 2;
     const int form = items * S <= ctx->num_sms ? 2 : items * S <= 2 * ctx->num_sms ? 1 : 0;
     const int share = ((p.max_pages + kSelTile - 1) / kSelTile + S - 1) / S * kSelTile;       // candidates per CTA at most
-    if (share > kSelCap)
-        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", p.max_pages, kSelMaxCluster * kSelCap);
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
     p.cluster = S;
     const size_t smem = (size_t)(share + 4) * sizeof(float);

@@ -627,3 +627,100 @@ def test_prefill_chunk_then_drafted_rows(ctx):
         assert torch.equal(one.cpu(), lst.cpu()[[i, m + i]])
         assert torch.equal(bits(o1), bits(out[[i, m + i]]))
     assert ctx.device_status() == AF.OK
+
+
+def test_two_streams_at_once(ctx):
+    """The calls keep nothing in the context's workspace: two streams may run them at the same time."""
+    made = []
+    for seed, lens in ((40, [900, 333, 64]), (41, [1500, 20])):
+        Hq, Hkv, D = 16, 4, 128
+        c = Cache(lens, Hkv, D, seed=seed)
+        q = torch.randn(len(lens), Hq, D, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+        B = len(lens)
+        new = lambda *s, dt=torch.int32: torch.zeros(*s, dtype=dt, device=DEV)  # noqa: E731
+        made.append((c, lens, q, q.to(DEV), new(B, Hkv, 12), new(B, Hkv), new(B, Hq, D, dt=torch.bfloat16), new(B, Hq, dt=torch.float32)))
+    desc = AF.attn_desc(16, 4, 128)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (c, lens, _, qd, lst, cnt, out, lse) in zip(streams, made):
+            ctx.page_bounds(desc, c.kv, c.bounds, len(lens), stream=s)
+            ctx.page_select(desc, qd, c.kv, c.bounds, 12, lst, cnt, stream=s)
+            ctx.attn_decode_pages(desc, qd, c.kv, lst, cnt, out, lse, stream=s)
+    torch.cuda.synchronize()
+    for c, lens, q, _, lst, cnt, out, lse in made:
+        want = PO.page_select(f64(q), c.codes.cpu().numpy(), c.scales.cpu().numpy(), c.table, lens, 12, 1, 2)
+        np.testing.assert_array_equal(lst.cpu().numpy(), want[0])
+        check_attention(out, lse, *PO.attn_pages(f64(q), f64(c.k), f64(c.v), c.table, lens, *want), 128)
+    assert ctx.device_status() == AF.OK
+
+
+def test_row_offsets_that_name_few_rows(ctx):
+    """A batch padded to a fixed number of rows and sequences, as a captured step has it: empty sequences, and rows behind the last."""
+    Hq, Hkv, D = 8, 2, 64
+    lens = [100, 40, 0, 0]
+    c = Cache(lens, Hkv, D, seed=50)
+    desc = AF.attn_desc(Hq, Hkv, D)
+    ctx.page_bounds(desc, c.kv, c.bounds, 4)
+    offs = torch.tensor([0, 1, 2, 2, 2], dtype=torch.int32, device=DEV)
+    g = torch.Generator().manual_seed(1)
+    qkv = torch.randn(4, (Hq + 2 * Hkv) * D, generator=g).to(torch.bfloat16)
+    full = lambda *s, dt: torch.full(s, 7, dtype=dt, device=DEV)  # noqa: E731
+    q, out, lse = full(4, Hq, D, dt=torch.bfloat16), full(4, Hq, D, dt=torch.bfloat16), full(4, Hq, dt=torch.float32)
+    lst, cnt = full(4, Hkv, 3, dt=torch.int32), full(4, Hkv, dt=torch.int32)
+    ctx.rope_append_bounds(desc, qkv.to(DEV), c.kv, c.bounds, q, None, None, 1e-6, 1e4, q_offsets=offs)
+    ctx.page_select(desc, q, c.kv, c.bounds, 3, lst, cnt, sink_pages=0, q_offsets=offs)
+    ctx.attn_decode_pages(desc, q, c.kv, lst, cnt, out, lse, q_offsets=offs)
+    assert ctx.device_status() == AF.OK
+    for t in (q, out, lse, lst, cnt):
+        assert (t[2:] == 7).all() and not (t[:2] == 7).all()
+    want = PO.page_select(f64(q), c.codes.cpu().numpy(), c.scales.cpu().numpy(), c.table, lens, 3, 0, 2, offs.tolist())
+    np.testing.assert_array_equal(lst[:2].cpu().numpy(), want[0][:2])
+    att = PO.attn_pages(f64(q), f64(c.kd), f64(c.vd), c.table, lens, lst.cpu().numpy(), cnt.cpu().numpy(), offs.tolist())
+    check_attention(out[:2], lse[:2], att[0][:2], att[1][:2], [s[:2] for s in att[2]], D)
+    # nothing at all
+    offs.zero_()
+    ctx.rope_append_bounds(desc, qkv.to(DEV), c.kv, c.bounds, q.fill_(3), None, None, 1e-6, 1e4, q_offsets=offs)
+    ctx.page_select(desc, q, c.kv, c.bounds, 3, lst.fill_(3), cnt, q_offsets=offs)
+    ctx.attn_decode_pages(desc, q, c.kv, lst, cnt, out.fill_(3), lse, q_offsets=offs)
+    assert ctx.device_status() == AF.OK
+    assert (q == 3).all() and (lst == 3).all() and (out == 3).all()
+
+
+def test_heads_of_every_group_size_and_a_large_pool_index(ctx):
+    """Pages far into the pools: element offsets beyond 32 bits."""
+    Hkv, D, pool = 8, 128, 140_000                                           # 140,000 pages x 8 heads x 16 x 128 elements > 2^31
+    k = torch.zeros(pool, Hkv, 16, D, dtype=torch.bfloat16, device=DEV)
+    v = torch.zeros_like(k)
+    pages = [pool - 1, pool - 77, 3]
+    g = torch.Generator().manual_seed(5)
+    k[pages] = torch.randn(3, Hkv, 16, D, generator=g).to(torch.bfloat16).to(DEV)
+    v[pages] = torch.randn(3, Hkv, 16, D, generator=g).to(torch.bfloat16).to(DEV)
+    codes, scales = AF.empty_page_bounds(pool, Hkv, D, DEV)
+    bounds = AF.make_page_bounds(codes, scales)
+    kv = AF.make_kv(k, v, torch.tensor([pages], dtype=torch.int32, device=DEV), torch.tensor([47], dtype=torch.int32, device=DEV))
+    small_k, small_v, table = f64(k[pages]), f64(v[pages]), np.array([[0, 1, 2]])
+    for G in (1, 2, 4, 8):
+        Hq = G * Hkv
+        desc = AF.attn_desc(Hq, Hkv, D)
+        qkv = torch.randn(1, (Hq + 2 * Hkv) * D, generator=g).to(torch.bfloat16)
+        q = torch.empty(1, Hq, D, dtype=torch.bfloat16, device=DEV)
+        ctx.page_bounds(desc, kv, bounds, 1)
+        ctx.rope_append_bounds(desc, qkv.to(DEV), kv, bounds, q, None, None, 1e-6, 1e4)
+        PO.rope_append(f64(qkv), small_k, small_v, table, [47], Hq, Hkv, None, None, 1e-6, 1e4)
+        np.testing.assert_array_equal(f64(k[pages]), small_k)
+        sc, ss = codes[pages].cpu().numpy(), scales[pages].cpu().numpy()
+        for i, n in enumerate((16, 16, 15)):
+            for h in range(Hkv):
+                want = PO.page_bounds(small_k[i, h, :n])
+                np.testing.assert_array_equal(sc[i, h], want[0])
+                np.testing.assert_array_equal(ss[i, h], want[1])
+        lst = torch.empty(1, Hkv, 2, dtype=torch.int32, device=DEV)
+        cnt = torch.empty(1, Hkv, dtype=torch.int32, device=DEV)
+        out, lse = torch.empty_like(q), torch.empty(1, Hq, device=DEV)
+        ctx.page_select(desc, q, kv, bounds, 2, lst, cnt, sink_pages=0, window_pages=1)
+        want = PO.page_select(f64(q), sc, ss, table, [47], 2, 0, 1)
+        np.testing.assert_array_equal(lst.cpu().numpy(), want[0])
+        ctx.attn_decode_pages(desc, q, kv, lst, cnt, out, lse)
+        check_attention(out, lse, *PO.attn_pages(f64(q), small_k, small_v, table, [47], *want), D)
+    assert ctx.device_status() == AF.OK

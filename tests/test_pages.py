@@ -127,7 +127,8 @@ def test_particular_refusals():
     assert f.call("page_select", policy=None) == INV
     assert f.call("page_select", list=None) == INV and f.call("page_select", count=None) == INV
     assert f.call("page_select", kv=_kv(f, max_pages_per_seq=393217)) == UNS
-    assert f.call("page_bounds", kv=_kv(f, max_pages_per_seq=(1 << 30))) == UNS
+    for name in ALL:
+        assert f.call(name, kv=_kv(f, max_pages_per_seq=(1 << 26) + 1)) == UNS
     assert f.call("attn_decode_pages", list=None) == INV and f.call("attn_decode_pages", count=None) == INV
     assert f.call("attn_decode_pages", top=0) == INV and f.call("attn_decode_pages", out=None) == INV
 
@@ -136,6 +137,45 @@ def test_particular_refusals():
 @pytest.mark.parametrize("name", ALL)
 def test_good_arguments_pass_the_checks_and_fail_loudly_without_a_gpu(name):
     assert Fake().call(name) == AF.ERR_CUDA
+
+
+def test_binding_checks_tensors_before_the_library_sees_them():
+    """Shapes and types of every tensor argument; a wrong one never reaches a kernel."""
+    ctx = AF.Context.__new__(AF.Context)
+    ctx._lib, ctx._h, ctx.device = AF.load_library(), None, 0
+    bf, i32 = torch.bfloat16, torch.int32
+    z = lambda *s, dt=bf: torch.zeros(*s, dtype=dt)  # noqa: E731
+    desc = AF.attn_desc(8, 2, 64)
+    k = z(6, 2, 16, 64)
+    kv = AF.make_kv(k, k, z(3, 4, dt=i32), z(3, dt=i32))
+    bounds = AF.make_page_bounds(*AF.empty_page_bounds(6, 2, 64, device="cpu"))
+    q, lst, cnt, offs = z(3, 8, 64), z(3, 2, 5, dt=i32), z(3, 2, dt=i32), z(4, dt=i32)
+    qkv = z(3, 12 * 64)
+    bad = [
+        lambda: ctx.rope_append_bounds(desc, z(3, 11 * 64), kv, bounds, q, None, None, 1e-6, 1e4),
+        lambda: ctx.rope_append_bounds(desc, qkv.float(), kv, bounds, q, None, None, 1e-6, 1e4),
+        lambda: ctx.rope_append_bounds(desc, qkv, kv, bounds, z(2, 8, 64), None, None, 1e-6, 1e4),
+        lambda: ctx.rope_append_bounds(desc, qkv, kv, bounds, q, z(32), None, 1e-6, 1e4),
+        lambda: ctx.rope_append_bounds(desc, z(4, 12 * 64), kv, bounds, z(4, 8, 64), None, None, 1e-6, 1e4),       # four sequences
+        lambda: ctx.rope_append_bounds(desc, qkv, kv, bounds, q, None, None, 1e-6, 1e4, q_offsets=offs.long()),
+        lambda: ctx.rope_append_bounds(AF.attn_desc(8, 2, 128), z(3, 12 * 128), kv, bounds, z(3, 8, 128), None, None, 1e-6, 1e4),
+        lambda: ctx.page_bounds(desc, kv, bounds, 4),
+        lambda: ctx.page_bounds(desc, kv, AF.make_page_bounds(*AF.empty_page_bounds(5, 2, 64, device="cpu")), 3),
+        lambda: ctx.page_bounds(desc, kv, bounds, 3, first_token=z(2, dt=i32)),
+        lambda: ctx.page_select(desc, q, kv, bounds, 6, lst, cnt),
+        lambda: ctx.page_select(desc, q, kv, bounds, 5, lst.long(), cnt),
+        lambda: ctx.page_select(desc, q, kv, bounds, 5, lst, z(3, 1, dt=i32)),
+        lambda: ctx.page_select(desc, q.half(), kv, bounds, 5, lst, cnt),
+        lambda: ctx.attn_decode_pages(desc, q, kv, lst, cnt, z(3, 7, 64)),
+        lambda: ctx.attn_decode_pages(desc, z(2, 8, 64), kv, lst, cnt, q),
+        lambda: ctx.attn_decode_pages(desc, q, kv, lst, cnt, q, z(3, 8)),
+        lambda: ctx.attn_decode_pages(desc, q, kv, lst.transpose(0, 1).contiguous(), cnt, q),
+        lambda: ctx.attn_decode_pages(desc, q, kv, lst, cnt, q),                                                   # not on the device
+    ]
+    for i, f in enumerate(bad):
+        with pytest.raises(AssertionError):
+            f()
+            print(i)
 
 
 def test_binding_checks_shapes():
