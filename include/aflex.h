@@ -543,6 +543,20 @@ AFLEX_API aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_
                                                const int32_t* page_list, const int32_t* page_count, int top_pages, int batch,
                                                const int32_t* q_offsets, int rows, void* out, float* lse, void* stream);
 
+/*
+ * aflex_decoder_layers with page-sparse attention: in every layer the append makes the key bounds of the page it writes, the
+ * layer's queries select pages, and attention reads those (three launches in the place of two).  bounds: HOST array
+ * [num_layers], one per layer's cache; policy: the same for all layers.  Everything else as aflex_decoder_layers, and the
+ * result for top_pages >= the pages of every sequence is that of aflex_decoder_layers up to rounding.  The bounds of the
+ * pages before each sequence's last must be those of the cache (aflex_page_bounds after a prefill).  Workspace from
+ * aflex_decoder_sparse_workspace_bytes.
+ */
+AFLEX_API aflex_status aflex_decoder_layers_sparse(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs,
+                                                   const aflex_key_bounds* bounds, const aflex_page_policy* policy, int num_layers,
+                                                   const void* x_in, int batch, int microbatch_depth, const int32_t* mb_offsets,
+                                                   void* x_out, void* stream);
+AFLEX_API size_t aflex_decoder_sparse_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int top_pages);
+
 /* ---- Host-side decisions of the data plane and the DVFS controller ------------------------
  *
  * Pure host computation on HOST pointers: nothing is launched and no GPU setting is read or

@@ -28,6 +28,7 @@ EXPORTS = (
     "aflex_add_rmsnorm", "aflex_rope_append", "aflex_attn_prefill", "aflex_af_decoder_layers", "aflex_af_workspace_bytes",
     "aflex_prefill_layers", "aflex_prefill_workspace_bytes",
     "aflex_rope_append_bounds", "aflex_page_bounds", "aflex_page_select", "aflex_attn_decode_pages",
+    "aflex_decoder_layers_sparse", "aflex_decoder_sparse_workspace_bytes",
     "aflex_eq2_layer_time", "aflex_curve_eval",
     "aflex_pipeline_makespan", "aflex_plan_microbatches", "aflex_dvfs_window", "aflex_dvfs_decode_step",
     "aflex_dvfs_prefill_pair",
@@ -180,6 +181,11 @@ def load_library() -> ctypes.CDLL:
                                       ctypes.POINTER(PagePolicy), ci, vp, ci, vp, vp, vp]
     lib.aflex_attn_decode_pages.restype = ci
     lib.aflex_attn_decode_pages.argtypes = [vp, ctypes.POINTER(AttnDesc), vp, ctypes.POINTER(KV), vp, vp, ci, ci, vp, ci, vp, vp, vp]
+    lib.aflex_decoder_layers_sparse.restype = ci
+    lib.aflex_decoder_layers_sparse.argtypes = [vp, ctypes.POINTER(DecoderDesc), ctypes.POINTER(KV), ctypes.POINTER(KeyBounds),
+                                                ctypes.POINTER(PagePolicy), ci, vp, ci, ci, ctypes.POINTER(ctypes.c_int32), vp, vp]
+    lib.aflex_decoder_sparse_workspace_bytes.restype = cs
+    lib.aflex_decoder_sparse_workspace_bytes.argtypes = [ctypes.POINTER(DecoderDesc), ci, ci]
     cd, dp, ip = ctypes.c_double, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)
     lib.aflex_eq2_layer_time.restype = cd
     lib.aflex_eq2_layer_time.argtypes = [cd, cd, cd, ci]
@@ -293,6 +299,10 @@ def decoder_desc(layer: LayerDesc, w_qkv, w_ln_attn, w_ln_ffn, w_q_norm, w_k_nor
 
 def decoder_workspace_bytes(layer: DecoderDesc, max_batch: int) -> int:
     return int(load_library().aflex_decoder_workspace_bytes(ctypes.byref(layer), max_batch))
+
+
+def decoder_sparse_workspace_bytes(layer: DecoderDesc, max_batch: int, top_pages: int) -> int:
+    return int(load_library().aflex_decoder_sparse_workspace_bytes(ctypes.byref(layer), max_batch, top_pages))
 
 
 def prefill_workspace_bytes(layer: DecoderDesc, max_tokens: int) -> int:
@@ -635,6 +645,21 @@ class Context:
         _match(desc, kv, batch)
         self._check(self._lib.aflex_attn_decode_pages(self._h, desc, _ptr(q), kv, _ptr(page_list), _ptr(page_count), top, batch, offs,
                                                       rows, _ptr(out), _ptr(lse), self._stream_of(q, stream)))
+
+    def decoder_layers_sparse(self, layers: Sequence[DecoderDesc], kvs: Sequence[KV], bounds: Sequence[KeyBounds], top_pages: int,
+                              x_in, x_out, sink_pages: int = 1, window_pages: int = 2, microbatch_depth: int = 1,
+                              mb_offsets: Optional[Sequence[int]] = None, stream=None) -> None:
+        """decoder_layers with page-sparse attention; bounds[l] are the key bounds of layer l's cache (the appended page's are updated)."""
+        assert len(layers) == len(kvs) == len(bounds) and len(layers) >= 1
+        for d, kv, b in zip(layers, kvs, bounds):
+            _match(d.layer.attn, kv, x_in.shape[0], b)
+        offs = None
+        if mb_offsets is not None:
+            offs = (ctypes.c_int32 * len(mb_offsets))(*[int(v) for v in mb_offsets])
+        la, ka, ba = (DecoderDesc * len(layers))(*layers), (KV * len(kvs))(*kvs), (KeyBounds * len(bounds))(*bounds)
+        self._check(self._lib.aflex_decoder_layers_sparse(self._h, la, ka, ba, PagePolicy(top_pages, sink_pages, window_pages), len(layers),
+                                                          _ptr(x_in), x_in.shape[0], microbatch_depth, offs, _ptr(x_out),
+                                                          self._stream_of(x_in, stream)))
 
     def _stream_of(self, t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
         """The given stream, or the current one of the ctx's device (without building a Stream object: these calls last microseconds)."""

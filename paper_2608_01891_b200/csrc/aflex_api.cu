@@ -718,6 +718,11 @@ namespace {
 struct DecoderWs {
     size_t a_attn, a_lin, rows_h, rows_qkv, rows_a, f_total, total;
 };
+// Page lists and counts of page-sparse attention (behind the other regions).
+size_t page_lists_bytes(const aflex_attn_desc* d, int max_batch, int top_pages) {
+    return align256((size_t)max_batch * d->num_kv_heads * top_pages * sizeof(int32_t)) +
+           align256((size_t)max_batch * d->num_kv_heads * sizeof(int32_t));
+}
 DecoderWs decoder_ws(const aflex_decoder_desc* d, int max_batch, size_t a_attn, int num_sms) {
     const aflex_layer_desc* L = &d->layer;
     const int D = L->attn.head_dim, A = L->attn.num_q_heads * D, H = L->hidden;
@@ -747,6 +752,11 @@ DecoderWs decoder_ws(const aflex_decoder_desc* d, int max_batch, size_t a_attn, 
 size_t aflex_decoder_workspace_bytes(const aflex_decoder_desc* layer, int max_batch) {
     if (!layer || max_batch < 1) return 0;
     return decoder_ws(layer, max_batch, attn_workspace_bytes(&layer->layer.attn, 4096), query_num_sms()).total;
+}
+
+size_t aflex_decoder_sparse_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int top_pages) {
+    if (!layer || max_batch < 1 || top_pages < 1) return 0;
+    return aflex_decoder_workspace_bytes(layer, max_batch) + 256 + page_lists_bytes(&layer->layer.attn, max_batch, top_pages);
 }
 
 aflex_status aflex_add_rmsnorm(aflex_ctx* ctx, const void* res, const void* add, const void* w, int T, int H, float eps,
@@ -828,18 +838,26 @@ aflex_status aflex_page_bounds(aflex_ctx* ctx, const aflex_attn_desc* desc, cons
     return page_bounds_launch(ctx, desc, kv, bounds, batch, first_token, reinterpret_cast<cudaStream_t>(stream));
 }
 
+namespace {
+aflex_status validate_policy(aflex_ctx* ctx, const char* what, const aflex_page_policy* policy) {
+    if (!policy) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: null page policy", what);
+    if (policy->sink_pages < 0 || policy->window_pages < 1 || policy->top_pages < 1 ||
+        (long long)policy->sink_pages + policy->window_pages > policy->top_pages)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: sink_pages %d >= 0, window_pages %d >= 1 and their sum <= top_pages %d are required",
+                         what, policy->sink_pages, policy->window_pages, policy->top_pages);
+    return AFLEX_OK;
+}
+}  // namespace
+
 aflex_status aflex_page_select(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,
                                const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch, const int32_t* q_offsets,
                                int rows, int32_t* page_list, int32_t* page_count, void* stream) {
     aflex_status s = validate_attn(ctx, desc, q, kv, batch, page_list);
     if (s == AFLEX_OK) s = validate_bounds(ctx, "page_select", bounds);
     if (s == AFLEX_OK) s = validate_rows(ctx, "page_select", kv, batch, q_offsets, rows);
+    if (s == AFLEX_OK) s = validate_policy(ctx, "page_select", policy);
     if (s != AFLEX_OK) return s;
-    if (!policy || !page_count) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "page_select: null argument");
-    if (policy->sink_pages < 0 || policy->window_pages < 1 || policy->top_pages < 1 ||
-        (long long)policy->sink_pages + policy->window_pages > policy->top_pages)
-        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "page_select: sink_pages %d >= 0, window_pages %d >= 1 and their sum <= top_pages %d are required",
-                         policy->sink_pages, policy->window_pages, policy->top_pages);
+    if (!page_count) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "page_select: null argument");
     CtxDevice dev(ctx);
     return page_select_launch(ctx, desc, q, kv, bounds, policy, batch, q_offsets, rows, page_list, page_count,
                               reinterpret_cast<cudaStream_t>(stream));
@@ -908,9 +926,11 @@ aflex_status make_offsets(aflex_ctx* ctx, int batch, int M, const int32_t* mb_of
 }
 }  // namespace
 
-aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs, int num_layers,
-                                  const void* x_in, int batch, int M, const int32_t* mb_offsets, void* x_out,
-                                  void* stream) {
+namespace {
+// The chain with dense attention (bounds == nullptr), or with page-sparse attention and the layers' key bounds.
+aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs, const aflex_key_bounds* bounds,
+                                const aflex_page_policy* policy, int num_layers, const void* x_in, int batch, int M,
+                                const int32_t* mb_offsets, void* x_out, void* stream) {
     if (!ctx) return AFLEX_ERR_INVALID_ARG;
     aflex_status s = validate_decoder_args(ctx, layers, kvs, num_layers, x_in, batch, x_out);
     if (s != AFLEX_OK) return s;
@@ -918,7 +938,8 @@ aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
     size_t need = 0;
     for (int l = 0; l < num_layers; ++l) {
         const DecoderWs w = decoder_ws(&layers[l], batch, attn_workspace_bytes(&layers[l].layer.attn, attn_grid(ctx)), ctx->num_sms);
-        if (w.total > need) need = w.total;
+        const size_t total = w.total + (bounds ? 256 + page_lists_bytes(&layers[l].layer.attn, batch, policy->top_pages) : 0);
+        if (total > need) need = total;
     }
     if (need > ctx->ws_bytes)
         return set_error(ctx, AFLEX_ERR_WORKSPACE, "decoder layers: need %zu workspace bytes, have %zu", need, ctx->ws_bytes);
@@ -957,6 +978,8 @@ aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
         bf* xn2 = reinterpret_cast<bf*>(p); p += w.rows_h;
         bf* yb = reinterpret_cast<bf*>(p); p += w.rows_h;
         char* ws_f = p;
+        int32_t* lists = reinterpret_cast<int32_t*>(ctx->ws + align256(w.total));
+        int32_t* counts = lists + align256((size_t)batch * Hkv * (bounds ? policy->top_pages : 0) * sizeof(int32_t)) / sizeof(int32_t);
         for (int i = 0; i < M; ++i) {
             const int r0 = offs[i], rows = offs[i + 1] - offs[i];
             const size_t oh = (size_t)r0 * H;
@@ -989,10 +1012,22 @@ aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
             kvi.page_table = kvs[l].page_table + (size_t)r0 * kvs[l].max_pages_per_seq;
             kvi.seq_lens = kvs[l].seq_lens + r0;
             kvi.seq_lens_host = kvs[l].seq_lens_host ? kvs[l].seq_lens_host + r0 : nullptr;
-            s = rope_append_launch(ctx, &L->attn, qkv + (size_t)r0 * NQ, &kvi, rows, d->w_q_norm, d->w_k_norm, d->rms_eps, d->rope_theta, qb + (size_t)r0 * A, sa);
-            if (s != AFLEX_OK) return s;
-            ctx->attn_q_final_once = true;      // q was written by the append kernel, which does not release its dependents early
-            s = attn_decode_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, rows, ab + (size_t)r0 * A, nullptr, ws_attn, w.a_attn, sa);
+            if (bounds) {
+                int32_t* list = lists + (size_t)r0 * Hkv * policy->top_pages;
+                int32_t* count = counts + (size_t)r0 * Hkv;
+                s = rope_append_bounds_launch(ctx, &L->attn, qkv + (size_t)r0 * NQ, &kvi, &bounds[l], rows, nullptr, rows, d->w_q_norm, d->w_k_norm,
+                                              d->rms_eps, d->rope_theta, qb + (size_t)r0 * A, sa);
+                if (s == AFLEX_OK)
+                    s = page_select_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, &bounds[l], policy, rows, nullptr, rows, list, count, sa);
+                if (s == AFLEX_OK)
+                    s = attn_decode_pages_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, list, count, policy->top_pages, rows, nullptr, rows,
+                                                 ab + (size_t)r0 * A, nullptr, sa);
+            } else {
+                s = rope_append_launch(ctx, &L->attn, qkv + (size_t)r0 * NQ, &kvi, rows, d->w_q_norm, d->w_k_norm, d->rms_eps, d->rope_theta, qb + (size_t)r0 * A, sa);
+                if (s != AFLEX_OK) return s;
+                ctx->attn_q_final_once = true;      // q was written by the append kernel, which does not release its dependents early
+                s = attn_decode_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, rows, ab + (size_t)r0 * A, nullptr, ws_attn, w.a_attn, sa);
+            }
             if (s != AFLEX_OK) return s;
             if (!fused) {
                 s = linear_launch(ctx, ab + (size_t)r0 * A, L->w_o, rows, A, H, ob + oh, ws_lin, w.a_lin, sa, kKLinearGemm, ctx->counters_a);
@@ -1034,6 +1069,29 @@ aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
     if (e == cudaSuccess) e = cudaStreamWaitEvent(user, ctx->ev_a_done, 0);
     if (e == cudaSuccess) e = cudaStreamWaitEvent(user, ctx->ev_f_done, 0);
     return check_cuda(ctx, e, "decoder layers: exit join");
+}
+
+}  // namespace
+
+aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs, int num_layers,
+                                  const void* x_in, int batch, int M, const int32_t* mb_offsets, void* x_out,
+                                  void* stream) {
+    return decoder_layers_run(ctx, layers, kvs, nullptr, nullptr, num_layers, x_in, batch, M, mb_offsets, x_out, stream);
+}
+
+aflex_status aflex_decoder_layers_sparse(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs,
+                                         const aflex_key_bounds* bounds, const aflex_page_policy* policy, int num_layers,
+                                         const void* x_in, int batch, int M, const int32_t* mb_offsets, void* x_out, void* stream) {
+    if (!ctx) return AFLEX_ERR_INVALID_ARG;
+    aflex_status s = validate_decoder_args(ctx, layers, kvs, num_layers, x_in, batch, x_out);
+    if (s == AFLEX_OK) s = validate_policy(ctx, "sparse decoder layers", policy);
+    if (s == AFLEX_OK && !bounds) s = set_error(ctx, AFLEX_ERR_INVALID_ARG, "sparse decoder layers: null key bounds");
+    for (int l = 0; l < num_layers && s == AFLEX_OK; ++l) {
+        s = validate_bounds(ctx, "sparse decoder layers", &bounds[l]);
+        if (s == AFLEX_OK) s = page_select_supported(ctx, &kvs[l]);
+    }
+    if (s != AFLEX_OK) return s;
+    return decoder_layers_run(ctx, layers, kvs, bounds, policy, num_layers, x_in, batch, M, mb_offsets, x_out, stream);
 }
 
 // ---- whole decoder layers over the tokens being prefilled -----------------------------------

@@ -957,6 +957,13 @@ static aflex_status select_attributes(aflex_ctx* ctx, int di) {
     return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
 }
 
+aflex_status page_select_supported(aflex_ctx* ctx, const aflex_kv* kv) {
+    if (kv->max_pages_per_seq > kSelMaxCluster * kSelCap)
+        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", kv->max_pages_per_seq,
+                         kSelMaxCluster * kSelCap);
+    return AFLEX_OK;
+}
+
 aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
                                 const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch, const int32_t* q_offsets,
                                 int rows, int32_t* page_list, int32_t* page_count, cudaStream_t st) {
@@ -969,8 +976,8 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.top = policy->top_pages; p.sink = policy->sink_pages; p.window = policy->window_pages;
     p.list = page_list; p.count = page_count; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
-    if (p.max_pages > kSelMaxCluster * kSelCap)
-        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: max_pages_per_seq %d (supported: up to %d)", p.max_pages, kSelMaxCluster * kSelCap);
+    aflex_status ok = page_select_supported(ctx, kv);
+    if (ok != AFLEX_OK) return ok;
     const int di = d->head_dim == 128;
     if (!ctx->select_attr_set[di]) {
         aflex_status s = select_attributes(ctx, di);

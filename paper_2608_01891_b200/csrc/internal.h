@@ -221,6 +221,7 @@ aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d,
 aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
                                 const aflex_key_bounds* bounds, const aflex_page_policy* policy, int batch, const int32_t* q_offsets,
                                 int rows, int32_t* page_list, int32_t* page_count, cudaStream_t st);
+aflex_status page_select_supported(aflex_ctx* ctx, const aflex_kv* kv);      // the limit on max_pages_per_seq
 aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
                                       const int32_t* page_list, const int32_t* page_count, int top_pages, int batch,
                                       const int32_t* q_offsets, int rows, void* out, float* lse, cudaStream_t st);

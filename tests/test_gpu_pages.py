@@ -629,6 +629,133 @@ def test_prefill_chunk_then_drafted_rows(ctx):
     assert ctx.device_status() == AF.OK
 
 
+TINY_MOE = IN.LayerConfig(33, "sparse-moe", 6, 8, 2, 64, 256, 384, num_experts=4, top_k=2, len_dist="uniform", len_lo=16, len_hi=600,
+                          rms_eps=1e-5, qk_norm=False)
+SPARSE_DENSE = IN.LayerConfig(34, "sparse-dense", 7, 16, 2, 128, 512, 640, len_dist="uniform", len_lo=1, len_hi=900)
+
+
+class Layers:
+    """`n` decoder layers of one configuration with a cache, key bounds and weights each."""
+
+    def __init__(self, cfg, n):
+        self.cfg, self.n = cfg, n
+        kvh = IN.make_paged_kv(cfg)
+        self.kvh = kvh
+        self.table, self.lens = kvh.page_table.to(DEV), kvh.seq_lens.to(DEV)
+        self.attn = AF.attn_desc(cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim)
+        self.w, self.descs, self.kvs, self.caches, self.bounds = [], [], [], [], []
+        for l in range(n):
+            w = {k: (None if t is None else t.to(DEV)) for k, t in vars(IN.make_decoder_weights(cfg, l)).items()}
+            layer = AF.layer_desc(self.attn, cfg.hidden, cfg.inter, w["o"], w["gate"], w["up"], w["down"], cfg.num_experts, cfg.top_k, w["router"])
+            k, v = kvh.k_cache.to(DEV, copy=True), kvh.v_cache.to(DEV, copy=True)
+            self.w.append(w)
+            self.descs.append(AF.decoder_desc(layer, w["qkv"], w["ln_attn"], w["ln_ffn"], w["q_norm"], w["k_norm"], cfg.rms_eps, cfg.rope_theta))
+            self.caches.append((k, v))
+            self.kvs.append(AF.make_kv(k, v, self.table, self.lens, kvh.seq_lens))
+            self.bounds.append(AF.make_page_bounds(*AF.empty_page_bounds(k.shape[0], cfg.num_kv_heads, cfg.head_dim, DEV)))
+        self.x = IN.make_hidden(cfg).to(DEV)
+
+    def reset(self, ctx):
+        for (k, v), kv, b in zip(self.caches, self.kvs, self.bounds):
+            k.copy_(self.kvh.k_cache)
+            v.copy_(self.kvh.v_cache)
+            ctx.page_bounds(self.attn, kv, b, self.cfg.batch)
+
+
+def rows_apart(a, b):
+    """Largest difference of a row over its largest value."""
+    a, b = f64(a), f64(b)
+    return (np.abs(a - b).max(-1) / np.abs(b).max(-1)).max()
+
+
+@pytest.mark.parametrize("cfg", [SPARSE_DENSE, TINY_MOE], ids=lambda c: c.name)
+@pytest.mark.parametrize("depth", [1, 2])
+def test_sparse_decoder_layers_with_every_page_are_the_dense_ones(cfg, depth):
+    L = Layers(cfg, 2)
+    top = int((int(L.kvh.seq_lens.max()) + 15) // 16)
+    ctx = AF.Context(0, AF.decoder_sparse_workspace_bytes(L.descs[0], cfg.batch, top))
+    try:
+        dense, sparse = torch.empty_like(L.x), torch.empty_like(L.x)
+        L.reset(ctx)
+        ctx.decoder_layers(L.descs, L.kvs, L.x, dense, depth)
+        caches = [(k.clone(), v.clone()) for k, v in L.caches]
+        L.reset(ctx)
+        ctx.decoder_layers_sparse(L.descs, L.kvs, L.bounds, top, L.x, sparse, microbatch_depth=depth)
+        assert ctx.device_status() == AF.OK
+        # two chains of the same bf16 roundings (some twenty a layer, each off by at most 2^-8 of its row's largest value, and
+        # adding up like independent ones): as far apart as the chain is from its definition elsewhere in these tests
+        assert rows_apart(sparse, dense) <= 2e-2
+        for (k, v), (kd, vd) in zip(L.caches, caches):
+            assert rows_apart(k, kd) <= 2e-2 and rows_apart(v, vd) <= 2e-2
+        # the bounds of every page are those of the cache as it now is
+        for (k, _), kv, b in zip(L.caches, L.kvs, L.bounds):
+            fresh = AF.make_page_bounds(*AF.empty_page_bounds(k.shape[0], cfg.num_kv_heads, cfg.head_dim, DEV))
+            ctx.page_bounds(L.attn, kv, fresh, cfg.batch)
+            assert all(torch.equal(x, y) for x, y in zip(b._keep, fresh._keep))
+    finally:
+        ctx.close()
+
+
+@pytest.mark.parametrize("cfg", [SPARSE_DENSE, TINY_MOE], ids=lambda c: c.name)
+def test_sparse_decoder_layer_is_its_operators_in_turn(cfg):
+    L = Layers(cfg, 1)
+    B, H, Hq, Hkv, D = cfg.batch, cfg.hidden, cfg.num_q_heads, cfg.num_kv_heads, cfg.head_dim
+    top, w = 5, L.w[0]
+    ctx = AF.Context(0, AF.decoder_sparse_workspace_bytes(L.descs[0], B, top))
+    try:
+        got = torch.empty_like(L.x)
+        L.reset(ctx)
+        ctx.decoder_layers_sparse(L.descs, L.kvs, L.bounds, top, L.x, got, sink_pages=0, window_pages=2)
+        after = [t.clone() for t in (*L.caches[0], *L.bounds[0]._keep)]
+        L.reset(ctx)
+        new = lambda *s, dt=torch.bfloat16: torch.empty(*s, dtype=dt, device=DEV)  # noqa: E731
+        xn, qkv, q, a, o, h1, y, out = new(B, H), new(B, (Hq + 2 * Hkv) * D), new(B, Hq, D), new(B, Hq, D), new(B, H), new(B, H), new(B, H), new(B, H)
+        lst, cnt = new(B, Hkv, top, dt=torch.int32), new(B, Hkv, dt=torch.int32)
+        layer_front(ctx, cfg, w, L.attn, L.x, xn, qkv)
+        ctx.rope_append_bounds(L.attn, qkv, L.kvs[0], L.bounds[0], q, w["q_norm"], w["k_norm"], cfg.rms_eps, cfg.rope_theta)
+        ctx.page_select(L.attn, q, L.kvs[0], L.bounds[0], top, lst, cnt, sink_pages=0, window_pages=2)
+        ctx.attn_decode_pages(L.attn, q, L.kvs[0], lst, cnt, a)
+        ctx.linear(a.view(B, -1), w["o"], o)
+        ctx.add_rmsnorm(L.x, o, w["ln_ffn"], cfg.rms_eps, h1, xn)
+        if cfg.num_experts:
+            ctx.ffn_moe(xn, w["gate"], w["up"], w["down"], cfg.top_k, y, w_router=w["router"])
+        else:
+            ctx.ffn_dense(xn, w["gate"], w["up"], w["down"], y)
+        ctx.add_rmsnorm(h1, y, None, 0.0, out, None)
+        assert ctx.device_status() == AF.OK
+        assert (cnt.max() == top) and int(L.kvh.seq_lens.max()) > 16 * top        # something had to be chosen
+        assert rows_apart(got, out) <= 2e-2
+        for x, z in zip(after, (*L.caches[0], *L.bounds[0]._keep)):
+            assert torch.equal(x, z)                                              # the same kernels on the same qkv
+    finally:
+        ctx.close()
+
+
+def test_sparse_decoder_layers_refusals():
+    cfg = SPARSE_DENSE
+    L = Layers(cfg, 1)
+    ctx = AF.Context(0, AF.decoder_sparse_workspace_bytes(L.descs[0], cfg.batch, 4))
+    try:
+        out = torch.empty_like(L.x)
+        run = lambda top, bounds=None, **kw: ctx.decoder_layers_sparse(L.descs, L.kvs, bounds or L.bounds, top, L.x, out, **kw)  # noqa: E731
+        small = AF.Context(0, 1 << 20)
+        with pytest.raises(AF.AflexError) as e:
+            small.decoder_layers_sparse(L.descs, L.kvs, L.bounds, 4, L.x, out)
+        assert e.value.status == AF.ERR_WORKSPACE
+        small.close()
+        for f, status in [(lambda: run(2), AF.ERR_INVALID_ARG), (lambda: run(4, window_pages=0), AF.ERR_INVALID_ARG),
+                          (lambda: run(4, bounds=[AF.KeyBounds(None, None)]), AF.ERR_INVALID_ARG), (lambda: run(4, microbatch_depth=99), AF.ERR_INVALID_ARG)]:
+            with pytest.raises(AF.AflexError) as e:
+                f()
+            assert e.value.status == status
+        assert ctx.launch_count() == 0
+        L.reset(ctx)
+        run(4)
+        assert ctx.device_status() == AF.OK
+    finally:
+        ctx.close()
+
+
 def test_two_streams_at_once(ctx):
     """The calls keep nothing in the context's workspace: two streams may run them at the same time."""
     made = []
