@@ -391,45 +391,55 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
         for (int r = r_first; r < nrows; r += r_step) {
             // (h_first - sub is the same for the whole warp)
             for (int h = h_first; h - sub < h_hi; h += h_step) {
-                uint4 ya[2], yb[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) { ya[u] = xa[u]; yb[u] = xb[u]; }
-                if (h - sub + h_step < h_hi) load(r, h + h_step);
-                else if (r + r_step < nrows) load(r + r_step, h_first);
+                uint32_t va[2][4], vc[2][4];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const uint32_t va[4] = {ya[u].x, ya[u].y, ya[u].z, ya[u].w}, vc[4] = {yb[u].x, yb[u].y, yb[u].z, yb[u].w};
-                    uint64_t a[4], c[4], rinv = pack_f32x2(1.f, 1.f);
+                    va[u][0] = xa[u].x; va[u][1] = xa[u].y; va[u][2] = xa[u].z; va[u][3] = xa[u].w;
+                    vc[u][0] = xb[u].x; vc[u][1] = xb[u].y; vc[u][2] = xb[u].z; vc[u][3] = xb[u].w;
+                }
+                if (h - sub + h_step < h_hi) load(r, h + h_step);
+                else if (r + r_step < nrows) load(r + r_step, h_first);
+                uint64_t rinv[2];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) { a[k] = widen_bf16x2(va[k]); c[k] = widen_bf16x2(vc[k]); }
+                for (int u = 0; u < 2; ++u) {
+                    float ri = 1.f;
                     if (p.w_qn) {
                         uint64_t s2 = 0;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) s2 = fma_f32x2(a[k], a[k], fma_f32x2(c[k], c[k], s2));
+                        for (int k = 0; k < 4; ++k) {
+                            const uint64_t a = widen_bf16x2(va[u][k]), c = widen_bf16x2(vc[u][k]);
+                            s2 = fma_f32x2(a, a, fma_f32x2(c, c, s2));
+                        }
                         float s0, s1;
                         unpack_f32x2(s2, s0, s1);
                         float ss = s0 + s1;
 #pragma unroll
                         for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                        const float ri = rsqrtf(ss / (float)D + p.eps);
-                        rinv = pack_f32x2(ri, ri);
+                        ri = rsqrtf(ss / (float)D + p.eps);
                     }
-                    uint32_t qa[4], qb[4];
+                    rinv[u] = pack_f32x2(ri, ri);
+                }
+                // the pair's rotation is read once for both heads, the result takes the input's place
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const ulonglong2 z0 = *reinterpret_cast<const ulonglong2*>(&rot.q[slot0 + r][k][0][l]);
-                        const ulonglong2 z1 = *reinterpret_cast<const ulonglong2*>(&rot.q[slot0 + r][k][1][l]);
+                for (int k = 0; k < 4; ++k) {
+                    const ulonglong2 z0 = *reinterpret_cast<const ulonglong2*>(&rot.q[slot0 + r][k][0][l]);
+                    const ulonglong2 z1 = *reinterpret_cast<const ulonglong2*>(&rot.q[slot0 + r][k][1][l]);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const uint64_t a = widen_bf16x2(va[u][k]), c = widen_bf16x2(vc[u][k]);
                         float x0, x1, y0, y1;
-                        unpack_f32x2(mul_f32x2(fma_f32x2(a[k], z0.x, mul_f32x2(c[k], z0.y)), rinv), x0, x1);
-                        unpack_f32x2(mul_f32x2(fma_f32x2(c[k], z1.x, mul_f32x2(a[k], z1.y)), rinv), y0, y1);
-                        qa[k] = pack_bf16x2(x0, x1);
-                        qb[k] = pack_bf16x2(y0, y1);
+                        unpack_f32x2(mul_f32x2(fma_f32x2(a, z0.x, mul_f32x2(c, z0.y)), rinv[u]), x0, x1);
+                        unpack_f32x2(mul_f32x2(fma_f32x2(c, z1.x, mul_f32x2(a, z1.y)), rinv[u]), y0, y1);
+                        va[u][k] = pack_bf16x2(x0, x1);
+                        vc[u][k] = pack_bf16x2(y0, y1);
                     }
-                    const uint4 oa = make_uint4(qa[0], qa[1], qa[2], qa[3]), ob = make_uint4(qb[0], qb[1], qb[2], qb[3]);
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
                     if (h + u * L::kTok < h_hi) {
                         uint4* dst = reinterpret_cast<uint4*>(p.q_out + ((size_t)(row0 + r) * p.Hq + h + u * L::kTok) * D);
-                        dst[l] = oa;
-                        dst[D / 16 + l] = ob;
+                        dst[l] = make_uint4(va[u][0], va[u][1], va[u][2], va[u][3]);
+                        dst[D / 16 + l] = make_uint4(vc[u][0], vc[u][1], vc[u][2], vc[u][3]);
                     }
                 }
             }
@@ -505,7 +515,7 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
                     }
 #pragma unroll
                     for (int off = 1; off < L::kPer; off <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, off);
-                    rinv = 1.0 / sqrt(ss / (double)D + (double)p.eps);
+                    rinv = rsqrt(ss / (double)D + (double)p.eps);
                 }
                 uint4 oa, ob;
                 __nv_bfloat16* qa = reinterpret_cast<__nv_bfloat16*>(&oa);
