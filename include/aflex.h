@@ -487,7 +487,7 @@ AFLEX_API aflex_status aflex_rope_append(aflex_ctx* ctx, const aflex_attn_desc* 
  *   codes  i8 [num_pages][Hkv][D / 8][2][8]   for channels 8 i .. 8 i + 7: the eight HI, then the eight LO
  *   scales u8 [num_pages][Hkv][D / 32]        e_c + 127
  * (2 D + D / 32 bytes beside the page's 64 D bytes of K and V).  They depend on the stored keys alone, not on how many calls
- * stored them.  Bounds of pages that no call has made yet must not be selected from.
+ * stored them.  Bounds that no call has made yet may hold anything: the pages that are chosen by them are arbitrary.
  */
 typedef struct { int8_t* codes; uint8_t* scales; } aflex_key_bounds;
 

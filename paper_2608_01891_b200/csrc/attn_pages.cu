@@ -96,6 +96,7 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t 
 // list), not the bytes; so as much as possible is loaded before it is known to be needed, and barriers are few.  A score
 // takes some 60 instructions on its way through the selection, which is why a long row's selection is spread over the cluster.
 constexpr int kSelTile = 16;
+constexpr uint32_t kScaleMax = 127 + 50;            // largest exponent of the bounds, as stored
 constexpr int kSelCap = 48 * 1024;                  // scores one CTA's shared memory holds
 constexpr int kSelMaxCluster = 8;
 constexpr int kSelRank = 64;                        // members of an interval that are ranked by comparing all pairs
@@ -195,7 +196,9 @@ __device__ __forceinline__ float score_tile(const Tile<D>& tile, const uint4 (&q
         int d[4] = {0, 0, 0, 0};
         mma_s8_16832(d, tile.x[0][c].x, tile.x[1][c].x, tile.x[0][c].y, tile.x[1][c].y, qf[c].x, qf[c].y);
         mma_s8_16832(d, tile.x[0][c].z, tile.x[1][c].z, tile.x[0][c].w, tile.x[1][c].w, qf[c].z, qf[c].w);
-        const float k0 = __uint_as_float(((tile.scale[0] >> (8 * c)) & 255u) << 23), k1 = __uint_as_float(((tile.scale[1] >> (8 * c)) & 255u) << 23);
+        // (bounds that nobody has made yet may hold any byte: none makes a score infinite or not a number)
+        const float k0 = __uint_as_float(min((tile.scale[0] >> (8 * c)) & 255u, kScaleMax) << 23);
+        const float k1 = __uint_as_float(min((tile.scale[1] >> (8 * c)) & 255u, kScaleMax) << 23);
         // the products are exact, so a fused multiply-add rounds like the sum alone
         s[0] = fmaf((float)d[0] * k0, fq[c].x, c ? s[0] : 0.f);
         s[1] = fmaf((float)d[1] * k0, fq[c].y, c ? s[1] : 0.f);
@@ -295,15 +298,10 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
             const int v = __shfl_up_sync(0xffffffffu, incl, off);
             if (lane >= off) incl += v;
         }
-        const int from = __ffs(__ballot_sync(0xffffffffu, incl - sum < need && incl >= need)) - 1;
+        const int from = __ffs(__ballot_sync(0xffffffffu, incl - sum < need && incl >= need)) - 1;     // (there is one: all are counted)
         need -= __shfl_sync(0xffffffffu, incl - sum, from);
-        bin = 255 - 8 * from;
-        while (true) {
-            inside = h[bin];
-            if (inside >= need) break;
-            need -= inside;
-            --bin;
-        }
+        for (bin = 255 - 8 * from; bin > 248 - 8 * from && h[bin] < need; --bin) need -= h[bin];
+        inside = h[bin];
     };
     each([&](int, float s, bool in) { if (in) atomicAdd(&sh.hist[interval(s)], 1); });
     divide();

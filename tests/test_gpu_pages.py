@@ -338,6 +338,27 @@ def test_selection_ties_and_odd_queries(ctx):
     np.testing.assert_array_equal(got[1], want[1])
 
 
+def test_selection_from_bounds_that_nobody_made(ctx):
+    """Any bytes as bounds: the lists are still lists of the sequence's pages."""
+    lens = [3000, 90, 16 * 40]
+    c = Cache(lens, 2, 64, seed=2)
+    g = torch.Generator().manual_seed(8)
+    q = (torch.randn(3, 4, 64, generator=g) * torch.exp(20 * torch.randn(3, 4, 64, generator=g))).to(torch.bfloat16)
+    q[0, 0, :3] = torch.tensor([float("nan"), float("inf"), -float("inf")])
+    for scales in ((0, 256), (250, 256), (0, 2), (255, 256)):
+        c.codes.copy_(torch.randint(-128, 128, c.codes.shape, generator=g).to(torch.int8))
+        c.scales.copy_(torch.randint(*scales, c.scales.shape, generator=g).to(torch.uint8))
+        for top in (7, 39):
+            lst, cnt = run_select(ctx, c, q, 4, top, 1, 2)
+            assert ctx.device_status() == AF.OK
+            for b, n in enumerate(lens):
+                pages = (n + 15) // 16
+                assert (cnt[b] == min(top, pages)).all()
+                for h in range(2):
+                    got = lst[b, h, :cnt[b, h]]
+                    assert (np.diff(got) > 0).all() and got[0] >= 0 and got[-1] == pages - 1 and (lst[b, h, cnt[b, h]:] == -1).all()
+
+
 @pytest.mark.parametrize("n_pages,rows", [(129, 1), (1024, 1), (5003, 2), (60001, 1)])
 def test_selection_over_long_caches(ctx, n_pages, rows):
     """Every cluster size; at 60001 pages the scores no longer fit one CTA's shared memory.  Pages are shared, so scores repeat."""
