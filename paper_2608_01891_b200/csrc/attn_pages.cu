@@ -12,6 +12,10 @@ namespace aflex {
 
 namespace {
 
+// A plain load, for what a preceding kernel may have written (queries, lists, lengths, bounds): these kernels may have started before that
+// one was done and wait for it, so the read-only path (ld.global.nc) would not be bound to see its stores.
+template <typename V> __device__ __forceinline__ V fetch(const V* p) { return *p; }
+
 constexpr int kPageTokens = 16;
 constexpr float kNegBig = -1.0e30f;
 
@@ -23,17 +27,17 @@ __device__ __forceinline__ RowSeq locate_row(int row, const int32_t* q_offsets, 
     at.b = row; at.back = 0; at.padding = false;
     if (q_offsets != nullptr) {
         // largest b with q_offsets[b] <= row: the lanes look at 32 sequences at a time (one load's latency for up to 32)
-        const int lane = threadIdx.x & 31, end = __ldg(q_offsets + batch);
+        const int lane = threadIdx.x & 31, end = fetch(q_offsets + batch);
         int lo = 0, span = batch;
         while (span > 1) {
             const int step = (span + 31) / 32, i = lane * step;
-            const unsigned le = __ballot_sync(0xffffffffu, i < span && __ldg(q_offsets + lo + (i < span ? i : 0)) <= row);
+            const unsigned le = __ballot_sync(0xffffffffu, i < span && fetch(q_offsets + lo + (i < span ? i : 0)) <= row);
             const int skip = max(__popc(le) - 1, 0) * step;
             lo += skip;
             span = min(step, span - skip);
         }
         at.b = lo;
-        at.back = __ldg(q_offsets + lo + 1) - 1 - row;
+        at.back = fetch(q_offsets + lo + 1) - 1 - row;
         at.padding = row >= end;
     }
     return at;
@@ -181,9 +185,9 @@ __device__ __forceinline__ void load_tile(Tile<D>& tile, const SelectParams& p, 
         const size_t slab = (size_t)id * p.Hkv + g;
         const uint4* src = reinterpret_cast<const uint4*>(p.codes + slab * (2 * D)) + l4;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) tile.x[r][c] = __ldg(src + c * 4);
-        if (D == 128) tile.scale[r] = __ldg(reinterpret_cast<const uint32_t*>(p.scales) + slab);
-        else tile.scale[r] = __ldg(reinterpret_cast<const uint16_t*>(p.scales) + slab);
+        for (int c = 0; c < D / 32; ++c) tile.x[r][c] = fetch(src + c * 4);
+        if (D == 128) tile.scale[r] = fetch(reinterpret_cast<const uint32_t*>(p.scales) + slab);
+        else tile.scale[r] = fetch(reinterpret_cast<const uint16_t*>(p.scales) + slab);
     }
 }
 // Scores of a tile's pages; lanes 4 i and 4 i + 1 return those of rows i and i + 8.
@@ -433,15 +437,15 @@ __global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_sele
     const bool quantises = warp < kBlocks;
     uint4 qx = make_uint4(0, 0, 0, 0);
     if (quantises && hl < p.G)
-        qx = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + hl) * D) + warp * 4 + l4);
+        qx = fetch(reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + hl) * D) + warp * 4 + l4);
     const RowSeq at = locate_row(row, p.q_offsets, p.batch);
-    const int len = __ldg(p.seq_lens + at.b);
+    const int len = fetch(p.seq_lens + at.b);
     const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
     // The lanes hold the page ids of two of the warp's tiles (lane / 16).  With one CTA the warp's tiles do not depend on the
     // length, so the first ids are loaded along with it (whatever the table's row holds beyond the sequence).
     auto page_ids = [&](int t) -> int {
         const long long j = p.sink + (long long)(t + (lane >> 4) * W) * kSelTile + (lane & 15);
-        return __ldg(table + min(j, (long long)p.max_pages - 1));
+        return fetch(table + min(j, (long long)p.max_pages - 1));
     };
     int t = warp, ids = S == 1 ? page_ids(t) : 0;
     const int pos = row_position(at, len, p.max_pages), n = pos >= 0 ? pos / kPageTokens + 1 : 0;
@@ -531,7 +535,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 3) page_select_rows_kernel(co
         const int i = warp + k * W, r = i / kBlocks;
         qx[k] = make_uint4(0, 0, 0, 0);
         if (r < nrows && hl < p.G)
-            qx[k] = __ldg(reinterpret_cast<const uint4*>(p.q + ((size_t)(row0 + r) * p.Hq + (size_t)g * p.G + hl) * D) + (i % kBlocks) * 4 + l4);
+            qx[k] = fetch(reinterpret_cast<const uint4*>(p.q + ((size_t)(row0 + r) * p.Hq + (size_t)g * p.G + hl) * D) + (i % kBlocks) * 4 + l4);
     }
     const RowSeq first = locate_row(row0, p.q_offsets, p.batch);
     const bool shared = !first.padding && first.back >= nrows - 1;                // all rows of the group in one sequence
@@ -539,7 +543,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 3) page_select_rows_kernel(co
     last.back -= nrows - 1;
     if (shared) at.back = first.back - rank;
     else if (rank < nrows) at = locate_row(row, p.q_offsets, p.batch);
-    const int len = __ldg(p.seq_lens + at.b);
+    const int len = fetch(p.seq_lens + at.b);
     const bool mine = rank < nrows && !at.padding;                                // this CTA has a row
     const int pos = mine ? row_position(at, len, p.max_pages) : -1, n = pos >= 0 ? pos / kPageTokens + 1 : 0;
     if (mine && pos < 0 && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
@@ -553,7 +557,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 3) page_select_rows_kernel(co
     const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
     auto page_ids = [&](int t) -> int {
         const long long j = p.sink + (long long)t * kSelTile + (lane & 15);
-        return __ldg(table + min(j, (long long)p.max_pages - 1));
+        return fetch(table + min(j, (long long)p.max_pages - 1));
     };
     int ids = page_ids(t0);
     if (cand > 0) {
@@ -812,19 +816,19 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
     const int32_t* list = p.list + item * p.top;
     auto entry = [&](int i0) -> int {
         const long long i = first + (long long)(i0 + lane) * stride;
-        return i < p.top ? __ldg(list + i) : -1;
+        return i < p.top ? fetch(list + i) : -1;
     };
     int next = entry(0);
-    const int total = max(0, min(p.top, __ldg(p.count + item)));
+    const int total = max(0, min(p.top, fetch(p.count + item)));
     uint4 qf[kSteps];                              // head lane / 4, channels 32 step + 8 (lane % 4) .. + 7
     {
         const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)row * p.Hq + (size_t)g * p.G + (hl < p.G ? hl : 0)) * D);
 #pragma unroll
-        for (int c = 0; c < kSteps; ++c) qf[c] = __ldg(src + c * 4 + l4);
+        for (int c = 0; c < kSteps; ++c) qf[c] = fetch(src + c * 4 + l4);
     }
     const RowSeq at = locate_row(row, p.q_offsets, p.batch);
     if (at.padding) return;                        // (the same for the whole cluster)
-    const int pos = row_position(at, __ldg(p.seq_lens + at.b), p.max_pages);
+    const int pos = row_position(at, fetch(p.seq_lens + at.b), p.max_pages);
     if (pos < 0 && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
     const int n = pos >= 0 ? max(0, (total - first + stride - 1) / stride) : 0;        // this warp's pages
     const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
@@ -840,7 +844,7 @@ __global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const 
             phys = 0; valid = 0;
             if (i + lane < n) {
                 if (next >= 0 && next <= pos / kPageTokens) {
-                    phys = __ldg(table + next);
+                    phys = fetch(table + next);
                     valid = min(kPageTokens, pos - next * kPageTokens + 1);
                 }
                 if (valid == 0 || phys < 0 || phys >= p.num_pages) { atomicExch(p.status, AFLEX_ERR_BOUNDS); phys = 0; valid = 0; }

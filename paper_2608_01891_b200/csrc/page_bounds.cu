@@ -23,6 +23,10 @@ namespace aflex {
 
 namespace {
 
+// A plain load, for what a preceding kernel may have written (projections, lengths): these kernels may have started before that
+// one was done and wait for it, so the read-only path (ld.global.nc) would not be bound to see its stores.
+template <typename V> __device__ __forceinline__ V fetch(const V* p) { return *p; }
+
 constexpr int kBoundsWarps = 8;
 constexpr int kBoundsThreads = kBoundsWarps * 32;
 constexpr int kPageTokens = 16;
@@ -176,9 +180,9 @@ __global__ void __launch_bounds__(kBoundsThreads) page_bounds_kernel(const Bound
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.y;
     const int first_page = blockIdx.x * p.pages_per_cta, my_page = first_page + lane;     // lane i holds the run's i-th page
-    const int raw = __ldg(p.seq_lens + b);
-    const int from = p.first_token ? __ldg(p.first_token + b) : 0;
-    int id = lane < p.pages_per_cta && my_page < p.max_pages ? __ldg(p.page_table + (size_t)b * p.max_pages + my_page) : 0;
+    const int raw = fetch(p.seq_lens + b);
+    const int from = p.first_token ? fetch(p.first_token + b) : 0;
+    int id = lane < p.pages_per_cta && my_page < p.max_pages ? fetch(p.page_table + (size_t)b * p.max_pages + my_page) : 0;
     if ((raw < 0 || raw > p.max_pages * kPageTokens) && blockIdx.x == 0 && threadIdx.x == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
     const int len = max(0, min(raw, p.max_pages * kPageTokens));
     const int pages = min(p.pages_per_cta, (len + kPageTokens - 1) / kPageTokens - first_page);
@@ -366,8 +370,8 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const uint4* s = src + min(h + u * L::kTok, h_hi - 1) * (D / 8);
-                xa[u] = __ldg(s);
-                xb[u] = __ldg(s + D / 16);
+                xa[u] = fetch(s);
+                xb[u] = fetch(s + D / 16);
             }
         };
         if (r_first < nrows) load(r_first, h_first);
@@ -474,7 +478,7 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
 #pragma unroll
             for (int k = 0; k < kPageTokens * D / 256; ++k) {
                 const int j = k * 32 + lane, r = j / (D / 8);
-                if (r < nrows) v[k] = __ldg(src + (size_t)r * heads * (D / 8) + j % (D / 8));
+                if (r < nrows) v[k] = fetch(src + (size_t)r * heads * (D / 8) + j % (D / 8));
             }
 #pragma unroll
             for (int k = 0; k < kPageTokens * D / 256; ++k) {
