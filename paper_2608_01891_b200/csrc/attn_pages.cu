@@ -103,6 +103,7 @@ constexpr int kSelTile = 16;
 constexpr uint32_t kScaleMax = 127 + 50;            // largest exponent of the bounds, as stored
 constexpr int kSelCap = 48 * 1024;                  // scores one CTA's shared memory holds
 constexpr int kSelMaxCluster = 8;
+constexpr int kSelTiles = 2;                        // tiles a warp has in flight (the lanes hold two tiles' page ids)
 constexpr int kSelRank = 64;                        // members of an interval that are ranked by comparing all pairs
 
 struct SelectParams {
@@ -283,13 +284,13 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     auto divide = [&]() {
         sync_all();                                                // the histograms are complete
         if (S > 1) {
-            if (tid < 256) {
+            for (int i = tid; i < 256; i += kThreads) {
                 uint32_t v[kSelMaxCluster], sum = 0;
 #pragma unroll
-                for (int s = 0; s < kSelMaxCluster; ++s) v[s] = ld_cluster_u32(cluster_map_shared(smem_u32(&sh.hist[tid]), (uint32_t)(s < S ? s : 0)));
+                for (int s = 0; s < kSelMaxCluster; ++s) v[s] = ld_cluster_u32(cluster_map_shared(smem_u32(&sh.hist[i]), (uint32_t)(s < S ? s : 0)));
 #pragma unroll
                 for (int s = 0; s < kSelMaxCluster; ++s) sum += s < S ? v[s] : 0u;
-                sh.sum[tid] = (int)sum;
+                sh.sum[i] = (int)sum;
             }
             __syncthreads();
         }
@@ -322,7 +323,7 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     };
     while (inside > kSelRank && inside > need) {
         sync_all();                                                // everybody has read the histograms
-        if (tid < 256) sh.hist[tid] = 0;
+        for (int i = tid; i < 256; i += kThreads) sh.hist[i] = 0;
         __syncthreads();
         const int shift = max(0, 24 - __clz(hi - lo));
         each([&](int j, float s, bool in) { if (in && member(j, s)) atomicAdd(&sh.hist[(value(j, s) - lo) >> shift], 1); });
@@ -415,9 +416,8 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     });
 }
 
-// W warps, T tiles per warp in flight.
-template <int D, int W, int T>
-__global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_select_kernel(const SelectParams p) {
+template <int D, int W>                             // W warps
+__global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const SelectParams p) {
     constexpr int kBlocks = D / 32;
     constexpr int kThreads = W * 32;
     extern __shared__ __align__(16) uint8_t smem_raw[];
@@ -429,7 +429,7 @@ __global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_sele
     const int row = (int)(item / p.Hkv), g = (int)(item % p.Hkv);
     const int hl = lane >> 2, l4 = lane & 3;
     if (S > 1) cluster_arrive();                                  // the cluster's CTAs have started: waited for below
-    if (tid < 256) sh.hist[tid] = 0;
+    for (int i = tid; i < 256; i += kThreads) sh.hist[i] = 0;
     if (tid == 0) sh.members = 0;
     pdl_launch_dependents();
     pdl_wait();
@@ -483,14 +483,14 @@ __global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_sele
         ids = page_ids(t);
     }
     while (t < t_end) {
-        Tile<D> tile[T];
+        Tile<D> tile[kSelTiles];
 #pragma unroll
-        for (int k = 0; k < T; ++k) load_tile<D>(tile[k], p, g, ids, k * 16, (t + k * W) * kSelTile, c1);
+        for (int k = 0; k < kSelTiles; ++k) load_tile<D>(tile[k], p, g, ids, k * 16, (t + k * W) * kSelTile, c1);
         const int t_now = t;
-        t += T * W;
+        t += kSelTiles * W;
         if (t < t_end) ids = page_ids(t);
 #pragma unroll
-        for (int k = 0; k < T; ++k) {
+        for (int k = 0; k < kSelTiles; ++k) {
             const float v = score_tile<D>(tile[k], qf, fq, p.G);
             const int j = (t_now + k * W) * kSelTile + hl + 8 * l4;
             if (l4 < 2 && j < c1) {
@@ -508,10 +508,10 @@ __global__ void __launch_bounds__(W * 32, T == 1 ? 4 : W == 8 ? 2 : 1) page_sele
 // -- read once per row they are what bounds the kernel above when rows are many: an SM takes some 32 bytes a cycle out of L2 --
 // and sends the scores to the CTA of the row, which then selects for its row alone.  Rows of different sequences in one group
 // (the host can only guess where sequences end) are scored by their own CTAs.
-constexpr int kRowsWarps = 8;
-template <int D>
-__global__ void __launch_bounds__(kRowsWarps * 32, 3) page_select_rows_kernel(const SelectParams p) {
-    constexpr int kBlocks = D / 32, W = kRowsWarps, kThreads = W * 32;
+constexpr int kRowsWorth = 1200;                    // rows x pages from which scoring them together pays
+template <int D, int W>
+__global__ void __launch_bounds__(W * 32, 24 / W) page_select_rows_kernel(const SelectParams p) {
+    constexpr int kBlocks = D / 32, kThreads = W * 32;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     const int R = p.cluster;
     uint4* queries = reinterpret_cast<uint4*>(smem_raw);                          // [R][kBlocks][32]
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, 3) page_select_rows_kernel(co
     const int rank = (int)(blockIdx.x % R), g = (int)(blockIdx.x / R % p.Hkv), row0 = (int)(blockIdx.x / R / p.Hkv) * R;
     const int nrows = min(R, p.rows - row0), row = row0 + rank;
     cluster_arrive();
-    if (tid < 256) sh.hist[tid] = 0;
+    for (int i = tid; i < 256; i += kThreads) sh.hist[i] = 0;
     if (tid == 0) sh.members = 0;
     pdl_launch_dependents();
     pdl_wait();
@@ -944,18 +944,19 @@ cudaError_t launch_cluster(void (*kernel)(const P), long long ctas, int threads,
 // ------------------------------------------------------------------------------------------ host
 typedef void (*SelectKernel)(const SelectParams);
 static const SelectKernel kSelectKernels[2][3] = {
-    {page_select_kernel<64, 8, 1>, page_select_kernel<64, 8, 2>, page_select_kernel<64, 16, 2>},
-    {page_select_kernel<128, 8, 1>, page_select_kernel<128, 8, 2>, page_select_kernel<128, 16, 2>}};
+    {page_select_kernel<64, 4>, page_select_kernel<64, 8>, page_select_kernel<64, 16>},
+    {page_select_kernel<128, 4>, page_select_kernel<128, 8>, page_select_kernel<128, 16>}};
+static const SelectKernel kSelectRowsKernels[2][2] = {{page_select_rows_kernel<64, 4>, page_select_rows_kernel<64, 8>},
+                                                      {page_select_rows_kernel<128, 4>, page_select_rows_kernel<128, 8>}};
 
 // Raises the kernels' shared-memory limits on the current device.
 static aflex_status select_attributes(aflex_ctx* ctx, int di) {
     cudaError_t e = cudaSuccess;
     for (int w = 0; w < 3 && e == cudaSuccess; ++w)
         e = cudaFuncSetAttribute(kSelectKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (kSelCap + 4) * (int)sizeof(float));
-    // (group's queries and scores: 8 * 4 * (512 + 32) bytes and 4 per page)
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(di ? page_select_rows_kernel<128> : page_select_rows_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 8 * 4 * 544 + kSelCap * (int)sizeof(float));
+    // (a group's queries and scores: 8 * 4 * (512 + 32) bytes and 4 per page)
+    for (int w = 0; w < 2 && e == cudaSuccess; ++w)
+        e = cudaFuncSetAttribute(kSelectRowsKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * 4 * 544 + kSelCap * (int)sizeof(float));
     return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
 }
 
@@ -987,25 +988,28 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
         ctx->select_attr_set[di] = true;
     }
     // Rows that share their sequence go in groups, if there are enough of them to fill the GPU one CTA each: as many as a
-    // sequence has (up to 8, a divisor of more), four where the sequences' numbers of rows differ.  Ungrouped against grouped,
-    // 32 query on 8 KV heads: 16 x 5 rows of 128 / 512 / 1024 / 2048 pages 12.8 / 25.5 / 48.8 / 88.4 against 16.0 / 18.5 / 28.0 /
-    // 43.9 us, 40 x 3 rows 14.9 / 34.4 / 59.2 / 107 against 20.6 / 31.9 / 41.7 / 66.5, 10 x 2 rows never better.
-    if (q_offsets != nullptr && rows >= 3LL * batch && items > ctx->num_sms && p.max_pages > 512 && p.max_pages <= kSelCap) {
+    // sequence has (up to 8, a divisor of more), four where the sequences' numbers of rows differ.  It pays by the rows and the
+    // length; alone against grouped, 32 query on 8 KV heads, 128 / 256 / 512 pages: 16 x 5 rows 11.0 / 15.2 / 22.5 against 10.5 /
+    // 11.2 / 15.4 us, 32 x 4 rows 11.8 / 16.5 / 27.4 against 15.8 / 16.8 / 25.1, 40 x 3 rows 12.0 / 17.2 / 27.8 against 14.6 / 18.9 / 26.8
+    // (4 warps per CTA; with 8, 640 CTAs do not fit at once: 18.6 for the 15.4, but 336 CTAs of 2000 pages take 23 us instead of 37).
+    if (q_offsets != nullptr && rows >= 2LL * batch && items > ctx->num_sms && p.max_pages <= kSelCap) {
         const int each = rows % batch == 0 ? rows / batch : 4;
         int R = each <= 8 ? each : 4;
         for (int r = 8; r >= 2 && each > 8; --r) if (each % r == 0) { R = r; break; }
-        const long long ctas = ((long long)rows + R - 1) / R * p.Hkv * R;
-        if (ctas > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
-        p.cluster = R;
-        const size_t smem = (size_t)R * (d->head_dim / 32) * (32 * sizeof(uint4) + 8 * sizeof(float)) + (size_t)p.max_pages * sizeof(float);
-        KernelScope scope(ctx, kKPageSelect, st);
-        return check_cuda(ctx, launch_cluster(di ? page_select_rows_kernel<128> : page_select_rows_kernel<64>, ctas, kRowsWarps * 32, smem, R, st, p),
-                          "page_select_rows_kernel launch");
+        if ((long long)R * p.max_pages >= kRowsWorth) {
+            const long long ctas = ((long long)rows + R - 1) / R * p.Hkv * R;
+            if (ctas > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
+            p.cluster = R;
+            const size_t smem = (size_t)R * (d->head_dim / 32) * (32 * sizeof(uint4) + 8 * sizeof(float)) + (size_t)p.max_pages * sizeof(float);
+            KernelScope scope(ctx, kKPageSelect, st);
+            const bool wide = ctas <= 3 * ctx->num_sms;             // 8 warps per CTA while an SM's three places hold all of them
+            return check_cuda(ctx, launch_cluster(kSelectRowsKernels[di][wide], ctas, wide ? 256 : 128, smem, R, st, p), "page_select_rows_kernel launch");
+        }
     }
     // A cluster per (row, KV head) where those are fewer than the SMs (and where the scores need the room), each CTA at least
-    // eight tiles; 16 warps per CTA while an SM has no second one, else 8 warps with two tiles or (more CTAs than fit that way)
-    // one tile in flight.  8 x 8192 pages: 34.0 / 22.6 / 11.9 us with 1 / 2 / 8 CTAs of 16 warps, 13.4 with 8 of 8 warps; 256 x up
-    // to 256 pages: 11.1 us with 16 warps, 6.2 and 8.9 with 8 and two or one tile; 640 x up to 512: 27.5, 19.0 and 15.6.
+    // eight tiles.  16 warps per CTA while an SM has no second one, 8 while two per SM hold all of them, else 4 (more CTAs at
+    // once, and a selection that fewer warps have to agree on).  8 x 8192 pages: 34.0 / 22.6 / 11.5 us with 1 / 2 / 8 CTAs of 16
+    // warps, 13.4 with 8 of 8; 192 x 256 pages: 6.0 and 7.8 us with 8 and 4 warps, 320 x 256: 10.8 and 8.5, 2048 x 256: 49 and 39.5.
     int S = 1;
     while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelCap) && p.max_pages > S * 8 * kSelTile) S *= 2;
     const int form = items * S <= ctx->num_sms ? 2 : items * S <= 2 * ctx->num_sms ? 1 : 0;
@@ -1014,7 +1018,7 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     p.cluster = S;
     const size_t smem = (size_t)(share + 4) * sizeof(float);
     KernelScope scope(ctx, kKPageSelect, st);
-    return check_cuda(ctx, launch_cluster(kSelectKernels[di][form], items * S, form == 2 ? 512 : 256, smem, S, st, p), "page_select_kernel launch");
+    return check_cuda(ctx, launch_cluster(kSelectKernels[di][form], items * S, 128 << form, smem, S, st, p), "page_select_kernel launch");
 }
 
 aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,

@@ -289,6 +289,8 @@ GROUPS = [  # Hq, Hkv, D, lens, top, sink, window, new, padding rows
     (8, 4, 64, [600, 90, 17, 450, 800, 33], 5, 1, 1, [9, 1, 0, 20, 7, 13], 5),      # groups across sequences and padding
     (8, 8, 64, [40, 500, 35], 4, 1, 1, [9, 9, 9], 0),           # rows that see everything beside rows that choose
     (8, 8, 64, [300, 200, 250], 3, 1, 2, [8, 8, 8], 0),         # nothing but the forced pages
+    (16, 8, 128, [200 + 31 * i for i in range(13)], 6, 1, 1, [6] * 13, 0),          # more than the GPU holds with eight warps each
+    (8, 8, 64, [150 + 31 * i for i in range(17)], 6, 1, 1, [1 + i % 7 for i in range(17)], 3),
 ]
 
 
