@@ -450,46 +450,14 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
         }
         return;
     }
-    // ---- value heads: copied as they are; key heads: a warp each
-    const int step = p.kv_ctas * kBoundsWarps;
-    if (group * kBoundsWarps < p.Hkv) {                   // (not where this CTA has values only)
-        if (rotates) {
-            const int c = c_rot;
-            const double ga = p.w_kn ? __bfloat162float(p.w_kn[c]) : 1.f, gc = p.w_kn ? __bfloat162float(p.w_kn[kHalf + c]) : 1.f;
-            double sn, cs;
-            sincos(reduced(s_rot, c), &sn, &cs);
-            for (int s = s_rot; s < min(slot1, s_rot + 4); ++s) {
-                rot.k[s][c & 7][0][c >> 3] = make_double2(ga * cs, gc * sn);
-                rot.k[s][c & 7][1][c >> 3] = make_double2(gc * cs, ga * sn);
-                const double next = cs * p.step_cos[c] - sn * p.step_sin[c];
-                sn = sn * p.step_cos[c] + cs * p.step_sin[c];
-                cs = next;
-            }
-        }
-        __syncthreads();
-    }
-    for (int i = group * kBoundsWarps + warp; i < 2 * p.Hkv; i += step) {
-        const int g = i < p.Hkv ? i : i - p.Hkv;
-        const size_t slab = (size_t)page * p.Hkv + g;
-        if (i >= p.Hkv) {
-            const uint4* src = reinterpret_cast<const uint4*>(p.qkv + ((size_t)row0 * heads + p.Hq + p.Hkv + g) * D);
-            uint4* dst = reinterpret_cast<uint4*>(p.v_cache + (slab * kPageTokens + slot0) * D);
-            uint4 v[kPageTokens * D / 256];
-#pragma unroll
-            for (int k = 0; k < kPageTokens * D / 256; ++k) {
-                const int j = k * 32 + lane, r = j / (D / 8);
-                if (r < nrows) v[k] = fetch(src + (size_t)r * heads * (D / 8) + j % (D / 8));
-            }
-#pragma unroll
-            for (int k = 0; k < kPageTokens * D / 256; ++k) {
-                const int j = k * 32 + lane;
-                if (j / (D / 8) < nrows) dst[j] = v[k];
-            }
-            continue;
-        }
-        uint4* kd = reinterpret_cast<uint4*>(p.k_cache + slab * kPageTokens * D);
-        const int end = slot0 + nrows;                              // slots [0, slot0) hold older keys, [slot0, end) are new
-        uint4 xa[L::kIter], xb[L::kIter];
+    // ---- a key or value head per warp, loaded before the rotations are made; values are copied as they are
+    const int i = group * kBoundsWarps + warp, g = i < p.Hkv ? i : i - p.Hkv;
+    const bool is_key = i < p.Hkv, is_value = !is_key && i < 2 * p.Hkv;
+    const size_t slab = (size_t)page * p.Hkv + g;
+    const int end = slot1;                                          // slots [0, slot0) hold older keys, [slot0, end) are new
+    uint4* kd = reinterpret_cast<uint4*>(p.k_cache + slab * kPageTokens * D);
+    uint4 xa[L::kIter], xb[L::kIter];
+    if (is_key) {
 #pragma unroll
         for (int it = 0; it < L::kIter; ++it) {
             const int t = min(it * L::kTok + sub, end - 1);
@@ -498,6 +466,38 @@ __global__ void __launch_bounds__(kBoundsThreads, 3) rope_append_bounds_kernel(c
             xa[it] = src[l];
             xb[it] = src[D / 16 + l];
         }
+    }
+    if (is_value) {
+        const uint4* src = reinterpret_cast<const uint4*>(p.qkv + ((size_t)row0 * heads + p.Hq + i) * D);
+        uint4* dst = reinterpret_cast<uint4*>(p.v_cache + (slab * kPageTokens + slot0) * D);
+        uint4 v[kPageTokens * D / 256];
+#pragma unroll
+        for (int k = 0; k < kPageTokens * D / 256; ++k) {
+            const int j = k * 32 + lane, r = j / (D / 8);
+            if (r < nrows) v[k] = fetch(src + (size_t)r * heads * (D / 8) + j % (D / 8));
+        }
+#pragma unroll
+        for (int k = 0; k < kPageTokens * D / 256; ++k) {
+            const int j = k * 32 + lane;
+            if (j / (D / 8) < nrows) dst[j] = v[k];
+        }
+    }
+    if (group * kBoundsWarps >= p.Hkv) return;                      // values only
+    if (rotates) {
+        const int c = c_rot;
+        const double ga = p.w_kn ? __bfloat162float(p.w_kn[c]) : 1.f, gc = p.w_kn ? __bfloat162float(p.w_kn[kHalf + c]) : 1.f;
+        double sn, cs;
+        sincos(reduced(s_rot, c), &sn, &cs);
+        for (int s = s_rot; s < min(slot1, s_rot + 4); ++s) {
+            rot.k[s][c & 7][0][c >> 3] = make_double2(ga * cs, gc * sn);
+            rot.k[s][c & 7][1][c >> 3] = make_double2(gc * cs, ga * sn);
+            const double next = cs * p.step_cos[c] - sn * p.step_sin[c];
+            sn = sn * p.step_cos[c] + cs * p.step_sin[c];
+            cs = next;
+        }
+    }
+    __syncthreads();
+    if (is_key) {
         Range16 range;
         range.reset();
 #pragma unroll
