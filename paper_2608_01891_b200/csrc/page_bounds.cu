@@ -256,7 +256,7 @@ struct AppendParams {
 // A CTA handles the rows of ONE page of one sequence (1 to 16 rows), so that whoever rotates the page's keys holds all of
 // them when the bounds are formed: a page among the pages touched by the call (located by a scan over the sequences) and a
 // group of heads.  In chunks a page's groups are neighbours, so that key CTAs (arithmetic in double) run next to query and
-// value CTAs (bytes): 64 against 70 us for 7420 rows of 64 + 2 x 8 heads.  One row per page: all key CTAs, the longest, first.
+// value CTAs (bytes): 58.2 against 64.0 us for 7420 rows of 64 + 2 x 8 heads.  One row per page: all key CTAs, the longest, first.
 //
 // Bound: qkv read and q, K, V written once.  Two rotary halves of eight channels per lane make every access 16 bytes.
 // Queries are rotated in fp32.  Keys (one head in ten on the shapes served here) are normalised and rotated in double and
@@ -603,8 +603,8 @@ aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d,
     }
     for (int i = 0; i < 64; ++i) { p.inv_freq[i] = ctx->rope_freq[i]; p.step_cos[i] = ctx->rope_step[0][i]; p.step_sin[i] = ctx->rope_step[1][i]; }
     p.status = ctx->dev_status;
-    // A page's K and V heads on one CTA per eight of them; its query heads 32 per CTA (7420 rows: 87 / 71 / 64.6 / 65.7 us with
-    // 8 / 16 / 32 / 64; 256 single rows: 10.5 / 7.6 / 6.9 / 6.9: every CTA locates its page and makes its rotations).
+    // A page's K and V heads on one CTA per eight of them; its query heads 32 per CTA (7420 rows: 79.2 / 63.0 / 58.2 / 59.6 us with
+    // 8 / 16 / 32 / 64; 256 single rows: 10.0 / 7.3 / 6.7 / 6.7: every CTA locates its page and makes its rotations).
     // m new tokens of a sequence touch at most (m + 14) / 16 + 1 pages.
     const long long tasks = q_offsets ? ((long long)rows + 14LL * batch) / 16 + batch : batch;
     p.kv_ctas = (2 * p.Hkv + kBoundsWarps - 1) / kBoundsWarps;
