@@ -230,19 +230,27 @@ def _row_args(rows: int, q_offsets: Optional[torch.Tensor]):
     return q_offsets.shape[0] - 1, _ptr(q_offsets)
 
 
-def _match(desc: "AttnDesc", kv: "KV", batch: int, bounds: "Optional[KeyBounds]" = None) -> None:
-    """The descriptors against the shapes of the tensors they were made from (structs made by hand are not checked)."""
+def _where(*tensors: torch.Tensor) -> int:
+    """The CUDA device of all of them; -1 on the host, -2 if they lie on several."""
+    device = tensors[0].get_device()
+    return device if all(t.get_device() == device for t in tensors) else -2
+
+
+def _match(device: int, desc: "AttnDesc", kv: "KV", batch: int, bounds: "Optional[KeyBounds]" = None) -> None:
+    """The descriptors against the tensors they were made from and the context's device (structs made by hand are not checked)."""
     shape = kv.__dict__.get("_shape")
     if shape is not None:
-        heads, tokens, dim, most = shape
+        heads, tokens, dim, most, there = shape
         assert heads == desc.num_kv_heads and tokens == desc.page_size and dim == desc.head_dim, "cache shape does not fit the descriptor"
         assert batch <= most, "more sequences than page table rows or lengths"
+        assert there == device, "the cache is not on the context's device"
     if bounds is not None:
         shape = bounds.__dict__.get("_shape")
         if shape is not None:
-            pages, heads, chunks = shape
+            pages, heads, chunks, there = shape
             assert heads == desc.num_kv_heads and chunks * 8 == desc.head_dim, "key bounds do not fit the descriptor"
             assert pages >= kv.num_pages, "key bounds of fewer pages than the cache has"
+            assert there == device, "the key bounds are not on the context's device"
 
 
 def attn_desc(num_q_heads: int, num_kv_heads: int, head_dim: int, sm_scale: float = 0.0) -> AttnDesc:
@@ -261,7 +269,7 @@ def make_kv(k_cache: torch.Tensor, v_cache: torch.Tensor, page_table: torch.Tens
         assert seq_lens_host.dtype == torch.int32 and seq_lens_host.device.type == "cpu"
         kv.seq_lens_host = _ptr(seq_lens_host)
     kv._keep = (k_cache, v_cache, page_table, seq_lens, seq_lens_host)
-    kv._shape = (*k_cache.shape[1:], min(page_table.shape[0], seq_lens.shape[0]))
+    kv._shape = (*k_cache.shape[1:], min(page_table.shape[0], seq_lens.shape[0]), _where(k_cache, v_cache, page_table, seq_lens))
     return kv
 
 
@@ -277,7 +285,7 @@ def make_page_bounds(codes: torch.Tensor, scales: torch.Tensor) -> KeyBounds:
     assert codes.dim() == 5 and codes.shape[3:] == (2, 8) and tuple(scales.shape) == (codes.shape[0], codes.shape[1], codes.shape[2] // 4)
     b = KeyBounds(_ptr(codes), _ptr(scales))
     b._keep = (codes, scales)
-    b._shape = tuple(codes.shape[:3])
+    b._shape = (*codes.shape[:3], _where(codes, scales))
     return b
 
 
@@ -609,16 +617,17 @@ class Context:
         for w in (w_q_norm, w_k_norm):
             assert w is None or (w.dtype == _BF16 and w.numel() == d), "a head norm is not bf16 [D]"
         batch, offs = _row_args(rows, q_offsets)
-        _match(desc, kv, batch, bounds)
+        _match(self.device, desc, kv, batch, bounds)
         self._check(self._lib.aflex_rope_append_bounds(self._h, desc, _ptr(qkv), kv, bounds, batch, offs, rows, _ptr(w_q_norm),
-                                                       _ptr(w_k_norm), rms_eps, rope_theta, _ptr(q_out), self._stream_of(qkv, stream)))
+                                                       _ptr(w_k_norm), rms_eps, rope_theta, _ptr(q_out),
+                                                       self._stream_of(stream, qkv, q_out, w_q_norm, w_k_norm, q_offsets)))
 
     def page_bounds(self, desc: AttnDesc, kv: KV, bounds: KeyBounds, batch: int, first_token=None, stream=None) -> None:
         """Key bounds of the pages of sequences 0 .. batch - 1 that hold a token at first_token[b] (i32 CUDA [B]; None: 0) or later."""
         assert first_token is None or (first_token.dtype == torch.int32 and first_token.numel() >= batch)
-        _match(desc, kv, batch, bounds)
-        st = torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
-        self._check(self._lib.aflex_page_bounds(self._h, desc, kv, bounds, batch, _ptr(first_token), st))
+        _match(self.device, desc, kv, batch, bounds)
+        self._check(self._lib.aflex_page_bounds(self._h, desc, kv, bounds, batch, _ptr(first_token),
+                                                self._stream_of(stream, first_token)))
 
     def page_select(self, desc: AttnDesc, q, kv: KV, bounds: KeyBounds, top_pages: int, page_list, page_count,
                     sink_pages: int = 1, window_pages: int = 2, q_offsets=None, stream=None) -> None:
@@ -628,9 +637,10 @@ class Context:
         assert page_list.dtype == torch.int32 and page_list.shape == (rows, hkv, top_pages), "page_list is not i32 [rows][Hkv][top_pages]"
         assert page_count.dtype == torch.int32 and page_count.shape == (rows, hkv), "page_count is not i32 [rows][Hkv]"
         batch, offs = _row_args(rows, q_offsets)
-        _match(desc, kv, batch, bounds)
+        _match(self.device, desc, kv, batch, bounds)
         self._check(self._lib.aflex_page_select(self._h, desc, _ptr(q), kv, bounds, PagePolicy(top_pages, sink_pages, window_pages),
-                                                batch, offs, rows, _ptr(page_list), _ptr(page_count), self._stream_of(q, stream)))
+                                                batch, offs, rows, _ptr(page_list), _ptr(page_count),
+                                                self._stream_of(stream, q, page_list, page_count, q_offsets)))
 
     def attn_decode_pages(self, desc: AttnDesc, q, kv: KV, page_list, page_count, out, lse=None, q_offsets=None, stream=None) -> None:
         """Attention of every row over the pages listed for it: page_list i32 CUDA [rows,Hkv,top_pages], page_count i32 CUDA [rows,Hkv]."""
@@ -642,9 +652,10 @@ class Context:
         assert out.dtype == _BF16 and out.numel() == n * desc.head_dim, "out is not bf16 [rows][Hq][D]"
         assert lse is None or (lse.dtype == torch.float32 and lse.numel() == n), "lse is not fp32 [rows][Hq]"
         batch, offs = _row_args(rows, q_offsets)
-        _match(desc, kv, batch)
+        _match(self.device, desc, kv, batch)
         self._check(self._lib.aflex_attn_decode_pages(self._h, desc, _ptr(q), kv, _ptr(page_list), _ptr(page_count), top, batch, offs,
-                                                      rows, _ptr(out), _ptr(lse), self._stream_of(q, stream)))
+                                                      rows, _ptr(out), _ptr(lse),
+                                                      self._stream_of(stream, q, page_list, page_count, out, lse, q_offsets)))
 
     def decoder_layers_sparse(self, layers: Sequence[DecoderDesc], kvs: Sequence[KV], bounds: Sequence[KeyBounds], top_pages: int,
                               x_in, x_out, sink_pages: int = 1, window_pages: int = 2, microbatch_depth: int = 1,
@@ -652,16 +663,20 @@ class Context:
         """decoder_layers with page-sparse attention; bounds[l] are the key bounds of layer l's cache (the appended page's are updated)."""
         assert len(layers) == len(kvs) == len(bounds) and len(layers) >= 1
         for d, kv, b in zip(layers, kvs, bounds):
-            _match(d.layer.attn, kv, x_in.shape[0], b)
+            _match(self.device, d.layer.attn, kv, x_in.shape[0], b)
         offs = None
         if mb_offsets is not None:
             offs = (ctypes.c_int32 * len(mb_offsets))(*[int(v) for v in mb_offsets])
         la, ka, ba = (DecoderDesc * len(layers))(*layers), (KV * len(kvs))(*kvs), (KeyBounds * len(bounds))(*bounds)
         self._check(self._lib.aflex_decoder_layers_sparse(self._h, la, ka, ba, PagePolicy(top_pages, sink_pages, window_pages), len(layers),
                                                           _ptr(x_in), x_in.shape[0], microbatch_depth, offs, _ptr(x_out),
-                                                          self._stream_of(x_in, stream)))
+                                                          self._stream_of(stream, x_in, x_out)))
 
-    def _stream_of(self, t: torch.Tensor, stream: Optional[torch.cuda.Stream]) -> int:
-        """The given stream, or the current one of the ctx's device (without building a Stream object: these calls last microseconds)."""
-        assert t.get_device() == self.device, "the tensors are not on the context's device"
-        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+    def _stream_of(self, stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> int:
+        """The given stream, or the current one of the ctx's device (without building a Stream object: these calls last microseconds),
+        once the tensors are known to lie on that device."""
+        device = self.device
+        for t in tensors:
+            if t is not None and t.get_device() != device:
+                raise AssertionError("the tensors are not on the context's device")
+        return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream

@@ -178,6 +178,52 @@ def test_binding_checks_tensors_before_the_library_sees_them():
             print(i)
 
 
+def test_binding_checks_where_every_tensor_lies():
+    """A tensor on another device than the context's (here: one that says so) is refused before the library sees its address."""
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 7
+
+    class Stream:
+        cuda_stream = 0
+
+    ctx = AF.Context.__new__(AF.Context)
+    ctx._lib, ctx._h, ctx.device = AF.load_library(), None, -1
+    bf, i32 = torch.bfloat16, torch.int32
+    z = lambda *s, dt=bf: torch.zeros(*s, dtype=dt)  # noqa: E731
+    desc = AF.attn_desc(8, 2, 64)
+    k = z(6, 2, 16, 64)
+    cache = dict(k_cache=k, v_cache=k, page_table=z(3, 4, dt=i32), seq_lens=z(3, dt=i32))
+    codes, scales = AF.empty_page_bounds(6, 2, 64, device="cpu")
+    kv, bounds = AF.make_kv(**cache), AF.make_page_bounds(codes, scales)
+    far_kv = AF.make_kv(**{n: t.as_subclass(Elsewhere) for n, t in cache.items()})
+    far_bounds = AF.make_page_bounds(codes.as_subclass(Elsewhere), scales.as_subclass(Elsewhere))
+    offs = z(4, dt=i32)
+    calls = {
+        "rope_append_bounds": dict(qkv=z(3, 12 * 64), kv=kv, bounds=bounds, q_out=z(3, 8, 64), w_q_norm=z(64), w_k_norm=z(64), rms_eps=1e-6,
+                                   rope_theta=1e4, q_offsets=offs),
+        "page_bounds": dict(kv=kv, bounds=bounds, batch=3, first_token=z(3, dt=i32)),
+        "page_select": dict(q=z(3, 8, 64), kv=kv, bounds=bounds, top_pages=5, page_list=z(3, 2, 5, dt=i32), page_count=z(3, 2, dt=i32),
+                            q_offsets=offs),
+        "attn_decode_pages": dict(q=z(3, 8, 64), kv=kv, page_list=z(3, 2, 5, dt=i32), page_count=z(3, 2, dt=i32), out=z(3, 8, 64),
+                                  lse=z(3, 8, dt=torch.float32), q_offsets=offs),
+    }
+    for name, args in calls.items():
+        call = getattr(ctx, name)
+        with pytest.raises(AF.AflexError):                       # all where it should be: it is the library that refuses (no context)
+            call(desc, **args, stream=Stream)
+        for arg, value in args.items():
+            far = {"kv": far_kv, "bounds": far_bounds}.get(arg, value.as_subclass(Elsewhere) if isinstance(value, torch.Tensor) else None)
+            if far is not None:
+                with pytest.raises(AssertionError, match="context's device"):
+                    call(desc, **{**args, arg: far}, stream=Stream)
+    split_kv = AF.make_kv(**{**cache, "page_table": cache["page_table"].as_subclass(Elsewhere)})
+    split_bounds = AF.make_page_bounds(codes, scales.as_subclass(Elsewhere))
+    for args in (dict(kv=split_kv, bounds=bounds), dict(kv=kv, bounds=split_bounds)):
+        with pytest.raises(AssertionError, match="context's device"):
+            ctx.page_bounds(desc, batch=3, stream=Stream, **args)
+
+
 def test_binding_checks_shapes():
     codes, scales = AF.empty_page_bounds(6, 2, 64, device="cpu")
     assert codes.shape == (6, 2, 8, 2, 8) and scales.shape == (6, 2, 2)
