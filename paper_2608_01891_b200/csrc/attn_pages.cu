@@ -103,6 +103,7 @@ constexpr int kSelTile = 16;
 constexpr uint32_t kScaleMax = 127 + 50;            // largest exponent of the bounds, as stored
 constexpr int kSelCap = 48 * 1024;                  // scores one CTA's shared memory holds
 constexpr int kSelMaxCluster = 8;
+constexpr size_t kSelRowsSmem = 190 * 1024;         // most dynamic shared memory of page_select_rows_kernel
 constexpr int kSelTiles = 2;                        // tiles a warp has in flight (the lanes hold two tiles' page ids)
 constexpr int kSelRank = 64;                        // members of an interval that are ranked by comparing all pairs
 
@@ -116,27 +117,27 @@ struct SelectParams {
     int batch, rows, max_pages, Hq, Hkv, G;
     long long num_pages;
     int top, sink, window;
-    int cluster;                   // CTAs per (row, KV head); rows per group
+    int cluster;                   // CTAs per (row, KV head), or per group of rows and KV head
+    int group, stride, row_warps;  // rows per group, floats per row of its scores, log2 of the warps that select for a row
     int32_t* list;                 // [rows][Hkv][top]
     int32_t* count;                // [rows][Hkv]
     int* status;
 };
 
-template <int W> struct SelectShared {
-    uint4 q[4][32];                // quantised queries as the lanes' B operands: two words of positive parts, two of negative
-    float f[4][8];                 // 2^f per block and head
+// What the (up to W) warps share that select for one row; CL: the most CTAs that they are spread over.
+template <int W, int CL> struct SelectShared {
     __align__(16) int hist[256];   // this CTA's
-    __align__(16) int sum[256];    // the cluster's
+    __align__(16) int sum[CL > 1 ? 256 : 4];       // the cluster's
     uint2 range[W];                // lowest and highest score of every warp, as ordered bits
-    uint2 all_range[kSelMaxCluster];
+    uint2 all_range[CL];
     int members;                   // of the interval that is ranked, in this CTA
-    int all_members[kSelMaxCluster];
-    uint2 member[kSelMaxCluster][kSelRank];        // (score, page) of every CTA's
-    uint2 rank[kSelRank];          // all of them in one piece
+    int all_members[CL];
+    uint2 member[CL][kSelRank];    // (score, page) of every CTA's
+    uint2 rank[CL > 1 ? kSelRank : 1];             // all of them in one piece
     float last_score;              // the last one to keep
     int last_page;
     int kept[W];                   // of every warp's run
-    int all_kept[kSelMaxCluster];  // of every CTA
+    int all_kept[CL];              // of every CTA
 };
 
 __device__ __forceinline__ int q_exponent(float a) {             // smallest e with a <= 127 * 2^e, within [-60, 50]
@@ -191,25 +192,38 @@ __device__ __forceinline__ void load_tile(Tile<D>& tile, const SelectParams& p, 
         else tile.scale[r] = fetch(reinterpret_cast<const uint16_t*>(p.scales) + slab);
     }
 }
-// Scores of a tile's pages; lanes 4 i and 4 i + 1 return those of rows i and i + 8.
+// Scores of a tile's pages: rows lane / 4 and + 8, MMA columns 2 (lane % 4) and + 1, in v as (row, column) 00, 01, 10, 11.
 template <int D>
-__device__ __forceinline__ float score_tile(const Tile<D>& tile, const uint4 (&qf)[D / 32], const float2 (&fq)[D / 32], int G) {
-    const int l4 = threadIdx.x & 3;
-    float s[4];
+__device__ __forceinline__ void tile_scales(const Tile<D>& tile, float (&k0)[D / 32], float (&k1)[D / 32]) {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+        // (bounds that nobody has made yet may hold any byte: none makes a score infinite or not a number)
+        k0[c] = __uint_as_float(min((tile.scale[0] >> (8 * c)) & 255u, kScaleMax) << 23);
+        k1[c] = __uint_as_float(min((tile.scale[1] >> (8 * c)) & 255u, kScaleMax) << 23);
+    }
+}
+template <int D>
+__device__ __forceinline__ void score_columns(const Tile<D>& tile, const float (&k0)[D / 32], const float (&k1)[D / 32],
+                                              const uint4 (&qf)[D / 32], const float2 (&fq)[D / 32], float (&v)[4]) {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
         int d[4] = {0, 0, 0, 0};
         mma_s8_16832(d, tile.x[0][c].x, tile.x[1][c].x, tile.x[0][c].y, tile.x[1][c].y, qf[c].x, qf[c].y);
         mma_s8_16832(d, tile.x[0][c].z, tile.x[1][c].z, tile.x[0][c].w, tile.x[1][c].w, qf[c].z, qf[c].w);
-        // (bounds that nobody has made yet may hold any byte: none makes a score infinite or not a number)
-        const float k0 = __uint_as_float(min((tile.scale[0] >> (8 * c)) & 255u, kScaleMax) << 23);
-        const float k1 = __uint_as_float(min((tile.scale[1] >> (8 * c)) & 255u, kScaleMax) << 23);
         // the products are exact, so a fused multiply-add rounds like the sum alone
-        s[0] = fmaf((float)d[0] * k0, fq[c].x, c ? s[0] : 0.f);
-        s[1] = fmaf((float)d[1] * k0, fq[c].y, c ? s[1] : 0.f);
-        s[2] = fmaf((float)d[2] * k1, fq[c].x, c ? s[2] : 0.f);
-        s[3] = fmaf((float)d[3] * k1, fq[c].y, c ? s[3] : 0.f);
+        v[0] = fmaf((float)d[0] * k0[c], fq[c].x, c ? v[0] : 0.f);
+        v[1] = fmaf((float)d[1] * k0[c], fq[c].y, c ? v[1] : 0.f);
+        v[2] = fmaf((float)d[2] * k1[c], fq[c].x, c ? v[2] : 0.f);
+        v[3] = fmaf((float)d[3] * k1[c], fq[c].y, c ? v[3] : 0.f);
     }
+}
+// The largest over a row's heads; lanes 4 i and 4 i + 1 return those of rows i and i + 8.
+template <int D>
+__device__ __forceinline__ float score_tile(const Tile<D>& tile, const uint4 (&qf)[D / 32], const float2 (&fq)[D / 32], int G) {
+    const int l4 = threadIdx.x & 3;
+    float k0[D / 32], k1[D / 32], s[4];
+    tile_scales<D>(tile, k0, k1);
+    score_columns<D>(tile, k0, k1, qf, fq, s);
     const bool h0 = 2 * l4 < G, h1 = 2 * l4 + 1 < G;
     float m0 = fmaxf(h0 ? s[0] : -INFINITY, h1 ? s[1] : -INFINITY);
     float m1 = fmaxf(h0 ? s[2] : -INFINITY, h1 ? s[3] : -INFINITY);
@@ -220,14 +234,14 @@ __device__ __forceinline__ float score_tile(const Tile<D>& tile, const uint4 (&q
     return l4 ? m1 : m0;
 }
 // The list of a row that sees n pages of which nothing has to be chosen: all of them, or the first and the last ones.
-__device__ __forceinline__ void list_without_choice(const SelectParams& p, long long item, int n, int threads) {
+__device__ __forceinline__ void list_without_choice(const SelectParams& p, long long item, int n, int tid, int threads) {
     int32_t* list = p.list + item * p.top;
-    for (int i = threadIdx.x; i < p.top; i += threads) {
+    for (int i = tid; i < p.top; i += threads) {
         int v = i < n ? i : -1;
         if (n > p.top && i >= p.sink) v = n - p.top + i;
         list[i] = v;
     }
-    if (threadIdx.x == 0) p.count[item] = min(n, p.top);
+    if (tid == 0) p.count[item] = min(n, p.top);
 }
 // What is listed in any case of a row that sees n > top pages, by one warp.
 __device__ __forceinline__ void list_forced(const SelectParams& p, long long item, int n) {
@@ -240,25 +254,26 @@ __device__ __forceinline__ void list_forced(const SelectParams& p, long long ite
 
 // Keeps the `keep` best of a row's `cand` candidates and writes them to list[sink ..], ascending.  This CTA (of S in the
 // cluster) holds the scores of [c0, c1); low and high are the extremes of what the thread has seen of them.  `share`: the most
-// tiles that a CTA holds.  The histogram and the member count are zero on entry.
-template <int W>
-__device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* scores, int S, int rank, int cand, int c0, int c1, int share,
+// tiles that a CTA holds.  The histogram and the member count are zero on entry.  `warps` neighbouring warps work on it (this
+// thread is number tid of theirs), which meet at hardware barrier `barrier`.
+template <int W, int CL>
+__device__ __forceinline__ void select_pages(SelectShared<W, CL>& sh, int tid, int warps, int barrier, const float* scores, int S, int rank, int cand, int c0, int c1, int share,
                                              float low, float high, int keep, int sink, int32_t* list) {
-    constexpr int kThreads = W * 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int threads = warps * 32, lane = tid & 31, warp = tid >> 5;
     const unsigned below = (1u << lane) - 1u;
     // ---- division.  What the CTAs tell one another goes through shared memory that is written before a barrier and read after.
+    auto sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory"); };
     auto sync_all = [&]() {
-        if (S > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();
+        if (CL > 1 && S > 1) { cluster_arrive(); cluster_wait(); } else sync();
     };
     auto bits_of = [](float s) -> uint32_t { const uint32_t u = __float_as_uint(s + 0.f); return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u); };
     auto score_of = [](uint32_t u) -> float { return __uint_as_float(u ^ ((u >> 31) ? 0x80000000u : 0xffffffffu)); };
     uint32_t lo = __reduce_min_sync(0xffffffffu, bits_of(low)), hi = __reduce_max_sync(0xffffffffu, bits_of(high));
     if (lane == 0) sh.range[warp] = make_uint2(lo, hi);
-    __syncthreads();
-    uint2 r = sh.range[lane % W];
+    sync();
+    uint2 r = sh.range[lane < warps ? lane : 0];
     lo = __reduce_min_sync(0xffffffffu, r.x); hi = __reduce_max_sync(0xffffffffu, r.y);
-    if (S > 1) {
+    if (CL > 1 && S > 1) {
         if (warp == 0 && lane < S) st_cluster_v2(cluster_map_shared(smem_u32(&sh.all_range[rank]), (uint32_t)lane), lo, hi);
         sync_all();
         r = sh.all_range[lane % S];
@@ -269,7 +284,7 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     const float per = 256.f / fmaxf(high - low, 1e-30f), shift_by = -low * per;
     auto interval = [&](float s) -> int { return max(0, min(255, (int)fmaf(s, per, shift_by))); };
     // f(candidate, its score, whether there is one) over the warp's run of the CTA's candidates, all lanes together
-    const int steps = (share * kSelTile + kThreads - 1) / kThreads;
+    const int steps = (share * kSelTile + threads - 1) / threads;
     const int j0 = c0 + warp * steps * 32 + lane, j1 = min(c1, c0 + (warp + 1) * steps * 32);
     auto each = [&](auto f) {
 #pragma unroll 2
@@ -283,18 +298,18 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     int need = keep, bin = 0, inside = 0;
     auto divide = [&]() {
         sync_all();                                                // the histograms are complete
-        if (S > 1) {
-            for (int i = tid; i < 256; i += kThreads) {
-                uint32_t v[kSelMaxCluster], sum = 0;
+        if (CL > 1 && S > 1) {
+            for (int i = tid; i < 256; i += threads) {
+                uint32_t v[CL], sum = 0;
 #pragma unroll
-                for (int s = 0; s < kSelMaxCluster; ++s) v[s] = ld_cluster_u32(cluster_map_shared(smem_u32(&sh.hist[i]), (uint32_t)(s < S ? s : 0)));
+                for (int s = 0; s < CL; ++s) v[s] = ld_cluster_u32(cluster_map_shared(smem_u32(&sh.hist[i]), (uint32_t)(s < S ? s : 0)));
 #pragma unroll
-                for (int s = 0; s < kSelMaxCluster; ++s) sum += s < S ? v[s] : 0u;
+                for (int s = 0; s < CL; ++s) sum += s < S ? v[s] : 0u;
                 sh.sum[i] = (int)sum;
             }
-            __syncthreads();
+            sync();
         }
-        const int* h = S > 1 ? sh.sum : sh.hist;
+        const int* h = CL > 1 && S > 1 ? sh.sum : sh.hist;
         const int4 a = *reinterpret_cast<const int4*>(h + 248 - 8 * lane), b = *reinterpret_cast<const int4*>(h + 252 - 8 * lane);
         const int sum = a.x + a.y + a.z + a.w + b.x + b.y + b.z + b.w;
         int incl = sum;
@@ -323,8 +338,8 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     };
     while (inside > kSelRank && inside > need) {
         sync_all();                                                // everybody has read the histograms
-        for (int i = tid; i < 256; i += kThreads) sh.hist[i] = 0;
-        __syncthreads();
+        for (int i = tid; i < 256; i += threads) sh.hist[i] = 0;
+        sync();
         const int shift = max(0, 24 - __clz(hi - lo));
         each([&](int j, float s, bool in) { if (in && member(j, s)) atomicAdd(&sh.hist[(value(j, s) - lo) >> shift], 1); });
         divide();
@@ -348,30 +363,30 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
         each([&](int j, float s, bool in) {
             if (in && member(j, s)) {
                 const int i = atomicAdd(&sh.members, 1);
-                if (S == 1) sh.member[0][i] = make_uint2(__float_as_uint(s), (uint32_t)j);       // (cluster or not: this CTA's)
+                if (CL == 1 || S == 1) sh.member[0][i] = make_uint2(__float_as_uint(s), (uint32_t)j);       // (cluster or not: this CTA's)
                 else for (int c = 0; c < S; ++c)
                     st_cluster_v2(cluster_map_shared(smem_u32(&sh.member[rank][i]), (uint32_t)c), __float_as_uint(s), (uint32_t)j);
             }
         });
-        __syncthreads();
-        if (S > 1) {
+        sync();
+        if (CL > 1 && S > 1) {
             if (tid < S) st_cluster_u32(cluster_map_shared(smem_u32(&sh.all_members[rank]), (uint32_t)tid), (uint32_t)sh.members);
             sync_all();
             const int m = lane < S ? sh.all_members[lane] : 0;
             int end = m;
 #pragma unroll
-            for (int off = 1; off < kSelMaxCluster; off <<= 1) {
+            for (int off = 1; off < CL; off <<= 1) {
                 const int v = __shfl_up_sync(0xffffffffu, end, off);
                 if (lane >= off) end += v;
             }
-            // warp w packs the lists of CTAs w, w + W, ...
-            for (int c = warp; c < S; c += W) {
+            // the warps pack the CTAs' lists in turn
+            for (int c = warp; c < S; c += warps) {
                 const int mc = __shfl_sync(0xffffffffu, m, c), to = __shfl_sync(0xffffffffu, end, c) - mc;
                 for (int i = lane; i < mc; i += 32) sh.rank[to + i] = sh.member[c][i];
             }
-            __syncthreads();
+            sync();
         }
-        const uint2* members = S > 1 ? sh.rank : sh.member[0];
+        const uint2* members = CL > 1 && S > 1 ? sh.rank : sh.member[0];
         if (tid < inside) {
             const float s = __uint_as_float(members[tid].x);
             const uint32_t j = members[tid].y;
@@ -383,7 +398,7 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
             }
             if (before == need - 1) { sh.last_score = s; sh.last_page = (int)j; }
         }
-        __syncthreads();
+        sync();
         last = bits_of(sh.last_score);
         last_page = sh.last_page;
     }
@@ -398,10 +413,10 @@ __device__ __forceinline__ void select_pages(SelectShared<W>& sh, const float* s
     each([&](int j, float s, bool in) { kept += in && keeps(j, s); });
     kept = __reduce_add_sync(0xffffffffu, kept);
     if (lane == 0) sh.kept[warp] = kept;
-    __syncthreads();
-    const int k = lane < W ? sh.kept[lane] : 0;
+    sync();
+    const int k = lane < warps ? sh.kept[lane] : 0;
     int base = __reduce_add_sync(0xffffffffu, lane < warp ? k : 0);
-    if (S > 1) {
+    if (CL > 1 && S > 1) {
         const uint32_t all = (uint32_t)__reduce_add_sync(0xffffffffu, k);
         if (tid < S) st_cluster_u32(cluster_map_shared(smem_u32(&sh.all_kept[rank]), (uint32_t)tid), all);
         sync_all();                                                // behind it nobody reads another CTA's shared memory
@@ -422,7 +437,9 @@ __global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const Selec
     constexpr int kThreads = W * 32;
     extern __shared__ __align__(16) uint8_t smem_raw[];
     float* scores = reinterpret_cast<float*>(smem_raw);            // of this CTA's candidates
-    __shared__ SelectShared<W> sh;
+    __shared__ SelectShared<W, kSelMaxCluster> sh;
+    __shared__ uint4 s_q[kBlocks][32];                            // quantised queries as the lanes' B operands: two words of positive parts, two of negative
+    __shared__ float s_f[kBlocks][8];                             // 2^f per block and head
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int S = p.cluster, rank = (int)(blockIdx.x % S);
     const long long item = blockIdx.x / S;
@@ -455,13 +472,13 @@ __global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const Selec
     const int cand = n - p.sink - p.window;                       // scored pages
     if (n <= p.top || keep == 0) {                                // nothing to choose (the same for the whole cluster)
         if (S > 1) cluster_wait();
-        if (rank == 0 && !at.padding) list_without_choice(p, item, n, kThreads);
+        if (rank == 0 && !at.padding) list_without_choice(p, item, n, tid, kThreads);
         return;
     }
     if (quantises) {
         float f;
-        quantise_block(qx, lane, sh.q[warp][lane], f);
-        if (l4 == 0) sh.f[warp][hl] = f;
+        quantise_block(qx, lane, s_q[warp][lane], f);
+        if (l4 == 0) s_f[warp][hl] = f;
     }
     if (rank == 0 && warp == W - 1) list_forced(p, item, n);
     __syncthreads();
@@ -469,8 +486,8 @@ __global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const Selec
     float2 fq[kBlocks];                                           // of this lane's two accumulator columns
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
-        qf[c] = sh.q[c][lane];
-        fq[c] = *reinterpret_cast<const float2*>(&sh.f[c][2 * l4]);
+        qf[c] = s_q[c][lane];
+        fq[c] = *reinterpret_cast<const float2*>(&s_f[c][2 * l4]);
     }
     if (S > 1) cluster_wait();
     // ---- scores of this CTA's candidates [c0, c1)
@@ -500,110 +517,150 @@ __global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const Selec
             }
         }
     }
-    select_pages<W>(sh, scores, S, rank, cand, c0, c1, share, low, high, keep, p.sink, list);
+    select_pages(sh, tid, W, 0, scores, S, rank, cand, c0, c1, share, low, high, keep, p.sink, list);
 }
 
-// The same for several rows of one sequence (drafted tokens, a prompt chunk): a cluster of `group` CTAs per `group` neighbouring
-// rows and KV head.  Each CTA scores a share of the pages for all of the rows, so that a page's bounds are read once for them
-// -- read once per row they are what bounds the kernel above when rows are many: an SM takes some 32 bytes a cycle out of L2 --
-// and sends the scores to the CTA of the row, which then selects for its row alone.  Rows of different sequences in one group
-// (the host can only guess where sequences end) are scored by their own CTAs.
-constexpr int kRowsWorth = 1200;                    // rows x pages from which scoring them together pays
-template <int D, int W>
-__global__ void __launch_bounds__(W * 32, 24 / W) page_select_rows_kernel(const SelectParams p) {
-    constexpr int kBlocks = D / 32, kThreads = W * 32;
+// The same for several rows of one sequence (drafted tokens, a prompt chunk): a CTA, or a cluster of them, per group of `group`
+// neighbouring rows and KV head.  Every warp scores a share of the pages for all of the rows, so that a page's bounds are read once
+// for them -- read once per row they are what bounds the kernel above when rows are many: an SM takes some 32 bytes a cycle out of
+// L2 -- with the columns of the MMA filled by as many rows as their heads fit.  The scores go to the shared memory of the CTA that
+// selects for the row, WR warps for each of its W / WR rows.  Rows of different sequences in one group (the host can only guess
+// where sequences end) are scored one after another by their own CTAs.
+template <int D, int W, int O>                      // W warps, O CTAs per SM
+__global__ void __launch_bounds__(W * 32, O) page_select_rows_kernel(const SelectParams p) {
+    constexpr int kBlocks = D / 32, kSlots = kSelMaxCluster;
     extern __shared__ __align__(16) uint8_t smem_raw[];
-    const int R = p.cluster;
-    uint4* queries = reinterpret_cast<uint4*>(smem_raw);                          // [R][kBlocks][32]
-    float* factors = reinterpret_cast<float*>(queries + R * kBlocks * 32);        // [R][kBlocks][8]
-    float* scores = factors + R * kBlocks * 8;                                    // of this CTA's row
-    __shared__ SelectShared<W> sh;
+    const int R = p.group, C = p.cluster;                                         // CTA i has rows i, i + C, ...
+    const int per = 8 / p.G, all_sets = (R + per - 1) / per;                      // rows that fill the MMA's 8 columns; sets of them
+    uint4* queries = reinterpret_cast<uint4*>(smem_raw);                          // [set][kBlocks][32]
+    float* factors = reinterpret_cast<float*>(queries + all_sets * kBlocks * 32); // [set][kBlocks][8]
+    float* scores = factors + all_sets * kBlocks * 8;                             // [slot][stride]
+    __shared__ SelectShared<W, 1> sh[kSlots];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int hl = lane >> 2, l4 = lane & 3;
-    const int rank = (int)(blockIdx.x % R), g = (int)(blockIdx.x / R % p.Hkv), row0 = (int)(blockIdx.x / R / p.Hkv) * R;
-    const int nrows = min(R, p.rows - row0), row = row0 + rank;
-    cluster_arrive();
-    for (int i = tid; i < 256; i += kThreads) sh.hist[i] = 0;
-    if (tid == 0) sh.members = 0;
+    const int rank = (int)(blockIdx.x % C), g = (int)(blockIdx.x / C % p.Hkv), row0 = (int)(blockIdx.x / C / p.Hkv) * R;
+    const int nrows = min(R, p.rows - row0);
+    const int WR = 1 << p.row_warps, row_threads = WR * 32;
+    const int slot = warp >> p.row_warps, my_row = rank + slot * C, t_row = tid & (row_threads - 1);              // what this warp selects for
+    if (C > 1) cluster_arrive();
+    if (slot < kSlots) {
+        for (int i = t_row; i < 256; i += row_threads) sh[slot].hist[i] = 0;
+        if (t_row == 0) sh[slot].members = 0;
+    }
     pdl_launch_dependents();
     pdl_wait();
-    // A warp quantises up to four (row, block) pairs of the group's queries; they are loaded before it is known which are needed.
+    // A warp quantises up to kPairs (set, block) pairs of the group's queries; they are loaded before it is known which are needed.
     constexpr int kPairs = kSelMaxCluster * kBlocks / W;
     uint4 qx[kPairs];
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
-        const int i = warp + k * W, r = i / kBlocks;
+        const int i = warp + k * W, r = i / kBlocks * per + hl / p.G;
         qx[k] = make_uint4(0, 0, 0, 0);
-        if (r < nrows && hl < p.G)
-            qx[k] = fetch(reinterpret_cast<const uint4*>(p.q + ((size_t)(row0 + r) * p.Hq + (size_t)g * p.G + hl) * D) + (i % kBlocks) * 4 + l4);
+        if (r < nrows)
+            qx[k] = fetch(reinterpret_cast<const uint4*>(p.q + ((size_t)(row0 + r) * p.Hq + (size_t)g * p.G + hl % p.G) * D) + (i % kBlocks) * 4 + l4);
     }
     const RowSeq first = locate_row(row0, p.q_offsets, p.batch);
     const bool shared = !first.padding && first.back >= nrows - 1;                // all rows of the group in one sequence
-    RowSeq at = first, last = first;
-    last.back -= nrows - 1;
-    if (shared) at.back = first.back - rank;
-    else if (rank < nrows) at = locate_row(row, p.q_offsets, p.batch);
-    const int len = fetch(p.seq_lens + at.b);
-    const bool mine = rank < nrows && !at.padding;                                // this CTA has a row
-    const int pos = mine ? row_position(at, len, p.max_pages) : -1, n = pos >= 0 ? pos / kPageTokens + 1 : 0;
-    if (mine && pos < 0 && tid == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    const int first_len = fetch(p.seq_lens + first.b);
     const int keep = p.top - p.sink - p.window, forced = p.sink + p.window;
-    // pages to score: of the group, as its last row sees them, or of this CTA's row
-    const int n_all = shared ? max(0, row_position(last, len, p.max_pages)) / kPageTokens + 1 : n;
-    const int cand = n_all > p.top && keep > 0 ? n_all - forced : 0;
-    const int ra = shared ? 0 : rank, rb = shared ? nrows : rank + 1;
-    const int t0 = shared ? rank * W + warp : warp, stride = shared ? R * W : W;
-    const int tiles = (cand + kSelTile - 1) / kSelTile;
-    const int32_t* table = p.page_table + (size_t)at.b * p.max_pages;
-    auto page_ids = [&](int t) -> int {
-        const long long j = p.sink + (long long)t * kSelTile + (lane & 15);
-        return fetch(table + min(j, (long long)p.max_pages - 1));
+    auto visible = [&](const RowSeq& at, int len) -> int {                        // pages a row sees
+        const int pos = row_position(at, len, p.max_pages);
+        return pos >= 0 ? pos / kPageTokens + 1 : 0;
     };
-    int ids = page_ids(t0);
-    if (cand > 0) {
+    const uint32_t scores_addr = smem_u32(scores);
+    // Scores of the first `cand` candidates of a sequence, tiles from t on, for the rows [ra, rb) of the group.
+    auto score = [&](int b, int cand, int ra, int rb, int t, int step) {
+        const int32_t* table = p.page_table + (size_t)b * p.max_pages;
+        auto page_ids = [&](int t) -> int {
+            const long long j = p.sink + (long long)t * kSelTile + (lane & 15);
+            return fetch(table + min(j, (long long)p.max_pages - 1));
+        };
+        const int tiles = (cand + kSelTile - 1) / kSelTile;
+        int ids = t < tiles ? page_ids(t) : 0;
+        for (; t < tiles; t += step) {
+            Tile<D> tile;
+            load_tile<D>(tile, p, g, ids, 0, t * kSelTile, cand);
+            if (t + step < tiles) ids = page_ids(t + step);
+            const int j0 = t * kSelTile + hl;
+            float k0[kBlocks], k1[kBlocks];
+            tile_scales<D>(tile, k0, k1);
+            for (int s = ra / per; s * per < rb; ++s) {
+                float v[4];                                                       // (page, column): (hl, 2 l4), (hl, 2 l4 + 1), (hl + 8, ..)
+                uint4 qf[kBlocks];
+                float2 fq[kBlocks];
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) {
-            const int i = warp + k * W;
-            if (i < R * kBlocks) {
-                float f;
-                quantise_block(qx[k], lane, queries[i * 32 + lane], f);
-                if (l4 == 0) factors[i * 8 + hl] = f;
+                for (int c = 0; c < kBlocks; ++c) {
+                    qf[c] = queries[(s * kBlocks + c) * 32 + lane];
+                    fq[c] = *reinterpret_cast<const float2*>(factors + (s * kBlocks + c) * 8 + 2 * l4);
+                }
+                score_columns<D>(tile, k0, k1, qf, fq, v);
+                auto put = [&](int r, int j, float s) {
+                    if (r < ra || r >= rb || j >= cand) return;
+                    if (C == 1) scores[r * p.stride + j] = s;
+                    else st_cluster_u32(cluster_map_shared(scores_addr + (uint32_t)(r / C * p.stride + j) * 4, (uint32_t)(r % C)), __float_as_uint(s));
+                };
+                if (p.G == 1) {
+                    const int r = s * per + 2 * l4;
+                    put(r, j0, v[0]); put(r + 1, j0, v[1]); put(r, j0 + 8, v[2]); put(r + 1, j0 + 8, v[3]);
+                } else {
+                    float m0 = fmaxf(v[0], v[1]), m1 = fmaxf(v[2], v[3]);
+                    if (p.G == 2) { put(s * per + l4, j0, m0); put(s * per + l4, j0 + 8, m1); }
+                    else {
+                        m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 1));
+                        m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 1));
+                        if (p.G == 8) {
+                            m0 = fmaxf(m0, __shfl_xor_sync(0xffffffffu, m0, 2));
+                            m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, 2));
+                        }
+                        // lanes 0 and 1 of a row's two or four store
+                        if (p.G == 4 || l4 < 2) put(s * per + (p.G == 4 ? l4 >> 1 : 0), j0 + 8 * (l4 & 1), l4 & 1 ? m1 : m0);
+                    }
+                }
             }
+        }
+    };
+    RowSeq last = first;
+    last.back -= nrows - 1;
+    const int n_all = shared ? visible(last, first_len) : 0;                      // pages that the group's last row sees
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+        const int i = warp + k * W;
+        if (i < all_sets * kBlocks) {
+            float f;
+            quantise_block(qx[k], lane, queries[i * 32 + lane], f);
+            if (l4 == 0) factors[i * 8 + hl] = f;
         }
     }
     __syncthreads();
-    cluster_wait();                                                               // the group's CTAs have started
-    const uint32_t scores_addr = smem_u32(scores);
-    for (int t = t0; t < tiles; t += stride) {
-        Tile<D> tile;
-        load_tile<D>(tile, p, g, ids, 0, t * kSelTile, cand);
-        if (t + stride < tiles) ids = page_ids(t + stride);
-        const int j = t * kSelTile + hl + 8 * l4;
-        for (int r = ra; r < rb; ++r) {
-            uint4 qf[kBlocks];
-            float2 fq[kBlocks];
-#pragma unroll
-            for (int c = 0; c < kBlocks; ++c) {
-                qf[c] = queries[(r * kBlocks + c) * 32 + lane];
-                fq[c] = *reinterpret_cast<const float2*>(factors + (r * kBlocks + c) * 8 + 2 * l4);
-            }
-            const float v = score_tile<D>(tile, qf, fq, p.G);
-            if (l4 < 2 && j < cand) st_cluster_u32(cluster_map_shared(scores_addr + (uint32_t)j * 4, (uint32_t)r), __float_as_uint(v));
+    if (C > 1) cluster_wait();                                                    // the group's CTAs have started
+    RowSeq at = first;
+    int len = first_len;
+    if (shared) {
+        at.back = first.back - my_row;
+        if (n_all > p.top && keep > 0) score(first.b, n_all - forced, 0, nrows, rank * W + warp, C * W);
+    } else {
+        for (int r = rank; r < nrows; r += C) {
+            const RowSeq here = locate_row(row0 + r, p.q_offsets, p.batch);
+            const int here_len = fetch(p.seq_lens + here.b), n = visible(here, here_len);
+            if (r == my_row) { at = here; len = here_len; }
+            if (n > p.top && keep > 0) score(here.b, n - forced, r, r + 1, warp, W);
         }
     }
-    cluster_arrive();
-    cluster_wait();                                                               // behind it nobody writes another CTA's shared memory
-    if (!mine) return;
-    const long long item = (long long)row * p.Hkv + g;
+    if (C > 1) { cluster_arrive(); cluster_wait(); } else __syncthreads();        // behind it nobody writes another CTA's shared memory
+    if (my_row >= nrows || at.padding) return;
+    const int n = visible(at, len);
+    if (n == 0 && t_row == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+    const long long item = (long long)(row0 + my_row) * p.Hkv + g;
     if (n <= p.top || keep == 0) {
-        list_without_choice(p, item, n, kThreads);
+        list_without_choice(p, item, n, t_row, row_threads);
         return;
     }
-    if (warp == W - 1) list_forced(p, item, n);
+    if (t_row < 32) list_forced(p, item, n);
     const int own = n - forced;                                                   // (an earlier row may see a page less)
+    const float* mine = scores + slot * p.stride;
     float low = INFINITY, high = -INFINITY;
-    for (int j = tid; j < own; j += kThreads) { low = fminf(low, scores[j]); high = fmaxf(high, scores[j]); }
-    select_pages<W>(sh, scores, 1, 0, own, 0, own, (own + kSelTile - 1) / kSelTile, low, high, keep, p.sink, p.list + item * p.top);
+    for (int j = t_row; j < own; j += row_threads) { low = fminf(low, mine[j]); high = fmaxf(high, mine[j]); }
+    select_pages(sh[slot], t_row, WR, 1 + slot, mine, 1, 0, own, 0, own, (own + kSelTile - 1) / kSelTile, low, high, keep, p.sink, p.list + item * p.top);
 }
 
 // ------------------------------------------------------------------------------------------ attention over listed pages
@@ -946,18 +1003,39 @@ typedef void (*SelectKernel)(const SelectParams);
 static const SelectKernel kSelectKernels[2][3] = {
     {page_select_kernel<64, 4>, page_select_kernel<64, 8>, page_select_kernel<64, 16>},
     {page_select_kernel<128, 4>, page_select_kernel<128, 8>, page_select_kernel<128, 16>}};
-static const SelectKernel kSelectRowsKernels[2][2] = {{page_select_rows_kernel<64, 4>, page_select_rows_kernel<64, 8>},
-                                                      {page_select_rows_kernel<128, 4>, page_select_rows_kernel<128, 8>}};
+static const SelectKernel kSelectRowsKernels[2][4] = {
+    {page_select_rows_kernel<64, 16, 1>, page_select_rows_kernel<64, 8, 2>, page_select_rows_kernel<64, 8, 3>, page_select_rows_kernel<64, 8, 4>},
+    {page_select_rows_kernel<128, 16, 1>, page_select_rows_kernel<128, 8, 2>, page_select_rows_kernel<128, 8, 3>, page_select_rows_kernel<128, 8, 4>}};
 
-// Raises the kernels' shared-memory limits on the current device.
+// Clusters of `cluster` CTAs that the current device holds at once.
+template <typename P>
+cudaError_t clusters_at_once(void (*kernel)(const P), int threads, size_t smem, int cluster, int* n) {
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)cluster);
+    lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    return cudaOccupancyMaxActiveClusters(n, kernel, &lc);
+}
+
+// Raises the kernels' shared-memory limits on the current device, and asks for the clusters that it holds.
 static aflex_status select_attributes(aflex_ctx* ctx, int di) {
     cudaError_t e = cudaSuccess;
     for (int w = 0; w < 3 && e == cudaSuccess; ++w)
         e = cudaFuncSetAttribute(kSelectKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (kSelCap + 4) * (int)sizeof(float));
-    // (a group's queries and scores: 8 * 4 * (512 + 32) bytes and 4 per page)
-    for (int w = 0; w < 2 && e == cudaSuccess; ++w)
-        e = cudaFuncSetAttribute(kSelectRowsKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * 4 * 544 + kSelCap * (int)sizeof(float));
-    return check_cuda(ctx, e, "cudaFuncSetAttribute(page select)");
+    for (int w = 0; w < 4 && e == cudaSuccess; ++w)
+        e = cudaFuncSetAttribute(kSelectRowsKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelRowsSmem);
+    for (int c = 2; c <= kSelMaxCluster && e == cudaSuccess; ++c) {
+        e = clusters_at_once(kSelectRowsKernels[di][0], 512, kSelRowsSmem, c, &ctx->select_clusters[di][0][c]);
+        if (e == cudaSuccess) e = clusters_at_once(kSelectRowsKernels[di][2], 256, 48 * 1024, c, &ctx->select_clusters[di][1][c]);
+    }
+    return check_cuda(ctx, e, "page select: kernel attributes");
 }
 
 aflex_status page_select_supported(aflex_ctx* ctx, const aflex_kv* kv) {
@@ -987,23 +1065,42 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
         if (s != AFLEX_OK) return s;
         ctx->select_attr_set[di] = true;
     }
-    // Rows that share their sequence go in groups, if there are enough of them to fill the GPU one CTA each: as many as a
-    // sequence has (up to 8, a divisor of more), four where the sequences' numbers of rows differ.  It pays by the rows and the
-    // length; alone against grouped, 32 query on 8 KV heads, 128 / 256 / 512 pages: 16 x 5 rows 11.0 / 15.2 / 22.5 against 10.5 /
-    // 11.2 / 15.4 us, 32 x 4 rows 11.8 / 16.5 / 27.4 against 15.8 / 16.8 / 25.1, 40 x 3 rows 12.0 / 17.2 / 27.8 against 14.6 / 18.9 / 26.8
-    // (4 warps per CTA; with 8, 640 CTAs do not fit at once: 18.6 for the 15.4, but 336 CTAs of 2000 pages take 23 us instead of 37).
-    if (q_offsets != nullptr && rows >= 2LL * batch && items > ctx->num_sms && p.max_pages <= kSelCap) {
+    // Rows that share their sequence go in groups: as many as a sequence has (up to 8, a divisor of more), four where the
+    // sequences' numbers of rows differ.  A group gets one CTA; more of them, as long as all clusters fit at once, where each
+    // still has eight tiles of pages, or where the scores need the room.  Warps per CTA and CTAs per SM: the fewest of the latter (with
+    // the most registers) that hold all CTAs at once; for long rows three CTAs of 8 warps where those are more warps (clusters of 3, 5,
+    // 6 and 7 pay from 2048 pages: 128 groups 57 instead of 66 us at 4096, 14.1 instead of 11.2 at 512).  Alone against grouped, 32 query
+    // on 8 KV heads: 16 x 5 rows of 128 / 256 / 512 pages 11.0 / 15.2 / 22.5 against 6.5 / 7.9 / 11.2 us, 32 x 4 rows 11.8 / 16.5 / 27.4
+    // against 7.1 / 9.4 / 17.1, 64 x 5 rows of 64 / 256 / 1024 pages 26 / 43 / 100 against 9.6 / 21 / 60, 1 x 8 rows of 1024 / 4096 pages 9.0 /
+    // 15.8 against 8.4 / 13.1.
+    if (q_offsets != nullptr && rows >= 2LL * batch) {
         const int each = rows % batch == 0 ? rows / batch : 4;
         int R = each <= 8 ? each : 4;
         for (int r = 8; r >= 2 && each > 8; --r) if (each % r == 0) { R = r; break; }
-        if ((long long)R * p.max_pages >= kRowsWorth) {
-            const long long ctas = ((long long)rows + R - 1) / R * p.Hkv * R;
-            if (ctas > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
-            p.cluster = R;
-            const size_t smem = (size_t)R * (d->head_dim / 32) * (32 * sizeof(uint4) + 8 * sizeof(float)) + (size_t)p.max_pages * sizeof(float);
+        const long long groups = ((long long)rows + R - 1) / R * p.Hkv;
+        const int per = 8 / p.G, sets = (R + per - 1) / per;
+        p.group = R;
+        p.stride = (p.max_pages + 3) / 4 * 4;
+        auto smem_of = [&](int C) -> size_t {
+            return (size_t)sets * (d->head_dim / 32) * (32 * sizeof(uint4) + 8 * sizeof(float)) + (size_t)((R + C - 1) / C) * p.stride * sizeof(float);
+        };
+        int C = 1, form = 0;
+        while (C < kSelMaxCluster && ((groups <= ctx->select_clusters[di][0][2 * C] && p.max_pages >= 2 * C * 8 * kSelTile) || smem_of(C) > kSelRowsSmem)) C *= 2;
+        if (C == 1 && groups > ctx->num_sms) form = groups <= 2 * ctx->num_sms ? 1 : groups <= 3 * ctx->num_sms ? 2 : 3;
+        if (p.max_pages >= 32 * kSelTile) {                         // three CTAs of 8 warps per SM where those are more warps
+            int more = 1;
+            for (int c = 2; c <= kSelMaxCluster; c = p.max_pages >= 128 * kSelTile ? c + 1 : 2 * c) if (groups <= ctx->select_clusters[di][1][c]) more = c;
+            if (more > 1 && more * 8 > C * (form ? 8 : 16)) { C = more; form = 2; }
+        }
+        // (few groups of short rows: a CTA per row and head is quicker)
+        if (smem_of(C) <= kSelRowsSmem && (groups * 3 >= ctx->num_sms || p.max_pages >= 16 * kSelTile)) {
+            if (groups * C > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
+            const int W = form == 0 ? 16 : 8, slots = (R + C - 1) / C, most = p.max_pages >= 16 * kSelTile ? W : 4;
+            p.cluster = C;
+            p.row_warps = 0;
+            while ((2 << p.row_warps) <= most && (slots << (p.row_warps + 1)) <= W) ++p.row_warps;
             KernelScope scope(ctx, kKPageSelect, st);
-            const bool wide = ctas <= 3 * ctx->num_sms;             // 8 warps per CTA while an SM's three places hold all of them
-            return check_cuda(ctx, launch_cluster(kSelectRowsKernels[di][wide], ctas, wide ? 256 : 128, smem, R, st, p), "page_select_rows_kernel launch");
+            return check_cuda(ctx, launch_cluster(kSelectRowsKernels[di][form], groups * C, W * 32, smem_of(C), C, st, p), "page_select_rows_kernel launch");
         }
     }
     // A cluster per (row, KV head) where those are fewer than the SMs (and where the scores need the room), each CTA at least
@@ -1041,20 +1138,7 @@ aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, 
     int* fit = ctx->pages_clusters[wide];          // clusters of 2, 3 .. 8 CTAs that the GPU holds at once
     if (!ctx->pages_attr_set[wide]) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        for (int s = 2; s <= kPagesMaxCluster && e == cudaSuccess; ++s) {
-            cudaLaunchConfig_t lc = {};
-            lc.gridDim = dim3((unsigned)s);
-            lc.blockDim = dim3(kPagesThreads);
-            lc.dynamicSmemBytes = smem;
-            cudaLaunchAttribute attr[1];
-            attr[0].id = cudaLaunchAttributeClusterDimension;
-            attr[0].val.clusterDim.x = (unsigned)s;
-            attr[0].val.clusterDim.y = 1;
-            attr[0].val.clusterDim.z = 1;
-            lc.attrs = attr;
-            lc.numAttrs = 1;
-            e = cudaOccupancyMaxActiveClusters(&fit[s], kernel, &lc);
-        }
+        for (int s = 2; s <= kPagesMaxCluster && e == cudaSuccess; ++s) e = clusters_at_once(kernel, kPagesThreads, smem, s, &fit[s]);
         if (e != cudaSuccess) return check_cuda(ctx, e, "attention over pages: kernel attributes");
         ctx->pages_attr_set[wide] = true;
     }

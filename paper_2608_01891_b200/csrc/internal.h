@@ -60,6 +60,7 @@ struct aflex_ctx {
     bool attn_attr_set[2] = {false, false};
     bool prefill_attr_set[2] = {false, false};   // shared-memory limit raised for attn_prefill_kernel<64 / 128> on this device
     bool select_attr_set[2] = {false, false};    // ... for page_select_kernel<64 / 128>
+    int select_clusters[2][2][9] = {};           // clusters of 2 .. 8 CTAs of page_select_rows_kernel (16 warps, 8 warps) that fit it at once
     bool bounds_attr_set[2] = {false, false};    // ... for page_bounds_kernel<64 / 128>
     bool pages_attr_set[2] = {false, false};     // ... for attn_decode_pages_kernel<64 / 128>
     int pages_clusters[2][9] = {};               // its clusters of 2 .. 8 CTAs that fit this device at once
