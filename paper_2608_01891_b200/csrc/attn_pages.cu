@@ -104,7 +104,6 @@ constexpr uint32_t kScaleMax = 127 + 50;            // largest exponent of the b
 constexpr int kSelCap = 48 * 1024;                  // scores one CTA's shared memory holds
 constexpr int kSelMaxCluster = 8;
 constexpr size_t kSelRowsSmem = 190 * 1024;         // most dynamic shared memory of page_select_rows_kernel
-constexpr int kSelTiles = 2;                        // tiles a warp has in flight (the lanes hold two tiles' page ids)
 constexpr int kSelRank = 64;                        // members of an interval that are ranked by comparing all pairs
 
 struct SelectParams {
@@ -431,10 +430,11 @@ __device__ __forceinline__ void select_pages(SelectShared<W, CL>& sh, int tid, i
     });
 }
 
-template <int D, int W>                             // W warps
-__global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const SelectParams p) {
+template <int D, int W, int O>                      // W warps, O CTAs per SM
+__global__ void __launch_bounds__(W * 32, O) page_select_kernel(const SelectParams p) {
     constexpr int kBlocks = D / 32;
     constexpr int kThreads = W * 32;
+    constexpr int kTiles = W * O <= 16 ? 2 : 1;                    // tiles a warp has in flight (the lanes hold two tiles' page ids)
     extern __shared__ __align__(16) uint8_t smem_raw[];
     float* scores = reinterpret_cast<float*>(smem_raw);            // of this CTA's candidates
     __shared__ SelectShared<W, kSelMaxCluster> sh;
@@ -500,14 +500,14 @@ __global__ void __launch_bounds__(W * 32, 16 / W) page_select_kernel(const Selec
         ids = page_ids(t);
     }
     while (t < t_end) {
-        Tile<D> tile[kSelTiles];
+        Tile<D> tile[kTiles];
 #pragma unroll
-        for (int k = 0; k < kSelTiles; ++k) load_tile<D>(tile[k], p, g, ids, k * 16, (t + k * W) * kSelTile, c1);
+        for (int k = 0; k < kTiles; ++k) load_tile<D>(tile[k], p, g, ids, k * 16, (t + k * W) * kSelTile, c1);
         const int t_now = t;
-        t += kSelTiles * W;
+        t += kTiles * W;
         if (t < t_end) ids = page_ids(t);
 #pragma unroll
-        for (int k = 0; k < kSelTiles; ++k) {
+        for (int k = 0; k < kTiles; ++k) {
             const float v = score_tile<D>(tile[k], qf, fq, p.G);
             const int j = (t_now + k * W) * kSelTile + hl + 8 * l4;
             if (l4 < 2 && j < c1) {
@@ -1000,9 +1000,10 @@ cudaError_t launch_cluster(void (*kernel)(const P), long long ctas, int threads,
 
 // ------------------------------------------------------------------------------------------ host
 typedef void (*SelectKernel)(const SelectParams);
-static const SelectKernel kSelectKernels[2][3] = {
-    {page_select_kernel<64, 4>, page_select_kernel<64, 8>, page_select_kernel<64, 16>},
-    {page_select_kernel<128, 4>, page_select_kernel<128, 8>, page_select_kernel<128, 16>}};
+static const SelectKernel kSelectKernels[2][5] = {
+    {page_select_kernel<64, 16, 1>, page_select_kernel<64, 8, 2>, page_select_kernel<64, 4, 4>, page_select_kernel<64, 4, 6>, page_select_kernel<64, 4, 8>},
+    {page_select_kernel<128, 16, 1>, page_select_kernel<128, 8, 2>, page_select_kernel<128, 4, 4>, page_select_kernel<128, 4, 6>,
+     page_select_kernel<128, 4, 8>}};
 static const SelectKernel kSelectRowsKernels[2][4] = {
     {page_select_rows_kernel<64, 16, 1>, page_select_rows_kernel<64, 8, 2>, page_select_rows_kernel<64, 8, 3>, page_select_rows_kernel<64, 8, 4>},
     {page_select_rows_kernel<128, 16, 1>, page_select_rows_kernel<128, 8, 2>, page_select_rows_kernel<128, 8, 3>, page_select_rows_kernel<128, 8, 4>}};
@@ -1027,7 +1028,7 @@ cudaError_t clusters_at_once(void (*kernel)(const P), int threads, size_t smem, 
 // Raises the kernels' shared-memory limits on the current device, and asks for the clusters that it holds.
 static aflex_status select_attributes(aflex_ctx* ctx, int di) {
     cudaError_t e = cudaSuccess;
-    for (int w = 0; w < 3 && e == cudaSuccess; ++w)
+    for (int w = 0; w < 5 && e == cudaSuccess; ++w)
         e = cudaFuncSetAttribute(kSelectKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (kSelCap + 4) * (int)sizeof(float));
     for (int w = 0; w < 4 && e == cudaSuccess; ++w)
         e = cudaFuncSetAttribute(kSelectRowsKernels[di][w], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSelRowsSmem);
@@ -1105,17 +1106,20 @@ aflex_status page_select_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const 
     }
     // A cluster per (row, KV head) where those are fewer than the SMs (and where the scores need the room), each CTA at least
     // eight tiles.  16 warps per CTA while an SM has no second one, 8 while two per SM hold all of them, else 4 (more CTAs at
-    // once, and a selection that fewer warps have to agree on).  8 x 8192 pages: 34.0 / 22.6 / 11.5 us with 1 / 2 / 8 CTAs of 16
-    // warps, 13.4 with 8 of 8; 192 x 256 pages: 6.0 and 7.8 us with 8 and 4 warps, 320 x 256: 10.8 and 8.5, 2048 x 256: 49 and 39.5.
+    // once, and a selection that fewer warps have to agree on) and as many CTAs per SM as hold all of them, with the registers that are
+    // left.  8 x 8192 pages: 34.0 / 22.6 / 11.5 us with 1 / 2 / 8 CTAs of 16 warps, 13.4 with 8 of 8; 192 x 256 pages: 6.0 and 7.8 us
+    // with 8 and 4 warps, 320 x 256: 10.8 and 8.5; 4 warps with 4 / 6 / 8 CTAs per SM: 512 x 256 pages 10.6 / 12.4 / 17.5, 640 x 256 17.1 /
+    // 13.4 / 18.0, 1024 x 64 10.7 / 9.6 / 7.8, 2560 x 64 28.9 / 19.5 / 21.4, 2560 x 256 50 / 42.5 / 50.
     int S = 1;
     while (S < kSelMaxCluster && (items * S < ctx->num_sms || p.max_pages > (long long)S * kSelCap) && p.max_pages > S * 8 * kSelTile) S *= 2;
-    const int form = items * S <= ctx->num_sms ? 2 : items * S <= 2 * ctx->num_sms ? 1 : 0;
+    const long long per_sm = (items * S + ctx->num_sms - 1) / ctx->num_sms;
+    const int form = per_sm <= 1 ? 0 : per_sm <= 2 ? 1 : per_sm <= 4 ? 2 : per_sm > 6 && per_sm <= 8 ? 4 : 3;
     const int share = ((p.max_pages + kSelTile - 1) / kSelTile + S - 1) / S * kSelTile;       // candidates per CTA at most
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "page select: rows * Hkv = %lld", items);
     p.cluster = S;
     const size_t smem = (size_t)(share + 4) * sizeof(float);
     KernelScope scope(ctx, kKPageSelect, st);
-    return check_cuda(ctx, launch_cluster(kSelectKernels[di][form], items * S, 128 << form, smem, S, st, p), "page_select_kernel launch");
+    return check_cuda(ctx, launch_cluster(kSelectKernels[di][form], items * S, form == 0 ? 512 : form == 1 ? 256 : 128, smem, S, st, p), "page_select_kernel launch");
 }
 
 aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv,
