@@ -700,8 +700,9 @@ struct PagesParams {
     int* status;
 };
 
-template <int D> struct PagesRing {
-    static constexpr int kStages = D == 128 ? 3 : 4;
+// O CTAs per SM: two (D = 64: three) with a deep ring, or one more with a ring of two.
+template <int D, int O> struct PagesRing {
+    static constexpr int kStages = D == 128 ? (O == 2 ? 3 : 2) : (O == 3 ? 4 : 2);
     static constexpr int kPageBytes = kPageTokens * D * 2;            // of K; as many of V
     static constexpr int kWarpBytes = kStages * 2 * kPageBytes;       // holds the warp's state (8 heads x D floats) at the end
     static constexpr int kBytes = kPagesWarps * kWarpBytes;
@@ -844,6 +845,7 @@ __device__ __forceinline__ void store_run(const PagesParams& p, int row, int g, 
 template <int D>
 __device__ __forceinline__ void copy_page(const PagesParams& p, size_t slab, int nv, uint32_t dst) {
     constexpr int kChunks = D / 8;                 // 16-byte chunks of a row
+    constexpr uint32_t kPageBytes = kPageTokens * D * 2;
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int k = 0; k < kPageTokens * kChunks / 32; ++k) {
@@ -851,13 +853,13 @@ __device__ __forceinline__ void copy_page(const PagesParams& p, size_t slab, int
         const uint32_t to = dst + (uint32_t)(r * (D * 2) + ((ch ^ swizzle(r)) << 4));
         // slots past the end may hold anything: K's scores are masked, V has to be zero
         copy16(to, p.k_cache + slab + c * 8, 16);
-        copy16(to + PagesRing<D>::kPageBytes, p.v_cache + slab + c * 8, r < nv ? 16 : 0);
+        copy16(to + kPageBytes, p.v_cache + slab + c * 8, r < nv ? 16 : 0);
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kPagesThreads) attn_decode_pages_kernel(const PagesParams p) {
-    typedef PagesRing<D> R;
+template <int D, int O>                             // O CTAs per SM
+__global__ void __launch_bounds__(kPagesThreads, O) attn_decode_pages_kernel(const PagesParams p) {
+    typedef PagesRing<D, O> R;
     constexpr int kSteps = D / 32;                 // 16-byte reads per lane and K row
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ PagesShared sh;
@@ -1137,12 +1139,15 @@ aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, 
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ctx->dev_status;
     const long long items = (long long)rows * p.Hkv;
     const bool wide = d->head_dim == 128;
-    void (*kernel)(const PagesParams) = wide ? attn_decode_pages_kernel<128> : attn_decode_pages_kernel<64>;
-    const int smem = wide ? PagesRing<128>::kBytes : PagesRing<64>::kBytes;
+    typedef void (*Kernel)(const PagesParams);
+    const Kernel kernels[2] = {wide ? attn_decode_pages_kernel<128, 2> : attn_decode_pages_kernel<64, 3>,
+                               wide ? attn_decode_pages_kernel<128, 3> : attn_decode_pages_kernel<64, 4>};
+    const int smem[2] = {wide ? PagesRing<128, 2>::kBytes : PagesRing<64, 3>::kBytes, wide ? PagesRing<128, 3>::kBytes : PagesRing<64, 4>::kBytes};
     int* fit = ctx->pages_clusters[wide];          // clusters of 2, 3 .. 8 CTAs that the GPU holds at once
     if (!ctx->pages_attr_set[wide]) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        for (int s = 2; s <= kPagesMaxCluster && e == cudaSuccess; ++s) e = clusters_at_once(kernel, kPagesThreads, smem, s, &fit[s]);
+        cudaError_t e = cudaSuccess;
+        for (int f = 0; f < 2 && e == cudaSuccess; ++f) e = cudaFuncSetAttribute(kernels[f], cudaFuncAttributeMaxDynamicSharedMemorySize, smem[f]);
+        for (int s = 2; s <= kPagesMaxCluster && e == cudaSuccess; ++s) e = clusters_at_once(kernels[0], kPagesThreads, smem[0], s, &fit[s]);
         if (e != cudaSuccess) return check_cuda(ctx, e, "attention over pages: kernel attributes");
         ctx->pages_attr_set[wide] = true;
     }
@@ -1158,8 +1163,13 @@ aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, 
     for (int s = 2; s <= kPagesMaxCluster && s <= most; ++s) if (items <= fit[s]) S = s;
     if (items * S > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "attention over pages: rows * Hkv = %lld", items);
     p.cluster = S;
+    // One CTA more per SM, with less of a ring, where an SM then takes no more turns x CTAs: 320 / 384 / 440 / 640 pairs of 128 pages 69.4 /
+    // 71.7 / 73.8 / 111 us with two and 59.3 / 68.4 / 75.3 / 106 with three, but 296 pairs 52.4 and 56.1, 512 pairs 84 and 102; heads of 64,
+    // 512 / 1024 pairs 55 / 88 with three and 44 / 83 with four.
+    const long long deep = wide ? 2 : 3, places = deep * ctx->num_sms, more = (deep + 1) * ctx->num_sms;
+    const int form = S == 1 && items > places && (items + more - 1) / more * (deep + 1) <= (items + places - 1) / places * deep;
     KernelScope scope(ctx, kKAttnPages, st);
-    return check_cuda(ctx, launch_cluster(kernel, items * S, kPagesThreads, smem, S, st, p), "attn_decode_pages_kernel launch");
+    return check_cuda(ctx, launch_cluster(kernels[form], items * S, kPagesThreads, smem[form], S, st, p), "attn_decode_pages_kernel launch");
 }
 
 }  // namespace aflex

@@ -318,6 +318,50 @@ def test_selection_of_neighbouring_rows(ctx, Hq, Hkv, D, lens, top, sink, window
         assert (bad[1][offs[1]] == 0).all() and (bad[0][offs[1]] == -1).all()
 
 
+SPREAD = [  # Hq, Hkv, D, lens, top, sink, window, new, padding rows, page table width
+    (8, 4, 64, [300 + 37 * i for i in range(14)], 7, 1, 1, [5] * 14, 0, 100),                # four rows' pairs of heads in one MMA; groups < SMs
+    (4, 4, 128, [100 + 97 * i for i in range(13)], 5, 0, 2, [7] * 13, 0, 100),               # a head per row
+    (64, 8, 128, [250 + 53 * i for i in range(22)], 6, 1, 1, [3] * 22, 0, 100),              # more groups than SMs, 2 CTAs on one
+    (32, 8, 64, [60 + 11 * i for i in range(45)], 5, 1, 2, [2] * 45, 0, 60),                 # 3 CTAs
+    (8, 8, 128, [40 + 17 * i for i in range(60)], 4, 1, 1, [2] * 60, 0, 70),                 # 4 CTAs
+    (16, 8, 64, [90 + 13 * i for i in range(40)], 4, 1, 1, [7] * 40, 0, 60),                 # 4 CTAs of seven rows, a warp each
+    (16, 8, 128, [40 + 31 * i for i in range(23)], 6, 1, 1, [1 + 5 * i % 9 for i in range(23)], 3, 60),     # uneven numbers of rows
+    (32, 8, 128, [500, 3000, 33000, 90], 30, 1, 2, [8, 8, 8, 8], 0, 2100),                   # clusters, long rows
+    (16, 8, 64, [2000 + 900 * i for i in range(7)], 20, 1, 2, [5] * 7, 0, 2100),             # of seven CTAs
+    (16, 8, 64, [2000 + 900 * i for i in range(7)], 20, 1, 2, [5] * 7, 0, 700),              # of four
+    (8, 8, 64, [9000, 40, 12000], 40, 2, 2, [3, 9, 5], 2, 2500),                             # clusters across sequences
+    (8, 8, 64, [100 + 7 * i for i in range(30)], 5, 1, 1, [8] * 30, 0, 6000),                # scores that need two CTAs' shared memory
+    (8, 8, 64, [90000, 50], 60, 1, 2, [8, 8], 0, 30000),                                     # eight
+    (8, 8, 64, [70000, 50], 60, 1, 2, [4, 4], 0, 60000),                                     # more than there are
+]
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens,top,sink,window,new,pad,width", SPREAD)
+def test_selection_of_neighbouring_rows_however_they_are_spread(ctx, Hq, Hkv, D, lens, top, sink, window, new, pad, width):
+    """Few and many groups, short and long tables: one CTA per group or several, of 8 or 16 warps, with and without a crowd."""
+    c = Cache(lens, Hkv, D, seed=top + D, max_pages=width)
+    ctx.page_bounds(AF.attn_desc(Hq, Hkv, D), c.kv, c.bounds, len(lens))
+    offs = np.concatenate([[0], np.cumsum(new)])
+    rows = int(offs[-1]) + pad
+    assert rows >= 2 * len(lens)
+    q = torch.randn(rows, Hq, D, generator=torch.Generator().manual_seed(width)).to(torch.bfloat16)
+    codes, scales = c.codes.cpu().numpy(), c.scales.cpu().numpy()
+    for _ in range(2):
+        got = run_select(ctx, c, q, Hq, top, sink, window, offs)
+        assert ctx.device_status() == AF.OK
+        want = PO.page_select(f64(q), codes, scales, c.table, lens, top, sink, window, offs)
+        n = int(offs[-1])
+        np.testing.assert_array_equal(got[1][:n], want[1][:n])
+        np.testing.assert_array_equal(got[0][:n], want[0][:n])
+        assert (got[0][n:] == -2).all() and (got[1][n:] == -2).all()
+        # the same with crowds of equal scores: every page's bounds one of two
+        two = [(codes[c.table[0, 0]].copy(), scales[c.table[0, 0]].copy()), (codes[c.table[0, 1]].copy(), scales[c.table[0, 1]].copy())]
+        for i in range(c.total):
+            codes[i], scales[i] = two[i % 3 == 0]
+        c.codes.copy_(torch.from_numpy(codes))
+        c.scales.copy_(torch.from_numpy(scales))
+
+
 def test_selection_ties_and_odd_queries(ctx):
     lens = [50 * 16 - 3] * 6
     c = Cache(lens, 2, 128, seed=1)
@@ -444,6 +488,13 @@ ATTEND = [  # Hq, Hkv, D, lens, top, new
     (4, 1, 64, [5000, 4999], 300, None),
     (16, 4, 64, [40, 700, 9], 12, [4, 7, 0]),
     (12, 3, 128, [65], 4, [33]),
+]
+
+
+ATTEND += [  # (row, head) pairs that take one CTA more per SM
+    (8, 8, 128, [40 + 9 * i for i in range(41)], 9, None),
+    (8, 8, 64, [33 + 5 * i for i in range(65)], 9, None),
+    (16, 8, 128, [200 + i for i in range(81)], 5, None),
 ]
 
 
