@@ -89,7 +89,7 @@ __device__ __forceinline__ void mma_s8_16832(int (&d)[4], uint32_t a0, uint32_t 
 // group's heads.  i_c is an integer below 2^19 and v_c exact in fp32, so the score, and with it the selection, is the same
 // bit for bit whatever computes it.
 //
-// One cluster of CTAs per (row, KV head), a contiguous share of the candidate pages each; a warp scores tiles of 16 pages with
+// One CTA, or a cluster with a contiguous share of the candidate pages each, per (row, KV head); a warp scores tiles of 16 pages with
 // integer MMAs, operands loaded from global memory straight into registers (the bounds' layout is the fragment's), and leaves
 // the scores in shared memory.  A histogram of 256 equal intervals between the lowest and the highest score, summed over the
 // cluster, tells the interval that holds the last page to keep, and the few pages of that interval are ranked by comparing all
@@ -1156,8 +1156,7 @@ aflex_status attn_decode_pages_launch(aflex_ctx* ctx, const aflex_attn_desc* d, 
     // dependent loads before the first page, the join), so a second wave costs more than an even split gains: 8 pairs of 128
     // pages 23.8 / 15.1 / 9.9 / 7.2 us with 1 / 2 / 4 / 8 CTAs each; 80 pairs 29.4 / 19.9 / 19.6 / 26.9 with 1 / 2 / 3 / 4; 256 of
     // up to 64 pages 26 / 32 / 43 with 1 / 2 / 4.  (Equal shares of all pairs' pages, cut anywhere and joined through global
-    // memory: 60 against 70 us at 304 pairs of 128, where one CTA each leaves a second wave of 8, but 52 against 47 at 256 and
-    // 93 against 84 at 512.)
+    // memory: 60 against 57 us at 304 pairs of 128, 52 against 47 at 256, 93 against 84 at 512.)
     const int most = (top_pages + kPagesWarps - 1) / kPagesWarps;
     int S = 1;
     for (int s = 2; s <= kPagesMaxCluster && s <= most; ++s) if (items <= fit[s]) S = s;
