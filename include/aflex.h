@@ -521,7 +521,7 @@ AFLEX_API aflex_status aflex_page_bounds(aflex_ctx* ctx, const aflex_attn_desc* 
  * (halves to even; NaN counts as 0; within [-127, 127]), i_c = sum_d Q_d (HI_d if Q_d > 0, else LO_d), v_c = i_c 2^e_c 2^f_c, and
  * s_h = ((v_0 + v_1) + v_2) + v_3 in fp32 (D = 64: v_0 + v_1).  A page's score is the largest s_h of the group's heads; of
  * equal scores the lower page goes first.  Every step but the fp32 additions is exact, so the result is the same bit for bit
- * on every run and for every way the work is split.
+ * on every run and for every way the work is split.  sm_scale takes no part (a positive one does not change the order).
  *   page_list  i32 [rows][Hkv][top_pages]  page indices within the sequence, ascending; -1 behind the last
  *   page_count i32 [rows][Hkv]             number of pages listed
  * A row without a valid length gets count 0.  max_pages_per_seq up to 393216 (6.3 M tokens); otherwise UNSUPPORTED.
