@@ -386,9 +386,9 @@ __device__ __forceinline__ void select_pages(SelectShared<W, CL>& sh, int tid, i
             sync();
         }
         const uint2* members = CL > 1 && S > 1 ? sh.rank : sh.member[0];
-        if (tid < inside) {
-            const float s = __uint_as_float(members[tid].x);
-            const uint32_t j = members[tid].y;
+        for (int m = tid; m < inside; m += threads) {              // (a row's one warp has fewer threads than there may be members)
+            const float s = __uint_as_float(members[m].x);
+            const uint32_t j = members[m].y;
             int before = 0;
 #pragma unroll 4
             for (int i = 0; i < inside; ++i) {
@@ -421,12 +421,13 @@ __device__ __forceinline__ void select_pages(SelectShared<W, CL>& sh, int tid, i
         sync_all();                                                // behind it nobody reads another CTA's shared memory
         base += __reduce_add_sync(0xffffffffu, lane < rank ? sh.all_kept[lane] : 0);
     }
-    int32_t* to = list + sink + base;
+    int32_t* to = list + sink;
     each([&](int j, float s, bool in) {
         const bool mine = in && keeps(j, s);
         const unsigned who = __ballot_sync(0xffffffffu, mine);
-        if (mine) to[__popc(who & below)] = sink + j;
-        to += __popc(who);
+        const int at = base + __popc(who & below);
+        if (mine && at < keep) to[at] = sink + j;                  // (exactly `keep` are kept; no store leaves their place in any case)
+        base += __popc(who);
     });
 }
 
