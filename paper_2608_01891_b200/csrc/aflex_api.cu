@@ -710,15 +710,16 @@ static bool decoder_fuse() {
 }
 
 // ---- whole decoder layers ------------------------------------------------------------------
-// Workspace: [A scratch | resid | xn | qkv | q | a | o | xn2 | y | F scratch].  The row-indexed
+// Workspace: [A scratch | resid | xn | qkv | q | a | o | xn2 | y | F scratch | page lists].  The row-indexed
 // buffers are touched by microbatch i only in rows of i, in the order A_{l,i} -> F_{l,i} ->
-// A_{l+1,i} that the events enforce; the A scratch is used on the attention stream only, the F
-// scratch on the FFN stream only.
+// A_{l+1,i} that the events enforce; the A scratch and the page lists are used on the attention stream only,
+// the F scratch on the FFN stream only.  All layers of a chain have ONE layout, each region as large as the layer that
+// needs most of it: A_{l+1,i} runs beside F_{l,j}, and buffers are handed from a layer to the next.
 namespace {
 struct DecoderWs {
     size_t a_attn, a_lin, rows_h, rows_qkv, rows_a, f_total, total;
 };
-// Page lists and counts of page-sparse attention (behind the other regions).
+// Page lists and counts of page-sparse attention.
 size_t page_lists_bytes(const aflex_attn_desc* d, int max_batch, int top_pages) {
     return align256((size_t)max_batch * d->num_kv_heads * top_pages * sizeof(int32_t)) +
            align256((size_t)max_batch * d->num_kv_heads * sizeof(int32_t));
@@ -746,6 +747,18 @@ DecoderWs decoder_ws(const aflex_decoder_desc* d, int max_batch, size_t a_attn, 
     w.f_total = layer_ws(L, max_batch, 0, num_sms).f_total;
     w.total = w.a_attn + w.a_lin + 5 * w.rows_h + w.rows_qkv + 2 * w.rows_a + w.f_total + 1024;
     return w;
+}
+// The layout of a chain of layers.
+DecoderWs chain_ws(const aflex_ctx* ctx, const aflex_decoder_desc* layers, int num_layers, int batch) {
+    DecoderWs c = {};
+    auto grow = [](size_t& a, size_t b) { if (b > a) a = b; };
+    for (int l = 0; l < num_layers; ++l) {
+        const DecoderWs w = decoder_ws(&layers[l], batch, attn_workspace_bytes(&layers[l].layer.attn, attn_grid(ctx)), ctx->num_sms);
+        grow(c.a_attn, w.a_attn); grow(c.a_lin, w.a_lin); grow(c.rows_h, w.rows_h); grow(c.rows_qkv, w.rows_qkv);
+        grow(c.rows_a, w.rows_a); grow(c.f_total, w.f_total);
+    }
+    c.total = c.a_attn + c.a_lin + 5 * c.rows_h + c.rows_qkv + 2 * c.rows_a + c.f_total + 1024;
+    return c;
 }
 }  // namespace
 
@@ -935,12 +948,13 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
     aflex_status s = validate_decoder_args(ctx, layers, kvs, num_layers, x_in, batch, x_out);
     if (s != AFLEX_OK) return s;
     const int H = layers[0].layer.hidden;
-    size_t need = 0;
-    for (int l = 0; l < num_layers; ++l) {
-        const DecoderWs w = decoder_ws(&layers[l], batch, attn_workspace_bytes(&layers[l].layer.attn, attn_grid(ctx)), ctx->num_sms);
-        const size_t total = w.total + (bounds ? 256 + page_lists_bytes(&layers[l].layer.attn, batch, policy->top_pages) : 0);
-        if (total > need) need = total;
+    const DecoderWs w = chain_ws(ctx, layers, num_layers, batch);
+    size_t lists_bytes = 0;
+    for (int l = 0; l < num_layers && bounds; ++l) {
+        const size_t b = page_lists_bytes(&layers[l].layer.attn, batch, policy->top_pages);
+        if (b > lists_bytes) lists_bytes = b;
     }
+    const size_t need = w.total + (bounds ? 256 + lists_bytes : 0);
     if (need > ctx->ws_bytes)
         return set_error(ctx, AFLEX_ERR_WORKSPACE, "decoder layers: need %zu workspace bytes, have %zu", need, ctx->ws_bytes);
     int32_t offs[kMaxMicrobatches + 1];
@@ -965,7 +979,6 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
         const aflex_layer_desc* L = &d->layer;
         const int Hq = L->attn.num_q_heads, Hkv = L->attn.num_kv_heads, D = L->attn.head_dim;
         const int A = Hq * D, NQ = (Hq + 2 * Hkv) * D, I = L->inter, E = L->num_experts;
-        const DecoderWs w = decoder_ws(d, batch, attn_workspace_bytes(&L->attn, attn_grid(ctx)), ctx->num_sms);
         char* p = ctx->ws;
         char* ws_attn = p; p += w.a_attn;
         char* ws_lin = p; p += w.a_lin;

@@ -1,0 +1,108 @@
+"""What the entry points launch, and with which addresses, on a stand-in for the CUDA runtime (host_runtime.cpp): the library's own
+objects, no GPU.  What only shows when kernels of two streams overlap, or with a second GPU, is decided here on the host."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2608_01891_b200 import aflex as AF
+from paper_2608_01891_b200 import build as B
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+P = 0x600000000000                          # an address that nothing follows
+
+
+class SelectArgs(ctypes.Structure):
+    """The argument of the page selection kernels, up to its outputs."""
+    _fields_ = ([(n, ctypes.c_uint64) for n in ("q", "codes", "scales", "page_table", "seq_lens", "q_offsets")]
+                + [(n, ctypes.c_int) for n in ("batch", "rows", "max_pages", "Hq", "Hkv", "G")] + [("num_pages", ctypes.c_longlong)]
+                + [(n, ctypes.c_int) for n in ("top", "sink", "window", "cluster", "group", "stride", "row_warps")]
+                + [("list", ctypes.c_uint64), ("count", ctypes.c_uint64)])
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    """The library on the stand-in, in the place of the real one."""
+    B.build()
+    objs = [os.path.join(B.HERE, "build", s + ".o") for s in B.SOURCES]
+    if not all(os.path.exists(o) for o in objs):
+        B.build(force=True)
+    tmp = tmp_path_factory.mktemp("host")
+    so, exports = str(tmp / "libaflex_host.so"), tmp / "exports"
+    exports.write_text("{ global: aflex_*; host_*; local: *; };")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(B.NVCC)), "include")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-shared", "-fPIC", "-I", cuda, "-o", so, *objs, os.path.join(HERE, "host_runtime.cpp"),
+                    f"-Wl,--version-script={exports}", "-Wl,--no-undefined"], check=True)
+    mp = pytest.MonkeyPatch()
+    mp.setattr(AF, "LIB_PATH", so)
+    mp.setattr(AF, "_lib", None)
+    lib = AF.load_library()
+    lib.host_launch_name.restype = ctypes.c_char_p
+    lib.host_launch_arg.restype = lib.host_launch_stream.restype = ctypes.c_void_p
+    yield lib
+    mp.undo()
+
+
+@pytest.fixture
+def ctx(host):
+    host.host_set_device(0)
+    c = AF.Context(0, 1 << 30)
+    host.host_forget()
+    yield c
+    c.close()
+
+
+def decoder(inter, experts=0, Hq=8, Hkv=2, D=64, hidden=256):
+    attn = AF.attn_desc(Hq, Hkv, D)
+    layer = AF.LayerDesc(attn, hidden, inter, experts, 2 if experts else 0, P, P, P, P, P if experts else None)
+    return AF.DecoderDesc(layer, P, P, P, None, None, 1e-6, 1e4)
+
+
+KV = AF.KV(P, P, 100, P, 10, P, None)
+
+
+def run_sparse(lib, ctx, layers, batch, top, depth):
+    """-> [(kernel name, device, stream, selection's arguments or None)]"""
+    lib.host_forget()
+    n = len(layers)
+    bounds = (AF.KeyBounds * n)(*[AF.KeyBounds(P, P)] * n)
+    st = lib.aflex_decoder_layers_sparse(ctx._h, (AF.DecoderDesc * n)(*layers), (AF.KV * n)(*[KV] * n), bounds, AF.PagePolicy(top, 1, 2), n, P, batch,
+                                         depth, None, P, None)
+    assert st == AF.OK, lib.aflex_last_error(ctx._h)
+    out = []
+    for i in range(lib.host_launch_count()):
+        name = lib.host_launch_name(i).decode()
+        arg = ctypes.cast(lib.host_launch_arg(i), ctypes.POINTER(SelectArgs)).contents if "page_select" in name else None
+        out.append((name, lib.host_launch_device(i), lib.host_launch_stream(i), arg))
+    return out
+
+
+def list_places(launched, batch, top, Hkv=2):
+    """(start, end) of the page lists and of the counts of every selection, and whether its arguments are what they should be."""
+    args = [a for *_, a in launched if a is not None]
+    assert args and all(a.top == top and a.Hkv == Hkv and a.rows == a.batch and a.rows <= batch for a in args)
+    return [(a.list, a.list + 4 * a.rows * Hkv * top) for a in args] + [(a.count, a.count + 4 * a.rows * Hkv) for a in args]
+
+
+@pytest.mark.parametrize("depth", [1, 2])
+@pytest.mark.parametrize("order", ["dense, MoE", "MoE, dense", "dense, MoE, dense"])
+def test_page_lists_lie_in_no_layers_scratch(host, ctx, depth, order):
+    """Layers with another FFN beside them have larger or smaller FFN scratch, which is used on another stream while the next layer's
+    lists are written.  A layer alone has its lists behind its scratch: in a chain every list has to lie behind every layer's."""
+    batch, top = 24, 5
+    kinds = {"dense": decoder(8192), "MoE": decoder(64, experts=4)}
+    alone = {}
+    for k, d in kinds.items():
+        alone[k] = min(a for a, _ in list_places(run_sparse(host, ctx, [d], batch, top, depth), batch, top))
+    assert alone["dense"] > alone["MoE"] + 100000                  # (the case tells the two apart)
+    chain = [kinds[k] for k in order.split(", ")]
+    launched = run_sparse(host, ctx, chain, batch, top, depth)
+    assert all(a >= max(alone.values()) for a, _ in list_places(launched, batch, top))
+    # and a workspace of the size that the library asks for holds them
+    small = AF.Context(0, max(AF.decoder_sparse_workspace_bytes(d, batch, top) for d in chain))
+    try:
+        assert all(host.host_allocated(ctypes.c_uint64(a), ctypes.c_uint64(b))
+                   for a, b in list_places(run_sparse(host, small, chain, batch, top, depth), batch, top))
+    finally:
+        small.close()
