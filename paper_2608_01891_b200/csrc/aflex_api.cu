@@ -1104,6 +1104,7 @@ aflex_status aflex_decoder_layers_sparse(aflex_ctx* ctx, const aflex_decoder_des
         if (s == AFLEX_OK) s = page_select_supported(ctx, &kvs[l]);
     }
     if (s != AFLEX_OK) return s;
+    CtxDevice dev(ctx);
     return decoder_layers_run(ctx, layers, kvs, bounds, policy, num_layers, x_in, batch, M, mb_offsets, x_out, stream);
 }
 

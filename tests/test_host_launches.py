@@ -106,3 +106,32 @@ def test_page_lists_lie_in_no_layers_scratch(host, ctx, depth, order):
                    for a, b in list_places(run_sparse(host, small, chain, batch, top, depth), batch, top))
     finally:
         small.close()
+
+
+@pytest.mark.parametrize("depth", [1, 2])
+@pytest.mark.parametrize("name", ["rope_append_bounds", "page_bounds", "page_select", "attn_decode_pages", "decoder_layers_sparse"])
+def test_launches_go_to_the_contexts_device_and_the_callers_comes_back(host, name, depth):
+    """The page-sparse entry points, called with another device current than the context's."""
+    ctx = AF.Context(1, 1 << 30)
+    host.host_set_device(0)
+    host.host_forget()
+    try:
+        d, kv, b, a = AF.attn_desc(8, 2, 64), ctypes.byref(KV), ctypes.byref(AF.KeyBounds(P, P)), AF.PagePolicy(5, 1, 2)
+        rows = 6 * depth
+        if name == "rope_append_bounds":
+            st = host.aflex_rope_append_bounds(ctx._h, d, P, kv, b, rows, None, rows, None, None, 1e-6, 1e4, P, None)
+        elif name == "page_bounds":
+            st = host.aflex_page_bounds(ctx._h, d, kv, b, rows, None, None)
+        elif name == "page_select":
+            st = host.aflex_page_select(ctx._h, d, P, kv, b, a, rows, None, rows, P, P, None)
+        elif name == "attn_decode_pages":
+            st = host.aflex_attn_decode_pages(ctx._h, d, P, kv, P, P, 5, rows, None, rows, P, None, None)
+        else:
+            st = AF.OK
+            run_sparse(host, ctx, [decoder(1024), decoder(64, experts=4)], rows, 5, depth)
+        assert st == AF.OK
+        n = host.host_launch_count()
+        assert n > 0 and all(host.host_launch_device(i) == 1 for i in range(n))
+        assert host.host_device() == 0
+    finally:
+        ctx.close()
