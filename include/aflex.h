@@ -536,7 +536,9 @@ AFLEX_API aflex_status aflex_page_select(aflex_ctx* ctx, const aflex_attn_desc* 
  *     s_j = sm_scale * <q, K_j>,  out = sum_j softmax(s)_j V_j -> bf16,  lse = ln sum_j exp(s_j)
  * A page that is listed twice counts twice.  An entry outside the pages the row sees, or with a bad page id, is left out
  * and raises AFLEX_ERR_BOUNDS.  With nothing to attend to out is 0 and lse -infinity.  fp32 scores and sums; P enters the
- * second product as the sum of two bf16 values.  out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  No workspace.
+ * second product as the sum of two bf16 values.  A score of -infinity weighs nothing (with no other: as with nothing to attend
+ * to); a score of +infinity or NaN makes its head's out and lse NaN, an infinite or NaN entry of an attended V that channel of
+ * out infinite or NaN.  out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  No workspace.
  * Deterministic run to run.
  */
 AFLEX_API aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,

@@ -17,7 +17,7 @@ namespace {
 template <typename V> __device__ __forceinline__ V fetch(const V* p) { return *p; }
 
 constexpr int kPageTokens = 16;
-constexpr float kNegBig = -1.0e30f;
+constexpr float kLowest = -3.402823466e38f;     // the lowest finite value: where running maxima start, so that no score lies below
 
 // Sequence of a row, and how many of the sequence's rows follow it; every lane of a warp takes part.  Rows behind the last
 // sequence's are padding: nothing is to be read, written or reported for them.
@@ -738,7 +738,7 @@ template <int D> struct PageState {
         for (int h = 0; h < D / 64; ++h)
 #pragma unroll
             for (int c = 0; c < 8; ++c) o[h][c][0] = o[h][c][1] = o[h][c][2] = o[h][c][3] = 0.f;
-        m = kNegBig;
+        m = kLowest;
         l = 0.f;
     }
 };
@@ -943,7 +943,7 @@ __global__ void __launch_bounds__(kPagesThreads, O) attn_decode_pages_kernel(con
     constexpr int kRuns = D / 4;                   // a head's outputs in runs of four channels
     for (int i = tid; i < p.G * kRuns; i += kPagesThreads) {
         const int h = i / kRuns, c = i % kRuns;
-        RunSum s = {kNegBig, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        RunSum s = {kLowest, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
         for (int w = 0; w < kPagesWarps; ++w) s.M = fmaxf(s.M, sh.m[w][h]);
 #pragma unroll
@@ -969,7 +969,7 @@ __global__ void __launch_bounds__(kPagesThreads, O) attn_decode_pages_kernel(con
             pl[s] = ld_cluster_f32(cluster_map_shared(smem_u32(&sh.cl[h]), from));
             v[s] = ld_cluster_f32x4(cluster_map_shared(smem_u32(state(0) + h * D + 4 * c), from));
         }
-        RunSum sum = {kNegBig, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        RunSum sum = {kLowest, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
 #pragma unroll
         for (int s = 0; s < kPagesMaxCluster; ++s) if (s < S) sum.M = fmaxf(sum.M, pm[s]);
 #pragma unroll
