@@ -493,7 +493,7 @@ typedef struct { int8_t* codes; uint8_t* scales; } aflex_key_bounds;
 
 /* Which pages a row reads: all of them while it sees at most top_pages; otherwise the first sink_pages, the last
  * window_pages (the row's own page among them) and the best-scored others, top_pages in all.
- * sink_pages >= 0, window_pages >= 1, sink_pages + window_pages <= top_pages. */
+ * sink_pages >= 0, window_pages >= 1, sink_pages + window_pages <= top_pages <= 2^26 (more: UNSUPPORTED). */
 typedef struct { int top_pages, sink_pages, window_pages; } aflex_page_policy;
 
 /*
@@ -538,7 +538,7 @@ AFLEX_API aflex_status aflex_page_select(aflex_ctx* ctx, const aflex_attn_desc* 
  * and raises AFLEX_ERR_BOUNDS.  With nothing to attend to out is 0 and lse -infinity.  fp32 scores and sums; P enters the
  * second product as the sum of two bf16 values.  A score of -infinity weighs nothing (with no other: as with nothing to attend
  * to); a score of +infinity or NaN makes its head's out and lse NaN, an infinite or NaN entry of an attended V that channel of
- * out infinite or NaN.  out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  No workspace.
+ * out infinite or NaN.  out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  No workspace.  top_pages up to 2^26.
  * Deterministic run to run.
  */
 AFLEX_API aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_kv* kv,

@@ -716,6 +716,7 @@ static bool decoder_fuse() {
 // the F scratch on the FFN stream only.  All layers of a chain have ONE layout, each region as large as the layer that
 // needs most of it: A_{l+1,i} runs beside F_{l,j}, and buffers are handed from a layer to the next.
 namespace {
+constexpr int kMaxPages = 1 << 26;      // of a sequence, and of a page list
 struct DecoderWs {
     size_t a_attn, a_lin, rows_h, rows_qkv, rows_a, f_total, total;
 };
@@ -768,7 +769,7 @@ size_t aflex_decoder_workspace_bytes(const aflex_decoder_desc* layer, int max_ba
 }
 
 size_t aflex_decoder_sparse_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int top_pages) {
-    if (!layer || max_batch < 1 || top_pages < 1) return 0;
+    if (!layer || max_batch < 1 || top_pages < 1 || top_pages > kMaxPages) return 0;
     return aflex_decoder_workspace_bytes(layer, max_batch) + 256 + page_lists_bytes(&layer->layer.attn, max_batch, top_pages);
 }
 
@@ -804,10 +805,14 @@ struct CtxDevice {
     }
     ~CtxDevice() { if (saved >= 0) cudaSetDevice(saved); }
 };
-// Positions are 32-bit.
+// Positions are 32-bit, and so are counters of list entries, which step by a block of threads.
 aflex_status validate_pages(aflex_ctx* ctx, const char* what, const aflex_kv* kv) {
-    if (kv->max_pages_per_seq > (1 << 26))
+    if (kv->max_pages_per_seq > kMaxPages)
         return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "%s: max_pages_per_seq %d (supported: up to 2^26)", what, kv->max_pages_per_seq);
+    return AFLEX_OK;
+}
+aflex_status validate_top(aflex_ctx* ctx, const char* what, int top_pages) {
+    if (top_pages > kMaxPages) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "%s: top_pages %d (supported: up to 2^26)", what, top_pages);
     return AFLEX_OK;
 }
 // Rows of a call: one per sequence, or `rows` rows laid out by q_offsets.
@@ -858,7 +863,7 @@ aflex_status validate_policy(aflex_ctx* ctx, const char* what, const aflex_page_
         (long long)policy->sink_pages + policy->window_pages > policy->top_pages)
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: sink_pages %d >= 0, window_pages %d >= 1 and their sum <= top_pages %d are required",
                          what, policy->sink_pages, policy->window_pages, policy->top_pages);
-    return AFLEX_OK;
+    return validate_top(ctx, what, policy->top_pages);
 }
 }  // namespace
 
@@ -884,6 +889,8 @@ aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc
     if (s != AFLEX_OK) return s;
     if (!page_list || !page_count || top_pages < 1)
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "attention over pages: null page_list / page_count or top_pages < 1");
+    s = validate_top(ctx, "attention over pages", top_pages);
+    if (s != AFLEX_OK) return s;
     CtxDevice dev(ctx);
     return attn_decode_pages_launch(ctx, desc, q, kv, page_list, page_count, top_pages, batch, q_offsets, rows, out, lse,
                                     reinterpret_cast<cudaStream_t>(stream));

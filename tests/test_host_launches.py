@@ -135,3 +135,20 @@ def test_launches_go_to_the_contexts_device_and_the_callers_comes_back(host, nam
         assert host.host_device() == 0
     finally:
         ctx.close()
+
+
+def test_no_more_listed_pages_than_32_bit_counters_take(host, ctx):
+    """Lists of more than 2^26 pages (as many as a sequence can have) are refused before anything is launched: counters of list
+    entries, stepping by a block of threads, would wrap near 2^31."""
+    most, d, kv, b = 1 << 26, AF.attn_desc(8, 2, 64), ctypes.byref(KV), ctypes.byref(AF.KeyBounds(P, P))
+    select = lambda top: host.aflex_page_select(ctx._h, d, P, kv, b, AF.PagePolicy(top, 1, 2), 3, None, 3, P, P, None)  # noqa: E731
+    attend = lambda top: host.aflex_attn_decode_pages(ctx._h, d, P, kv, P, P, top, 3, None, 3, P, None, None)  # noqa: E731
+    layers = lambda top: host.aflex_decoder_layers_sparse(  # noqa: E731
+        ctx._h, (AF.DecoderDesc * 1)(decoder(64)), (AF.KV * 1)(KV), b, AF.PagePolicy(top, 1, 2), 1, P, 3, 1, None, P, None)
+    for call in (select, attend, layers):
+        for top in (most + 1, 2147483647, 2147483647 - 4):
+            assert call(top) == AF.ERR_UNSUPPORTED
+    assert host.host_launch_count() == 0
+    assert select(most) == AF.OK and attend(most) == AF.OK
+    assert layers(most) == AF.ERR_WORKSPACE
+    assert AF.decoder_sparse_workspace_bytes(decoder(64), 3, most + 1) == 0 < AF.decoder_sparse_workspace_bytes(decoder(64), 3, most)
