@@ -662,6 +662,9 @@ class Context:
                               mb_offsets: Optional[Sequence[int]] = None, stream=None) -> None:
         """decoder_layers with page-sparse attention; bounds[l] are the key bounds of layer l's cache (the appended page's are updated)."""
         assert len(layers) == len(kvs) == len(bounds) and len(layers) >= 1
+        for x in (x_in, x_out):
+            assert x.dtype == _BF16 and x.numel() == x_in.shape[0] * layers[0].layer.hidden, "hidden states are not bf16 [B][H]"
+        assert mb_offsets is None or len(mb_offsets) > microbatch_depth, "mb_offsets are not microbatch_depth + 1 rows"
         for d, kv, b in zip(layers, kvs, bounds):
             _match(self.device, d.layer.attn, kv, x_in.shape[0], b)
         offs = None

@@ -5,6 +5,7 @@ import os
 import subprocess
 
 import pytest
+import torch
 
 from paper_2608_01891_b200 import aflex as AF
 from paper_2608_01891_b200 import build as B
@@ -152,3 +153,27 @@ def test_no_more_listed_pages_than_32_bit_counters_take(host, ctx):
     assert select(most) == AF.OK and attend(most) == AF.OK
     assert layers(most) == AF.ERR_WORKSPACE
     assert AF.decoder_sparse_workspace_bytes(decoder(64), 3, most + 1) == 0 < AF.decoder_sparse_workspace_bytes(decoder(64), 3, most)
+
+
+def test_sparse_layers_check_the_hidden_states_and_offsets_before_the_library_sees_them():
+    """As the operators do: a tensor of another type or size would be read or written past its end."""
+    class Stream:
+        cuda_stream = 0
+
+    ctx = AF.Context.__new__(AF.Context)
+    ctx._lib, ctx._h, ctx.device = AF.load_library(), None, -1
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
+    k = z(6, 2, 16, 64)
+    i32 = torch.int32
+    kv = AF.make_kv(k, k, z(3, 4, dt=i32), z(3, dt=i32))
+    bounds = AF.make_page_bounds(*AF.empty_page_bounds(6, 2, 64, device="cpu"))
+    x = z(3, 256)
+    call = lambda x_in=x, x_out=x, **kw: ctx.decoder_layers_sparse([decoder(64)], [kv], [bounds], 5, x_in, x_out, stream=Stream, **kw)  # noqa: E731
+    with pytest.raises(AF.AflexError):                                 # all as it should be: it is the library that refuses (no context)
+        call()
+    with pytest.raises(AF.AflexError):
+        call(microbatch_depth=2, mb_offsets=[0, 1, 3])
+    for kw in (dict(x_in=x.float()), dict(x_out=x.half()), dict(x_in=z(3, 248), x_out=z(3, 248)), dict(x_out=z(2, 256)), dict(x_out=z(3, 128)),
+               dict(x_in=z(3 * 256)), dict(microbatch_depth=2, mb_offsets=[0, 3])):
+        with pytest.raises(AssertionError):
+            call(**kw)
