@@ -400,7 +400,9 @@ AFLEX_API aflex_status aflex_decoder_layers(aflex_ctx* ctx, const aflex_decoder_
                                             int num_layers, const void* x_in, int batch, int microbatch_depth,
                                             const int32_t* mb_offsets, void* x_out, void* stream);
 
-/* Workspace bytes that suffice for aflex_decoder_layers on this layer shape.  Pure host computation. */
+/* Workspace bytes that suffice for aflex_decoder_layers on this layer shape.  Pure host computation.  A chain of layers with
+ * different FFNs needs the largest of its layers' figures.  Where their attention shapes differ too it can need more (every region is
+ * as large as the layer that needs most of it): AFLEX_ERR_WORKSPACE then names the size. */
 AFLEX_API size_t aflex_decoder_workspace_bytes(const aflex_decoder_desc* layer, int max_batch);
 
 /*

@@ -961,6 +961,14 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
         const size_t b = page_lists_bytes(&layers[l].layer.attn, batch, policy->top_pages);
         if (b > lists_bytes) lists_bytes = b;
     }
+    // Row r of the projections and of the attention side starts where it does in the widest layer: a microbatch's rows stay apart
+    // from the others' in every layer.
+    int most_qkv = 0, most_a = 0;
+    for (int l = 0; l < num_layers; ++l) {
+        const aflex_attn_desc& t = layers[l].layer.attn;
+        if ((t.num_q_heads + 2 * t.num_kv_heads) * t.head_dim > most_qkv) most_qkv = (t.num_q_heads + 2 * t.num_kv_heads) * t.head_dim;
+        if (t.num_q_heads * t.head_dim > most_a) most_a = t.num_q_heads * t.head_dim;
+    }
     const size_t need = w.total + (bounds ? 256 + lists_bytes : 0);
     if (need > ctx->ws_bytes)
         return set_error(ctx, AFLEX_ERR_WORKSPACE, "decoder layers: need %zu workspace bytes, have %zu", need, ctx->ws_bytes);
@@ -1003,6 +1011,7 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
         for (int i = 0; i < M; ++i) {
             const int r0 = offs[i], rows = offs[i + 1] - offs[i];
             const size_t oh = (size_t)r0 * H;
+            bf *const qkv_i = qkv + (size_t)r0 * most_qkv, *const q_i = qb + (size_t)r0 * most_a, *const a_i = ab + (size_t)r0 * most_a;
             // ---- A_{l,i}
             if (l > 0 && !serial) {
                 e = cudaStreamWaitEvent(sa, ctx->ev_f[i], 0);     // F_{l-1,i} has returned this microbatch
@@ -1025,7 +1034,7 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
                 if (l == 0) s = add_rmsnorm_launch(ctx, reinterpret_cast<const bf*>(x_in) + oh, nullptr, d->w_ln_attn, rows, H, d->rms_eps, resid + oh, xn + oh, sa);
                 else s = add_rmsnorm_launch(ctx, resid + oh, yb + oh, d->w_ln_attn, rows, H, d->rms_eps, resid + oh, xn + oh, sa);
                 if (s != AFLEX_OK) return s;
-                s = linear_launch(ctx, xn + oh, d->w_qkv, rows, H, NQ, qkv + (size_t)r0 * NQ, ws_lin, w.a_lin, sa, kKQkvGemm, ctx->counters_a);
+                s = linear_launch(ctx, xn + oh, d->w_qkv, rows, H, NQ, qkv_i, ws_lin, w.a_lin, sa, kKQkvGemm, ctx->counters_a);
                 if (s != AFLEX_OK) return s;
             }
             aflex_kv kvi = kvs[l];
@@ -1035,22 +1044,22 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
             if (bounds) {
                 int32_t* list = lists + (size_t)r0 * Hkv * policy->top_pages;
                 int32_t* count = counts + (size_t)r0 * Hkv;
-                s = rope_append_bounds_launch(ctx, &L->attn, qkv + (size_t)r0 * NQ, &kvi, &bounds[l], rows, nullptr, rows, d->w_q_norm, d->w_k_norm,
-                                              d->rms_eps, d->rope_theta, qb + (size_t)r0 * A, sa);
+                s = rope_append_bounds_launch(ctx, &L->attn, qkv_i, &kvi, &bounds[l], rows, nullptr, rows, d->w_q_norm, d->w_k_norm,
+                                              d->rms_eps, d->rope_theta, q_i, sa);
                 if (s == AFLEX_OK)
-                    s = page_select_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, &bounds[l], policy, rows, nullptr, rows, list, count, sa);
+                    s = page_select_launch(ctx, &L->attn, q_i, &kvi, &bounds[l], policy, rows, nullptr, rows, list, count, sa);
                 if (s == AFLEX_OK)
-                    s = attn_decode_pages_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, list, count, policy->top_pages, rows, nullptr, rows,
-                                                 ab + (size_t)r0 * A, nullptr, sa);
+                    s = attn_decode_pages_launch(ctx, &L->attn, q_i, &kvi, list, count, policy->top_pages, rows, nullptr, rows,
+                                                 a_i, nullptr, sa);
             } else {
-                s = rope_append_launch(ctx, &L->attn, qkv + (size_t)r0 * NQ, &kvi, rows, d->w_q_norm, d->w_k_norm, d->rms_eps, d->rope_theta, qb + (size_t)r0 * A, sa);
+                s = rope_append_launch(ctx, &L->attn, qkv_i, &kvi, rows, d->w_q_norm, d->w_k_norm, d->rms_eps, d->rope_theta, q_i, sa);
                 if (s != AFLEX_OK) return s;
                 ctx->attn_q_final_once = true;      // q was written by the append kernel, which does not release its dependents early
-                s = attn_decode_launch(ctx, &L->attn, qb + (size_t)r0 * A, &kvi, rows, ab + (size_t)r0 * A, nullptr, ws_attn, w.a_attn, sa);
+                s = attn_decode_launch(ctx, &L->attn, q_i, &kvi, rows, a_i, nullptr, ws_attn, w.a_attn, sa);
             }
             if (s != AFLEX_OK) return s;
             if (!fused) {
-                s = linear_launch(ctx, ab + (size_t)r0 * A, L->w_o, rows, A, H, ob + oh, ws_lin, w.a_lin, sa, kKLinearGemm, ctx->counters_a);
+                s = linear_launch(ctx, a_i, L->w_o, rows, A, H, ob + oh, ws_lin, w.a_lin, sa, kKLinearGemm, ctx->counters_a);
                 if (s != AFLEX_OK) return s;
             }
             if (!serial) {
@@ -1062,9 +1071,9 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
             if (fused) {
                 const aflex_decoder_desc* dn = fuse_next ? &layers[l + 1] : nullptr;
                 const int NQn = dn ? (dn->layer.attn.num_q_heads + 2 * dn->layer.attn.num_kv_heads) * dn->layer.attn.head_dim : 0;
-                s = dense_fused_run(ctx, ab + (size_t)r0 * A, L->w_o, A, resid + oh, d->w_ln_ffn, d->rms_eps, xn2 + oh, L->w_gate, L->w_up,
+                s = dense_fused_run(ctx, a_i, L->w_o, A, resid + oh, d->w_ln_ffn, d->rms_eps, xn2 + oh, L->w_gate, L->w_up,
                                     L->w_down, rows, H, I, yb + oh, ws_f, w.f_total, sf, dn ? dn->w_ln_attn : nullptr, dn ? dn->rms_eps : 0.f,
-                                    xn + oh, dn ? dn->w_qkv : nullptr, NQn, dn ? qkv + (size_t)r0 * NQn : nullptr);
+                                    xn + oh, dn ? dn->w_qkv : nullptr, NQn, dn ? qkv_i : nullptr);
             } else {
                 s = add_rmsnorm_launch(ctx, resid + oh, ob + oh, d->w_ln_ffn, rows, H, d->rms_eps, resid + oh, xn2 + oh, sf);
                 if (s != AFLEX_OK) return s;

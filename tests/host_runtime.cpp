@@ -22,7 +22,7 @@ struct { dim3 grid, block; size_t smem; void* stream; } pushed;
 void note(const void* kernel, void* stream, void** args) {
     Launch l = {names()[kernel], device, stream, {}};
     // (only of the kernels whose arguments are looked at: one structure of at least as many bytes)
-    if (l.name.find("page_select") != std::string::npos) memcpy(l.arg, args[0], sizeof l.arg);
+    if (l.name.find("page_select") != std::string::npos || l.name.find("attn_decode_pages") != std::string::npos) memcpy(l.arg, args[0], sizeof l.arg);
     launches.push_back(l);
 }
 int encode_tiled() { return 0; }

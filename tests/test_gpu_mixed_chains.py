@@ -99,3 +99,60 @@ def test_sparse_chain_of_dense_and_moe_layers_is_the_dense_chain_with_every_page
         assert rows_apart(sparse, dense) <= 4.3e-2 and np.isfinite(f64(dense)).all()
     finally:
         ctx.close()
+
+
+NARROW, WIDE, LARGE = shape(63, "narrow", 1408), shape(64, "wide", 1408, Hq=16), shape(65, "large-heads", 1408, Hq=8, Hkv=8, D=128)
+NARROW_MOE = shape(66, "narrow-moe", 192, 4, Hq=4, Hkv=4)
+ATTENTION_MIXES = [(NARROW, WIDE), (LARGE, NARROW, NARROW), (NARROW, NARROW_MOE, LARGE)]
+
+
+@pytest.mark.parametrize("sparse", [False, True], ids=["dense", "sparse"])
+@pytest.mark.parametrize("depth", [1, 2])
+@pytest.mark.parametrize("cfgs", ATTENTION_MIXES, ids=lambda c: "-".join(x.name for x in c))
+def test_chain_of_layers_with_different_heads_is_its_layers_in_turn(cfgs, depth, sparse):
+    c = Chain(cfgs)
+    top = (int(c.lens.max()) + 15) // 16
+    ctx = AF.Context(0, 1 << 28)
+    try:
+        def run(layers, x, y):
+            part = lambda t: [t[l] for l in layers]  # noqa: E731
+            if sparse:
+                ctx.decoder_layers_sparse(part(c.descs), part(c.kvs()), part(c.bounds), top, x, y, microbatch_depth=depth)
+            else:
+                ctx.decoder_layers(part(c.descs), part(c.kvs()), x, y, depth)
+
+        got, want = torch.empty_like(c.x), c.x.clone()
+        c.reset(ctx)
+        for l in range(len(cfgs)):
+            run([l], want, want)
+        after = c.state()
+        c.reset(ctx)
+        run(range(len(cfgs)), c.x, got)
+        assert ctx.device_status() == AF.OK
+        # two chains of the same bf16 roundings, as above: sqrt(2 x 3 x 20) 2^-8
+        assert rows_apart(got, want) <= 4.3e-2 and np.isfinite(f64(want)).all()
+        n = 2 * len(cfgs)                                                       # keys and values
+        assert all(rows_apart(a, b) <= 4.3e-2 for a, b in zip(c.state()[:n], after[:n]))
+    finally:
+        ctx.close()
+
+
+@pytest.mark.parametrize("cfgs", ATTENTION_MIXES, ids=lambda c: "-".join(x.name for x in c))
+def test_sparse_chain_of_layers_with_different_heads_in_microbatches(cfgs):
+    """Two microbatches on two streams, against each of them alone on one."""
+    c, top, half = Chain(cfgs), 6, BATCH // 2
+    ctx = AF.Context(0, 1 << 28)
+    try:
+        want = torch.empty_like(c.x)
+        c.reset(ctx)
+        for r0 in (0, half):
+            ctx.decoder_layers_sparse(c.descs, c.kvs(r0, r0 + half), c.bounds, top, c.x[r0:r0 + half], want[r0:r0 + half])
+        after = c.state()
+        for _ in range(10):
+            got = torch.zeros_like(want)
+            c.reset(ctx)
+            ctx.decoder_layers_sparse(c.descs, c.kvs(), c.bounds, top, c.x, got, microbatch_depth=2)
+            assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(c.state(), after))
+        assert ctx.device_status() == AF.OK
+    finally:
+        ctx.close()

@@ -22,6 +22,13 @@ class SelectArgs(ctypes.Structure):
                 + [("list", ctypes.c_uint64), ("count", ctypes.c_uint64)])
 
 
+class AttendArgs(ctypes.Structure):
+    """The argument of the kernel of attention over listed pages, up to its outputs."""
+    _fields_ = ([(n, ctypes.c_uint64) for n in ("q", "k_cache", "v_cache", "page_table", "seq_lens", "q_offsets", "list", "count")]
+                + [(n, ctypes.c_int) for n in ("batch", "rows", "max_pages", "Hq", "Hkv", "G", "top", "cluster")] + [("num_pages", ctypes.c_longlong)]
+                + [("scale_log2", ctypes.c_float), ("out", ctypes.c_uint64), ("lse", ctypes.c_uint64)])
+
+
 @pytest.fixture(scope="module")
 def host(tmp_path_factory):
     """The library on the stand-in, in the place of the real one."""
@@ -64,7 +71,7 @@ KV = AF.KV(P, P, 100, P, 10, P, None)
 
 
 def run_sparse(lib, ctx, layers, batch, top, depth):
-    """-> [(kernel name, device, stream, selection's arguments or None)]"""
+    """-> [(kernel name, device, stream, arguments of selection and attention, else None)]"""
     lib.host_forget()
     n = len(layers)
     bounds = (AF.KeyBounds * n)(*[AF.KeyBounds(P, P)] * n)
@@ -74,14 +81,15 @@ def run_sparse(lib, ctx, layers, batch, top, depth):
     out = []
     for i in range(lib.host_launch_count()):
         name = lib.host_launch_name(i).decode()
-        arg = ctypes.cast(lib.host_launch_arg(i), ctypes.POINTER(SelectArgs)).contents if "page_select" in name else None
+        kind = SelectArgs if "page_select" in name else AttendArgs if "attn_decode_pages" in name else None
+        arg = kind.from_buffer_copy(ctypes.string_at(lib.host_launch_arg(i), ctypes.sizeof(kind))) if kind else None
         out.append((name, lib.host_launch_device(i), lib.host_launch_stream(i), arg))
     return out
 
 
 def list_places(launched, batch, top, Hkv=2):
     """(start, end) of the page lists and of the counts of every selection, and whether its arguments are what they should be."""
-    args = [a for *_, a in launched if a is not None]
+    args = [a for *_, a in launched if isinstance(a, SelectArgs)]
     assert args and all(a.top == top and a.Hkv == Hkv and a.rows == a.batch and a.rows <= batch for a in args)
     return [(a.list, a.list + 4 * a.rows * Hkv * top) for a in args] + [(a.count, a.count + 4 * a.rows * Hkv) for a in args]
 
@@ -107,6 +115,24 @@ def test_page_lists_lie_in_no_layers_scratch(host, ctx, depth, order):
                    for a, b in list_places(run_sparse(host, small, chain, batch, top, depth), batch, top))
     finally:
         small.close()
+
+
+@pytest.mark.parametrize("inter", [1024, 64])
+def test_rows_of_a_microbatch_lie_apart_from_the_others_in_every_layer(host, ctx, inter):
+    """Attention output of A_{l+1,i} is written while F_{l,j} reads that of its own rows (the output projection is part of the FFN's
+    kernel), so no layer, however wide its heads together, may have a microbatch's rows where another layer has another one's."""
+    batch, depth = 12, 3
+    chain = [decoder(inter, Hq=4, Hkv=2), decoder(inter, Hq=16, Hkv=2), decoder(inter, Hq=8, Hkv=8, D=128), decoder(inter, Hq=4, Hkv=4)]
+    args = [a for *_, a in run_sparse(host, ctx, chain, batch, 5, depth) if isinstance(a, AttendArgs)]
+    assert len(args) == depth * len(chain)
+    assert all(a.Hq == d.layer.attn.num_q_heads and a.rows == batch // depth for a, d in zip(args, [d for d in chain for _ in range(depth)]))
+    for of in (lambda a: a.q, lambda a: a.out):
+        rows = [[] for _ in range(depth)]
+        for i, (a, d) in enumerate(zip(args, [d for d in chain for _ in range(depth)])):
+            rows[i % depth].append((of(a), of(a) + 2 * a.rows * a.Hq * d.layer.attn.head_dim))
+        for i in range(depth):
+            for j in range(i):
+                assert all(b0 <= a1 or b1 <= a0 for a0, b0 in rows[i] for a1, b1 in rows[j])
 
 
 @pytest.mark.parametrize("depth", [1, 2])
