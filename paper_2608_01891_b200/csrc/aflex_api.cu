@@ -1125,7 +1125,8 @@ aflex_status aflex_decoder_layers_sparse(aflex_ctx* ctx, const aflex_decoder_des
 }
 
 // ---- whole decoder layers over the tokens being prefilled -----------------------------------
-// Workspace: [linear scratch | resid | xn | qkv | q | a | o | xn2 | y | F scratch], rows = prompt tokens.
+// Workspace: [linear scratch | resid | xn | qkv | q | a | o | xn2 | y | F scratch], rows = prompt tokens; one layout for all layers
+// of the chain, since resid and y are handed from a layer to the next.
 namespace {
 struct PrefillWs {
     size_t a_lin, rows_h, rows_qkv, rows_a, f_total, total;
@@ -1167,17 +1168,20 @@ aflex_status aflex_prefill_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
     aflex_status s = validate_decoder_args(ctx, layers, kvs, num_layers, x_in, batch, x_out);
     if (s != AFLEX_OK) return s;
     const int H = layers[0].layer.hidden;
-    size_t need = 0;
+    PrefillWs w = {};
+    auto grow = [](size_t& a, size_t b) { if (b > a) a = b; };
     for (int l = 0; l < num_layers; ++l) {
         if (kvs[l].seq_lens_host)
             for (int b = 0; b < batch; ++b)
                 if (q_offsets_host[b + 1] - q_offsets_host[b] > kvs[l].seq_lens_host[b])
                     return set_error(ctx, AFLEX_ERR_INVALID_ARG, "prefill layers: sequence %d has more new tokens than cached tokens", b);
-        const PrefillWs w = prefill_ws(&layers[l], T, ctx->num_sms);
-        if (w.total > need) need = w.total;
+        const PrefillWs one = prefill_ws(&layers[l], T, ctx->num_sms);
+        grow(w.a_lin, one.a_lin); grow(w.rows_h, one.rows_h); grow(w.rows_qkv, one.rows_qkv); grow(w.rows_a, one.rows_a);
+        grow(w.f_total, one.f_total);
     }
-    if (need > ctx->ws_bytes)
-        return set_error(ctx, AFLEX_ERR_WORKSPACE, "prefill layers: need %zu workspace bytes, have %zu", need, ctx->ws_bytes);
+    w.total = w.a_lin + 5 * w.rows_h + w.rows_qkv + 2 * w.rows_a + w.f_total + 1024;
+    if (w.total > ctx->ws_bytes)
+        return set_error(ctx, AFLEX_ERR_WORKSPACE, "prefill layers: need %zu workspace bytes, have %zu", w.total, ctx->ws_bytes);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
     typedef __nv_bfloat16 bf;
     for (int l = 0; l < num_layers; ++l) {
@@ -1185,7 +1189,6 @@ aflex_status aflex_prefill_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
         const aflex_layer_desc* L = &d->layer;
         const int Hq = L->attn.num_q_heads, Hkv = L->attn.num_kv_heads, D = L->attn.head_dim;
         const int A = Hq * D, NQ = (Hq + 2 * Hkv) * D, I = L->inter, E = L->num_experts;
-        const PrefillWs w = prefill_ws(d, T, ctx->num_sms);
         char* p = ctx->ws;
         char* ws_lin = p; p += w.a_lin;
         bf* resid = reinterpret_cast<bf*>(p); p += w.rows_h;

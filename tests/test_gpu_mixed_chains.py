@@ -156,3 +156,27 @@ def test_sparse_chain_of_layers_with_different_heads_in_microbatches(cfgs):
         assert ctx.device_status() == AF.OK
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("cfgs", ATTENTION_MIXES, ids=lambda c: "-".join(x.name for x in c))
+def test_prefill_chain_of_layers_with_different_heads_is_its_layers_in_turn(cfgs):
+    c = Chain(cfgs)
+    new = [int(n) // 2 + 1 for n in c.lens.tolist()]
+    offs = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32)
+    x = torch.randn(int(offs[-1]), cfgs[0].hidden, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(DEV)
+    ctx = AF.Context(0, 1 << 30)
+    try:
+        got, want = torch.empty_like(x), x.clone()
+        c.reset(ctx)
+        for d, kv in zip(c.descs, c.kvs()):
+            ctx.prefill_layers([d], [kv], want, offs.to(DEV), offs, want)
+        after = c.state()
+        c.reset(ctx)
+        ctx.prefill_layers(c.descs, c.kvs(), x, offs.to(DEV), offs, got)
+        assert ctx.device_status() == AF.OK
+        # the same kernels in the same order; between two layers the chain normalises the sum before it is rounded
+        assert rows_apart(got, want) <= 4.3e-2 and np.isfinite(f64(want)).all()
+        n = 2 * len(cfgs)
+        assert all(rows_apart(a, b) <= 4.3e-2 for a, b in zip(c.state()[:n], after[:n]))
+    finally:
+        ctx.close()
