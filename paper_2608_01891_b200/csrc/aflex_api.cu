@@ -1231,12 +1231,12 @@ aflex_status aflex_prefill_layers(aflex_ctx* ctx, const aflex_decoder_desc* laye
 // ---- A/F pair: Attention side on ctx_a's device, FFN side on ctx_f's device ----------------
 // A-side workspace: [attn scratch | linear scratch | xn | qkv | q | a | o | h1 | back]
 // F-side workspace: [h1_f | xn2 | y | out_f | F scratch]
+// One layout for all layers of the chain: what F returned is read by the next layer.
 namespace {
 struct PairWs {
     size_t a_attn, a_lin, rows_h, rows_qkv, rows_a, a_total, f_scratch, f_total;
 };
-PairWs pair_ws(const aflex_decoder_desc* d, int max_batch, size_t a_attn, int num_sms) {
-    const DecoderWs w = decoder_ws(d, max_batch, a_attn, num_sms);
+PairWs pair_ws(const DecoderWs& w) {
     PairWs p;
     p.a_attn = w.a_attn; p.a_lin = w.a_lin; p.rows_h = w.rows_h; p.rows_qkv = w.rows_qkv; p.rows_a = w.rows_a;
     p.a_total = w.a_attn + w.a_lin + 4 * w.rows_h + w.rows_qkv + 2 * w.rows_a + 1024;
@@ -1253,7 +1253,7 @@ struct DeviceGuard {
 
 size_t aflex_af_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int ffn_side) {
     if (!layer || max_batch < 1) return 0;
-    const PairWs w = pair_ws(layer, max_batch, attn_workspace_bytes(&layer->layer.attn, 4096), query_num_sms());
+    const PairWs w = pair_ws(decoder_ws(layer, max_batch, attn_workspace_bytes(&layer->layer.attn, 4096), query_num_sms()));
     return ffn_side ? w.f_total : w.a_total;
 }
 
@@ -1265,16 +1265,11 @@ aflex_status aflex_af_decoder_layers(aflex_ctx* ca, aflex_ctx* cf, const aflex_d
     aflex_status s = validate_decoder_args(ca, layers, kvs, num_layers, x_in, batch, x_out);
     if (s != AFLEX_OK) return s;
     const int H = layers[0].layer.hidden;
-    size_t need_a = 0, need_f = 0;
-    for (int l = 0; l < num_layers; ++l) {
-        const PairWs w = pair_ws(&layers[l], batch, attn_workspace_bytes(&layers[l].layer.attn, attn_grid(ca)), ca->num_sms);
-        if (w.a_total > need_a) need_a = w.a_total;
-        if (w.f_total > need_f) need_f = w.f_total;
-    }
-    if (need_a > ca->ws_bytes)
-        return set_error(ca, AFLEX_ERR_WORKSPACE, "A/F pair: attention side needs %zu workspace bytes, has %zu", need_a, ca->ws_bytes);
-    if (need_f > cf->ws_bytes)
-        return set_error(ca, AFLEX_ERR_WORKSPACE, "A/F pair: FFN side needs %zu workspace bytes, has %zu", need_f, cf->ws_bytes);
+    const PairWs w = pair_ws(chain_ws(ca, layers, num_layers, batch));
+    if (w.a_total > ca->ws_bytes)
+        return set_error(ca, AFLEX_ERR_WORKSPACE, "A/F pair: attention side needs %zu workspace bytes, has %zu", w.a_total, ca->ws_bytes);
+    if (w.f_total > cf->ws_bytes)
+        return set_error(ca, AFLEX_ERR_WORKSPACE, "A/F pair: FFN side needs %zu workspace bytes, has %zu", w.f_total, cf->ws_bytes);
     int32_t offs[kMaxMicrobatches + 1];
     s = make_offsets(ca, batch, M, mb_offsets, offs);
     if (s != AFLEX_OK) return s;
@@ -1295,7 +1290,6 @@ aflex_status aflex_af_decoder_layers(aflex_ctx* ca, aflex_ctx* cf, const aflex_d
         const aflex_layer_desc* L = &d->layer;
         const int Hq = L->attn.num_q_heads, Hkv = L->attn.num_kv_heads, D = L->attn.head_dim;
         const int A = Hq * D, NQ = (Hq + 2 * Hkv) * D, I = L->inter, E = L->num_experts;
-        const PairWs w = pair_ws(d, batch, attn_workspace_bytes(&L->attn, attn_grid(ca)), ca->num_sms);
         char* p = ca->ws;
         char* ws_attn = p; p += w.a_attn;
         char* ws_lin = p; p += w.a_lin;

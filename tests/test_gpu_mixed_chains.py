@@ -180,3 +180,28 @@ def test_prefill_chain_of_layers_with_different_heads_is_its_layers_in_turn(cfgs
         assert all(rows_apart(a, b) <= 4.3e-2 for a, b in zip(c.state()[:n], after[:n]))
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("depth", [1, 2])
+@pytest.mark.parametrize("cfgs", ATTENTION_MIXES, ids=lambda c: "-".join(x.name for x in c))
+def test_pair_of_contexts_on_layers_with_different_heads_is_its_layers_in_turn(cfgs, depth):
+    """(Every layer hands rounded hidden states over, so the chain and its layers alone launch the same kernels on the same rows.)"""
+    c = Chain(cfgs)
+    ca, cf = AF.Context(0, 1 << 28), AF.Context(0, 1 << 28)
+    try:
+        got, want = torch.zeros_like(c.x), c.x.clone()
+        c.reset(ca)
+        for d, kv in zip(c.descs, c.kvs()):
+            AF.af_decoder_layers(ca, cf, [d], [kv], want, want, depth)
+        torch.cuda.synchronize()
+        after = c.state()
+        c.reset(ca)
+        AF.af_decoder_layers(ca, cf, c.descs, c.kvs(), c.x, got, depth)
+        torch.cuda.synchronize()
+        assert ca.device_status() == AF.OK and cf.device_status() == AF.OK
+        assert torch.equal(got, want) and torch.isfinite(got).all()
+        n = 2 * len(cfgs)
+        assert all(torch.equal(a, b) for a, b in zip(c.state()[:n], after[:n]))
+    finally:
+        ca.close()
+        cf.close()
