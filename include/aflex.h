@@ -416,7 +416,7 @@ AFLEX_API size_t aflex_decoder_workspace_bytes(const aflex_decoder_desc* layer, 
  *   PF:  out = h1 + FFN(rmsnorm(h1))      dense SwiGLU or top-k MoE (router logits from w_router)
  * x_in, x_out: bf16 [T][H], T = q_offsets_host[batch] (x_out may alias x_in); q_offsets: DEVICE i32 [batch + 1];
  * q_offsets_host: HOST copy.  One stream, no microbatching (both groups are compute-bound here).  Workspace from
- * aflex_prefill_workspace_bytes(layer, T).  Errors as aflex_decoder_layers and aflex_attn_prefill.
+ * aflex_prefill_workspace_bytes(layer, T); of layers that differ, as aflex_decoder_workspace_bytes.  Errors as aflex_decoder_layers and aflex_attn_prefill.
  */
 AFLEX_API aflex_status aflex_prefill_layers(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs,
                                             int num_layers, const void* x_in, int batch, const int32_t* q_offsets,
@@ -449,7 +449,8 @@ AFLEX_API aflex_status aflex_af_decoder_layers(aflex_ctx* ctx_a, aflex_ctx* ctx_
                                                const aflex_kv* kvs, int num_layers, const void* x_in, int batch,
                                                int microbatch_depth, const int32_t* mb_offsets, void* x_out,
                                                void* stream);
-/* Workspace bytes each side needs for aflex_af_decoder_layers (pure host computation). */
+/* Workspace bytes each side needs for aflex_af_decoder_layers (pure host computation); of layers that differ, as
+ * aflex_decoder_workspace_bytes. */
 AFLEX_API size_t aflex_af_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int ffn_side);
 
 /*
