@@ -562,6 +562,108 @@ AFLEX_API aflex_status aflex_decoder_layers_sparse(aflex_ctx* ctx, const aflex_d
                                                    void* x_out, void* stream);
 AFLEX_API size_t aflex_decoder_sparse_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int top_pages);
 
+/* ---- Caches of 16 or 8 bits, and drafted tokens ---------------------------------------------
+ *
+ * Decode attention is bound by reading the KV cache (the paper's Sections 1-2).  A cache of 8 bits halves those bytes, and
+ * drafted tokens share them: several rows of a sequence, in a row or as a tree, are verified with one reading of its cache
+ * (no counterpart in the paper; the operators' definitions are below).  A step is
+ *     aflex_cache_append  ->  aflex_attn_draft  ->  (the tokens are verified)  ->  aflex_cache_accept
+ * or aflex_draft_layers for the first two inside whole decoder layers.  aflex_cache_convert makes an 8-bit cache of a bf16 one that
+ * aflex_prefill_layers filled, and gives it back to the operators that read bf16.
+ *
+ * An 8-bit cache keeps one scale per token and KV head for K and one for V.  For a token's head x (bf16 values, keys after
+ * norm and rotation), in fp32, every step rounded to nearest:
+ *     a = max_d |x_d|,  scale = max(a * fl(1 / TOP), 2^-64),  code_d = round(x_d * fl(1 / scale)),   x_d stands for code_d * scale
+ * AFLEX_CACHE_INT8: TOP = 127, whole numbers; AFLEX_CACHE_E4M3: TOP = 448, e4m3 values.  A head with an infinite or NaN entry
+ * gets scale NaN and codes 0.  Scales of caches that other code fills may be any number >= 0.
+ */
+typedef enum { AFLEX_CACHE_BF16 = 0, AFLEX_CACHE_INT8 = 1, AFLEX_CACHE_E4M3 = 2 } aflex_cache_format;
+typedef struct {
+    aflex_kv kv;           /* as above; of an 8-bit cache k_cache, v_cache are the codes, one byte each, [num_pages][Hkv][page_size][D] */
+    int format;            /* aflex_cache_format */
+    float* k_scales;       /* fp32 [num_pages][Hkv][page_size], NULL for bf16 */
+    float* v_scales;
+} aflex_cache;
+
+/*
+ * Rows.  With draft == NULL, or draft->q_offsets == NULL, there is one row per sequence, the token being decoded at position
+ * seq_lens[b] - 1 (rows == batch).  With q_offsets (DEVICE i32 [batch + 1], starting at 0, not decreasing) row q_offsets[b] + i is
+ * drafted token i of sequence b, of m = q_offsets[b+1] - q_offsets[b]; its K/V slot is that of token seq_lens[b] - m + i, so that the
+ * cache holds the sequence's seq_lens[b] - m earlier tokens first and the drafted ones behind them.  m = 0 is allowed.  `rows` is the
+ * number of rows that the tensors have; rows from q_offsets[batch] on are padding and neither read nor written.
+ *   positions  DEVICE i32 [rows] or NULL: what the rotary embedding takes as each row's position (a tree's token: earlier tokens +
+ *              depth); NULL: that of its slot.
+ *   mask       DEVICE u32 [rows][mask_words] or NULL: bit j % 32 of word j / 32 tells whether the row sees drafted token j of its
+ *              sequence (its own token's bit included); tokens from 32 * mask_words on are not seen.  NULL: drafted token i sees
+ *              0 .. i.  Every row sees all earlier tokens.
+ * A sequence whose length is outside [1, 16 * max_pages_per_seq] or shorter than m raises AFLEX_ERR_BOUNDS in the status word.
+ */
+typedef struct {
+    const int32_t* q_offsets;
+    const int32_t* positions;
+    const uint32_t* mask;
+    int mask_words;        /* 1 .. 2^20 with a mask */
+} aflex_draft;
+
+/*
+ * The q / k / v step of the decoder layer on qkv bf16 [rows][(Hq + 2 Hkv) * D]: optional head norms and rotary embedding as in
+ * aflex_rope_append, q_out bf16 [rows][Hq][D], and the rows' K/V slots written in the cache's format.  Keys are formed in fp64 and
+ * rounded to fp32, then bf16, then quantised; queries in fp32.  No two rows may have the same slot.  A row of a sequence that raises
+ * AFLEX_ERR_BOUNDS writes nothing; one with a bad page id writes q_out only, and raises it too.
+ */
+AFLEX_API aflex_status aflex_cache_append(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* qkv, const aflex_cache* cache,
+                                          int batch, const aflex_draft* draft, int rows, const void* w_q_norm, const void* w_k_norm,
+                                          float rms_eps, float rope_theta, void* q_out, void* stream);
+
+/*
+ * Tokens first_token[b] .. seq_lens[b] - 1 (first_token: DEVICE i32 [batch], NULL = 0; lengths of src, 0 allowed) of every sequence
+ * from cache src into cache dst, one of which is bf16 and the other of 8 bits.  Each has its own page table; seq_lens of dst is not
+ * read.  bf16 -> 8 bits: as aflex_cache_append quantises.  8 bits -> bf16: code * scale in fp32, rounded.  Other slots of dst stay.
+ * A page with a bad id in either raises AFLEX_ERR_BOUNDS and is left out.  The caches must not overlap; of a destination page that
+ * several sequences share, all must hold the same tokens.
+ */
+AFLEX_API aflex_status aflex_cache_convert(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_cache* src, const aflex_cache* dst,
+                                           int batch, const int32_t* first_token, void* stream);
+
+/*
+ * Attention of every row over the tokens that it sees:
+ *     s_j = sm_scale * <q, K_j>,  out = sum_j softmax(s)_j V_j -> bf16,  lse = ln sum_j exp(s_j)
+ * q, out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  The cache's codes enter the products exactly; of an 8-bit cache a row's
+ * queries are scaled by a power of two (entries below 2^-31 of the head's largest lose precision).  fp32 scores and sums; the weights of
+ * V enter the second product as the sum of two bf16 values (bf16 cache), or (8 bits) in fp16 with the token's scale multiplied in, each off
+ * by at most half a step of fp16 or 2^-33 of the row's largest.
+ * A row that sees no token, or whose sequence raises AFLEX_ERR_BOUNDS, gets out 0 and lse -infinity.  A score of -infinity weighs
+ * nothing; a score of +infinity or NaN makes its head's out and lse NaN.  A token with infinite or NaN values, or such a scale, makes
+ * out of the rows that see it infinite or NaN, in the channel at least (their lse may be NaN too), and does not touch the others.
+ * A bad page id raises AFLEX_ERR_BOUNDS (page 0 is read instead).  Uses the workspace: aflex_attn_draft_workspace_bytes.
+ * The result is the same from run to run.
+ */
+AFLEX_API aflex_status aflex_attn_draft(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_cache* cache, int batch,
+                                        const aflex_draft* draft, int rows, void* out, float* lse, void* stream);
+AFLEX_API size_t aflex_attn_draft_workspace_bytes(const aflex_attn_desc* desc);
+
+/*
+ * After verification: of every sequence, drafted token path[b][k] moves to the place of drafted token k, for k < path_len[b], in all of
+ * `caches` (HOST array [num_caches], of one format: the layers' caches).  base i32 [batch]: tokens before the drafted ones; path i32
+ * [batch][path_stride], ascending; path_len i32 [batch], 0 allowed (all DEVICE).  K, V and their scales are moved as they are.  The
+ * sequence's new length is base[b] + path_len[b]; what lies behind is left.  A path that does not ascend, or leaves the seq_lens[b]
+ * tokens that the caches hold, raises AFLEX_ERR_BOUNDS and moves nothing of that sequence.  No page may belong to two of the sequences
+ * unless it is full of earlier tokens.
+ */
+AFLEX_API aflex_status aflex_cache_accept(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_cache* caches, int num_caches,
+                                          int batch, const int32_t* base, const int32_t* path, int path_stride, const int32_t* path_len,
+                                          void* stream);
+
+/*
+ * Whole decoder layers over the rows: as aflex_decoder_layers, with aflex_cache_append and aflex_attn_draft in the place of append and
+ * attention; caches: HOST array [num_layers].  x_in, x_out bf16 [rows][H] (x_out may alias x_in); padding rows are computed but no
+ * cache slot is written for them.  One stream.  Workspace from aflex_draft_workspace_bytes(layer, rows); of layers that differ, as
+ * aflex_decoder_workspace_bytes.
+ */
+AFLEX_API aflex_status aflex_draft_layers(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_cache* caches, int num_layers,
+                                          const void* x_in, int batch, const aflex_draft* draft, int rows, void* x_out, void* stream);
+AFLEX_API size_t aflex_draft_workspace_bytes(const aflex_decoder_desc* layer, int max_rows);
+
 /* ---- Host-side decisions of the data plane and the DVFS controller ------------------------
  *
  * Pure host computation on HOST pointers: nothing is launched and no GPU setting is read or

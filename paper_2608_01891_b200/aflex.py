@@ -29,6 +29,8 @@ EXPORTS = (
     "aflex_prefill_layers", "aflex_prefill_workspace_bytes",
     "aflex_rope_append_bounds", "aflex_page_bounds", "aflex_page_select", "aflex_attn_decode_pages",
     "aflex_decoder_layers_sparse", "aflex_decoder_sparse_workspace_bytes",
+    "aflex_cache_append", "aflex_cache_convert", "aflex_attn_draft", "aflex_attn_draft_workspace_bytes", "aflex_cache_accept",
+    "aflex_draft_layers", "aflex_draft_workspace_bytes",
     "aflex_eq2_layer_time", "aflex_curve_eval",
     "aflex_pipeline_makespan", "aflex_plan_microbatches", "aflex_dvfs_window", "aflex_dvfs_decode_step",
     "aflex_dvfs_prefill_pair",
@@ -52,6 +54,17 @@ class KeyBounds(ctypes.Structure):
 
 class PagePolicy(ctypes.Structure):
     _fields_ = [("top_pages", ctypes.c_int), ("sink_pages", ctypes.c_int), ("window_pages", ctypes.c_int)]
+
+
+CACHE_BF16, CACHE_INT8, CACHE_E4M3 = range(3)
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("kv", KV), ("format", ctypes.c_int), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class Draft(ctypes.Structure):
+    _fields_ = [("q_offsets", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("mask_words", ctypes.c_int)]
 
 
 class LayerDesc(ctypes.Structure):
@@ -186,6 +199,21 @@ def load_library() -> ctypes.CDLL:
                                                 ctypes.POINTER(PagePolicy), ci, vp, ci, ci, ctypes.POINTER(ctypes.c_int32), vp, vp]
     lib.aflex_decoder_sparse_workspace_bytes.restype = cs
     lib.aflex_decoder_sparse_workspace_bytes.argtypes = [ctypes.POINTER(DecoderDesc), ci, ci]
+    cache, draft, desc = ctypes.POINTER(Cache), ctypes.POINTER(Draft), ctypes.POINTER(AttnDesc)
+    lib.aflex_cache_append.restype = ci
+    lib.aflex_cache_append.argtypes = [vp, desc, vp, cache, ci, draft, ci, vp, vp, ctypes.c_float, ctypes.c_float, vp, vp]
+    lib.aflex_cache_convert.restype = ci
+    lib.aflex_cache_convert.argtypes = [vp, desc, cache, cache, ci, vp, vp]
+    lib.aflex_attn_draft.restype = ci
+    lib.aflex_attn_draft.argtypes = [vp, desc, vp, cache, ci, draft, ci, vp, vp, vp]
+    lib.aflex_attn_draft_workspace_bytes.restype = cs
+    lib.aflex_attn_draft_workspace_bytes.argtypes = [desc]
+    lib.aflex_cache_accept.restype = ci
+    lib.aflex_cache_accept.argtypes = [vp, desc, cache, ci, ci, vp, vp, ci, vp, vp]
+    lib.aflex_draft_layers.restype = ci
+    lib.aflex_draft_layers.argtypes = [vp, ctypes.POINTER(DecoderDesc), cache, ci, vp, ci, draft, ci, vp, vp]
+    lib.aflex_draft_workspace_bytes.restype = cs
+    lib.aflex_draft_workspace_bytes.argtypes = [ctypes.POINTER(DecoderDesc), ci]
     cd, dp, ip = ctypes.c_double, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int32)
     lib.aflex_eq2_layer_time.restype = cd
     lib.aflex_eq2_layer_time.argtypes = [cd, cd, cd, ci]
@@ -287,6 +315,78 @@ def make_page_bounds(codes: torch.Tensor, scales: torch.Tensor) -> KeyBounds:
     b._keep = (codes, scales)
     b._shape = (*codes.shape[:3], _where(codes, scales))
     return b
+
+
+_CACHE_FORMATS = {torch.bfloat16: CACHE_BF16, torch.int8: CACHE_INT8, torch.float8_e4m3fn: CACHE_E4M3}
+
+
+def empty_cache(num_pages: int, num_kv_heads: int, head_dim: int, dtype=torch.int8, device="cuda"):
+    """(k, v, k_scales, v_scales) of a cache of that type (bfloat16, int8 or float8_e4m3fn), zeroed; the scales are None for bfloat16."""
+    shape = (num_pages, num_kv_heads, 16, head_dim)
+    k, v = (torch.zeros(shape, dtype=torch.uint8 if dtype != _BF16 else _BF16, device=device) for _ in range(2))
+    if dtype == _BF16:
+        return k, v, None, None
+    ks, vs = (torch.zeros(shape[:3], dtype=torch.float32, device=device) for _ in range(2))
+    return k.view(dtype), v.view(dtype), ks, vs
+
+
+def make_cache(k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, seq_lens: torch.Tensor, k_scales: Optional[torch.Tensor] = None,
+               v_scales: Optional[torch.Tensor] = None, seq_lens_host: Optional[torch.Tensor] = None) -> Cache:
+    """A cache of bfloat16, int8 or float8_e4m3fn (told by k's type): k, v CUDA [num_pages,Hkv,16,D], of the 8-bit types with scales fp32 CUDA
+    [num_pages,Hkv,16]; the rest as make_kv.  The returned struct borrows the tensors: keep them alive."""
+    assert k.dtype in _CACHE_FORMATS and v.dtype == k.dtype and k.dim() == 4 and k.shape == v.shape, "k and v are not a cache of a supported type"
+    fmt = _CACHE_FORMATS[k.dtype]
+    assert (fmt == CACHE_BF16) == (k_scales is None) == (v_scales is None), "an 8-bit cache has scales, a bf16 cache none"
+    for x in (k_scales, v_scales):
+        assert x is None or (x.dtype == torch.float32 and x.shape == k.shape[:3]), "scales are not fp32 [num_pages][Hkv][16]"
+    assert page_table.dtype == torch.int32 and page_table.dim() == 2 and seq_lens.dtype == torch.int32
+    kv = KV(_ptr(k), _ptr(v), k.shape[0], _ptr(page_table), page_table.shape[1], _ptr(seq_lens), None)
+    if seq_lens_host is not None:
+        assert seq_lens_host.dtype == torch.int32 and seq_lens_host.device.type == "cpu" and seq_lens_host.numel() >= seq_lens.numel()
+        kv.seq_lens_host = _ptr(seq_lens_host)
+    c = Cache(kv, fmt, _ptr(k_scales), _ptr(v_scales))
+    c._keep = (k, v, page_table, seq_lens, k_scales, v_scales, seq_lens_host)
+    there = [t for t in c._keep[:6] if t is not None]
+    c._shape = (*k.shape[1:], min(page_table.shape[0], seq_lens.shape[0]), _where(*there))
+    return c
+
+
+def draft_rows(q_offsets: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None) -> Draft:
+    """Which sequence each row belongs to and what it sees (see the header): q_offsets i32 CUDA [B+1], positions i32 CUDA [rows], mask i32 (bits)
+    CUDA [rows, words].  The returned struct borrows the tensors: keep them alive."""
+    for t in (q_offsets, positions):
+        assert t is None or (t.dtype == torch.int32 and t.dim() == 1)
+    assert mask is None or (mask.dtype == torch.int32 and mask.dim() == 2 and mask.shape[1] >= 1)
+    d = Draft(_ptr(q_offsets), _ptr(positions), _ptr(mask), 0 if mask is None else mask.shape[1])
+    d._keep = (q_offsets, positions, mask)
+    return d
+
+
+def tree_rows(parents: Sequence[Sequence[int]]):
+    """Host helper: mask bits and depths of drafted trees.  parents[b][i] is the number of token i's parent among sequence b's drafted tokens, -1 for
+    one that follows the earlier tokens; a parent comes before its children.  -> (mask i32 CPU [rows, words], depth i32 CPU [rows]); a row's
+    position is the number of its sequence's earlier tokens plus its depth."""
+    rows, words = sum(len(p) for p in parents), max([1] + [(len(p) + 31) // 32 for p in parents])
+    sets, depth = [], []
+    for tree in parents:
+        first = len(sets)
+        for i, parent in enumerate(tree):
+            if not -1 <= parent < i:
+                raise ValueError(f"token {i}'s parent is {parent}: a parent comes before its children")
+            up = first + parent
+            sets.append((sets[up] if parent >= 0 else 0) | 1 << i)
+            depth.append(depth[up] + 1 if parent >= 0 else 0)
+    bits = [[(s >> 32 * w) & 0xffffffff for w in range(words)] for s in sets]
+    mask = torch.tensor([[x - (1 << 32) if x >= 1 << 31 else x for x in row] for row in bits], dtype=torch.int32).view(rows, words)
+    return mask, torch.tensor(depth, dtype=torch.int32)
+
+
+def attn_draft_workspace_bytes(desc: AttnDesc) -> int:
+    return int(load_library().aflex_attn_draft_workspace_bytes(ctypes.byref(desc)))
+
+
+def draft_workspace_bytes(layer: "DecoderDesc", max_rows: int) -> int:
+    return int(load_library().aflex_draft_workspace_bytes(ctypes.byref(layer), max_rows))
 
 
 def layer_desc(attn: AttnDesc, hidden: int, inter: int, w_o, w_gate, w_up, w_down, num_experts: int = 0,
@@ -674,6 +774,80 @@ class Context:
         self._check(self._lib.aflex_decoder_layers_sparse(self._h, la, ka, ba, PagePolicy(top_pages, sink_pages, window_pages), len(layers),
                                                           _ptr(x_in), x_in.shape[0], microbatch_depth, offs, _ptr(x_out),
                                                           self._stream_of(stream, x_in, x_out)))
+
+    # ---- caches of 16 or 8 bits, and drafted tokens.  draft: None for one row per sequence, else draft_rows(...) (see the header).
+    def _draft_args(self, desc: AttnDesc, cache: Cache, rows: int, draft: Optional[Draft], what: str):
+        """(batch, draft, tensors to find on the context's device), once they fit the cache and one another."""
+        kept = draft.__dict__.get("_keep", (None, None, None)) if draft is not None else (None, None, None)
+        batch = rows if kept[0] is None else kept[0].shape[0] - 1
+        assert kept[1] is None or kept[1].numel() >= rows, "fewer positions than rows"
+        assert kept[2] is None or kept[2].shape[0] >= rows, "a mask of fewer rows than " + what
+        self._match_cache(desc, cache, batch)
+        return batch, draft, kept
+
+    def _match_cache(self, desc: AttnDesc, cache: Cache, batch: int) -> None:
+        shape = cache.__dict__.get("_shape")
+        if shape is not None:
+            heads, tokens, dim, most, there = shape
+            assert heads == desc.num_kv_heads and tokens == desc.page_size and dim == desc.head_dim, "cache shape does not fit the descriptor"
+            assert batch <= most, "more sequences than page table rows or lengths"
+            assert there == self.device, "the cache is not on the context's device"
+
+    def cache_append(self, desc: AttnDesc, qkv, cache: Cache, q_out, w_q_norm, w_k_norm, rms_eps: float, rope_theta: float,
+                     draft: Optional[Draft] = None, stream=None) -> None:
+        """Head norms, rotary embedding and K/V append of the rows of qkv bf16 [rows, (Hq + 2 Hkv) * D] -> q_out bf16 [rows,Hq,D], the cache's slots."""
+        rows = qkv.shape[0]
+        hq, hkv, d = desc.num_q_heads, desc.num_kv_heads, desc.head_dim
+        assert qkv.dtype == _BF16 and qkv.numel() == rows * (hq + 2 * hkv) * d, "qkv is not bf16 [rows][(Hq + 2 Hkv) * D]"
+        assert q_out.dtype == _BF16 and q_out.numel() == rows * hq * d, "q_out is not bf16 [rows][Hq][D]"
+        for w in (w_q_norm, w_k_norm):
+            assert w is None or (w.dtype == _BF16 and w.numel() == d), "a head norm is not bf16 [D]"
+        batch, draft, kept = self._draft_args(desc, cache, rows, draft, "qkv")
+        self._check(self._lib.aflex_cache_append(self._h, desc, _ptr(qkv), cache, batch, draft, rows, _ptr(w_q_norm), _ptr(w_k_norm), rms_eps,
+                                                 rope_theta, _ptr(q_out), self._stream_of(stream, qkv, q_out, w_q_norm, w_k_norm, *kept)))
+
+    def cache_convert(self, desc: AttnDesc, src: Cache, dst: Cache, batch: int, first_token=None, stream=None) -> None:
+        """Tokens first_token[b] (i32 CUDA [B]; None: 0) .. of sequences 0 .. batch - 1 from one cache into the other: bf16 -> 8 bits or back."""
+        assert first_token is None or (first_token.dtype == torch.int32 and first_token.numel() >= batch)
+        self._match_cache(desc, src, batch)
+        self._match_cache(desc, dst, batch)
+        self._check(self._lib.aflex_cache_convert(self._h, desc, src, dst, batch, _ptr(first_token), self._stream_of(stream, first_token)))
+
+    def attn_draft(self, desc: AttnDesc, q, cache: Cache, out, lse=None, draft: Optional[Draft] = None, stream=None) -> None:
+        """Attention of every row of q bf16 [rows,Hq,D] over the tokens of its sequence that it sees -> out, lse fp32 [rows,Hq]."""
+        rows = q.shape[0]
+        n = rows * desc.num_q_heads
+        assert q.dtype == _BF16 and q.numel() == n * desc.head_dim, "q is not bf16 [rows][Hq][D]"
+        assert out.dtype == _BF16 and out.numel() == n * desc.head_dim, "out is not bf16 [rows][Hq][D]"
+        assert lse is None or (lse.dtype == torch.float32 and lse.numel() == n), "lse is not fp32 [rows][Hq]"
+        batch, draft, kept = self._draft_args(desc, cache, rows, draft, "q")
+        self._check(self._lib.aflex_attn_draft(self._h, desc, _ptr(q), cache, batch, draft, rows, _ptr(out), _ptr(lse),
+                                               self._stream_of(stream, q, out, lse, *kept)))
+
+    def cache_accept(self, desc: AttnDesc, caches: Sequence[Cache], batch: int, base, path, path_len, stream=None) -> None:
+        """Moves drafted token path[b, k] of every sequence to the place of drafted token k (k < path_len[b]) in all of the caches: base and path_len
+        i32 CUDA [B], path i32 CUDA [B, n]."""
+        assert len(caches) >= 1
+        assert base.dtype == torch.int32 and base.numel() >= batch and path_len.dtype == torch.int32 and path_len.numel() >= batch
+        assert path.dtype == torch.int32 and path.dim() == 2 and path.shape[0] >= batch
+        for c in caches:
+            self._match_cache(desc, c, batch)
+        ca = caches if isinstance(caches, ctypes.Array) else (Cache * len(caches))(*caches)
+        self._check(self._lib.aflex_cache_accept(self._h, desc, ca, len(caches), batch, _ptr(base), _ptr(path), path.shape[1], _ptr(path_len),
+                                                 self._stream_of(stream, base, path, path_len)))
+
+    def draft_layers(self, layers: Sequence[DecoderDesc], caches: Sequence[Cache], x_in, x_out, draft: Optional[Draft] = None, stream=None) -> None:
+        """Runs len(layers) whole decoder layers over drafted tokens (or one token per sequence): x_in bf16 [rows,H] -> x_out; caches[l] is layer l's
+        cache (the rows' slots are written)."""
+        assert len(layers) == len(caches) and len(layers) >= 1
+        rows = x_in.shape[0]
+        for x in (x_in, x_out):
+            assert x.dtype == _BF16 and x.numel() == rows * layers[0].layer.hidden, "hidden states are not bf16 [rows][H]"
+        for d, c in zip(layers, caches):
+            batch, draft, kept = self._draft_args(d.layer.attn, c, rows, draft, "x_in")
+        la, ca = (DecoderDesc * len(layers))(*layers), (Cache * len(caches))(*caches)
+        self._check(self._lib.aflex_draft_layers(self._h, la, ca, len(layers), _ptr(x_in), batch, draft, rows, _ptr(x_out),
+                                                 self._stream_of(stream, x_in, x_out, *kept)))
 
     def _stream_of(self, stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> int:
         """The given stream, or the current one of the ctx's device (without building a Stream object: these calls last microseconds),

@@ -47,10 +47,10 @@ static EncodeTiledFn get_encode_fn() {
 // by everything the encoding depends on (address, extents, stride, box, promotion).
 namespace {
 struct TmapKey {
-    const void* base; uint64_t rows, cols, stride; uint32_t box_rows, box_cols; bool promote;
+    const void* base; uint64_t rows, cols, stride; uint32_t box_rows, box_cols; bool promote, bytes;
     bool operator==(const TmapKey& o) const {
         return base == o.base && rows == o.rows && cols == o.cols && stride == o.stride && box_rows == o.box_rows &&
-               box_cols == o.box_cols && promote == o.promote;
+               box_cols == o.box_cols && promote == o.promote && bytes == o.bytes;
     }
 };
 struct TmapCache {
@@ -62,28 +62,36 @@ struct TmapCache {
 thread_local TmapCache g_tmap_cache;
 }  // namespace
 
-bool encode_tmap_2d_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t row_stride_bytes,
-                         uint32_t box_rows, uint32_t box_cols, bool promote_l2_256) {
+static bool encode_tmap(CUtensorMap* out, const TmapKey& key, CUtensorMapDataType type, CUtensorMapSwizzle swizzle) {
     TmapCache& cache = g_tmap_cache;
-    const TmapKey key{base, rows, cols, row_stride_bytes, box_rows, box_cols, promote_l2_256};
     for (int i = 0; i < cache.used; ++i) {
         if (cache.keys[i] == key) { *out = cache.maps[i]; return true; }
     }
     EncodeTiledFn fn = get_encode_fn();
     if (!fn) return false;
-    cuuint64_t dims[2] = {cols, rows};
-    cuuint64_t strides[1] = {row_stride_bytes};
-    cuuint32_t box[2] = {box_cols, box_rows};
+    cuuint64_t dims[2] = {key.cols, key.rows};
+    cuuint64_t strides[1] = {key.stride};
+    cuuint32_t box[2] = {key.box_cols, key.box_rows};
     cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                    promote_l2_256 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+    CUresult r = fn(out, type, 2, const_cast<void*>(key.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                    key.promote ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B : CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return false;
     const int slot = cache.used < TmapCache::kEntries ? cache.used++ : (cache.next = (cache.next + 1) % TmapCache::kEntries);
     cache.keys[slot] = key;
     cache.maps[slot] = *out;
     return true;
+}
+
+bool encode_tmap_2d_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t row_stride_bytes,
+                         uint32_t box_rows, uint32_t box_cols, bool promote_l2_256) {
+    return encode_tmap(out, TmapKey{base, rows, cols, row_stride_bytes, box_rows, box_cols, promote_l2_256, false},
+                       CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+bool encode_tmap_rows_u8(CUtensorMap* out, const void* base, uint64_t rows, uint32_t row_bytes, uint32_t box_rows) {
+    return encode_tmap(out, TmapKey{base, rows, row_bytes, row_bytes, box_rows, row_bytes, true, true}, CU_TENSOR_MAP_DATA_TYPE_UINT8,
+                       row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -398,7 +406,7 @@ static const char* kKernelNames[kKKindCount] = {
     "attn_decode", "linear_gemm", "down_gemm", "gateup_gemm", "router_logits",
     "moe_route", "moe_gather", "moe_gateup_gemm", "moe_down_gemm", "moe_combine",
     "add_rmsnorm", "qkv_gemm", "rope_append", "attn_prefill", "gemm_chain", "append_bounds", "page_bounds",
-    "page_select", "attn_pages"};
+    "page_select", "attn_pages", "cache_append", "cache_convert", "cache_accept", "attn_draft"};
 
 int aflex_num_kernel_kinds(void) { return kKKindCount; }
 
@@ -749,12 +757,13 @@ DecoderWs decoder_ws(const aflex_decoder_desc* d, int max_batch, size_t a_attn, 
     w.total = w.a_attn + w.a_lin + 5 * w.rows_h + w.rows_qkv + 2 * w.rows_a + w.f_total + 1024;
     return w;
 }
-// The layout of a chain of layers.
-DecoderWs chain_ws(const aflex_ctx* ctx, const aflex_decoder_desc* layers, int num_layers, int batch) {
+// The layout of a chain of layers; draft: of aflex_draft_layers, whose attention kernel has other scratch.
+DecoderWs chain_ws(const aflex_ctx* ctx, const aflex_decoder_desc* layers, int num_layers, int batch, bool draft = false) {
     DecoderWs c = {};
     auto grow = [](size_t& a, size_t b) { if (b > a) a = b; };
     for (int l = 0; l < num_layers; ++l) {
-        const DecoderWs w = decoder_ws(&layers[l], batch, attn_workspace_bytes(&layers[l].layer.attn, attn_grid(ctx)), ctx->num_sms);
+        const aflex_attn_desc* a = &layers[l].layer.attn;
+        const DecoderWs w = decoder_ws(&layers[l], batch, draft ? attn_draft_workspace_bytes(a, ctx->num_sms) : attn_workspace_bytes(a, attn_grid(ctx)), ctx->num_sms);
         grow(c.a_attn, w.a_attn); grow(c.a_lin, w.a_lin); grow(c.rows_h, w.rows_h); grow(c.rows_qkv, w.rows_qkv);
         grow(c.rows_a, w.rows_a); grow(c.f_total, w.f_total);
     }
@@ -766,6 +775,11 @@ DecoderWs chain_ws(const aflex_ctx* ctx, const aflex_decoder_desc* layers, int n
 size_t aflex_decoder_workspace_bytes(const aflex_decoder_desc* layer, int max_batch) {
     if (!layer || max_batch < 1) return 0;
     return decoder_ws(layer, max_batch, attn_workspace_bytes(&layer->layer.attn, 4096), query_num_sms()).total;
+}
+
+size_t aflex_draft_workspace_bytes(const aflex_decoder_desc* layer, int max_rows) {
+    if (!layer || max_rows < 1) return 0;
+    return decoder_ws(layer, max_rows, attn_draft_workspace_bytes(&layer->layer.attn, query_num_sms()), query_num_sms()).total;
 }
 
 size_t aflex_decoder_sparse_workspace_bytes(const aflex_decoder_desc* layer, int max_batch, int top_pages) {
@@ -896,7 +910,114 @@ aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc
                                     reinterpret_cast<cudaStream_t>(stream));
 }
 
+// ---- caches of 16 or 8 bits, and drafted tokens ------------------------------------------------
 namespace {
+aflex_status validate_cache(aflex_ctx* ctx, const char* what, const aflex_attn_desc* desc, const aflex_cache* cache, int batch,
+                            const void* in, const void* out) {
+    if (!ctx) return AFLEX_ERR_INVALID_ARG;
+    if (!cache) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: null cache", what);
+    aflex_status s = validate_attn(ctx, desc, in, &cache->kv, batch, out);
+    if (s == AFLEX_OK) s = validate_pages(ctx, what, &cache->kv);
+    if (s != AFLEX_OK) return s;
+    if (cache->format != AFLEX_CACHE_BF16 && cache->format != AFLEX_CACHE_INT8 && cache->format != AFLEX_CACHE_E4M3)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: cache format %d", what, cache->format);
+    if (cache->format != AFLEX_CACHE_BF16 && (!cache->k_scales || !cache->v_scales))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: an 8-bit cache needs scales", what);
+    if (cache->format == AFLEX_CACHE_BF16 && (cache->k_scales || cache->v_scales))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: a bf16 cache has no scales", what);
+    if (!aligned16(cache->k_scales) || !aligned16(cache->v_scales))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: pointers must be 16-byte aligned", what);
+    return AFLEX_OK;
+}
+aflex_status validate_draft(aflex_ctx* ctx, const char* what, const aflex_draft* draft, int batch, int rows) {
+    if (rows < 1 || ((!draft || !draft->q_offsets) && rows != batch))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: rows = %d (batch %d; without q_offsets one row per sequence)", what, rows, batch);
+    if (draft && draft->mask && (draft->mask_words < 1 || draft->mask_words > 1 << 20))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: mask_words = %d (1 .. 2^20)", what, draft->mask_words);
+    return AFLEX_OK;
+}
+}  // namespace
+
+aflex_status aflex_cache_append(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* qkv, const aflex_cache* cache, int batch,
+                                const aflex_draft* draft, int rows, const void* w_q_norm, const void* w_k_norm, float rms_eps,
+                                float rope_theta, void* q_out, void* stream) {
+    aflex_status s = validate_cache(ctx, "cache append", desc, cache, batch, qkv, q_out);
+    if (s == AFLEX_OK) s = validate_draft(ctx, "cache append", draft, batch, rows);
+    if (s != AFLEX_OK) return s;
+    if (!(rope_theta > 0.f) || !(rms_eps >= 0.f))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "cache append: rope_theta must be > 0 and rms_eps >= 0");
+    CtxDevice dev(ctx);
+    return cache_append_launch(ctx, desc, qkv, cache, batch, draft, rows, w_q_norm, w_k_norm, rms_eps, rope_theta, q_out,
+                               reinterpret_cast<cudaStream_t>(stream));
+}
+
+aflex_status aflex_cache_convert(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_cache* src, const aflex_cache* dst, int batch,
+                                 const int32_t* first_token, void* stream) {
+    aflex_status s = ctx && (!src || !dst) ? set_error(ctx, AFLEX_ERR_INVALID_ARG, "cache convert: null cache") : AFLEX_OK;
+    if (s == AFLEX_OK) s = validate_cache(ctx, "cache convert", desc, src, batch, src ? src->kv.k_cache : nullptr, src ? src->kv.v_cache : nullptr);
+    if (s != AFLEX_OK) return s;
+    aflex_cache to = *dst;                                    // (seq_lens of dst is not read, and may be null)
+    to.kv.seq_lens = src->kv.seq_lens;
+    to.kv.seq_lens_host = nullptr;
+    s = validate_cache(ctx, "cache convert", desc, &to, batch, to.kv.k_cache, to.kv.v_cache);
+    if (s != AFLEX_OK) return s;
+    if ((src->format == AFLEX_CACHE_BF16) == (dst->format == AFLEX_CACHE_BF16))
+        return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "cache convert: one cache has to be bf16 and the other of 8 bits");
+    CtxDevice dev(ctx);
+    return cache_convert_launch(ctx, desc, src, dst, batch, first_token, reinterpret_cast<cudaStream_t>(stream));
+}
+
+aflex_status aflex_attn_draft(aflex_ctx* ctx, const aflex_attn_desc* desc, const void* q, const aflex_cache* cache, int batch,
+                              const aflex_draft* draft, int rows, void* out, float* lse, void* stream) {
+    aflex_status s = validate_cache(ctx, "draft attention", desc, cache, batch, q, out);
+    if (s == AFLEX_OK) s = validate_draft(ctx, "draft attention", draft, batch, rows);
+    if (s != AFLEX_OK) return s;
+    CtxDevice dev(ctx);
+    return attn_draft_launch(ctx, desc, q, cache, batch, draft, rows, out, lse, ctx->ws, ctx->ws_bytes, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t aflex_attn_draft_workspace_bytes(const aflex_attn_desc* desc) {
+    if (!desc || (desc->head_dim != 64 && desc->head_dim != 128)) return 0;
+    return attn_draft_workspace_bytes(desc, query_num_sms());
+}
+
+aflex_status aflex_cache_accept(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_cache* caches, int num_caches, int batch,
+                                const int32_t* base, const int32_t* path, int path_stride, const int32_t* path_len, void* stream) {
+    if (!ctx) return AFLEX_ERR_INVALID_ARG;
+    if (!caches || num_caches < 1 || !base || !path || !path_len || path_stride < 1)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "cache accept: null argument, num_caches < 1 or path_stride < 1");
+    for (int l = 0; l < num_caches; ++l) {
+        aflex_status s = validate_cache(ctx, "cache accept", desc, &caches[l], batch, caches[l].kv.k_cache, caches[l].kv.v_cache);
+        if (s != AFLEX_OK) return s;
+        if (caches[l].format != caches[0].format) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "cache accept: caches of different formats");
+    }
+    CtxDevice dev(ctx);
+    return cache_accept_launch(ctx, desc, caches, num_caches, batch, base, path, path_stride, path_len, reinterpret_cast<cudaStream_t>(stream));
+}
+
+namespace {
+// One layer's weights and sizes, on `rows` rows.
+aflex_status validate_decoder_layer(aflex_ctx* ctx, const aflex_decoder_desc* layers, int l, int rows) {
+    const aflex_decoder_desc* d = &layers[l];
+    const aflex_layer_desc* L = &d->layer;
+    const int H = layers[0].layer.hidden;
+    aflex_status s = AFLEX_OK;
+    if (L->hidden != H) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: layer %d has another hidden size", l);
+    if (!d->w_qkv || !d->w_ln_attn || !d->w_ln_ffn || !L->w_o || !L->w_gate || !L->w_up || !L->w_down)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: layer %d has a null weight", l);
+    if (!aligned16(d->w_qkv) || !aligned16(d->w_ln_attn) || !aligned16(d->w_ln_ffn) || !aligned16(L->w_o) ||
+        !aligned16(L->w_gate) || !aligned16(L->w_up) || !aligned16(L->w_down))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: pointers must be 16-byte aligned");
+    if (!(d->rope_theta > 0.f) || !(d->rms_eps >= 0.f))
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: rope_theta must be > 0 and rms_eps >= 0");
+    if (L->num_experts == 0) s = validate_ffn_dims(ctx, rows, H, L->inter);
+    else {
+        s = validate_moe(ctx, rows, H, L->inter, L->num_experts, L->top_k);
+        if (s == AFLEX_OK && !L->w_router) s = set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: MoE layer %d needs w_router", l);
+    }
+    return s;
+}
+
 // Argument checks shared by the single-GPU chain and the A/F pair.  Errors are recorded on ctx.
 aflex_status validate_decoder_args(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs, int num_layers,
                                    const void* x_in, int batch, const void* x_out) {
@@ -904,25 +1025,9 @@ aflex_status validate_decoder_args(aflex_ctx* ctx, const aflex_decoder_desc* lay
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: null argument or num_layers < 1");
     if (!aligned16(x_in) || !aligned16(x_out))
         return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: pointers must be 16-byte aligned");
-    const int H = layers[0].layer.hidden;
     for (int l = 0; l < num_layers; ++l) {
-        const aflex_decoder_desc* d = &layers[l];
-        const aflex_layer_desc* L = &d->layer;
-        aflex_status s = validate_attn(ctx, &L->attn, x_in, &kvs[l], batch, x_out);
-        if (s != AFLEX_OK) return s;
-        if (L->hidden != H) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: layer %d has another hidden size", l);
-        if (!d->w_qkv || !d->w_ln_attn || !d->w_ln_ffn || !L->w_o || !L->w_gate || !L->w_up || !L->w_down)
-            return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: layer %d has a null weight", l);
-        if (!aligned16(d->w_qkv) || !aligned16(d->w_ln_attn) || !aligned16(d->w_ln_ffn) || !aligned16(L->w_o) ||
-            !aligned16(L->w_gate) || !aligned16(L->w_up) || !aligned16(L->w_down))
-            return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: pointers must be 16-byte aligned");
-        if (!(d->rope_theta > 0.f) || !(d->rms_eps >= 0.f))
-            return set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: rope_theta must be > 0 and rms_eps >= 0");
-        if (L->num_experts == 0) s = validate_ffn_dims(ctx, batch, H, L->inter);
-        else {
-            s = validate_moe(ctx, batch, H, L->inter, L->num_experts, L->top_k);
-            if (s == AFLEX_OK && !L->w_router) s = set_error(ctx, AFLEX_ERR_INVALID_ARG, "decoder layers: MoE layer %d needs w_router", l);
-        }
+        aflex_status s = validate_attn(ctx, &layers[l].layer.attn, x_in, &kvs[l], batch, x_out);
+        if (s == AFLEX_OK) s = validate_decoder_layer(ctx, layers, l, batch);
         if (s != AFLEX_OK) return s;
     }
     return AFLEX_OK;
@@ -947,15 +1052,18 @@ aflex_status make_offsets(aflex_ctx* ctx, int batch, int M, const int32_t* mb_of
 }  // namespace
 
 namespace {
-// The chain with dense attention (bounds == nullptr), or with page-sparse attention and the layers' key bounds.
+// Caches and rows of aflex_draft_layers.
+struct DraftChain { const aflex_cache* caches; const aflex_draft* draft; int sequences; };
+// The chain with dense attention, with page-sparse attention and the layers' key bounds (bounds != nullptr), or over rows of drafted
+// tokens (drafted != nullptr: validated by the caller, `batch` is the number of rows, M = 1 and kvs is not looked at).
 aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_kv* kvs, const aflex_key_bounds* bounds,
                                 const aflex_page_policy* policy, int num_layers, const void* x_in, int batch, int M,
-                                const int32_t* mb_offsets, void* x_out, void* stream) {
+                                const int32_t* mb_offsets, void* x_out, void* stream, const DraftChain* drafted = nullptr) {
     if (!ctx) return AFLEX_ERR_INVALID_ARG;
-    aflex_status s = validate_decoder_args(ctx, layers, kvs, num_layers, x_in, batch, x_out);
+    aflex_status s = drafted ? AFLEX_OK : validate_decoder_args(ctx, layers, kvs, num_layers, x_in, batch, x_out);
     if (s != AFLEX_OK) return s;
     const int H = layers[0].layer.hidden;
-    const DecoderWs w = chain_ws(ctx, layers, num_layers, batch);
+    const DecoderWs w = chain_ws(ctx, layers, num_layers, batch, drafted != nullptr);
     size_t lists_bytes = 0;
     for (int l = 0; l < num_layers && bounds; ++l) {
         const size_t b = page_lists_bytes(&layers[l].layer.attn, batch, policy->top_pages);
@@ -1037,11 +1145,16 @@ aflex_status decoder_layers_run(aflex_ctx* ctx, const aflex_decoder_desc* layers
                 s = linear_launch(ctx, xn + oh, d->w_qkv, rows, H, NQ, qkv_i, ws_lin, w.a_lin, sa, kKQkvGemm, ctx->counters_a);
                 if (s != AFLEX_OK) return s;
             }
-            aflex_kv kvi = kvs[l];
-            kvi.page_table = kvs[l].page_table + (size_t)r0 * kvs[l].max_pages_per_seq;
-            kvi.seq_lens = kvs[l].seq_lens + r0;
-            kvi.seq_lens_host = kvs[l].seq_lens_host ? kvs[l].seq_lens_host + r0 : nullptr;
-            if (bounds) {
+            aflex_kv kvi = drafted ? drafted->caches[l].kv : kvs[l];
+            kvi.page_table += (size_t)r0 * kvi.max_pages_per_seq;
+            kvi.seq_lens += r0;
+            if (kvi.seq_lens_host) kvi.seq_lens_host += r0;
+            if (drafted) {
+                s = cache_append_launch(ctx, &L->attn, qkv_i, &drafted->caches[l], drafted->sequences, drafted->draft, rows, d->w_q_norm, d->w_k_norm,
+                                        d->rms_eps, d->rope_theta, q_i, sa);
+                if (s == AFLEX_OK)
+                    s = attn_draft_launch(ctx, &L->attn, q_i, &drafted->caches[l], drafted->sequences, drafted->draft, rows, a_i, nullptr, ws_attn, w.a_attn, sa);
+            } else if (bounds) {
                 int32_t* list = lists + (size_t)r0 * Hkv * policy->top_pages;
                 int32_t* count = counts + (size_t)r0 * Hkv;
                 s = rope_append_bounds_launch(ctx, &L->attn, qkv_i, &kvi, &bounds[l], rows, nullptr, rows, d->w_q_norm, d->w_k_norm,
@@ -1122,6 +1235,22 @@ aflex_status aflex_decoder_layers_sparse(aflex_ctx* ctx, const aflex_decoder_des
     if (s != AFLEX_OK) return s;
     CtxDevice dev(ctx);
     return decoder_layers_run(ctx, layers, kvs, bounds, policy, num_layers, x_in, batch, M, mb_offsets, x_out, stream);
+}
+
+aflex_status aflex_draft_layers(aflex_ctx* ctx, const aflex_decoder_desc* layers, const aflex_cache* caches, int num_layers,
+                                const void* x_in, int batch, const aflex_draft* draft, int rows, void* x_out, void* stream) {
+    if (!ctx) return AFLEX_ERR_INVALID_ARG;
+    if (!layers || !caches || !x_in || !x_out || num_layers < 1)
+        return set_error(ctx, AFLEX_ERR_INVALID_ARG, "draft layers: null argument or num_layers < 1");
+    aflex_status s = validate_draft(ctx, "draft layers", draft, batch, rows);
+    for (int l = 0; l < num_layers && s == AFLEX_OK; ++l) {
+        s = validate_cache(ctx, "draft layers", &layers[l].layer.attn, &caches[l], batch, x_in, x_out);
+        if (s == AFLEX_OK) s = validate_decoder_layer(ctx, layers, l, rows);
+    }
+    if (s != AFLEX_OK) return s;
+    CtxDevice dev(ctx);
+    const DraftChain drafted = {caches, draft, batch};
+    return decoder_layers_run(ctx, layers, nullptr, nullptr, nullptr, num_layers, x_in, rows, 1, nullptr, x_out, stream, &drafted);
 }
 
 // ---- whole decoder layers over the tokens being prefilled -----------------------------------

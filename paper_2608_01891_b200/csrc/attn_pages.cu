@@ -7,46 +7,11 @@
 
 #include "internal.h"
 #include "ptx.cuh"
+#include "rows.cuh"
 
 namespace aflex {
 
 namespace {
-
-// A plain load, for what a preceding kernel may have written (queries, lists, lengths, bounds): these kernels may have started before that
-// one was done and wait for it, so the read-only path (ld.global.nc) would not be bound to see its stores.
-template <typename V> __device__ __forceinline__ V fetch(const V* p) { return *p; }
-
-constexpr int kPageTokens = 16;
-constexpr float kLowest = -3.402823466e38f;     // the lowest finite value: where running maxima start, so that no score lies below
-
-// Sequence of a row, and how many of the sequence's rows follow it; every lane of a warp takes part.  Rows behind the last
-// sequence's are padding: nothing is to be read, written or reported for them.
-struct RowSeq { int b, back; bool padding; };
-__device__ __forceinline__ RowSeq locate_row(int row, const int32_t* q_offsets, int batch) {
-    RowSeq at;
-    at.b = row; at.back = 0; at.padding = false;
-    if (q_offsets != nullptr) {
-        // largest b with q_offsets[b] <= row: the lanes look at 32 sequences at a time (one load's latency for up to 32)
-        const int lane = threadIdx.x & 31, end = fetch(q_offsets + batch);
-        int lo = 0, span = batch;
-        while (span > 1) {
-            const int step = (span + 31) / 32, i = lane * step;
-            const unsigned le = __ballot_sync(0xffffffffu, i < span && fetch(q_offsets + lo + (i < span ? i : 0)) <= row);
-            const int skip = max(__popc(le) - 1, 0) * step;
-            lo += skip;
-            span = min(step, span - skip);
-        }
-        at.b = lo;
-        at.back = fetch(q_offsets + lo + 1) - 1 - row;
-        at.padding = row >= end;
-    }
-    return at;
-}
-// Position of the row in its sequence of `len` tokens; -1 where the inputs give none.
-__device__ __forceinline__ int row_position(const RowSeq& at, int len, int max_pages) {
-    const int pos = len - 1 - at.back;
-    return !at.padding && at.back >= 0 && pos >= 0 && len <= max_pages * kPageTokens ? pos : -1;
-}
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }

@@ -27,7 +27,7 @@ enum KernelKind {
     kKAttnDecode = 0, kKLinearGemm, kKDownGemm, kKGateUpGemm, kKRouterLogits,
     kKMoeRoute, kKMoeGather, kKMoeGateUpGemm, kKMoeDownGemm, kKMoeCombine,
     kKAddRmsNorm, kKQkvGemm, kKRopeAppend, kKAttnPrefill, kKGemmChain, kKAppendBounds, kKPageBounds,
-    kKPageSelect, kKAttnPages, kKKindCount
+    kKPageSelect, kKAttnPages, kKCacheAppend, kKCacheConvert, kKCacheAccept, kKAttnDraft, kKKindCount
 };
 constexpr int kProfMaxSlots = 8192;
 struct ProfSlot { cudaEvent_t start, stop; int kind; };
@@ -63,6 +63,7 @@ struct aflex_ctx {
     int select_clusters[2][2][9] = {};           // clusters of 2 .. 8 CTAs of page_select_rows_kernel (16 warps, 8 warps) that fit it at once
     bool bounds_attr_set[2] = {false, false};    // ... for page_bounds_kernel<64 / 128>
     bool pages_attr_set[2] = {false, false};     // ... for attn_decode_pages_kernel<64 / 128>
+    bool draft_attr_set[2][3] = {};              // ... for the kernels of attn_draft.cu [head size][format]
     int pages_clusters[2][9] = {};               // its clusters of 2 .. 8 CTAs that fit this device at once
     float rope_theta = 0.f;       // what rope_freq and rope_step (cosine, sine of one position's angle) were made for
     int rope_dim = 0;
@@ -135,6 +136,8 @@ inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 // 128-byte swizzle (box_cols * 2 must be 128).  Returns false on driver error.
 bool encode_tmap_2d_bf16(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t row_stride_bytes,
                          uint32_t box_rows, uint32_t box_cols, bool promote_l2_256);
+// The same for rows of bytes, boxes of whole rows of 128 or 64 bytes with the swizzle of that width.
+bool encode_tmap_rows_u8(CUtensorMap* out, const void* base, uint64_t rows, uint32_t row_bytes, uint32_t box_rows);
 
 // ---- attention (attn_decode.cu)
 int attn_grid(const aflex_ctx* ctx);                                    // persistent CTAs per launch
@@ -211,6 +214,23 @@ aflex_status add_rmsnorm_launch(aflex_ctx* ctx, const void* res, const void* add
 aflex_status rope_append_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* qkv, const aflex_kv* kv, int batch,
                                 const void* w_qn, const void* w_kn, float eps, float theta, void* q_out, cudaStream_t st,
                                 const int32_t* q_offsets = nullptr, int rows = 0);
+
+// The frequencies of rope_theta and a head size in the ctx, as long as they stay the same (a few microseconds of host time for a launch of
+// as many); kv_cache.cu.
+void rope_tables(aflex_ctx* ctx, float theta, int head_dim);
+
+// ---- caches of 16 or 8 bits (kv_cache.cu) and attention of drafted tokens over them (attn_draft.cu).  draft == nullptr: one row per
+// sequence (rows == batch).
+aflex_status cache_append_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* qkv, const aflex_cache* cache, int batch,
+                                 const aflex_draft* draft, int rows, const void* w_qn, const void* w_kn, float eps, float theta,
+                                 void* q_out, cudaStream_t st);
+aflex_status cache_convert_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const aflex_cache* src, const aflex_cache* dst, int batch,
+                                  const int32_t* first_token, cudaStream_t st);
+aflex_status cache_accept_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const aflex_cache* caches, int num_caches, int batch,
+                                 const int32_t* base, const int32_t* path, int path_stride, const int32_t* path_len, cudaStream_t st);
+size_t attn_draft_workspace_bytes(const aflex_attn_desc* d, int num_sms);
+aflex_status attn_draft_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_cache* cache, int batch,
+                               const aflex_draft* draft, int rows, void* out, float* lse, char* ws, size_t ws_bytes, cudaStream_t st);
 
 // ---- page-sparse decode attention: key bounds (page_bounds.cu), selection and attention (attn_pages.cu).  q_offsets == nullptr:
 // one row per sequence (rows == batch).

@@ -18,26 +18,14 @@
 
 #include "internal.h"
 #include "ptx.cuh"
+#include "rows.cuh"
 
 namespace aflex {
 
 namespace {
 
-// A plain load, for what a preceding kernel may have written (projections, lengths): these kernels may have started before that
-// one was done and wait for it, so the read-only path (ld.global.nc) would not be bound to see its stores.
-template <typename V> __device__ __forceinline__ V fetch(const V* p) { return *p; }
-
 constexpr int kBoundsWarps = 8;
 constexpr int kBoundsThreads = kBoundsWarps * 32;
-constexpr int kPageTokens = 16;
-
-// Lane layout of both kernels: D / 16 lanes hold one token's key, lane l the channels [8 l, 8 l + 8) and
-// [D / 2 + 8 l, D / 2 + 8 l + 8) -- the two halves a rotary pair comes from; 32 / (D / 16) tokens per warp at a time.
-template <int D> struct Lanes {
-    static constexpr int kPer = D / 16;           // lanes per token
-    static constexpr int kTok = 32 / kPer;        // tokens per warp at a time
-    static constexpr int kIter = kPageTokens / kTok;
-};
 
 // Larger / smaller of two bf16 pairs; the other operand where one is NaN.
 __device__ __forceinline__ uint32_t max_pair(uint32_t a, uint32_t b) {
@@ -63,25 +51,6 @@ struct Range16 {                                  // running extremes of this la
         for (int i = 0; i < 8; ++i) { hi[i] = max_pair(hi[i], v[i]); lo[i] = min_pair(lo[i], v[i]); }
     }
 };
-
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t pack_f32x2(float x, float y) {
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
-    return d;
-}
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ uint64_t widen_bf16x2(uint32_t v) { return pack_f32x2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 
 // Smallest e with a <= 127 * 2^e, within [-60, 50]; -60 for a == 0.
 __device__ __forceinline__ int block_exponent(float a) {
@@ -591,16 +560,7 @@ aflex_status rope_append_bounds_launch(aflex_ctx* ctx, const aflex_attn_desc* d,
     p.v_cache = (__nv_bfloat16*)const_cast<void*>(kv->v_cache);
     p.codes = bounds->codes; p.scales = bounds->scales;
     p.eps = eps;
-    // the frequencies of the last theta and head size (a few microseconds of host time for a launch of as many)
-    if (ctx->rope_theta != theta || ctx->rope_dim != d->head_dim) {
-        for (int i = 0; i < d->head_dim / 2; ++i) {
-            ctx->rope_freq[i] = pow((double)theta, -2.0 * i / (double)d->head_dim);
-            ctx->rope_step[0][i] = cos(ctx->rope_freq[i]);
-            ctx->rope_step[1][i] = sin(ctx->rope_freq[i]);
-        }
-        ctx->rope_theta = theta;
-        ctx->rope_dim = d->head_dim;
-    }
+    rope_tables(ctx, theta, d->head_dim);
     for (int i = 0; i < 64; ++i) { p.inv_freq[i] = ctx->rope_freq[i]; p.step_cos[i] = ctx->rope_step[0][i]; p.step_sin[i] = ctx->rope_step[1][i]; }
     p.status = ctx->dev_status;
     // A page's K and V heads on one CTA per eight of them; its query heads 32 per CTA (7420 rows: 79.2 / 63.0 / 58.2 / 59.6 us with
