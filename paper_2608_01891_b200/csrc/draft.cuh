@@ -20,13 +20,13 @@ struct DraftParams {
     const int32_t* seq_lens;
     const int32_t* q_offsets;      // null: one row per sequence
     const uint32_t* mask;          // [rows][mask_words] or null
-    int mask_words, batch, rows, max_pages, Hq, Hkv, G, rpt;
+    int mask_words, batch, rows, max_pages, Hq, Hkv, G, g_shift, rpt_shift;      // G = 2^g_shift; rows per tile: 2^rpt_shift
     long long num_pages;
     float scale_log2;
     __nv_bfloat16* out;
     float* lse;
-    float* o_part;                 // [CTA][2][lines][D]: unnormalised sums of an item's piece
-    float* ml_part;                // [CTA][2][lines][2]: reference of the weights (log2 units), their sum
+    float* parts;                  // [CTA][2][slot]: of an item's piece, [lines][2] reference of the weights (log2 units) and their sum, then
+                                   // [lines][D] unnormalised sums
     int* counters;                 // [items] pieces done, zero on entry and on exit
     int* status;
 };
@@ -51,31 +51,38 @@ __device__ __forceinline__ DraftSeq draft_seq(const DraftParams& p, int b) {
 }
 
 template <int kTokens> struct DraftList {
-    int rpt;
+    static constexpr int kShift = kTokens == 128 ? 7 : 6;
+    static_assert(kTokens == 1 << kShift, "");
+    int rpt_shift;
     bool causal;
-    __device__ DraftList(const DraftParams& p) : rpt(p.rpt), causal(p.mask == nullptr) {}
-    __device__ int tiles(const DraftSeq& s) const { return (s.m + rpt - 1) / rpt; }
+    __device__ DraftList(const DraftParams& p) : rpt_shift(p.rpt_shift), causal(p.mask == nullptr) {}
+    __device__ int tiles(const DraftSeq& s) const { return (s.m + (1 << rpt_shift) - 1) >> rpt_shift; }
     // tokens that the rows of a tile may see, units of one of its items (the empty one among them)
     __device__ int sees(const DraftSeq& s, int tile) const {
-        return !s.ok ? 0 : causal ? s.ctx + (int)min((long long)s.m, (long long)(tile + 1) * rpt) : s.len;
+        return !s.ok ? 0 : causal ? s.ctx + (int)min((long long)s.m, (long long)(tile + 1) << rpt_shift) : s.len;
     }
-    __device__ int units(const DraftSeq& s, int tile) const { return 1 + (sees(s, tile) + kTokens - 1) / kTokens; }
-    // sum over i = 1 .. x of ceil(i / (kTokens / rpt)); rpt divides kTokens
+    __device__ int units(const DraftSeq& s, int tile) const { return 1 + ((sees(s, tile) + kTokens - 1) >> kShift); }
+    // sum over i = 1 .. x of ceil(i / q), q = tiles whose rows make a unit of tokens (a power of two)
     __device__ long long ramp(long long x) const {
-        const int q = kTokens / rpt;
-        const long long y = x / q, z = x % q;
-        return q * (y * (y + 1) / 2) + z * (y + 1);
+        const int qs = kShift - rpt_shift;
+        const long long y = x >> qs, z = x - (y << qs);
+        return ((y * (y + 1)) << qs >> 1) + z * (y + 1);
     }
-    // units of the sequence's first `n` tiles, for one KV head; all but a sequence's last tile are full, and with a = ceil(ctx / rpt) a full
-    // tile t's tokens are ceil((a + t + 1) / (kTokens / rpt)) units
+    // units of the sequence's first `n` tiles, for one KV head; all but a sequence's last tile are full, and with a = ceil(ctx / rows per tile)
+    // a full tile t's tokens are ceil((a + t + 1) / q) units
     __device__ long long before(const DraftSeq& s, int n) const {
         if (n == 0) return 0;
-        if (!causal || !s.ok) return (long long)n * units(s, 0);
+        if (!causal || !s.ok || n == 1) return (long long)n * units(s, 0);
         const int full = min(n, tiles(s) - 1);
-        const long long a = (s.ctx + rpt - 1) / rpt;
+        const long long a = (s.ctx + (1 << rpt_shift) - 1) >> rpt_shift;
         return ramp(a + full) - ramp(a) + full + (n > full ? units(s, n - 1) : 0);
     }
 };
+
+// Quotients of whole numbers >= 0, which seldom need 64 bits.
+__device__ __forceinline__ long long draft_div(long long a, long long b) {
+    return (unsigned long long)(a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
+}
 
 // A place in the list: unit u of the item (tile of sequence b, KV head g); position `pos` of all.
 template <int kTokens> struct DraftWalk {
@@ -95,8 +102,8 @@ template <int kTokens> struct DraftWalk {
         id = (seq_tiles + tile) * p.Hkv;
         nu = list.units(s, tile);
         const long long in = rel - list.before(s, tile) * p.Hkv;
-        g = (int)(in / nu);
-        u = (int)(in % nu);
+        g = (int)draft_div(in, nu);
+        u = (int)(in - (long long)g * nu);
     }
     // n units on, inside the item or to the start of the next one; `end`: the list's length
     __device__ void advance(const DraftParams& p, const DraftList<kTokens>& list, int n, long long end) {
@@ -114,18 +121,17 @@ template <int kTokens> struct DraftWalk {
     }
 };
 
-// What a CTA finds out about the list before it starts: its share [x0, x1), and where x0 is.
+// What a CTA finds out about the list before it starts: its share [x0, x1), and where x0 is.  The first `more` CTAs have each + 1 units,
+// the others `each`.
 struct DraftShare {
-    long long total, x0, x1, seq_first;
-    int seq, seq_tiles, ctas;
+    long long total, each, x0, x1, seq_first;
+    int more, ctas, seq, seq_tiles;
+    __device__ long long begin(int c) const { return each * c + min(c, more); }
+    __device__ int cta_of(long long x) const {
+        const long long first = (each + 1) * more;
+        return (int)(x < first ? draft_div(x, each + 1) : more + draft_div(x - first, each));
+    }
 };
-__device__ __forceinline__ long long draft_share_begin(long long total, int c, int ctas) { return total * c / ctas; }
-__device__ __forceinline__ int draft_cta_of(long long x, long long total, int ctas) {
-    int c = (int)min((long long)ctas - 1, x * ctas / total);
-    while (c > 0 && draft_share_begin(total, c, ctas) > x) --c;
-    while (c + 1 < ctas && draft_share_begin(total, c + 1, ctas) <= x) ++c;
-    return c;
-}
 // All kThreads threads of the CTA, thread t a run of sequences; returns after a barrier.
 template <int kTokens, int kThreads>
 __device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList<kTokens>& list, DraftShare& out) {
@@ -160,12 +166,17 @@ __device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList
         total += s_units[w];
     }
     total *= p.Hkv;
-    const int ctas = (int)min((long long)gridDim.x, total);
-    const long long x0 = (int)blockIdx.x < ctas ? draft_share_begin(total, blockIdx.x, ctas) : 0;
+    DraftShare share;
+    share.total = total;
+    share.ctas = (int)min((long long)gridDim.x, total);
+    share.each = share.ctas > 0 ? draft_div(total, share.ctas) : 0;
+    share.more = share.ctas > 0 ? (int)(total - share.each * share.ctas) : 0;
+    const bool works = (int)blockIdx.x < share.ctas;
+    const long long x0 = works ? share.begin(blockIdx.x) : 0;
     if (tid == 0) {
-        out.total = total; out.ctas = ctas;
+        out.total = total; out.each = share.each; out.more = share.more; out.ctas = share.ctas;
         out.x0 = x0;
-        out.x1 = (int)blockIdx.x < ctas ? draft_share_begin(total, blockIdx.x + 1, ctas) : 0;
+        out.x1 = works ? share.begin(blockIdx.x + 1) : 0;
     }
     u_before *= p.Hkv;
     if (x0 >= u_before && x0 < u_before + units * p.Hkv) {

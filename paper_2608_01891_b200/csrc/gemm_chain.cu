@@ -159,7 +159,6 @@ struct StepOrder {
 };
 
 __device__ __forceinline__ float chain_silu(float z) { return __fdividef(z, 1.0f + __expf(-z)); }
-__device__ __forceinline__ void fence_proxy_async_all() { asm volatile("fence.proxy.async;" ::: "memory"); }
 __device__ __forceinline__ int seg_tile0(const ChainPhase& P, int seg) {
     int t = 0;
     for (int g = 0; g < seg; ++g) t += P.seg_tiles[g];
