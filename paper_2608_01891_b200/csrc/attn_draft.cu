@@ -51,53 +51,23 @@ template <int D, int F, int NT> struct DraftForm {
     static_assert(kSize % 1024 == 0, "swizzled blocks are aligned to their pattern");
 };
 
-struct UnitMeta {
-    int units, t0, sees, ctx;      // units of the piece (0: the share ends), first token, tokens the tile's rows may see, earlier tokens of the sequence
-    int row0, lines, i0, m, g;     // first row and lines of the tile, number of the first row and of all rows in the sequence, KV head
-    int item, slot, whole;
-    long long first, last;         // positions of the item's first and last unit with tokens
-};
-
 template <int W> struct __align__(8) DraftShared {            // W: compute warps
     uint64_t told[kStages], full[kStages], empty[kStages];     // told: the unit's description is there
-    uint64_t pieces;
-    UnitMeta meta[kStages];
+    uint64_t meet, pieces;         // the compute warps; copies of pieces to be joined
+    DraftPiece meta[kStages];
     float m[2][W][kMaxLines], l[2][W][kMaxLines];              // of pieces in turn
     float3 carry[kMaxLines];       // while pieces are joined: reference and sum so far, and what the sums before are to be multiplied by
     DraftShare share;
     int merges;                    // items that this CTA has to join at the end
-    UnitMeta merge[2];
+    DraftPiece merge[2];
     volatile int abort;
 };
-
-// (the L2 cache is told to fetch the neighbouring heads' scales with them)
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-// One arrival, when this thread's copies so far have landed.
-__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
 
 // Byte offset of a token's 16-byte chunk inside a page's K or V block, as the tiled copies write it.
 template <int kRow> __device__ __forceinline__ uint32_t chunk_at(int t, int ch) {
     if (kRow == 256) return (uint32_t)((ch >> 3) * (kPageTokens * 128) + t * 128 + (((ch & 7) ^ (t & 7)) << 4));
     if (kRow == 128) return (uint32_t)(t * 128 + ((ch ^ (t & 7)) << 4));
     return (uint32_t)(t * 64 + ((ch ^ ((t >> 1) & 3)) << 4));
-}
-
-// Four codes as two pairs of fp16, exactly.
-template <int F> __device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
-    if (F == AFLEX_CACHE_INT8) {
-        w ^= 0x80808080u;
-        const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));      // 1024 + 128
-        const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
-        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), off), y = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
-        lo = *reinterpret_cast<const uint32_t*>(&x);
-        hi = *reinterpret_cast<const uint32_t*>(&y);
-    } else {
-        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
-    }
 }
 
 // Four codes of K as two pairs of fp16: of int8 (code + 128) * 2^-24, the subnormal numbers whose bits are the byte's -- what they add, 128
@@ -143,7 +113,7 @@ template <int D, int NT> struct LineState {        // of a warp: a lane's lines 
 template <int kRow> __device__ __forceinline__ int k_chunk(int c, int l4) { return kRow == 256 ? (c >> 1) * 8 + 2 * l4 + (c & 1) : kRow == 128 ? 2 * l4 + c : l4; }
 
 template <int D, int F, int NT>
-__device__ __forceinline__ void load_queries(LineState<D, NT>& st, const DraftParams& p, const UnitMeta& u) {
+__device__ __forceinline__ void load_queries(LineState<D, NT>& st, const DraftParams& p, const DraftPiece& u) {
     constexpr int kRow = DraftForm<D, F, NT>::kRow;
     const int lane = threadIdx.x & 31, hl = lane >> 2, l4 = lane & 3;
 #pragma unroll
@@ -202,17 +172,9 @@ __device__ __forceinline__ void load_queries(LineState<D, NT>& st, const DraftPa
     }
 }
 
-// Whether drafted token j (negative: an earlier token) is seen by row i of its sequence.
-__device__ __forceinline__ bool sees_drafted(const DraftParams& p, int row, int i, int j, int m) {
-    if (j < 0) return true;
-    if (j >= m) return false;
-    if (p.mask == nullptr) return j <= i;
-    return (j >> 5) < p.mask_words && ((fetch(p.mask + (size_t)row * p.mask_words + (j >> 5)) >> (j & 31)) & 1u);
-}
-
 // N pages for one warp: K of the first at kp and its V behind it, the scales at sp; tokens tp .. of the sequence, of which the first `seen` count.
 template <int D, int F, int NT, int N>
-__device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftParams& p, const UnitMeta& u, const uint8_t* kp, const float* sp, int tp, int seen, bool masked) {
+__device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftParams& p, const DraftPiece& u, const uint8_t* kp, const float* sp, int tp, int seen, bool masked) {
     typedef DraftForm<D, F, NT> S;
     constexpr int kRow = S::kRow, kPageBytes = 2 * S::kBlock, kPageScales = S::kScales / 4;
     const int lane = threadIdx.x & 31, hl = lane >> 2, l4 = lane & 3;
@@ -463,24 +425,6 @@ __device__ __forceinline__ void park(const LineState<D, NT>& st, uint8_t* to, fl
 
 constexpr int kCarry = 2 * kMaxLines;                 // references and sums before a slot's lines
 template <int D> constexpr int kSlot = kCarry + kMaxLines * D;      // floats of a piece's slot
-template <int W> __device__ __forceinline__ void compute_sync() { asm volatile("bar.sync 1, %0;" ::"n"(W * 32) : "memory"); }
-
-struct RunSum {
-    float M, L;
-    float4 acc;
-};
-__device__ __forceinline__ void add_piece(RunSum& s, float m, float l, const float4& v) {
-    const float f = fast_exp2(m - s.M);            // (s.M: the largest m of all pieces)
-    s.L = fmaf(l, f, s.L);
-    s.acc.x = fmaf(v.x, f, s.acc.x); s.acc.y = fmaf(v.y, f, s.acc.y); s.acc.z = fmaf(v.z, f, s.acc.z); s.acc.w = fmaf(v.w, f, s.acc.w);
-}
-template <int D>
-__device__ __forceinline__ void store_run(const DraftParams& p, const UnitMeta& u, int line, int c, const RunSum& s) {
-    const float inv = s.L == 0.f ? 0.f : __frcp_rn(s.L);            // a line with nothing to attend to: zeros
-    const size_t hq = (size_t)(u.row0 + (line >> p.g_shift)) * p.Hq + (size_t)u.g * p.G + (line & (p.G - 1));
-    reinterpret_cast<uint2*>(p.out + hq * D)[c] = make_uint2(pack_bf16x2(s.acc.x * inv, s.acc.y * inv), pack_bf16x2(s.acc.z * inv, s.acc.w * inv));
-    if (p.lse != nullptr && c == 0) p.lse[hq] = s.L == 0.f ? -INFINITY : (s.M + __log2f(s.L)) * 0.6931471805599453f;
-}
 
 template <int D, int F, int NT>
 __global__ void __launch_bounds__(DraftForm<D, F, NT>::kThreads, 2)
@@ -498,6 +442,7 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             mbar_init(&sh.told[s], 1);
             mbar_init(&sh.empty[s], W);
         }
+        mbar_init(&sh.meet, W);
         mbar_init(&sh.pieces, 1);
         sh.abort = 0;
         sh.merges = 0;
@@ -531,14 +476,8 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         else w.pos = share.x1;
         while (ok && w.pos < share.x1) {
             if (w.u == 0 && w.nu > 1) { w.advance(p, list, 1, share.total); continue; }
-            const int u0 = w.u, u1 = (int)min((long long)w.nu, w.u + (share.x1 - w.pos));       // (u0 = 0: an item without tokens)
-            UnitMeta meta;
-            meta.units = u1 - u0; meta.t0 = (u0 - 1) * S::kTokens;
-            meta.sees = list.sees(w.s, w.tile); meta.ctx = w.s.ctx;
-            meta.i0 = w.tile << p.rpt_shift; meta.row0 = w.s.o0 + meta.i0; meta.m = w.s.m; meta.g = w.g;
-            meta.lines = min(1 << p.rpt_shift, w.s.m - meta.i0) * p.G;
-            meta.item = w.id + w.g; meta.slot = u0 > 1 ? 0 : 1; meta.whole = u0 <= 1 && u1 == w.nu;
-            meta.first = w.pos - u0 + 1; meta.last = w.pos - u0 + w.nu - 1;
+            const DraftPiece meta = draft_piece(p, list, w, share.x1);
+            const int u0 = w.u, u1 = u0 + meta.units;
             const int32_t* table = p.page_table + (size_t)w.b * p.max_pages;
             auto page_id = [&](int u) -> int {
                 const int i = (u - 1) * S::kPages + page;
@@ -590,6 +529,14 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         // ------------------------------------------------------------------ compute
         LineState<D, NT> st;
         int pieces = 0;
+        uint32_t met = 0;
+        auto meet = [&]() -> bool {                // the compute warps (a bounded wait: a warp that has given up does not come)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.meet);
+            const bool came = mbar_wait(&sh.meet, met & 1);
+            ++met;
+            return __all_sync(0xffffffffu, came);
+        };
         pdl_wait();
         int stage = 0, parity = 0, left = 0, tp = 0, seen = 0, plain = 0;       // of the piece: units to come, the warp's next token ..
         for (;;) {
@@ -597,7 +544,7 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                 bool ok = mbar_wait(&sh.told[stage], parity);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) { if (lane == 0) { sh.abort = 1; atomicExch(p.status, AFLEX_ERR_TIMEOUT); } break; }
-                const UnitMeta& u = sh.meta[stage];
+                const DraftPiece& u = sh.meta[stage];
                 left = u.units;
                 if (left == 0) break;              // the end of the share
                 seen = u.sees;
@@ -628,8 +575,8 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                 float(&pl)[W][kMaxLines] = sh.l[pieces & 1];
                 ++pieces;
                 park<D, F, NT>(st, mine, pm[warp], pl[warp]);
-                const UnitMeta piece = sh.meta[stage];
-                compute_sync<W>();
+                const DraftPiece piece = sh.meta[stage];
+                if (!meet()) { if (lane == 0) { sh.abort = 1; atomicExch(p.status, AFLEX_ERR_TIMEOUT); } break; }
                 float* slot = p.parts + ((size_t)blockIdx.x * 2 + piece.slot) * kSlot<D>;
 #pragma unroll 1                                   // (here and below: code that runs once a piece is kept small, it is seldom in the instruction cache)
                 for (int i = threadIdx.x; i < piece.lines * kRuns; i += W * 32) {
@@ -651,7 +598,7 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                 if (lane == 0) mbar_arrive(&sh.empty[stage]);
                 if (!piece.whole) {
                     // the last of the item's CTAs to get here joins the pieces (offsets that decrease could name more items than there are counters)
-                    compute_sync<W>();
+                    if (!meet()) { if (lane == 0) { sh.abort = 1; atomicExch(p.status, AFLEX_ERR_TIMEOUT); } break; }
                     if (threadIdx.x == 0) {
                         __threadfence();
                         if (piece.item >= kAttnCounterCap) atomicExch(p.status, AFLEX_ERR_BOUNDS);
@@ -679,7 +626,7 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     uint32_t phase = 0;
 #pragma unroll 1
     for (int j = 0; j < sh.merges; ++j) {
-        const UnitMeta u = sh.merge[j];
+        const DraftPiece u = sh.merge[j];
         const int c0 = sh.share.cta_of(u.first), n = sh.share.cta_of(u.last) - c0 + 1;
         const uint32_t bytes = (uint32_t)(kCarry + u.lines * D) * 4;
         const int at_once = (kStages * S::kSize - S::kLines * D * 4) / (int)bytes;
@@ -773,9 +720,13 @@ aflex_status launch_f(aflex_ctx* ctx, const aflex_cache* cache, int grid, const 
 
 // ------------------------------------------------------------------------------------------ host
 static int draft_grid(int num_sms) { return 2 * num_sms; }
+size_t attn_draft_wide_workspace_bytes(int head_dim, int num_sms);                    // attn_draft_wide.cu
+aflex_status attn_draft_wide_launch(aflex_ctx* ctx, const aflex_cache* cache, int head_dim, const DraftParams& p, cudaStream_t st);
 
 size_t attn_draft_workspace_bytes(const aflex_attn_desc* d, int num_sms) {
-    return align256((size_t)draft_grid(num_sms) * 2 * (kCarry + kMaxLines * d->head_dim) * sizeof(float));
+    const size_t narrow = align256((size_t)draft_grid(num_sms) * 2 * (kCarry + kMaxLines * d->head_dim) * sizeof(float));
+    const size_t wide = attn_draft_wide_workspace_bytes(d->head_dim, num_sms);
+    return narrow > wide ? narrow : wide;
 }
 
 aflex_status attn_draft_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_cache* cache, int batch,
@@ -791,18 +742,20 @@ aflex_status attn_draft_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const v
     p.batch = batch; p.rows = rows; p.max_pages = kv->max_pages_per_seq;
     p.Hq = d->num_q_heads; p.Hkv = d->num_kv_heads; p.G = p.Hq / p.Hkv; p.num_pages = kv->num_pages;
     p.g_shift = p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3;
-    p.rpt_shift = ((long long)rows << p.g_shift) <= 8LL * batch ? 3 - p.g_shift : 4 - p.g_shift;
+    // Lines per tile by the lines of an average sequence: 8, 16, or 256 on the tensor cores.
+    const long long lines = (long long)rows << p.g_shift;
+    p.rpt_shift = (lines <= 8LL * batch ? 3 : lines <= 16LL * batch ? 4 : 8) - p.g_shift;
     const float scale = d->sm_scale != 0.f ? d->sm_scale : 1.0f / sqrtf((float)D);
     p.scale_log2 = scale * 1.4426950408889634f;
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ctx->dev_status;
     p.counters = ctx->counters_attn;
-    Arena arena(ws, ws_bytes);
-    p.parts = arena.take<float>((size_t)grid * 2 * (kCarry + kMaxLines * D));
-    if (arena.overflow)
-        return set_error(ctx, AFLEX_ERR_WORKSPACE, "draft attention: need %zu workspace bytes, have %zu", attn_draft_workspace_bytes(d, ctx->num_sms), ws_bytes);
+    const size_t need = attn_draft_workspace_bytes(d, ctx->num_sms);
+    if (ws_bytes < need) return set_error(ctx, AFLEX_ERR_WORKSPACE, "draft attention: need %zu workspace bytes, have %zu", need, ws_bytes);
+    p.parts = reinterpret_cast<float*>(ws);
     // m rows of a sequence are at most m / 2^rpt_shift + 1 tiles
     const long long items = (((long long)rows >> p.rpt_shift) + batch) * p.Hkv;
     if (items > kAttnCounterCap) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "draft attention: %d rows of %d sequences (supported: up to 2^20 tiles of %d rows x KV heads)", rows, batch, 1 << p.rpt_shift);
+    if (p.rpt_shift + p.g_shift == 8) return attn_draft_wide_launch(ctx, cache, D, p, st);
     typedef aflex_status (*Launch)(aflex_ctx*, const aflex_cache*, int, const DraftParams&, cudaStream_t);
     const Launch launch[2][3] = {{launch_f<64, AFLEX_CACHE_BF16>, launch_f<64, AFLEX_CACHE_INT8>, launch_f<64, AFLEX_CACHE_E4M3>},
                                  {launch_f<128, AFLEX_CACHE_BF16>, launch_f<128, AFLEX_CACHE_INT8>, launch_f<128, AFLEX_CACHE_E4M3>}};

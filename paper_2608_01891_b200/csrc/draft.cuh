@@ -5,9 +5,12 @@
 // unit in front (what starting and joining an item costs).  All items' units in a list, cut anywhere into equal shares, a share per CTA:
 // no plan on the host, which does not know the lengths, and no CTA that is left with a long sequence.
 #pragma once
+#include <cuda_fp16.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "internal.h"
+#include "ptx.cuh"
 #include "rows.cuh"
 
 namespace aflex {
@@ -62,9 +65,10 @@ template <int kTokens> struct DraftList {
         return !s.ok ? 0 : causal ? s.ctx + (int)min((long long)s.m, (long long)(tile + 1) << rpt_shift) : s.len;
     }
     __device__ int units(const DraftSeq& s, int tile) const { return 1 + ((sees(s, tile) + kTokens - 1) >> kShift); }
-    // sum over i = 1 .. x of ceil(i / q), q = tiles whose rows make a unit of tokens (a power of two)
+    // sum over i = 1 .. x of ceil(i / q), q = tiles whose rows make a unit of tokens (a power of two); of k i where a tile's rows are k units
     __device__ long long ramp(long long x) const {
         const int qs = kShift - rpt_shift;
+        if (qs < 0) return (x * (x + 1) / 2) << -qs;
         const long long y = x >> qs, z = x - (y << qs);
         return ((y * (y + 1)) << qs >> 1) + z * (y + 1);
     }
@@ -74,6 +78,7 @@ template <int kTokens> struct DraftList {
         if (n == 0) return 0;
         if (!causal || !s.ok || n == 1) return (long long)n * units(s, 0);
         const int full = min(n, tiles(s) - 1);
+        if (rpt_shift > kShift) return (long long)full * (1 + ((s.ctx + kTokens - 1) >> kShift)) + ramp(full) + (n > full ? units(s, n - 1) : 0);
         const long long a = (s.ctx + (1 << rpt_shift) - 1) >> rpt_shift;
         return ramp(a + full) - ramp(a) + full + (n > full ? units(s, n - 1) : 0);
     }
@@ -120,6 +125,35 @@ template <int kTokens> struct DraftWalk {
         nu = list.units(s, tile);
     }
 };
+
+// A piece: a run of units of one item.
+struct DraftPiece {
+    int units, t0, sees, ctx;      // units with tokens, or 1 for an item without (0: the share ends); first token, tokens the tile's rows may see, earlier tokens
+    int row0, lines, i0, m, g;     // first row and lines of the tile, number of the first row and of all rows in the sequence, KV head
+    int item, slot, whole;
+    long long first, last;         // positions of the item's first and last unit with tokens
+};
+// The piece that starts at w (not at the empty unit of an item that has tokens) and ends with the item or at x1.
+template <int kTokens>
+__device__ __forceinline__ DraftPiece draft_piece(const DraftParams& p, const DraftList<kTokens>& list, const DraftWalk<kTokens>& w, long long x1) {
+    DraftPiece d;
+    const int u1 = (int)min((long long)w.nu, w.u + (x1 - w.pos));                        // (w.u = 0: an item without tokens)
+    d.units = u1 - w.u; d.t0 = (w.u - 1) * kTokens;
+    d.sees = list.sees(w.s, w.tile); d.ctx = w.s.ctx;
+    d.i0 = w.tile << p.rpt_shift; d.row0 = w.s.o0 + d.i0; d.m = w.s.m; d.g = w.g;
+    d.lines = min(1 << p.rpt_shift, w.s.m - d.i0) * p.G;
+    d.item = w.id + w.g; d.slot = w.u > 1 ? 0 : 1; d.whole = w.u <= 1 && u1 == w.nu;
+    d.first = w.pos - w.u + 1; d.last = w.pos - w.u + w.nu - 1;
+    return d;
+}
+
+// Whether drafted token j (negative: an earlier token) is seen by row i of its sequence.
+__device__ __forceinline__ bool sees_drafted(const DraftParams& p, int row, int i, int j, int m) {
+    if (j < 0) return true;
+    if (j >= m) return false;
+    if (p.mask == nullptr) return j <= i;
+    return (j >> 5) < p.mask_words && ((fetch(p.mask + (size_t)row * p.mask_words + (j >> 5)) >> (j & 31)) & 1u);
+}
 
 // What a CTA finds out about the list before it starts: its share [x0, x1), and where x0 is.  The first `more` CTAs have each + 1 units,
 // the others `each`.
@@ -190,6 +224,46 @@ __device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList
         }
     }
     __syncthreads();
+}
+
+// Sums of one run of four channels of a line over pieces.
+struct RunSum {
+    float M, L;
+    float4 acc;
+};
+__device__ __forceinline__ void add_piece(RunSum& s, float m, float l, const float4& v) {
+    const float f = fast_exp2(m - s.M);            // (s.M: the largest m of all pieces)
+    s.L = fmaf(l, f, s.L);
+    s.acc.x = fmaf(v.x, f, s.acc.x); s.acc.y = fmaf(v.y, f, s.acc.y); s.acc.z = fmaf(v.z, f, s.acc.z); s.acc.w = fmaf(v.w, f, s.acc.w);
+}
+template <int D>
+__device__ __forceinline__ void store_run(const DraftParams& p, const DraftPiece& u, int line, int c, const RunSum& s) {
+    const float inv = s.L == 0.f ? 0.f : __frcp_rn(s.L);       // a line with nothing to attend to: zeros
+    const size_t hq = (size_t)(u.row0 + (line >> p.g_shift)) * p.Hq + (size_t)u.g * p.G + (line & (p.G - 1));
+    reinterpret_cast<uint2*>(p.out + hq * D)[c] = make_uint2(pack_bf16x2(s.acc.x * inv, s.acc.y * inv), pack_bf16x2(s.acc.z * inv, s.acc.w * inv));
+    if (p.lse != nullptr && c == 0) p.lse[hq] = s.L == 0.f ? -INFINITY : (s.M + __log2f(s.L)) * 0.6931471805599453f;
+}
+
+// Four codes as two pairs of fp16, exactly.
+template <int F> __device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    if (F == AFLEX_CACHE_INT8) {
+        w ^= 0x80808080u;
+        const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));      // 1024 + 128
+        const uint32_t a = __byte_perm(w, 0x64646464u, 0x4140), b = __byte_perm(w, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), off), y = __hsub2(*reinterpret_cast<const __half2*>(&b), off);
+        lo = *reinterpret_cast<const uint32_t*>(&x);
+        hi = *reinterpret_cast<const uint32_t*>(&y);
+    } else {
+        asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+    }
+}
+
+// 16 bytes of scales (the L2 cache is told to fetch the neighbouring heads' with them), and one arrival when this thread's copies so far have landed.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
 }  // namespace aflex

@@ -63,7 +63,7 @@ struct aflex_ctx {
     int select_clusters[2][2][9] = {};           // clusters of 2 .. 8 CTAs of page_select_rows_kernel (16 warps, 8 warps) that fit it at once
     bool bounds_attr_set[2] = {false, false};    // ... for page_bounds_kernel<64 / 128>
     bool pages_attr_set[2] = {false, false};     // ... for attn_decode_pages_kernel<64 / 128>
-    bool draft_attr_set[2][3][2] = {};           // ... for the kernels of attn_draft.cu [head size][format][eights of lines]
+    bool draft_attr_set[2][3][3] = {};           // ... for the kernels of attn_draft.cu [head size][format][8 lines, 16, 256]
     int pages_clusters[2][9] = {};               // its clusters of 2 .. 8 CTAs that fit this device at once
     float rope_theta = 0.f;       // what rope_freq and rope_step (cosine, sine of one position's angle) were made for
     int rope_dim = 0;

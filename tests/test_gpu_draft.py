@@ -271,6 +271,9 @@ ATTEND = [  # Hq, Hkv, D, lens, rows per sequence (None: one), kind of mask
     (8, 1, 128, [130, 70], [130, 70], "none"),                            # nothing to attend to
     (8, 4, 128, [1500, 1100], [700, 300], "chain"),
     (8, 1, 64, [400, 1000], [300, 150], "any"),
+    (4, 4, 64, [900, 33, 700], [600, 20, 257], "chain"),                  # more rows per tile than tokens per unit
+    (8, 1, 128, [9000, 5000, 129], [24, 3, 129], "tree"),                 # tiles in one place and in two, shared by several CTAs
+    (16, 2, 128, [130, 1], [16, 1], "chain"),
 ]
 
 
