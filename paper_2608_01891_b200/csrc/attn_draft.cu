@@ -454,8 +454,8 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     // The lengths, the row offsets and the page table are inputs of the step, never written by a kernel of this library, so the plan and the
     // first page ids are made while the preceding kernel is still draining; what it may have written (q, the cache, partial results,
     // counters) waits for it, per role.
-    const DraftList<S::kTokens> list(p);
-    draft_plan<S::kTokens, kThreads>(p, list, sh.share);
+    const DraftList<S::kTokens, 1> list(p);
+    draft_plan<kThreads>(p, list, sh.share);
 
     if (warp == W) {
         // ------------------------------------------------------------------ producer
@@ -471,13 +471,13 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         const int page = lane % S::kPages, kv = (lane / S::kPages) & 1, part = lane / (2 * S::kPages);
         const bool copies = lane < 2 * S::kPages * (F == AFLEX_CACHE_BF16 ? S::kRow / 128 : 1);
         const uint64_t policy = policy_evict_first();                  // (the cache is read once)
-        DraftWalk<S::kTokens> w;
+        DraftWalk<S::kTokens, 1> w;
         if (share.x0 < share.x1) w.start(p, list, share.x0, share.seq, share.seq_first, share.seq_tiles);
         else w.pos = share.x1;
         while (ok && w.pos < share.x1) {
             if (w.u == 0 && w.nu > 1) { w.advance(p, list, 1, share.total); continue; }
             const DraftPiece meta = draft_piece(p, list, w, share.x1);
-            const int u0 = w.u, u1 = u0 + meta.units;
+            const int u0 = w.u, u1 = w.until(share.x1);
             const int32_t* table = p.page_table + (size_t)w.b * p.max_pages;
             auto page_id = [&](int u) -> int {
                 const int i = (u - 1) * S::kPages + page;

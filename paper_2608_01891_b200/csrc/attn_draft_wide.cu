@@ -8,11 +8,13 @@
 //   data path   a producer warp brings pages; of an 8-bit cache they are widened to fp16 by a warp group of its own, exactly (the scales are the
 //               softmax's business), into the swizzled layout that the tensor cores read; a bf16 cache's pages are copied into that layout by TMA
 //               and the warp group only looks at the V of drafted tokens.  K is a K-major operand, V (as stored) an MN-major one
-//   softmax     two warp groups, a line per thread; statistics, references and weights as in attn_draft.cu.  The weights of an 8-bit cache are
+//   softmax     eight warps per place, sixteen lines each, read from TMEM as fragments (two lines x 32 tokens per thread), so that a token's
+//               scales, which every line needs, are loaded once for two lines and by four lanes at a time (with a line per thread the loads of scales alone
+//               took longer than the products); statistics, references and weights as in attn_draft.cu.  The weights of an 8-bit cache are
 //               stored back over the scores they came from, in fp16; those of a bf16 cache as two bf16 parts, which fill the place of the
 //               scores, and the second product is issued for each part
 //
-// Bound: of long trees the exponentials (16 per cycle and SM against 8192 multiply-adds) and the products about equally; of short ones with few lines
+// Bound: of long trees the exponentials (16 per cycle and SM against 4096 multiply-adds) and the products about equally; of short ones with few lines
 // the widening and the read of the cache.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -31,9 +33,10 @@ constexpr int kBM = 128;                           // lines per tile
 constexpr int kBN = 128;                           // cached tokens per step
 constexpr int kUnitPages = kBN / kPageTokens;
 constexpr int kWideLines = 2 * kBM;
-constexpr int kWideThreads = 512;                  // warp groups: softmax of places 0 and 1, producer + issuer, widening
-constexpr int kRegsSoftmax = 184, kRegsIssue = 64, kRegsWiden = 80;
-static_assert(256 * kRegsSoftmax + 128 * kRegsIssue + 128 * kRegsWiden <= 512 * 128, "the warp groups share what the block was launched with");
+constexpr int kSoftmaxWarps = 16;                  // [place][half of 32 lines][32 lines]
+constexpr int kWideThreads = (kSoftmaxWarps + 8) * 32;       // and the warp groups of producer + issuer, and of widening
+constexpr int kRegsSoftmax = 88, kRegsIssue = 64, kRegsWiden = 64;
+static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + 128 * kRegsIssue + 128 * kRegsWiden <= kWideThreads * 80, "the warp groups share what the block was launched with");
 constexpr int kPieceRing = 4;
 
 template <int D, int F> struct WideForm {
@@ -51,7 +54,8 @@ template <int D, int F> struct WideForm {
 struct __align__(16) WideShared {
     float4 scale[2][kBN / 2];                      // by step: of two tokens, K's scales and log2 of V's
     float4 inv[2][kBN / 4];                        // 1 / V's, of four tokens
-    float2 state[2][kBM];                          // of one tile in two places: references and sums
+    float2 state[2][kBM];                          // by place: references and sums of a finished piece
+    float factor[2][kBM];                          // by place: what a line's products count, in log2 units
     uint32_t bad[4][kBN / 32];                     // by step: tokens whose V holds an infinity or NaN (bf16)
     uint64_t told[kPieceRing], left[kPieceRing];   // a piece's description is there, everybody has read it
     uint64_t raw_full[4], raw_empty[3];            // pages have landed (bf16: in their slot), have been widened
@@ -69,6 +73,29 @@ template <int F> __device__ __forceinline__ uint32_t wide_idesc(uint32_t n) {
     const uint32_t d = umma_idesc_bf16(kBM, n);
     return F == AFLEX_CACHE_BF16 ? d : d & ~((1u << 7) | (1u << 10));                     // fp16 operands
 }
+
+// TMEM fragments: 16 lines x 128 columns (element 4 i + 2 y + e: line lane / 4 + 8 y, column 8 i + 2 (lane % 4) + e), and stores of 16 lines x 64
+// columns (element 2 i + y: line lane / 4 + 8 y, column 4 i + lane % 4): a pair of the one packed is an element of the other.
+#define R4(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3])
+#define R16(a, i) R4(a, i), R4(a, i + 4), R4(a, i + 8), R4(a, i + 12)
+#define I4(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3])
+#define I16(a, i) I4(a, i), I4(a, i + 4), I4(a, i + 8), I4(a, i + 12)
+template <int kAt> __device__ __forceinline__ void tmem_ld_16x256b_x4_at(uint32_t taddr, uint32_t (&r)[64]) {      // 32 columns into elements kAt ..
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];" : R16(r, kAt) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];" : R16(r, 0) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_16x256b_x4(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), I16(r, 0) : "memory");
+}
+template <int kAt> __device__ __forceinline__ void tmem_st_16x128b_x8_at(uint32_t taddr, const uint32_t (&r)[32]) {      // 32 columns from elements kAt ..
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), I16(r, kAt) : "memory");
+}
+#undef R4
+#undef R16
+#undef I4
+#undef I16
 
 // Floats of a piece's slot in global memory: [line][2] reference and sum, then [run of four channels][line][4] sums.
 constexpr int kWideCarry = 2 * kWideLines;
@@ -89,25 +116,25 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, group = warp >> 2;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kPieceRing; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.left[i], 13); }       // 8 softmax, 4 widening warps, the issuer
+        for (int i = 0; i < kPieceRing; ++i) { mbar_init(&sh.told[i], 1); mbar_init(&sh.left[i], kSoftmaxWarps + 5); }       // softmax and widening warps, the issuer
         for (int i = 0; i < 4; ++i) {
             mbar_init(&sh.raw_full[i], S::kWidens ? 33 : 1);
             mbar_init(&sh.full[i], 4);
             mbar_init(&sh.empty[i], 1);
         }
         for (int i = 0; i < 3; ++i) mbar_init(&sh.raw_empty[i], 4);
-        for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_ready[i], 4); mbar_init(&sh.s_ready[i], 1); mbar_init(&sh.p_ready[i], 4); mbar_init(&sh.pv_done[i], 1); }
-        mbar_init(&sh.meet, 8);
+        for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_ready[i], 8); mbar_init(&sh.s_ready[i], 1); mbar_init(&sh.p_ready[i], 8); mbar_init(&sh.pv_done[i], 1); }
+        mbar_init(&sh.meet, kSoftmaxWarps);
         sh.abort = 0;
         sh.merges = 0;
         fence_mbar_init();
         if (!S::kWidens) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); }
     }
-    if (warp == 9) { tmem_alloc(&sh.tmem_base, 512); tmem_relinquish(); }
+    if (warp == kSoftmaxWarps + 1) { tmem_alloc(&sh.tmem_base, 512); tmem_relinquish(); }
     pdl_launch_dependents();
-    const DraftList<kBN> list(p);                  // (lengths, offsets and page table are no kernel's output: the plan need not wait)
+    const DraftList<kBN, 2> list(p);                  // (lengths, offsets and page table are no kernel's output: the plan need not wait)
     tc_fence_before();
-    draft_plan<kBN, kWideThreads>(p, list, sh.share);
+    draft_plan<kWideThreads>(p, list, sh.share);
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
 
@@ -118,39 +145,45 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         return __all_sync(0xffffffffu, ok);
     };
 
-    if (group == 2) {
+    if (group == 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
-        if (warp == 8) {
+        if (warp == kSoftmaxWarps) {
             // -------------------------------------------------------------- producer: pieces and their pages
             const uint64_t policy = policy_evict_first();
             int pieces = 0, tile_no = 0;           // (tile_no: K and V tiles so far, two a step)
             bool ok = true;
-            DraftWalk<kBN> w;
+            DraftWalk<kBN, 2> w;
             const long long x1 = sh.share.x1, total = sh.share.total;
             if (sh.share.x0 < x1) w.start(p, list, sh.share.x0, sh.share.seq, sh.share.seq_first, sh.share.seq_tiles);
             else w.pos = x1;
             while (ok && w.pos < x1) {
                 if (w.u == 0 && w.nu > 1) { w.advance(p, list, 1, total); continue; }
-                ok = wait(&sh.left[pieces % kPieceRing], ((pieces / kPieceRing) & 1) ^ 1);
-                if (!ok) break;
-                const int units = draft_piece(p, list, w, x1).units;
-                const int u0 = w.u, sees = list.sees(w.s, w.tile), g = w.g;
-                if (lane == 0) {
-                    sh.piece[pieces % kPieceRing] = draft_piece(p, list, w, x1);
-                    mbar_arrive(&sh.told[pieces % kPieceRing]);
+                const int places = w.until(x1) - w.u;
+                int units, t0, sees;
+                {
+                    const DraftPiece d = draft_piece(p, list, w, x1);
+                    units = d.units; t0 = d.t0; sees = d.sees;
+                    if (units == 0) { w.advance(p, list, places, total); continue; }      // (the second place of the CTA's before)
+                    ok = wait(&sh.left[pieces % kPieceRing], ((pieces / kPieceRing) & 1) ^ 1);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        sh.piece[pieces % kPieceRing] = d;
+                        mbar_arrive(&sh.told[pieces % kPieceRing]);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
                 ++pieces;
+                const int g = w.g;
                 const int32_t* table = p.page_table + (size_t)w.b * p.max_pages;
                 const int page = lane & 7, part = lane >> 3;              // bf16: one box per (half, page)
-                auto page_id = [&](int u) -> int {
-                    const int i = (u - 1) * kUnitPages + page;
-                    return u >= 1 && i * kPageTokens < sees ? fetch(table + i) : 0;
+                auto page_id = [&](int t) -> int {                        // of the unit with tokens t ..
+                    const int i = t / kPageTokens + page;
+                    return t >= 0 && i * kPageTokens < sees ? fetch(table + i) : 0;
                 };
-                int id = page_id(u0);
-                for (int u = u0; u < u0 + units && ok && u >= 1; ++u) {
-                    const int id_next = u + 1 < u0 + units ? page_id(u + 1) : 0;
-                    const int np = min(kUnitPages, (sees - (u - 1) * kBN + kPageTokens - 1) / kPageTokens);
+                int id = page_id(t0);
+                for (int t = t0, left = units; left > 0 && ok && t >= 0; t += kBN, --left) {
+                    const int id_next = left > 1 ? page_id(t + kBN) : 0;
+                    const int np = min(kUnitPages, (sees - t + kPageTokens - 1) / kPageTokens);
                     if (page < np && (id < 0 || id >= p.num_pages)) { if (part == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
                     if (tile_no == 0) pdl_wait();
                     for (int isv = 0; isv < 2 && ok; ++isv, ++tile_no) {
@@ -180,7 +213,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     }
                     id = id_next;
                 }
-                if (ok) w.advance(p, list, units, total);
+                if (ok) w.advance(p, list, places, total);
             }
             if (ok) ok = wait(&sh.left[pieces % kPieceRing], ((pieces / kPieceRing) & 1) ^ 1);
             if (ok && lane == 0) {
@@ -188,15 +221,38 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 mbar_arrive(&sh.told[pieces % kPieceRing]);
             }
             if (!ok) give_up();
-        } else if (warp == 9) {
+        } else if (warp == kSoftmaxWarps + 1) {
             // -------------------------------------------------------------- issuer of the products (one thread)
             if (lane == 0) {
+                constexpr uint32_t kTileLo = S::kTile >> 4;
                 const uint32_t idesc_s = wide_idesc<F>(kBN);
                 const uint32_t idesc_pv = wide_idesc<F>(D) | (1u << 16);  // B operand (V) is MN-major
-                int slot = 0, loaded = 0;          // K and V tiles so far; pieces with queries
-                uint32_t done[2] = {0, 0};         // steps of either place so far
+                const uint32_t q_lo = desc_lo(smem_u32(sq), 16), k_lo = desc_lo(smem_u32(skv), 16), v_lo = desc_lo(smem_u32(skv), S::kHalf);
+                // (everything kept by increments: between a place's weights and its next scores this thread is what all wait for)
+                uint32_t ks = 0, kp = 0, vs = 1, vp = 0;                  // slot and parity of the next K and V; K(t) V(t) take turns
+                uint32_t p0 = 0, p1 = 0;                                  // parities of the places' weights
                 bool ok = true;
-                for (int pc = 0; ok; ++pc) {
+                uint32_t pc = 0, loaded = 0;
+                auto next = [](uint32_t& slot, uint32_t& parity) { slot += 2; if (slot >= S::kSlots) { slot -= S::kSlots; parity ^= 1; } };
+                auto issue_s = [&](uint32_t i) {                          // scores of place i with the next K
+                    const uint32_t to = tmem + i * kBN, a = q_lo + i * kTileLo, bk = k_lo + ks * kTileLo;
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j)
+                        umma_ss(to, a + (uint32_t)(((j / 4) * S::kHalf + (j % 4) * 32) >> 4), bk + (uint32_t)(((j / 4) * S::kHalf + (j % 4) * 32) >> 4), idesc_s, j > 0 ? 1u : 0u);
+                    umma_commit(&sh.s_ready[i]);
+                };
+                auto issue_pv = [&](uint32_t i, bool first) {             // place i's weights with the next V
+                    const uint32_t to = tmem + kOCol + i * D, a = tmem + i * kBN, bv = v_lo + vs * kTileLo;
+#pragma unroll
+                    for (int part = 0; part < (F == AFLEX_CACHE_BF16 ? 2 : 1); ++part)
+#pragma unroll
+                        for (int j = 0; j < kBN / 16; ++j)
+                            umma_ts(to, a + (uint32_t)(part * 64 + j * 8), bv + (uint32_t)((j * 2048) >> 4), idesc_pv, part > 0 || j > 0 ? 1u : first ? 0u : 1u);
+                    umma_commit(&sh.pv_done[i]);
+                };
+                auto have_k = [&]() { ok = ok && mbar_wait(&sh.full[ks], kp); tc_fence_after(); return ok; };
+                auto done_k = [&]() { umma_commit(&sh.empty[ks]); next(ks, kp); };
+                for (; ok; ++pc) {
                     ok = mbar_wait(&sh.told[pc % kPieceRing], (pc / kPieceRing) & 1);
                     if (!ok) break;
                     const DraftPiece& d = sh.piece[pc % kPieceRing];
@@ -205,60 +261,57 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     mbar_arrive(&sh.left[pc % kPieceRing]);
                     if (end) break;
                     if (units == 0) continue;
-                    for (int i = 0; i < 2 && ok; ++i) ok = mbar_wait(&sh.q_ready[i], loaded & 1);
+                    ok = mbar_wait(&sh.q_ready[0], loaded & 1) && mbar_wait(&sh.q_ready[1], loaded & 1);
                     ++loaded;
-                    if (!ok) break;
-                    // S of step t in place i; the place's S / P columns are free once its previous P V has been issued: the pipe runs in order
-                    auto issue_s = [&](int t, int i) {
-                        const int j = slot + 2 * t, s = j % S::kSlots;
-                        ok = ok && mbar_wait(&sh.full[s], (j / S::kSlots) & 1);
-                        if (!ok) return;
-                        tc_fence_after();
-                        const uint32_t k_lo = desc_lo(smem_u32(skv + s * S::kTile), 16), q_lo = desc_lo(smem_u32(sq + i * S::kTile), 16);
-#pragma unroll
-                        for (int ks = 0; ks < D / 16; ++ks)
-                            umma_ss(tmem + (uint32_t)(i * kBN), q_lo + (uint32_t)(((ks / 4) * S::kHalf + (ks % 4) * 32) >> 4),
-                                    k_lo + (uint32_t)(((ks / 4) * S::kHalf + (ks % 4) * 32) >> 4), idesc_s, ks > 0 ? 1u : 0u);
-                        umma_commit(&sh.s_ready[i]);
-                    };
-                    auto free_k = [&](int t) { umma_commit(&sh.empty[(slot + 2 * t) % S::kSlots]); };
-                    // the first steps: of both places, 0; of one tile, 0 and 1
-                    issue_s(0, 0);
-                    if (two && ok) issue_s(0, 1);
-                    if (ok) free_k(0);
-                    if (!two && units > 1 && ok) { issue_s(1, 1); if (ok) free_k(1); }
-                    for (int t = 0; t < units && ok; ++t) {
-                        const int jv = slot + 2 * t + 1, sv = jv % S::kSlots;
-                        for (int i = two ? 0 : t & 1; i < (two ? 2 : (t & 1) + 1) && ok; ++i) {
-                            ok = mbar_wait(&sh.p_ready[i], done[i] & 1);
-                            ok = ok && mbar_wait(&sh.full[sv], (jv / S::kSlots) & 1);
+                    // The pipe runs in order: a place's scores may be issued over its weights as soon as their product has been.
+                    if (two) {
+                        if (!have_k()) break;
+                        issue_s(0);
+                        issue_s(1);
+                        done_k();
+                        for (int t = 0; t < units; ++t) {
+                            const bool more = t + 1 < units;
+                            ok = ok && mbar_wait(&sh.full[vs], vp) && mbar_wait(&sh.p_ready[0], p0);
                             if (!ok) break;
+                            p0 ^= 1;
                             tc_fence_after();
-                            const bool first = two ? t == 0 : t < 2;
-                            const uint32_t v_lo = desc_lo(smem_u32(skv + sv * S::kTile), S::kHalf);
-#pragma unroll
-                            for (int part = 0; part < (F == AFLEX_CACHE_BF16 ? 2 : 1); ++part)
-#pragma unroll
-                                for (int ks = 0; ks < kBN / 16; ++ks)
-                                    umma_ts(tmem + kOCol + (uint32_t)(i * D), tmem + (uint32_t)(i * kBN + part * 64 + ks * 8), v_lo + (uint32_t)((ks * 2048) >> 4), idesc_pv,
-                                            (!first || ks > 0 || part > 0) ? 1u : 0u);
-                            umma_commit(&sh.pv_done[i]);
-                            ++done[i];
-                            // (the slot of V first: the widening of the step after next waits for it)
-                            if (!two || i == 1) umma_commit(&sh.empty[sv]);
-                            if (two && t + 1 < units) { issue_s(t + 1, i); if (i == 1 && ok) free_k(t + 1); }
-                            if (!two && t + 2 < units) { issue_s(t + 2, i); if (ok) free_k(t + 2); }
+                            issue_pv(0, t == 0);
+                            if (more) { if (!have_k()) break; issue_s(0); }
+                            ok = mbar_wait(&sh.p_ready[1], p1);
+                            if (!ok) break;
+                            p1 ^= 1;
+                            tc_fence_after();
+                            issue_pv(1, t == 0);
+                            umma_commit(&sh.empty[vs]);
+                            next(vs, vp);
+                            if (more) { issue_s(1); done_k(); }
+                        }
+                    } else {
+                        for (uint32_t i = 0; i < 2 && (int)i < units; ++i) {
+                            if (!have_k()) break;
+                            issue_s(i);
+                            done_k();
+                        }
+                        for (int t = 0; t < units && ok; ++t) {
+                            const uint32_t i = t & 1;
+                            ok = mbar_wait(&sh.full[vs], vp) && mbar_wait(&sh.p_ready[i], i ? p1 : p0);
+                            if (!ok) break;
+                            if (i) p1 ^= 1; else p0 ^= 1;
+                            tc_fence_after();
+                            issue_pv(i, t < 2);
+                            umma_commit(&sh.empty[vs]);
+                            next(vs, vp);
+                            if (t + 2 < units) { if (!have_k()) break; issue_s(i); done_k(); }
                         }
                     }
-                    slot += 2 * units;
                 }
                 if (!ok) { sh.abort = 1; atomicExch(p.status, AFLEX_ERR_TIMEOUT); }
             }
         }
-    } else if (group == 3) {
+    } else if (group == 5) {
         // ------------------------------------------------------------------ widening; bf16: a look at the V of drafted tokens
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsWiden));
-        const int tid = threadIdx.x - 384;
+        const int tid = threadIdx.x - (kWideThreads - 128);
         int tile_no = 0, step = 0;
         bool ok = true;
         for (int pc = 0; ok; ++pc) {
@@ -292,24 +345,27 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                 reinterpret_cast<float*>(sh.inv[step & 1])[tid] = n == n ? n : 0.f;
                             }
                         }
-                        // a chunk of 16 codes at a time: two chunks of 16 bytes of the tile, half c / 4
-                        constexpr int kPer = D / 16, kRows = 128 / kPer;  // chunks per token, tokens per turn of the group
-                        const int c = tid % kPer, row = tid / kPer;
-                        uint8_t* half = to + (c >> 2) * S::kHalf;
+                        // chunks of 16 codes, each two chunks of 16 bytes of the tile, half c / 4; half of the thread's are loaded before the first
+                        // is widened
+                        constexpr int kPer = D / 16, kRows = 128 / kPer, kTurns = kBN / kRows;      // chunks per token, tokens per turn of the group
+                        const int c = tid % kPer, row = tid / kPer;       // (kRows is a multiple of 8: a token's last three bits are row's)
+                        uint8_t* half = to + (c >> 2) * S::kHalf + row * 128;
                         const uint32_t at0 = (uint32_t)((((c & 3) * 2) ^ (row & 7)) << 4), at1 = at0 ^ 16;
 #pragma unroll
-                        for (int it = 0; it < kBN / kRows; ++it) {
-                            const int token = it * kRows + row;           // (kRows is a multiple of 8: token & 7 == row & 7)
-                            uint4 x = *reinterpret_cast<const uint4*>(raw + token * D + c * 16);
-                            if (isv && token >= here) x = make_uint4(0, 0, 0, 0);          // slots behind the last token may hold anything
-                            uint4 a, b;
-                            if (token >= here && isv) a = b = make_uint4(0, 0, 0, 0);
-                            else {
-                                widen4<F>(x.x, a.x, a.y); widen4<F>(x.y, a.z, a.w);
-                                widen4<F>(x.z, b.x, b.y); widen4<F>(x.w, b.z, b.w);
+                        for (int h = 0; h < 2; ++h) {
+                            uint4 x[kTurns / 2];
+#pragma unroll
+                            for (int it = 0; it < kTurns / 2; ++it) x[it] = *reinterpret_cast<const uint4*>(raw + ((h * (kTurns / 2) + it) * kRows + row) * D + c * 16);
+#pragma unroll
+                            for (int it = 0; it < kTurns / 2; ++it) {
+                                const int turn = h * (kTurns / 2) + it;
+                                uint4 a, b;
+                                widen4<F>(x[it].x, a.x, a.y); widen4<F>(x[it].y, a.z, a.w);
+                                widen4<F>(x[it].z, b.x, b.y); widen4<F>(x[it].w, b.z, b.w);
+                                if (isv && turn * kRows + row >= here) a = b = make_uint4(0, 0, 0, 0);      // slots behind the last token may hold anything
+                                *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at0) = a;
+                                *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at1) = b;
                             }
-                            *reinterpret_cast<uint4*>(half + token * 128 + at0) = a;
-                            *reinterpret_cast<uint4*>(half + token * 128 + at1) = b;
                         }
                         fence_proxy_async();
                         __syncwarp();
@@ -346,16 +402,16 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         }
         if (!ok) give_up();
     } else {
-        // ------------------------------------------------------------------ softmax: a line per thread
+        // ------------------------------------------------------------------ softmax: 16 lines per warp, two (and a quarter of the tokens) per thread
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-        const int place = group, w4 = warp & 3, row = w4 * 32 + lane;
-        const uint32_t lane_base = tmem + ((uint32_t)(w4 * 32) << 16);
+        const int place = warp >> 3, row0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16, hl = lane >> 2, l4 = lane & 3;
+        const uint32_t lane_base = tmem + ((uint32_t)row0 << 16);
         const uint32_t s_addr = lane_base + (uint32_t)(place * kBN), o_addr = lane_base + kOCol;
         int steps_before = 0;                      // of all pieces: the ring's position
         uint32_t done = 0;                         // steps of this place
         bool ok = true;
         uint32_t met = 0;
-        auto meet = [&]() -> bool {                // both softmax groups (a bounded wait: a warp that has given up does not come)
+        auto meet = [&]() -> bool {                // all softmax warps (a bounded wait: a warp that has given up does not come)
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.meet);
             const bool came = wait(&sh.meet, met & 1);
@@ -366,167 +422,195 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         for (int pc = 0; ok; ++pc) {
             ok = wait(&sh.told[pc % kPieceRing], (pc / kPieceRing) & 1);
             if (!ok) break;
-            const DraftPiece d = sh.piece[pc % kPieceRing];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.left[pc % kPieceRing]);
+            const DraftPiece& d = sh.piece[pc % kPieceRing];          // (left when the piece is done)
             if (d.units == 0) break;
             const int units = d.t0 < 0 ? 0 : d.units;
             const bool two = d.lines > kBM;
-            const int line = two ? place * kBM + row : row;
-            const bool there = line < d.lines;
-            const bool busy = (two ? place * kBM : 0) + w4 * 32 < d.lines;                  // (a warp without lines only keeps step)
-            const int mine = line >> p.g_shift, qrow = d.row0 + mine, qi = d.i0 + mine;
-            float c = p.scale_log2;
-            if (units > 0) {
-                // ---- this line's queries into the place's tile, two halves of 128 bytes, swizzled
-                uint8_t* tile = sq + place * S::kTile + row * 128;
-                const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)(there ? qrow : d.row0) * p.Hq + (size_t)d.g * p.G + (line & (p.G - 1))) * D);
-                if (busy) {
-                    uint32_t big = 0;
-                    if (S::kWidens) {
-#pragma unroll 4
-                        for (int k = 0; k < D / 8; ++k) {
-                            const uint4 v = fetch(src + k);
-                            big = __vmaxu2(big, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
-                        }
-                        big = max(big & 0xffffu, big >> 16);
-                    }
-                    // largest in [2^e, 2^(e + 1)): times 2^(14 - e); tiny lines by 2^126
-                    const int e = max((int)(big >> 7) - 127, -112);
-                    const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
-                    if (S::kWidens) c = big >= 0x7f80u ? __uint_as_float(0x7fc00000u) : p.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
-#pragma unroll 4
-                    for (int k = 0; k < D / 8; ++k) {
-                        uint4 v = fetch(src + k);
-                        if (!there) v = make_uint4(0, 0, 0, 0);
-                        if (S::kWidens) {
-                            uint32_t* x = reinterpret_cast<uint32_t*>(&v);
+            const int line0 = (two ? place * kBM : 0) + row0;         // of the warp's first row
+            const bool busy = line0 < d.lines;                        // (a warp without lines only keeps step)
+            if (units > 0 && busy) {
+                // ---- the warp's queries into the place's tile, two halves of 128 bytes, swizzled; D / 8 lanes for a line
+                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kTurns = 16 / kAtOnce;
+                const int sub = lane / kLanes, ch = lane % kLanes;
+                uint4 v[kTurns];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const __half2 h = __floats2half2_rn(__uint_as_float(x[i] << 16) * up, __uint_as_float(x[i] & 0xffff0000u) * up);
-                                x[i] = *reinterpret_cast<const uint32_t*>(&h);
-                            }
+                for (int it = 0; it < kTurns; ++it) {
+                    const int line = line0 + it * kAtOnce + sub;
+                    v[it] = make_uint4(0, 0, 0, 0);
+                    if (line < d.lines)
+                        v[it] = fetch(reinterpret_cast<const uint4*>(p.q + ((size_t)(d.row0 + (line >> p.g_shift)) * p.Hq + (size_t)d.g * p.G + (line & (p.G - 1))) * D) + ch);
+                }
+#pragma unroll
+                for (int it = 0; it < kTurns; ++it) {
+                    const int row = row0 + it * kAtOnce + sub;
+                    float c = p.scale_log2;
+                    if (S::kWidens) {
+                        uint32_t* x = reinterpret_cast<uint32_t*>(&v[it]);
+                        uint32_t big = __vmaxu2(__vmaxu2(x[0] & 0x7fff7fffu, x[1] & 0x7fff7fffu), __vmaxu2(x[2] & 0x7fff7fffu, x[3] & 0x7fff7fffu));
+                        big = max(big & 0xffffu, big >> 16);
+#pragma unroll
+                        for (int off = 1; off < kLanes; off <<= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, off));
+                        // largest in [2^e, 2^(e + 1)): times 2^(14 - e); tiny lines by 2^126
+                        const int e = max((int)(big >> 7) - 127, -112);
+                        const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+                        c = big >= 0x7f80u ? __uint_as_float(0x7fc00000u) : p.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const __half2 h = __floats2half2_rn(__uint_as_float(x[i] << 16) * up, __uint_as_float(x[i] & 0xffff0000u) * up);
+                            x[i] = *reinterpret_cast<const uint32_t*>(&h);
                         }
-                        *reinterpret_cast<uint4*>(tile + (k >> 3) * S::kHalf + (((k & 7) ^ (row & 7)) << 4)) = v;
                     }
+                    *reinterpret_cast<uint4*>(sq + place * S::kTile + (ch >> 3) * S::kHalf + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) = v[it];
+                    if (ch == 0) sh.factor[place][row] = c;
                 }
                 fence_proxy_async();
             }
             __syncwarp();
             if (units > 0 && lane == 0) mbar_arrive(&sh.q_ready[place]);
-            float m = kLowest, l = 0.f;
-            const int first = two ? 0 : place, by = two ? 1 : 2;
+            float m[2] = {kLowest, kLowest}, l[2] = {0.f, 0.f}, c[2] = {0.f, 0.f};
+            if (units > 0 && busy) { c[0] = sh.factor[place][row0 + hl]; c[1] = sh.factor[place][row0 + hl + 8]; }
+            const int plain = min(d.ctx, d.sees), t0 = d.t0;
             int mine_steps = 0;
-            for (int t = first; t < units && ok; t += by, ++done, ++mine_steps) {
-                const int step = steps_before + t, jv = 2 * step + 1, sv = jv % S::kSlots, col0 = d.t0 + t * kBN;
+            for (int t = two ? 0 : place; t < units && ok; t += two ? 1 : 2, ++done, ++mine_steps) {
+                const int step = steps_before + t, jv = 2 * step + 1, sv = jv % S::kSlots;
                 ok = wait(&sh.s_ready[place], done & 1);
-                const bool masked = col0 + kBN > min(d.ctx, d.sees);
+                const bool masked = t0 + (t + 1) * kBN > plain;
                 if (S::kWidens || masked) ok = ok && wait(&sh.full[sv], (jv / S::kSlots) & 1);      // (the scales, and what is known of V)
                 if (!ok) break;
-                tc_fence_after();
                 if (busy) {
-                    float x[kBN];
-#pragma unroll
-                    for (int c0 = 0; c0 < kBN; c0 += 16) tmem_ld_32x32b_x16(s_addr + (uint32_t)c0, *reinterpret_cast<uint32_t(*)[16]>(&x[c0]));
+                    tc_fence_after();
+                    uint32_t x[64];                // scores, then weights
+                    tmem_ld_16x256b_x4_at<0>(s_addr, x);
+                    tmem_ld_16x256b_x4_at<16>(s_addr + 32, x);
+                    tmem_ld_16x256b_x4_at<32>(s_addr + 64, x);
+                    tmem_ld_16x256b_x4_at<48>(s_addr + 96, x);
                     tmem_ld_wait();
-                    const uint64_t cc = pack_f32x2(c, c);
+                    float mx[2] = {-INFINITY, -INFINITY};
+                    const ulonglong2* scales = reinterpret_cast<const ulonglong2*>(sh.scale[step & 1]) + l4;
+                    const uint64_t cc[2] = {pack_f32x2(c[0], c[0]), pack_f32x2(c[1], c[1])};
 #pragma unroll
-                    for (int j = 0; j < kBN; j += 2) {
-                        uint64_t v = mul_f32x2(pack_f32x2(x[j], x[j + 1]), cc);
-                        if (S::kWidens) {
-                            const ulonglong2 sc = *reinterpret_cast<const ulonglong2*>(&sh.scale[step & 1][j >> 1]);
-                            v = fma_f32x2(v, sc.x, sc.y);
+                    for (int i = 0; i < 16; ++i) {
+                        ulonglong2 sc;
+                        if (S::kWidens) sc = scales[4 * i];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            uint64_t v = mul_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), cc[y]);
+                            if (S::kWidens) v = fma_f32x2(v, sc.x, sc.y);
+                            float a, b;
+                            unpack_f32x2(v, a, b);
+                            x[4 * i + 2 * y] = __float_as_uint(a);
+                            x[4 * i + 2 * y + 1] = __float_as_uint(b);
                         }
-                        unpack_f32x2(v, x[j], x[j + 1]);
                     }
-                    bool poison = false;
+                    bool poison[2] = {false, false};
                     if (masked) {
 #pragma unroll
-                        for (int q = 0; q < kBN / 32; ++q) {
-                            // which of 32 tokens this line sees
-                            const int j0 = col0 + 32 * q - d.ctx;         // drafted token of the first of them
-                            uint32_t see = 0xffffffffu;
-                            const int last = d.sees - (col0 + 32 * q);    // tokens behind the last do not count
-                            if (last < 32) see = last <= 0 ? 0u : (1u << last) - 1u;
-                            if (j0 + 31 >= 0 && see != 0) {
-                                uint32_t drafted;                         // bits of tokens j0 .. j0 + 31, earlier ones set
-                                const uint32_t early = j0 < 0 ? (1u << -j0) - 1u : 0u;
-                                if (p.mask == nullptr) {
-                                    const int upto = qi - j0 + 1;         // tokens 0 .. qi
-                                    drafted = upto >= 32 ? 0xffffffffu : upto <= 0 ? 0u : (1u << upto) - 1u;
-                                } else {
-                                    auto word = [&](int i) -> uint32_t { return there && i >= 0 && i < p.mask_words ? fetch(p.mask + (size_t)qrow * p.mask_words + i) : 0u; };
-                                    const int wi = j0 >> 5, sft = j0 & 31;                  // (arithmetic shift: -1 for tokens before the first)
-                                    drafted = __funnelshift_r(word(wi), word(wi + 1), (uint32_t)sft);
-                                    const int over = d.m - j0;            // bits of tokens that there are
-                                    if (over < 32) drafted &= over <= 0 ? 0u : (1u << over) - 1u;
-                                }
-                                see &= drafted | early;
-                            }
-                            if (!there) see = 0;
-                            if (!S::kWidens && (see & sh.bad[step & 3][q])) poison = true;
+                        for (int y = 0; y < 2; ++y) {
+                            const int line = line0 + hl + 8 * y, mine = line >> p.g_shift, qi = d.i0 + mine;
+                            const bool there = line < d.lines;
+                            const uint32_t* mask = p.mask + (size_t)(d.row0 + mine) * p.mask_words;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) if (!(see >> j & 1u)) x[32 * q + j] = -INFINITY;
+                            for (int q = 0; q < 4; ++q) {
+                                // which of 32 tokens this line sees
+                                const int t32 = t0 + t * kBN + 32 * q, j0 = t32 - d.ctx;                // the first of them, its number among the drafted
+                                uint32_t see = 0xffffffffu;
+                                const int last = d.sees - t32;            // tokens behind the last do not count
+                                if (last < 32) see = last <= 0 ? 0u : (1u << last) - 1u;
+                                if (j0 + 31 >= 0 && see != 0) {
+                                    uint32_t drafted;                     // bits of tokens j0 .. j0 + 31, earlier ones set
+                                    const uint32_t early = j0 < 0 ? (1u << -j0) - 1u : 0u;
+                                    if (p.mask == nullptr) {
+                                        const int upto = qi - j0 + 1;     // tokens 0 .. qi
+                                        drafted = upto >= 32 ? 0xffffffffu : upto <= 0 ? 0u : (1u << upto) - 1u;
+                                    } else {
+                                        auto word = [&](int i) -> uint32_t { return there && i >= 0 && i < p.mask_words ? fetch(mask + i) : 0u; };
+                                        const int wi = j0 >> 5, sft = j0 & 31;              // (arithmetic shift: -1 for tokens before the first)
+                                        drafted = __funnelshift_r(word(wi), word(wi + 1), (uint32_t)sft);
+                                        const int over = d.m - j0;        // bits of tokens that there are
+                                        if (over < 32) drafted &= over <= 0 ? 0u : (1u << over) - 1u;
+                                    }
+                                    see &= drafted | early;
+                                }
+                                if (!there) see = 0;
+                                if (!S::kWidens && (see & sh.bad[step & 3][q])) poison[y] = true;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                    for (int e = 0; e < 2; ++e)
+                                        if (!(see >> (8 * i + 2 * l4 + e) & 1u)) x[4 * (4 * q + i) + 2 * y + e] = 0xff800000u;
+                            }
                         }
                     }
-                    float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
-                    for (int j = 0; j < kBN; j += 4) {
-                        mx0 = fmaxf(mx0, x[j]); mx1 = fmaxf(mx1, x[j + 1]); mx2 = fmaxf(mx2, x[j + 2]); mx3 = fmaxf(mx3, x[j + 3]);
-                    }
-                    const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+                    for (int i = 0; i < 16; ++i)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) mx[y] = fmaxf(mx[y], fmaxf(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])));
                     // weights are 2^(x - m), m the running maximum less 8: below 2^15 until a score outgrows it
-                    if (__any_sync(0xffffffffu, mx > m + 15.f)) {
-                        const float mn = fmaxf(m, mx - 8.f), corr = fast_exp2(m - mn);
-                        m = mn;
-                        l *= corr;
+                    if (__any_sync(0xffffffffu, mx[0] > m[0] + 15.f || mx[1] > m[1] + 15.f)) {
+                        float corr[2];
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
+                            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
+                            const float mn = fmaxf(m[y], mx[y] - 8.f);
+                            corr[y] = fast_exp2(m[y] - mn);
+                            m[y] = mn;
+                            l[y] *= corr[y];
+                        }
                         if (mine_steps > 0) {
                             ok = wait(&sh.pv_done[place], (done - 1) & 1);
-                            if (!ok) break;                // (leaves the steps; noticed below)
+                            if (!ok) break;
                             tc_fence_after();
-#pragma unroll
-                            for (int c0 = 0; c0 < D; c0 += 16) {
+#pragma unroll 1
+                            for (int c0 = 0; c0 < D; c0 += 32) {
                                 uint32_t r[16];
-                                tmem_ld_32x32b_x16(o_addr + (uint32_t)(place * D + c0), r);
+                                tmem_ld_16x256b_x4(o_addr + (uint32_t)(place * D + c0), r);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(__uint_as_float(r[j]) * corr);
-                                tmem_st_32x32b_x16(o_addr + (uint32_t)(place * D + c0), r);
+                                for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr[(i >> 1) & 1]);
+                                tmem_st_16x256b_x4(o_addr + (uint32_t)(place * D + c0), r);
                             }
                         }
                     }
-                    const uint64_t m2 = pack_f32x2(-m, -m), one = pack_f32x2(1.f, 1.f);
-                    uint64_t l0 = 0, l1 = 0;
+                    uint32_t hi[32], lo[32];
+                    const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 1]) + l4;
+                    const uint64_t one = pack_f32x2(1.f, 1.f), m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
+                    uint64_t sum[2] = {0, 0};
 #pragma unroll
-                    for (int c0 = 0; c0 < kBN; c0 += 32) {
-                        uint32_t hi[16], lo[16];
+                    for (int i = 0; i < 16; ++i) {
+                        uint64_t n = one;
+                        if (S::kWidens) { const float2 v = invs[4 * i]; n = pack_f32x2(v.x, v.y); }
 #pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
+                        for (int y = 0; y < 2; ++y) {
                             float w0, w1;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(x[c0 + j], x[c0 + j + 1]), one, m2), w0, w1);
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), one, m2[y]), w0, w1);
                             w0 = fast_exp2(w0);
                             w1 = fast_exp2(w1);
-                            uint64_t& sum = j & 2 ? l1 : l0;
+                            sum[y] = fma_f32x2(pack_f32x2(w0, w1), n, sum[y]);
+                            uint32_t& h = hi[2 * i + y];
                             if (S::kWidens) {
-                                const float2 n = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(sh.inv[step & 1]) + c0 + j);
-                                sum = fma_f32x2(pack_f32x2(w0, w1), pack_f32x2(n.x, n.y), sum);
-                                const __half2 h = __floats2half2_rn(w0, w1);
-                                hi[j >> 1] = *reinterpret_cast<const uint32_t*>(&h);
+                                const __half2 f = __floats2half2_rn(w0, w1);
+                                h = *reinterpret_cast<const uint32_t*>(&f);
                             } else {
-                                sum = fma_f32x2(pack_f32x2(w0, w1), one, sum);
-                                hi[j >> 1] = pack_bf16x2(w0, w1);
-                                lo[j >> 1] = pack_bf16x2(w0 - __uint_as_float(hi[j >> 1] << 16), w1 - __uint_as_float(hi[j >> 1] & 0xffff0000u));
+                                h = pack_bf16x2(w0, w1);
+                                lo[2 * i + y] = pack_bf16x2(w0 - __uint_as_float(h << 16), w1 - __uint_as_float(h & 0xffff0000u));
                             }
                         }
-                        tmem_st_32x32b_x16(s_addr + (uint32_t)(c0 / 2), hi);
-                        if (!S::kWidens) tmem_st_32x32b_x16(s_addr + 64 + (uint32_t)(c0 / 2), lo);
+                    }
+                    tmem_st_16x128b_x8_at<0>(s_addr, hi);
+                    tmem_st_16x128b_x8_at<16>(s_addr + 32, hi);
+                    if (!S::kWidens) {
+                        tmem_st_16x128b_x8_at<0>(s_addr + 64, lo);
+                        tmem_st_16x128b_x8_at<16>(s_addr + 96, lo);
                     }
                     tmem_st_wait();
-                    float a, b, e, f;
-                    unpack_f32x2(l0, a, b);
-                    unpack_f32x2(l1, e, f);
-                    l += (a + b) + (e + f);
-                    if (poison) l = __uint_as_float(0x7fc00000u);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        float a, b;
+                        unpack_f32x2(sum[y], a, b);
+                        l[y] += a + b;
+                        if (poison[y]) l[y] = __uint_as_float(0x7fc00000u);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -537,68 +621,83 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             // ---- the piece is done: normalised to the output, or its sums to the CTA's slot
             if (mine_steps > 0) ok = wait(&sh.pv_done[place], (done - 1) & 1);
             if (!ok) break;
-            float* slot = p.parts + ((size_t)blockIdx.x * 2 + d.slot) * kWideSlot<D>;
-            float f[2] = {0.f, 0.f};               // what the places' sums count; 0: nothing is there
-            int ch0 = 0, ch1 = D;                  // channels that this thread stores
-            if (two || units == 0) f[place] = units > 0 ? 1.f : 0.f;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                l[y] += __shfl_xor_sync(0xffffffffu, l[y], 1);
+                l[y] += __shfl_xor_sync(0xffffffffu, l[y], 2);
+            }
+            float f[2][2] = {{1.f, 0.f}, {1.f, 0.f}};       // [line][this place's sums, the other's]: what they count
+            const bool use[2] = {mine_steps > 0, !two && (place == 1 ? units > 0 : units > 1)};      // (an empty place's accumulator holds anything)
+            int ch0 = 0, ch1 = D;
+            tc_fence_after();
             if (!two) {
-                // both groups learn of both states, and store half of the channels each
-                sh.state[place][row] = make_float2(m, l);
-                tc_fence_after();
+                // one tile in two places: both learn of the other's states, and store half of the channels each
+                if (l4 == 0) {
+                    sh.state[place][row0 + hl] = make_float2(m[0], l[0]);
+                    sh.state[place][row0 + hl + 8] = make_float2(m[1], l[1]);
+                }
                 tc_fence_before();
                 ok = meet();
                 if (!ok) break;
-                const float2 other = sh.state[place ^ 1][row];
-                const float M = fmaxf(m, other.x), mine_f = fast_exp2(m - M), other_f = fast_exp2(other.x - M);
-                l = l * mine_f + other.y * other_f;
-                m = M;
-                if (units > 0) {                   // (an empty place's accumulator holds anything)
-                    f[place] = mine_steps > 0 ? mine_f : 0.f;
-                    f[place ^ 1] = place == 1 || units > 1 ? other_f : 0.f;
+                tc_fence_after();
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const float2 other = sh.state[place ^ 1][row0 + hl + 8 * y];
+                    const float M = fmaxf(m[y], other.x);
+                    f[y][0] = fast_exp2(m[y] - M);
+                    f[y][1] = fast_exp2(other.x - M);
+                    l[y] = l[y] * f[y][0] + other.y * f[y][1];
+                    m[y] = M;
                 }
                 ch0 = place * (D / 2);
                 ch1 = ch0 + D / 2;
             }
-            tc_fence_after();
             if (busy) {
-                const bool use0 = two ? place == 0 && units > 0 : units > 0, use1 = two ? place == 1 && units > 0 : units > 1;
-                const float inv = l == 0.f ? 0.f : __frcp_rn(l);
-                const size_t hq = (size_t)(there ? qrow : d.row0) * p.Hq + (size_t)d.g * p.G + (line & (p.G - 1));
-                uint4* out = reinterpret_cast<uint4*>(p.out + hq * D);
-#pragma unroll 1
-                for (int c0 = ch0; c0 < ch1; c0 += 16) {
-                    float x[16];
+                float* slot = p.parts + ((size_t)blockIdx.x * 2 + d.slot) * kWideSlot<D>;
+                const bool whole = d.whole;
+                float inv[2];
+                size_t hq[2];
+                bool there[2];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (i == 0 ? use0 : use1) {
-                            uint32_t r[16];
-                            tmem_ld_32x32b_x16(o_addr + (uint32_t)(i * D + c0), r);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) x[j] = fmaf(__uint_as_float(r[j]), f[i], x[j]);
-                        }
-                    }
-                    if (there && d.whole) {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) w[j >> 1] = pack_bf16x2(x[j] * inv, x[j + 1] * inv);
-                        out[c0 / 8] = make_uint4(w[0], w[1], w[2], w[3]);
-                        out[c0 / 8 + 1] = make_uint4(w[4], w[5], w[6], w[7]);
-                    } else if (there) {
-#pragma unroll
-                        for (int j = 0; j < 16; j += 4)
-                            __stcg(reinterpret_cast<float4*>(slot + kWideCarry) + ((c0 + j) >> 2) * kWideLines + line, make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]));
+                for (int y = 0; y < 2; ++y) {
+                    const int line = line0 + hl + 8 * y;
+                    there[y] = line < d.lines;
+                    hq[y] = (size_t)(d.row0 + (line >> p.g_shift)) * p.Hq + (size_t)d.g * p.G + (line & (p.G - 1));
+                    inv[y] = l[y] == 0.f ? 0.f : __frcp_rn(l[y]);
+                    if (there[y] && ch0 == 0 && l4 == 0) {
+                        if (!whole) __stcg(reinterpret_cast<float2*>(slot) + line, make_float2(m[y], l[y]));
+                        else if (p.lse != nullptr) p.lse[hq[y]] = l[y] == 0.f ? -INFINITY : (m[y] + __log2f(l[y])) * 0.6931471805599453f;
                     }
                 }
-                if (there && ch0 == 0) {
-                    if (!d.whole) __stcg(reinterpret_cast<float2*>(slot) + line, make_float2(m, l));
-                    else if (p.lse != nullptr) p.lse[hq] = l == 0.f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
+#pragma unroll 1
+                for (int c0 = ch0; c0 < ch1; c0 += 32) {
+                    float x[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+                    for (int o = 0; o < 2; ++o) {
+                        if (use[o]) {
+                            uint32_t r[16];
+                            tmem_ld_16x256b_x4(o_addr + (uint32_t)((place ^ o) * D + c0), r);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x[i] = fmaf(__uint_as_float(r[i]), f[(i >> 1) & 1][o], x[i]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const int ch = c0 + 8 * i + 2 * l4;
+                            if (!there[y]) continue;
+                            if (whole) *reinterpret_cast<uint32_t*>(p.out + hq[y] * D + ch) = pack_bf16x2(x[4 * i + 2 * y] * inv[y], x[4 * i + 2 * y + 1] * inv[y]);
+                            else __stcg(reinterpret_cast<float2*>(slot + kWideCarry + ((ch >> 2) * kWideLines + line0 + hl + 8 * y) * 4 + (ch & 2)), make_float2(x[4 * i + 2 * y], x[4 * i + 2 * y + 1]));
+                        }
                 }
             }
             tc_fence_before();
-            if (!two || !d.whole) {                // the next piece's products go where the other group still reads; the slot has to be complete
+            // the next piece's products go where the other place still reads; a slot has to be complete
+            if (!two || !d.whole) {
                 ok = meet();
                 if (!ok) break;
             }
@@ -611,14 +710,16 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     sh.merge[sh.merges++] = d;
                 }
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.left[pc % kPieceRing]);
         }
-        // ---- join the pieces of the items that this CTA was the last one to work on, a line per thread
+        // ---- join the pieces of the items that this CTA was the last one to work on, half of a line per thread
         ok = ok && meet();
         if (ok) {
             __threadfence();
             for (int j = 0; j < sh.merges; ++j) {
                 const DraftPiece& d = sh.merge[j];
-                const int c0 = sh.share.cta_of(d.first), n = sh.share.cta_of(d.last) - c0 + 1, line = threadIdx.x;
+                const int c0 = sh.share.cta_of(d.first), n = sh.share.cta_of(d.last) - c0 + 1, line = threadIdx.x % kWideLines, part_of = threadIdx.x / kWideLines;
                 if (line >= d.lines) continue;
                 auto part = [&](int k) -> const float* { return p.parts + ((size_t)(c0 + k) * 2 + (k == 0 ? 1 : 0)) * kWideSlot<D>; };       // (the first CTA's second slot)
                 float M = kLowest, L = 0.f;
@@ -629,7 +730,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 }
                 constexpr int kAtOnce = 8;         // runs of four channels
 #pragma unroll 1
-                for (int r0 = 0; r0 < D / 4; r0 += kAtOnce) {
+                for (int r0 = part_of * (D / 8); r0 < (part_of + 1) * (D / 8); r0 += kAtOnce) {
                     float4 acc[kAtOnce];
 #pragma unroll
                     for (int r = 0; r < kAtOnce; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -651,7 +752,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+    if (warp == kSoftmaxWarps + 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
 }
 
 template <int D, int F>

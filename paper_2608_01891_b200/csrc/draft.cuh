@@ -2,7 +2,8 @@
 //
 // A tile is a run of up to `rpt` rows of one sequence; its lines are the rows' queries of one KV head's group.  An item is a tile and a
 // KV head; it has one unit of kTokens cached tokens after another, up to the last token that a row of the tile may see, and one empty
-// unit in front (what starting and joining an item costs).  All items' units in a list, cut anywhere into equal shares, a share per CTA:
+// unit in front (what starting and joining an item costs).  In the kernel whose tiles are 256 lines, a unit of more than 128 lines takes two places.
+// All items' units in a list, cut anywhere into equal shares, a share per CTA:
 // no plan on the host, which does not know the lengths, and no CTA that is left with a long sequence.
 #pragma once
 #include <cuda_fp16.h>
@@ -53,18 +54,22 @@ __device__ __forceinline__ DraftSeq draft_seq(const DraftParams& p, int b) {
     return s;
 }
 
-template <int kTokens> struct DraftList {
+template <int kTokens, int kFull> struct DraftList {        // kFull: places of a full tile's unit
     static constexpr int kShift = kTokens == 128 ? 7 : 6;
     static_assert(kTokens == 1 << kShift, "");
-    int rpt_shift;
+    int rpt_shift, g_shift;
     bool causal;
-    __device__ DraftList(const DraftParams& p) : rpt_shift(p.rpt_shift), causal(p.mask == nullptr) {}
+    __device__ DraftList(const DraftParams& p) : rpt_shift(p.rpt_shift), g_shift(p.g_shift), causal(p.mask == nullptr) {}
     __device__ int tiles(const DraftSeq& s) const { return (s.m + (1 << rpt_shift) - 1) >> rpt_shift; }
-    // tokens that the rows of a tile may see, units of one of its items (the empty one among them)
+    // tokens that the rows of a tile may see, units of one of its items, places of a unit, places of the item (the empty one among them)
     __device__ int sees(const DraftSeq& s, int tile) const {
         return !s.ok ? 0 : causal ? s.ctx + (int)min((long long)s.m, (long long)(tile + 1) << rpt_shift) : s.len;
     }
-    __device__ int units(const DraftSeq& s, int tile) const { return 1 + ((sees(s, tile) + kTokens - 1) >> kShift); }
+    __device__ int units(const DraftSeq& s, int tile) const { return (sees(s, tile) + kTokens - 1) >> kShift; }
+    __device__ int weight(const DraftSeq& s, int tile) const {
+        return kFull == 1 || (min(1 << rpt_shift, s.m - (tile << rpt_shift)) << g_shift) <= 128 ? 1 : kFull;
+    }
+    __device__ int places(const DraftSeq& s, int tile) const { return 1 + weight(s, tile) * units(s, tile); }
     // sum over i = 1 .. x of ceil(i / q), q = tiles whose rows make a unit of tokens (a power of two); of k i where a tile's rows are k units
     __device__ long long ramp(long long x) const {
         const int qs = kShift - rpt_shift;
@@ -72,15 +77,20 @@ template <int kTokens> struct DraftList {
         const long long y = x >> qs, z = x - (y << qs);
         return ((y * (y + 1)) << qs >> 1) + z * (y + 1);
     }
-    // units of the sequence's first `n` tiles, for one KV head; all but a sequence's last tile are full, and with a = ceil(ctx / rows per tile)
+    // places of the sequence's first `n` tiles, for one KV head; all but a sequence's last tile are full, and with a = ceil(ctx / rows per tile)
     // a full tile t's tokens are ceil((a + t + 1) / q) units
     __device__ long long before(const DraftSeq& s, int n) const {
         if (n == 0) return 0;
-        if (!causal || !s.ok || n == 1) return (long long)n * units(s, 0);
         const int full = min(n, tiles(s) - 1);
-        if (rpt_shift > kShift) return (long long)full * (1 + ((s.ctx + kTokens - 1) >> kShift)) + ramp(full) + (n > full ? units(s, n - 1) : 0);
-        const long long a = (s.ctx + (1 << rpt_shift) - 1) >> rpt_shift;
-        return ramp(a + full) - ramp(a) + full + (n > full ? units(s, n - 1) : 0);
+        long long sum = 0;
+        if (full > 0) {
+            const long long a = (s.ctx + (1 << rpt_shift) - 1) >> rpt_shift;
+            if (!s.ok) sum = 0;
+            else if (!causal) sum = (long long)full * units(s, 0);
+            else if (rpt_shift > kShift) sum = (long long)full * ((s.ctx + kTokens - 1) >> kShift) + ramp(full);
+            else sum = ramp(a + full) - ramp(a);
+        }
+        return full + kFull * sum + (n > full ? places(s, n - 1) : 0);
     }
 };
 
@@ -89,12 +99,13 @@ __device__ __forceinline__ long long draft_div(long long a, long long b) {
     return (unsigned long long)(a | b) >> 32 ? a / b : (long long)((uint32_t)a / (uint32_t)b);
 }
 
-// A place in the list: unit u of the item (tile of sequence b, KV head g); position `pos` of all.
-template <int kTokens> struct DraftWalk {
+// A place in the list: place u of the item (tile of sequence b, KV head g), of nu; position `pos` of all.
+template <int kTokens, int kFull> struct DraftWalk {
+    typedef DraftList<kTokens, kFull> List;
     long long pos;
     int b, tile, g, u, nu, id;     // id: number of the tile's first item
     DraftSeq s;
-    __device__ void start(const DraftParams& p, const DraftList<kTokens>& list, long long x, int seq, long long seq_first, int seq_tiles) {
+    __device__ void start(const DraftParams& p, const List& list, long long x, int seq, long long seq_first, int seq_tiles) {
         pos = x; b = seq;
         s = draft_seq(p, b);
         const long long rel = x - seq_first;
@@ -105,13 +116,13 @@ template <int kTokens> struct DraftWalk {
         }
         tile = lo;
         id = (seq_tiles + tile) * p.Hkv;
-        nu = list.units(s, tile);
+        nu = list.places(s, tile);
         const long long in = rel - list.before(s, tile) * p.Hkv;
         g = (int)draft_div(in, nu);
         u = (int)(in - (long long)g * nu);
     }
-    // n units on, inside the item or to the start of the next one; `end`: the list's length
-    __device__ void advance(const DraftParams& p, const DraftList<kTokens>& list, int n, long long end) {
+    // n places on, inside the item or to the start of the next one; `end`: the list's length
+    __device__ void advance(const DraftParams& p, const List& list, int n, long long end) {
         pos += n; u += n;
         if (u < nu || pos >= end) return;
         u = 0;
@@ -122,28 +133,30 @@ template <int kTokens> struct DraftWalk {
             tile = 0;
             do s = draft_seq(p, ++b); while (s.m == 0);      // (there is another, or pos would be the end)
         }
-        nu = list.units(s, tile);
+        nu = list.places(s, tile);
     }
+    __device__ int until(long long x1) const { return (int)min((long long)nu, u + (x1 - pos)); }      // the item's places before x1
 };
 
-// A piece: a run of units of one item.
+// A piece: a run of units of one item.  A unit belongs to the CTA that has its first place.
 struct DraftPiece {
-    int units, t0, sees, ctx;      // units with tokens, or 1 for an item without (0: the share ends); first token, tokens the tile's rows may see, earlier tokens
+    int units, t0, sees, ctx;      // units with tokens, or 1 for an item without (t0 < 0); first token, tokens the tile's rows may see, earlier tokens
     int row0, lines, i0, m, g;     // first row and lines of the tile, number of the first row and of all rows in the sequence, KV head
     int item, slot, whole;
     long long first, last;         // positions of the item's first and last unit with tokens
 };
-// The piece that starts at w (not at the empty unit of an item that has tokens) and ends with the item or at x1.
-template <int kTokens>
-__device__ __forceinline__ DraftPiece draft_piece(const DraftParams& p, const DraftList<kTokens>& list, const DraftWalk<kTokens>& w, long long x1) {
+// The piece that starts at w (not at the empty place of an item that has tokens) and ends with the item or at x1; no units: nothing to do.
+template <int kTokens, int kFull>
+__device__ __forceinline__ DraftPiece draft_piece(const DraftParams& p, const DraftList<kTokens, kFull>& list, const DraftWalk<kTokens, kFull>& w, long long x1) {
     DraftPiece d;
-    const int u1 = (int)min((long long)w.nu, w.u + (x1 - w.pos));                        // (w.u = 0: an item without tokens)
-    d.units = u1 - w.u; d.t0 = (w.u - 1) * kTokens;
+    const int wt = list.weight(w.s, w.tile), all = list.units(w.s, w.tile);
+    const int k0 = w.u == 0 ? -1 : (w.u - 1 + wt - 1) / wt, k1 = w.u == 0 ? 0 : (w.until(x1) - 1 + wt - 1) / wt;
+    d.units = k1 - k0; d.t0 = k0 * kTokens;
     d.sees = list.sees(w.s, w.tile); d.ctx = w.s.ctx;
     d.i0 = w.tile << p.rpt_shift; d.row0 = w.s.o0 + d.i0; d.m = w.s.m; d.g = w.g;
-    d.lines = min(1 << p.rpt_shift, w.s.m - d.i0) * p.G;
-    d.item = w.id + w.g; d.slot = w.u > 1 ? 0 : 1; d.whole = w.u <= 1 && u1 == w.nu;
-    d.first = w.pos - w.u + 1; d.last = w.pos - w.u + w.nu - 1;
+    d.lines = min(1 << p.rpt_shift, w.s.m - d.i0) << p.g_shift;
+    d.item = w.id + w.g; d.slot = k0 > 0 ? 0 : 1; d.whole = k0 <= 0 && k1 == all;
+    d.first = w.pos - w.u + 1; d.last = d.first + (long long)wt * (all - 1);
     return d;
 }
 
@@ -167,8 +180,8 @@ struct DraftShare {
     }
 };
 // All kThreads threads of the CTA, thread t a run of sequences; returns after a barrier.
-template <int kTokens, int kThreads>
-__device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList<kTokens>& list, DraftShare& out) {
+template <int kThreads, int kTokens, int kFull>
+__device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList<kTokens, kFull>& list, DraftShare& out) {
     __shared__ long long s_units[kThreads / 32];
     __shared__ int s_tiles[kThreads / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -202,7 +215,7 @@ __device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList
     total *= p.Hkv;
     DraftShare share;
     share.total = total;
-    share.ctas = (int)min((long long)gridDim.x, total);
+    share.ctas = (int)min((long long)gridDim.x, max(total / kFull, min(total, 1LL)));       // (at least a unit's places each)
     share.each = share.ctas > 0 ? draft_div(total, share.ctas) : 0;
     share.more = share.ctas > 0 ? (int)(total - share.each * share.ctas) : 0;
     const bool works = (int)blockIdx.x < share.ctas;
