@@ -35,7 +35,7 @@ constexpr int kUnitPages = kBN / kPageTokens;
 constexpr int kWideLines = 2 * kBM;
 constexpr int kSoftmaxWarps = 16;                  // [place][half of 32 lines][32 lines]
 constexpr int kWideThreads = (kSoftmaxWarps + 8) * 32;       // and the warp groups of producer + issuer, and of widening
-constexpr int kRegsSoftmax = 88, kRegsIssue = 64, kRegsWiden = 64;
+constexpr int kRegsSoftmax = 80, kRegsIssue = 80, kRegsWiden = 80;
 static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + 128 * kRegsIssue + 128 * kRegsWiden <= kWideThreads * 80, "the warp groups share what the block was launched with");
 constexpr int kPieceRing = 4;
 
@@ -69,28 +69,39 @@ struct __align__(16) WideShared {
     volatile int abort;
 };
 
+// Two weights of a line as operand: fp16, or the two bf16 parts.
+template <int F> __device__ __forceinline__ void pack_weights(float w0, float w1, uint32_t& hi, uint32_t& lo) {
+    if (F == AFLEX_CACHE_BF16) {
+        hi = pack_bf16x2(w0, w1);
+        lo = pack_bf16x2(w0 - __uint_as_float(hi << 16), w1 - __uint_as_float(hi & 0xffff0000u));
+    } else {
+        const __half2 f = __floats2half2_rn(w0, w1);
+        hi = *reinterpret_cast<const uint32_t*>(&f);
+    }
+}
+
 template <int F> __device__ __forceinline__ uint32_t wide_idesc(uint32_t n) {
     const uint32_t d = umma_idesc_bf16(kBM, n);
     return F == AFLEX_CACHE_BF16 ? d : d & ~((1u << 7) | (1u << 10));                     // fp16 operands
 }
 
-// TMEM fragments: 16 lines x 128 columns (element 4 i + 2 y + e: line lane / 4 + 8 y, column 8 i + 2 (lane % 4) + e), and stores of 16 lines x 64
+// TMEM fragments: 16 lines x 32 columns (element 4 i + 2 y + e: line lane / 4 + 8 y, column 8 i + 2 (lane % 4) + e), and of 16 lines x 32 packed
 // columns (element 2 i + y: line lane / 4 + 8 y, column 4 i + lane % 4): a pair of the one packed is an element of the other.
 #define R4(a, i) "=r"(a[i]), "=r"(a[i + 1]), "=r"(a[i + 2]), "=r"(a[i + 3])
 #define R16(a, i) R4(a, i), R4(a, i + 4), R4(a, i + 8), R4(a, i + 12)
 #define I4(a, i) "r"(a[i]), "r"(a[i + 1]), "r"(a[i + 2]), "r"(a[i + 3])
 #define I16(a, i) I4(a, i), I4(a, i + 4), I4(a, i + 8), I4(a, i + 12)
-template <int kAt> __device__ __forceinline__ void tmem_ld_16x256b_x4_at(uint32_t taddr, uint32_t (&r)[64]) {      // 32 columns into elements kAt ..
-    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];" : R16(r, kAt) : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ void tmem_ld_16x256b_x4(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];" : R16(r, 0) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_st_16x256b_x4(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), I16(r, 0) : "memory");
 }
-template <int kAt> __device__ __forceinline__ void tmem_st_16x128b_x8_at(uint32_t taddr, const uint32_t (&r)[32]) {      // 32 columns from elements kAt ..
-    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), I16(r, kAt) : "memory");
+__device__ __forceinline__ void tmem_ld_16x128b_x8(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x128b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];" : R16(r, 0) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_16x128b_x8(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr), I16(r, 0) : "memory");
 }
 #undef R4
 #undef R16
@@ -247,7 +258,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     for (int part = 0; part < (F == AFLEX_CACHE_BF16 ? 2 : 1); ++part)
 #pragma unroll
                         for (int j = 0; j < kBN / 16; ++j)
-                            umma_ts(to, a + (uint32_t)(part * 64 + j * 8), bv + (uint32_t)((j * 2048) >> 4), idesc_pv, part > 0 || j > 0 ? 1u : first ? 0u : 1u);
+                            umma_ts(to, a + (uint32_t)((j >> 2) * 64 + part * 32 + (j & 3) * 8), bv + (uint32_t)((j * 2048) >> 4), idesc_pv, part > 0 || j > 0 ? 1u : first ? 0u : 1u);
                     umma_commit(&sh.pv_done[i]);
                 };
                 auto have_k = [&]() { ok = ok && mbar_wait(&sh.full[ks], kp); tc_fence_after(); return ok; };
@@ -479,138 +490,160 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 if (!ok) break;
                 if (busy) {
                     tc_fence_after();
-                    uint32_t x[64];                // scores, then weights
-                    tmem_ld_16x256b_x4_at<0>(s_addr, x);
-                    tmem_ld_16x256b_x4_at<16>(s_addr + 32, x);
-                    tmem_ld_16x256b_x4_at<32>(s_addr + 64, x);
-                    tmem_ld_16x256b_x4_at<48>(s_addr + 96, x);
-                    tmem_ld_wait();
-                    float mx[2] = {-INFINITY, -INFINITY};
-                    const ulonglong2* scales = reinterpret_cast<const ulonglong2*>(sh.scale[step & 1]) + l4;
-                    const uint64_t cc[2] = {pack_f32x2(c[0], c[0]), pack_f32x2(c[1], c[1])};
+                    // Half of the tokens at a time, whose weights go where their scores were: both halves' scores would not fit the registers.
+#pragma unroll 1
+                    for (int half = 0; half < 2 && ok; ++half) {
+                        uint32_t x0[16], x1[16];   // scores of 32 tokens each
+                        tmem_ld_16x256b_x4(s_addr + (uint32_t)(half * 64), x0);
+                        tmem_ld_16x256b_x4(s_addr + (uint32_t)(half * 64 + 32), x1);
+                        const ulonglong2* scales = reinterpret_cast<const ulonglong2*>(sh.scale[step & 1]) + half * 32 + l4;
+                        const uint64_t cc[2] = {pack_f32x2(c[0], c[0]), pack_f32x2(c[1], c[1])};
+                        tmem_ld_wait();
+                        auto scaled = [&](uint32_t (&x)[16], int first) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        ulonglong2 sc;
-                        if (S::kWidens) sc = scales[4 * i];
+                            for (int i = 0; i < 4; ++i) {
+                                ulonglong2 sc;
+                                if (S::kWidens) sc = scales[first + 4 * i];
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            uint64_t v = mul_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), cc[y]);
-                            if (S::kWidens) v = fma_f32x2(v, sc.x, sc.y);
-                            float a, b;
-                            unpack_f32x2(v, a, b);
-                            x[4 * i + 2 * y] = __float_as_uint(a);
-                            x[4 * i + 2 * y + 1] = __float_as_uint(b);
-                        }
-                    }
-                    bool poison[2] = {false, false};
-                    if (masked) {
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int line = line0 + hl + 8 * y, mine = line >> p.g_shift, qi = d.i0 + mine;
-                            const bool there = line < d.lines;
-                            const uint32_t* mask = p.mask + (size_t)(d.row0 + mine) * p.mask_words;
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) {
-                                // which of 32 tokens this line sees
-                                const int t32 = t0 + t * kBN + 32 * q, j0 = t32 - d.ctx;                // the first of them, its number among the drafted
-                                uint32_t see = 0xffffffffu;
-                                const int last = d.sees - t32;            // tokens behind the last do not count
-                                if (last < 32) see = last <= 0 ? 0u : (1u << last) - 1u;
-                                if (j0 + 31 >= 0 && see != 0) {
-                                    uint32_t drafted;                     // bits of tokens j0 .. j0 + 31, earlier ones set
-                                    const uint32_t early = j0 < 0 ? (1u << -j0) - 1u : 0u;
-                                    if (p.mask == nullptr) {
-                                        const int upto = qi - j0 + 1;     // tokens 0 .. qi
-                                        drafted = upto >= 32 ? 0xffffffffu : upto <= 0 ? 0u : (1u << upto) - 1u;
-                                    } else {
-                                        auto word = [&](int i) -> uint32_t { return there && i >= 0 && i < p.mask_words ? fetch(mask + i) : 0u; };
-                                        const int wi = j0 >> 5, sft = j0 & 31;              // (arithmetic shift: -1 for tokens before the first)
-                                        drafted = __funnelshift_r(word(wi), word(wi + 1), (uint32_t)sft);
-                                        const int over = d.m - j0;        // bits of tokens that there are
-                                        if (over < 32) drafted &= over <= 0 ? 0u : (1u << over) - 1u;
-                                    }
-                                    see &= drafted | early;
+                                for (int y = 0; y < 2; ++y) {
+                                    uint64_t v = mul_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), cc[y]);
+                                    if (S::kWidens) v = fma_f32x2(v, sc.x, sc.y);
+                                    float a, b;
+                                    unpack_f32x2(v, a, b);
+                                    x[4 * i + 2 * y] = __float_as_uint(a);
+                                    x[4 * i + 2 * y + 1] = __float_as_uint(b);
                                 }
-                                if (!there) see = 0;
-                                if (!S::kWidens && (see & sh.bad[step & 3][q])) poison[y] = true;
+                            }
+                        };
+                        scaled(x0, 0);
+                        scaled(x1, 16);
+                        if (masked) {
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
+                            for (int y = 0; y < 2; ++y) {
+                                const int line = line0 + hl + 8 * y, mine = line >> p.g_shift, qi = d.i0 + mine;
+                                const bool there = line < d.lines;
+                                const uint32_t* mask = p.mask + (size_t)(d.row0 + mine) * p.mask_words;
 #pragma unroll
-                                    for (int e = 0; e < 2; ++e)
-                                        if (!(see >> (8 * i + 2 * l4 + e) & 1u)) x[4 * (4 * q + i) + 2 * y + e] = 0xff800000u;
+                                for (int q = 0; q < 2; ++q) {
+                                    // which of 32 tokens this line sees
+                                    const int t32 = t0 + t * kBN + 64 * half + 32 * q, j0 = t32 - d.ctx;       // the first of them, its number among the drafted
+                                    uint32_t see = 0xffffffffu;
+                                    const int last = d.sees - t32;        // tokens behind the last do not count
+                                    if (last < 32) see = last <= 0 ? 0u : (1u << last) - 1u;
+                                    if (j0 + 31 >= 0 && see != 0) {
+                                        uint32_t drafted;                 // bits of tokens j0 .. j0 + 31, earlier ones set
+                                        const uint32_t early = j0 < 0 ? (1u << -j0) - 1u : 0u;
+                                        if (p.mask == nullptr) {
+                                            const int upto = qi - j0 + 1; // tokens 0 .. qi
+                                            drafted = upto >= 32 ? 0xffffffffu : upto <= 0 ? 0u : (1u << upto) - 1u;
+                                        } else {
+                                            auto word = [&](int i) -> uint32_t { return there && i >= 0 && i < p.mask_words ? fetch(mask + i) : 0u; };
+                                            const int wi = j0 >> 5, sft = j0 & 31;          // (arithmetic shift: -1 for tokens before the first)
+                                            drafted = __funnelshift_r(word(wi), word(wi + 1), (uint32_t)sft);
+                                            const int over = d.m - j0;    // bits of tokens that there are
+                                            if (over < 32) drafted &= over <= 0 ? 0u : (1u << over) - 1u;
+                                        }
+                                        see &= drafted | early;
+                                    }
+                                    if (!there) see = 0;
+                                    if (!S::kWidens && (see & sh.bad[step & 3][2 * half + q])) l[y] = __uint_as_float(0x7fc00000u);
+                                    see >>= 2 * l4;
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                        for (int e = 0; e < 2; ++e)
+                                            if (!(see >> (8 * i + e) & 1u)) (q ? x1 : x0)[4 * i + 2 * y + e] = 0xff800000u;
+                                }
                             }
                         }
-                    }
+                        float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) mx[y] = fmaxf(mx[y], fmaxf(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])));
-                    // weights are 2^(x - m), m the running maximum less 8: below 2^15 until a score outgrows it
-                    if (__any_sync(0xffffffffu, mx[0] > m[0] + 15.f || mx[1] > m[1] + 15.f)) {
-                        float corr[2];
+                            for (int y = 0; y < 2; ++y)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
-                            mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
-                            const float mn = fmaxf(m[y], mx[y] - 8.f);
-                            corr[y] = fast_exp2(m[y] - mn);
-                            m[y] = mn;
-                            l[y] *= corr[y];
-                        }
-                        if (mine_steps > 0) {
-                            ok = wait(&sh.pv_done[place], (done - 1) & 1);
-                            if (!ok) break;
-                            tc_fence_after();
+                                for (int e = 0; e < 2; ++e) mx[y] = fmaxf(mx[y], fmaxf(__uint_as_float(x0[4 * i + 2 * y + e]), __uint_as_float(x1[4 * i + 2 * y + e])));
+                        // weights are 2^(x - m), m the running maximum less 8: below 2^15 until a score outgrows it
+                        if (__any_sync(0xffffffffu, mx[0] > m[0] + 15.f || mx[1] > m[1] + 15.f)) {
+                            float corr[2];
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
+                                mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
+                                const float mn = fmaxf(m[y], ceilf(mx[y]) - 8.f);         // (whole: what was rounded is scaled exactly)
+                                corr[y] = fast_exp2(m[y] - mn);
+                                m[y] = mn;
+                                l[y] *= corr[y];
+                            }
+                            if (mine_steps > 0) {
+                                ok = wait(&sh.pv_done[place], (done - 1) & 1);
+                                if (!ok) break;
+                                tc_fence_after();
 #pragma unroll 1
-                            for (int c0 = 0; c0 < D; c0 += 32) {
-                                uint32_t r[16];
-                                tmem_ld_16x256b_x4(o_addr + (uint32_t)(place * D + c0), r);
+                                for (int c0 = 0; c0 < D; c0 += 32) {
+                                    uint32_t r[16];
+                                    tmem_ld_16x256b_x4(o_addr + (uint32_t)(place * D + c0), r);
+                                    tmem_ld_wait();
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr[(i >> 1) & 1]);
+                                    tmem_st_16x256b_x4(o_addr + (uint32_t)(place * D + c0), r);
+                                }
+                            }
+                            if (half == 1) {       // and the weights of the first half
+                                uint32_t hi[16], lo[16];
+                                tmem_st_wait();
+                                tmem_ld_16x128b_x8(s_addr, hi);
+                                if (!S::kWidens) tmem_ld_16x128b_x8(s_addr + 32, lo);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * corr[(i >> 1) & 1]);
-                                tmem_st_16x256b_x4(o_addr + (uint32_t)(place * D + c0), r);
+                                for (int i = 0; i < 16; ++i) {
+                                    float w0, w1;
+                                    if (S::kWidens) {
+                                        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[i]));
+                                        w0 = f.x; w1 = f.y;
+                                    } else {
+                                        w0 = __uint_as_float(hi[i] << 16) + __uint_as_float(lo[i] << 16);
+                                        w1 = __uint_as_float(hi[i] & 0xffff0000u) + __uint_as_float(lo[i] & 0xffff0000u);
+                                    }
+                                    pack_weights<F>(w0 * corr[i & 1], w1 * corr[i & 1], hi[i], lo[i]);
+                                }
+                                tmem_st_16x128b_x8(s_addr, hi);
+                                if (!S::kWidens) tmem_st_16x128b_x8(s_addr + 32, lo);
                             }
                         }
-                    }
-                    uint32_t hi[32], lo[32];
-                    const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 1]) + l4;
-                    const uint64_t one = pack_f32x2(1.f, 1.f), m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
-                    uint64_t sum[2] = {0, 0};
+                        uint32_t hi[16], lo[16];
+                        const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 1]) + half * 32 + l4;
+                        const uint64_t one = pack_f32x2(1.f, 1.f), m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
+                        uint64_t sum[2] = {0, 0};
+                        auto weights = [&](const uint32_t (&x)[16], int first) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        uint64_t n = one;
-                        if (S::kWidens) { const float2 v = invs[4 * i]; n = pack_f32x2(v.x, v.y); }
+                            for (int i = 0; i < 4; ++i) {
+                                uint64_t n = one;
+                                if (S::kWidens) { const float2 v = invs[first + 4 * i]; n = pack_f32x2(v.x, v.y); }
+#pragma unroll
+                                for (int y = 0; y < 2; ++y) {
+                                    float w0, w1;
+                                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), one, m2[y]), w0, w1);
+                                    w0 = fast_exp2(w0);
+                                    w1 = fast_exp2(w1);
+                                    sum[y] = fma_f32x2(pack_f32x2(w0, w1), n, sum[y]);
+                                    pack_weights<F>(w0, w1, hi[first / 2 + 2 * i + y], lo[first / 2 + 2 * i + y]);
+                                }
+                            }
+                        };
+                        weights(x0, 0);
+                        weights(x1, 16);
+                        tmem_st_16x128b_x8(s_addr + (uint32_t)(half * 64), hi);
+                        if (!S::kWidens) tmem_st_16x128b_x8(s_addr + (uint32_t)(half * 64 + 32), lo);
 #pragma unroll
                         for (int y = 0; y < 2; ++y) {
-                            float w0, w1;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), one, m2[y]), w0, w1);
-                            w0 = fast_exp2(w0);
-                            w1 = fast_exp2(w1);
-                            sum[y] = fma_f32x2(pack_f32x2(w0, w1), n, sum[y]);
-                            uint32_t& h = hi[2 * i + y];
-                            if (S::kWidens) {
-                                const __half2 f = __floats2half2_rn(w0, w1);
-                                h = *reinterpret_cast<const uint32_t*>(&f);
-                            } else {
-                                h = pack_bf16x2(w0, w1);
-                                lo[2 * i + y] = pack_bf16x2(w0 - __uint_as_float(h << 16), w1 - __uint_as_float(h & 0xffff0000u));
-                            }
+                            float a, b;
+                            unpack_f32x2(sum[y], a, b);
+                            l[y] += a + b;
                         }
                     }
-                    tmem_st_16x128b_x8_at<0>(s_addr, hi);
-                    tmem_st_16x128b_x8_at<16>(s_addr + 32, hi);
-                    if (!S::kWidens) {
-                        tmem_st_16x128b_x8_at<0>(s_addr + 64, lo);
-                        tmem_st_16x128b_x8_at<16>(s_addr + 96, lo);
-                    }
+                    if (!ok) break;
                     tmem_st_wait();
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        float a, b;
-                        unpack_f32x2(sum[y], a, b);
-                        l[y] += a + b;
-                        if (poison[y]) l[y] = __uint_as_float(0x7fc00000u);
-                    }
                 }
                 tc_fence_before();
                 __syncwarp();
