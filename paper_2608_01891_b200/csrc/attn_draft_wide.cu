@@ -34,9 +34,7 @@ constexpr int kBN = 128;                           // cached tokens per step
 constexpr int kUnitPages = kBN / kPageTokens;
 constexpr int kWideLines = 2 * kBM;
 constexpr int kSoftmaxWarps = 16;                  // [place][half of 32 lines][32 lines]
-constexpr int kWideThreads = (kSoftmaxWarps + 8) * 32;       // and the warp groups of producer + issuer, and of widening
-constexpr int kRegsSoftmax = 80, kRegsIssue = 80, kRegsWiden = 80;
-static_assert(kSoftmaxWarps * 32 * kRegsSoftmax + 128 * kRegsIssue + 128 * kRegsWiden <= kWideThreads * 80, "the warp groups share what the block was launched with");
+constexpr int kWideThreads = (kSoftmaxWarps + 8) * 32;       // and producer, issuer (and two idle), four that widen: 80 registers a thread
 constexpr int kPieceRing = 4;
 
 template <int D, int F> struct WideForm {
@@ -157,7 +155,6 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     };
 
     if (group == 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsIssue));
         if (warp == kSoftmaxWarps) {
             // -------------------------------------------------------------- producer: pieces and their pages
             const uint64_t policy = policy_evict_first();
@@ -321,7 +318,6 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         }
     } else if (group == 5) {
         // ------------------------------------------------------------------ widening; bf16: a look at the V of drafted tokens
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsWiden));
         const int tid = threadIdx.x - (kWideThreads - 128);
         int tile_no = 0, step = 0;
         bool ok = true;
@@ -356,23 +352,31 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                 reinterpret_cast<float*>(sh.inv[step & 1])[tid] = n == n ? n : 0.f;
                             }
                         }
-                        // chunks of 16 codes, each two chunks of 16 bytes of the tile, half c / 4; half of the thread's are loaded before the first
-                        // is widened
+                        // Chunks of 16 codes become two of 16 bytes of the tile, in half c / 4.  Four lanes of eight take a chunk's second eight codes first,
+                        // the other four in rows of the other parity: so both the 8-byte loads and the 16-byte stores of a warp meet every
+                        // bank equally often.  Half of the thread's chunks are loaded before the first is widened
                         constexpr int kPer = D / 16, kRows = 128 / kPer, kTurns = kBN / kRows;      // chunks per token, tokens per turn of the group
                         const int c = tid % kPer, row = tid / kPer;       // (kRows is a multiple of 8: a token's last three bits are row's)
+                        const uint32_t second = (uint32_t)((c >> 2) ^ row) & 1;
                         uint8_t* half = to + (c >> 2) * S::kHalf + row * 128;
-                        const uint32_t at0 = (uint32_t)((((c & 3) * 2) ^ (row & 7)) << 4), at1 = at0 ^ 16;
+                        const uint8_t* from = raw + row * D + c * 16 + second * 8;
+                        const uint32_t at0 = (uint32_t)((((c & 3) * 2 + second) ^ (row & 7)) << 4), at1 = at0 ^ 16;
+                        const int other = 8 - 16 * (int)second;
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            uint4 x[kTurns / 2];
+                            uint2 x[kTurns / 2], y[kTurns / 2];
 #pragma unroll
-                            for (int it = 0; it < kTurns / 2; ++it) x[it] = *reinterpret_cast<const uint4*>(raw + ((h * (kTurns / 2) + it) * kRows + row) * D + c * 16);
+                            for (int it = 0; it < kTurns / 2; ++it) {
+                                const uint8_t* at = from + (h * (kTurns / 2) + it) * kRows * D;
+                                x[it] = *reinterpret_cast<const uint2*>(at);
+                                y[it] = *reinterpret_cast<const uint2*>(at + other);
+                            }
 #pragma unroll
                             for (int it = 0; it < kTurns / 2; ++it) {
                                 const int turn = h * (kTurns / 2) + it;
                                 uint4 a, b;
                                 widen4<F>(x[it].x, a.x, a.y); widen4<F>(x[it].y, a.z, a.w);
-                                widen4<F>(x[it].z, b.x, b.y); widen4<F>(x[it].w, b.z, b.w);
+                                widen4<F>(y[it].x, b.x, b.y); widen4<F>(y[it].y, b.z, b.w);
                                 if (isv && turn * kRows + row >= here) a = b = make_uint4(0, 0, 0, 0);      // slots behind the last token may hold anything
                                 *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at0) = a;
                                 *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at1) = b;
@@ -414,7 +418,6 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         if (!ok) give_up();
     } else {
         // ------------------------------------------------------------------ softmax: 16 lines per warp, two (and a quarter of the tokens) per thread
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
         const int place = warp >> 3, row0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16, hl = lane >> 2, l4 = lane & 3;
         const uint32_t lane_base = tmem + ((uint32_t)row0 << 16);
         const uint32_t s_addr = lane_base + (uint32_t)(place * kBN), o_addr = lane_base + kOCol;
@@ -570,7 +573,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                             for (int y = 0; y < 2; ++y) {
                                 mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
                                 mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
-                                const float mn = fmaxf(m[y], ceilf(mx[y]) - 8.f);         // (whole: what was rounded is scaled exactly)
+                                const float mn = mx[y] > m[y] + 15.f ? ceilf(mx[y]) - 8.f : m[y];          // (whole: what was rounded is scaled exactly)
                                 corr[y] = fast_exp2(m[y] - mn);
                                 m[y] = mn;
                                 l[y] *= corr[y];
