@@ -8,6 +8,7 @@ loaded, or a call returns a non-OK status, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional, Sequence
 
@@ -61,6 +62,10 @@ CACHE_BF16, CACHE_INT8, CACHE_E4M3 = range(3)
 
 class Cache(ctypes.Structure):
     _fields_ = [("kv", KV), ("format", ctypes.c_int), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+    _shape = None                                  # (what make_cache knows of the tensors)
+
+
+_SHAPE = operator.attrgetter("_shape")
 
 
 class Draft(ctypes.Structure):
@@ -786,7 +791,9 @@ class Context:
         return batch, draft, kept
 
     def _match_cache(self, desc: AttnDesc, cache: Cache, batch: int) -> None:
-        shape = cache.__dict__.get("_shape")
+        self._match_shape(desc, cache._shape, batch)
+
+    def _match_shape(self, desc: AttnDesc, shape, batch: int) -> None:
         if shape is not None:
             heads, tokens, dim, most, there = shape
             assert heads == desc.num_kv_heads and tokens == desc.page_size and dim == desc.head_dim, "cache shape does not fit the descriptor"
@@ -830,9 +837,13 @@ class Context:
         assert len(caches) >= 1
         assert base.dtype == torch.int32 and base.numel() >= batch and path_len.dtype == torch.int32 and path_len.numel() >= batch
         assert path.dtype == torch.int32 and path.dim() == 2 and path.shape[0] >= batch
-        for c in caches:
-            self._match_cache(desc, c, batch)
-        ca = caches if isinstance(caches, ctypes.Array) else (Cache * len(caches))(*caches)
+        ca = caches
+        if not isinstance(caches, ctypes.Array):
+            for shape in set(map(_SHAPE, caches)):                        # (one, of layers alike)
+                self._match_shape(desc, shape, batch)
+            raw = b"".join(caches)                                        # (element by element the array of 64 takes four times as long)
+            assert len(raw) == len(caches) * ctypes.sizeof(Cache), "not a sequence of caches"
+            ca = (Cache * len(caches)).from_buffer_copy(raw)
         self._check(self._lib.aflex_cache_accept(self._h, desc, ca, len(caches), batch, _ptr(base), _ptr(path), path.shape[1], _ptr(path_len),
                                                  self._stream_of(stream, base, path, path_len)))
 

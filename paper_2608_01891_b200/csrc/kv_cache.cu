@@ -434,8 +434,8 @@ __global__ void __launch_bounds__(kThreads) cache_convert_kernel(const ConvertPa
 // ------------------------------------------------------------------------------------------ acceptance
 constexpr int kAcceptCaches = 64;                  // caches per launch
 struct AcceptCache { uint8_t* k; uint8_t* v; float* ks; float* vs; const int32_t* table; const int32_t* lens; long long num_pages; int max_pages; };
-struct AcceptParams {
-    AcceptCache cache[kAcceptCaches];
+template <int N> struct AcceptParams {             // of up to N caches: a launch copies all of its arguments
+    AcceptCache cache[N];
     const int32_t* base; const int32_t* path; const int32_t* count;
     int batch, stride, Hkv, row_bytes;
     int* status;
@@ -444,24 +444,25 @@ struct AcceptParams {
 // A warp moves one (sequence, KV head, K or V) of one cache, 16-byte words of four to sixteen tokens at a time.  The path ascends,
 // so a token never moves up: a source that is still to be read lies behind every place that has been written, and within a step all
 // reads come before the writes.  Bound: the chain of dependent loads (path -> page ids -> tokens); a tree's path is a few KB per head.
-__global__ void __launch_bounds__(kThreads) cache_accept_kernel(const __grid_constant__ AcceptParams p) {
+template <int N> __global__ void __launch_bounds__(kThreads) cache_accept_kernel(const __grid_constant__ AcceptParams<N> p) {
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (2 * p.Hkv + kWarps - 1) / kWarps, b = blockIdx.x / per, head = (int)(blockIdx.x % per) * kWarps + warp;
     const AcceptCache& c = p.cache[blockIdx.y];
     if (head >= 2 * p.Hkv) return;
-    const int n = fetch(p.count + b), base = fetch(p.base + b), len = fetch(c.lens + b);
     const int32_t* path = p.path + (size_t)b * p.stride;
+    const int n = fetch(p.count + b), base = fetch(p.base + b), len = fetch(c.lens + b);
+    auto from_path = [&](int k) -> int { return k < p.stride ? fetch(path + k) : 0; };
+    const int first = from_path(lane);             // (whatever the length: no second trip to memory for most paths)
     // the whole path is looked at before anything moves: it has to ascend inside the sequence
     bool bad = n < 0 || n > p.stride || base < 0 || len < 0 || len > c.max_pages * kPageTokens;
+    int before = -1;
     for (int k0 = 0; k0 < n && !bad; k0 += 32) {
-        const int k = k0 + lane;
-        bool wrong = false;
-        if (k < n) {
-            const int s = fetch(path + k);
-            wrong = s < (k > 0 ? fetch(path + k - 1) + 1 : 0) || (long long)base + s >= len;
-        }
-        bad = __any_sync(0xffffffffu, wrong);
+        const int s = k0 == 0 ? first : from_path(k0 + lane);
+        int last = __shfl_up_sync(0xffffffffu, s, 1);
+        if (lane == 0) last = before;
+        before = __shfl_sync(0xffffffffu, s, 31);
+        bad = __any_sync(0xffffffffu, k0 + lane < n && (s <= last || (long long)base + s >= len));
     }
     if (bad) {
         if (lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
@@ -476,33 +477,35 @@ __global__ void __launch_bounds__(kThreads) cache_accept_kernel(const __grid_con
         const int page = fetch(table + t / kPageTokens);
         return page >= 0 && page < c.num_pages ? ((long long)page * p.Hkv + g) * kPageTokens + t % kPageTokens : -1;
     };
-    for (int k0 = 0; k0 < n; k0 += 4 * at_once) {
-        // lane i knows the k0 + i-th move (4 * at_once is at most 32)
+    for (int k0 = 0; k0 < n; k0 += 32) {
+        // lane i knows the k0 + i-th move
         long long from = -1, to = -1;
-        const int k = k0 + lane;
-        if (lane < 4 * at_once && k < n) {
-            const int s = fetch(path + k);
-            if (s != k) {
-                from = place(base + s);
-                to = place(base + k);
-                if (from < 0 || to < 0) { atomicExch(p.status, AFLEX_ERR_BOUNDS); from = to = -1; }
-            }
+        const int k = k0 + lane, s = k0 == 0 ? first : from_path(k);
+        if (k < n && s != k) {
+            from = place(base + s);
+            to = place(base + k);
+            if (from < 0 || to < 0) { atomicExch(p.status, AFLEX_ERR_BOUNDS); from = to = -1; }
         }
+        const uint32_t moves = __ballot_sync(0xffffffffu, from >= 0);
+        if (moves == 0) continue;
         float scale = 0.f;
         if (scales != nullptr && from >= 0) scale = scales[from];
-        uint4 x[4];
-        long long dst[4];
+        for (int i0 = 0; i0 < 32 && moves >> i0 != 0; i0 += 4 * at_once) {
+            uint4 x[4];
+            long long dst[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = u * at_once + lane / words;
-            const long long src = __shfl_sync(0xffffffffu, from, i);
-            dst[u] = __shfl_sync(0xffffffffu, to, i);
-            if (src >= 0) x[u] = *reinterpret_cast<const uint4*>(data + src * p.row_bytes + w * 16);
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * at_once + lane / words;
+                const long long src = __shfl_sync(0xffffffffu, from, i);
+                dst[u] = __shfl_sync(0xffffffffu, to, i);
+                if (src >= 0) x[u] = *reinterpret_cast<const uint4*>(data + src * p.row_bytes + w * 16);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (dst[u] >= 0) *reinterpret_cast<uint4*>(data + dst[u] * p.row_bytes + w * 16) = x[u];
+            __syncwarp();
         }
-        __syncwarp();
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (dst[u] >= 0) *reinterpret_cast<uint4*>(data + dst[u] * p.row_bytes + w * 16) = x[u];
         if (scales != nullptr && to >= 0) scales[to] = scale;
         __syncwarp();
     }
@@ -589,28 +592,34 @@ aflex_status cache_convert_launch(aflex_ctx* ctx, const aflex_attn_desc* d, cons
                       "cache_convert_kernel launch");
 }
 
-aflex_status cache_accept_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const aflex_cache* caches, int num_caches, int batch,
-                                 const int32_t* base, const int32_t* path, int path_stride, const int32_t* path_len, cudaStream_t st) {
-    AcceptParams p;
+template <int N>
+static aflex_status accept_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const aflex_cache* caches, int num_caches, int batch,
+                                  const int32_t* base, const int32_t* path, int path_stride, const int32_t* path_len, cudaStream_t st) {
+    AcceptParams<N> p;
     p.base = base; p.path = path; p.count = path_len;
     p.batch = batch; p.stride = path_stride; p.Hkv = d->num_kv_heads;
     p.row_bytes = d->head_dim * (caches[0].format == AFLEX_CACHE_BF16 ? 2 : 1);
     p.status = ctx->dev_status;
     const long long ctas = (long long)batch * ((2 * p.Hkv + kWarps - 1) / kWarps);
     if (ctas > 0x7fffffffLL) return set_error(ctx, AFLEX_ERR_UNSUPPORTED, "cache accept: batch * Hkv");
-    for (int l0 = 0; l0 < num_caches; l0 += kAcceptCaches) {
-        const int n = num_caches - l0 < kAcceptCaches ? num_caches - l0 : kAcceptCaches;
-        for (int l = 0; l < n; ++l) {
-            const aflex_cache& c = caches[l0 + l];
-            p.cache[l] = {(uint8_t*)const_cast<void*>(c.kv.k_cache), (uint8_t*)const_cast<void*>(c.kv.v_cache), c.k_scales, c.v_scales,
-                          c.kv.page_table, c.kv.seq_lens, (long long)c.kv.num_pages, c.kv.max_pages_per_seq};
-        }
-        for (int l = n; l < kAcceptCaches; ++l) p.cache[l] = p.cache[0];
-        KernelScope scope(ctx, kKCacheAccept, st);
-        aflex_status s = check_cuda(ctx, launch_pdl(cache_accept_kernel, dim3((unsigned)ctas, (unsigned)n), dim3(kThreads), 0, st, p), "cache_accept_kernel launch");
-        if (s != AFLEX_OK) return s;
+    for (int l = 0; l < N; ++l) {
+        const aflex_cache& c = caches[l < num_caches ? l : 0];
+        p.cache[l] = {(uint8_t*)const_cast<void*>(c.kv.k_cache), (uint8_t*)const_cast<void*>(c.kv.v_cache), c.k_scales, c.v_scales,
+                      c.kv.page_table, c.kv.seq_lens, (long long)c.kv.num_pages, c.kv.max_pages_per_seq};
     }
-    return AFLEX_OK;
+    KernelScope scope(ctx, kKCacheAccept, st);
+    return check_cuda(ctx, launch_pdl(cache_accept_kernel<N>, dim3((unsigned)ctas, (unsigned)num_caches), dim3(kThreads), 0, st, p), "cache_accept_kernel launch");
+}
+
+aflex_status cache_accept_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const aflex_cache* caches, int num_caches, int batch,
+                                 const int32_t* base, const int32_t* path, int path_stride, const int32_t* path_len, cudaStream_t st) {
+    aflex_status s = AFLEX_OK;
+    for (int l0 = 0; l0 < num_caches && s == AFLEX_OK; l0 += kAcceptCaches) {
+        const int n = num_caches - l0 < kAcceptCaches ? num_caches - l0 : kAcceptCaches;
+        s = n <= 4 ? accept_launch<4>(ctx, d, caches + l0, n, batch, base, path, path_stride, path_len, st)
+                   : accept_launch<kAcceptCaches>(ctx, d, caches + l0, n, batch, base, path, path_stride, path_len, st);
+    }
+    return s;
 }
 
 }  // namespace aflex
