@@ -312,7 +312,7 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-                const float mn = fmaxf(st.m[n][e], v - 8.f);
+                const float mn = v > st.m[n][e] + 15.f ? v - 8.f : st.m[n][e];          // (a line's bits do not depend on who else's moves)
                 corr[e] = fast_exp2(st.m[n][e] - mn);
                 st.m[n][e] = mn;
                 st.l[n][e] *= corr[e];
