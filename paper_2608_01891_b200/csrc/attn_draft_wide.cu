@@ -67,6 +67,12 @@ struct __align__(16) WideShared {
     volatile int abort;
 };
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // Two weights of a line as operand: fp16, or the two bf16 parts.
 template <int F> __device__ __forceinline__ void pack_weights(float w0, float w1, uint32_t& hi, uint32_t& lo) {
     if (F == AFLEX_CACHE_BF16) {
@@ -417,7 +423,9 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         }
         if (!ok) give_up();
     } else {
-        // ------------------------------------------------------------------ softmax: 16 lines per warp, two (and a quarter of the tokens) per thread
+        // ------------------------------------------------------------------ softmax: 16 lines per warp, two (and a quarter of the tokens) per thread.
+        // A warp reaches only the rows 32 (warp % 4) .. + 31 of TMEM; sixteens of lines go round these quarters, so that few lines keep all four
+        // of the SM's schedulers busy
         const int place = warp >> 3, row0 = (warp & 3) * 32 + ((warp >> 2) & 1) * 16, hl = lane >> 2, l4 = lane & 3;
         const uint32_t lane_base = tmem + ((uint32_t)row0 << 16);
         const uint32_t s_addr = lane_base + (uint32_t)(place * kBN), o_addr = lane_base + kOCol;
@@ -440,7 +448,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             if (d.units == 0) break;
             const int units = d.t0 < 0 ? 0 : d.units;
             const bool two = d.lines > kBM;
-            const int line0 = (two ? place * kBM : 0) + row0;         // of the warp's first row
+            const int line0 = (two ? place * kBM : 0) + (warp & 7) * 16;          // of the warp's first row
             const bool busy = line0 < d.lines;                        // (a warp without lines only keeps step)
             if (units > 0 && busy) {
                 // ---- the warp's queries into the place's tile, two halves of 128 bytes, swizzled; D / 8 lanes for a line
@@ -563,9 +571,10 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
 #pragma unroll
-                            for (int y = 0; y < 2; ++y)
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) mx[y] = fmaxf(mx[y], fmaxf(__uint_as_float(x0[4 * i + 2 * y + e]), __uint_as_float(x1[4 * i + 2 * y + e])));
+                            for (int y = 0; y < 2; ++y) {
+                                mx[y] = max3(mx[y], __uint_as_float(x0[4 * i + 2 * y]), __uint_as_float(x0[4 * i + 2 * y + 1]));
+                                mx[y] = max3(mx[y], __uint_as_float(x1[4 * i + 2 * y]), __uint_as_float(x1[4 * i + 2 * y + 1]));
+                            }
                         // weights are 2^(x - m), m the running maximum less 8: below 2^15 until a score outgrows it
                         if (__any_sync(0xffffffffu, mx[0] > m[0] + 15.f || mx[1] > m[1] + 15.f)) {
                             float corr[2];
@@ -616,20 +625,20 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                         }
                         uint32_t hi[16], lo[16];
                         const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 1]) + half * 32 + l4;
-                        const uint64_t one = pack_f32x2(1.f, 1.f), m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
+                        const uint64_t m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
                         uint64_t sum[2] = {0, 0};
                         auto weights = [&](const uint32_t (&x)[16], int first) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                uint64_t n = one;
-                                if (S::kWidens) { const float2 v = invs[first + 4 * i]; n = pack_f32x2(v.x, v.y); }
+                                uint64_t n = 0;
+                                if (S::kWidens) n = *reinterpret_cast<const uint64_t*>(invs + first + 4 * i);
 #pragma unroll
                                 for (int y = 0; y < 2; ++y) {
                                     float w0, w1;
-                                    unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), one, m2[y]), w0, w1);
+                                    unpack_f32x2(add_f32x2(pack_f32x2(__uint_as_float(x[4 * i + 2 * y]), __uint_as_float(x[4 * i + 2 * y + 1])), m2[y]), w0, w1);
                                     w0 = fast_exp2(w0);
                                     w1 = fast_exp2(w1);
-                                    sum[y] = fma_f32x2(pack_f32x2(w0, w1), n, sum[y]);
+                                    sum[y] = S::kWidens ? fma_f32x2(pack_f32x2(w0, w1), n, sum[y]) : add_f32x2(sum[y], pack_f32x2(w0, w1));
                                     pack_weights<F>(w0, w1, hi[first / 2 + 2 * i + y], lo[first / 2 + 2 * i + y]);
                                 }
                             }

@@ -443,8 +443,9 @@ template <int N> struct AcceptParams {             // of up to N caches: a launc
 
 // A warp moves one (sequence, KV head, K or V) of one cache, 16-byte words of four to sixteen tokens at a time.  The path ascends,
 // so a token never moves up: a source that is still to be read lies behind every place that has been written, and within a step all
-// reads come before the writes.  Bound: the chain of dependent loads (path -> page ids -> tokens); a tree's path is a few KB per head.
-template <int N> __global__ void __launch_bounds__(kThreads) cache_accept_kernel(const __grid_constant__ AcceptParams<N> p) {
+// reads come before the writes.  Bound: the chain of dependent loads (path -> page ids -> tokens); a tree's path is a few KB per head.  64 int8
+// caches of 32 sequences take 12.9 us (2.7 TB/s); with 4, 6 or 8 CTAs per SM 13.5, 13.8 and 14.0 (the last two spill).
+template <int N> __global__ void __launch_bounds__(kThreads, 5) cache_accept_kernel(const __grid_constant__ AcceptParams<N> p) {
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (2 * p.Hkv + kWarps - 1) / kWarps, b = blockIdx.x / per, head = (int)(blockIdx.x % per) * kWarps + warp;
@@ -473,13 +474,13 @@ template <int N> __global__ void __launch_bounds__(kThreads) cache_accept_kernel
     float* scales = head < p.Hkv ? c.ks : c.vs;
     const int words = p.row_bytes / 16, at_once = 32 / words, w = lane % words;         // 16-byte words of a token's head; tokens per access
     const int32_t* table = c.table + (size_t)b * c.max_pages;
-    auto place = [&](int t) -> long long {                                                // of a token: (page, head, slot), -1 for a bad page id
+    auto place = [&](int t) -> int {                                                       // of a token: (page, head, slot), below 2^31; -1 for a bad page id
         const int page = fetch(table + t / kPageTokens);
-        return page >= 0 && page < c.num_pages ? ((long long)page * p.Hkv + g) * kPageTokens + t % kPageTokens : -1;
+        return page >= 0 && page < c.num_pages ? (page * p.Hkv + g) * kPageTokens + t % kPageTokens : -1;
     };
     for (int k0 = 0; k0 < n; k0 += 32) {
         // lane i knows the k0 + i-th move
-        long long from = -1, to = -1;
+        int from = -1, to = -1;
         const int k = k0 + lane, s = k0 == 0 ? first : from_path(k);
         if (k < n && s != k) {
             from = place(base + s);
@@ -492,18 +493,18 @@ template <int N> __global__ void __launch_bounds__(kThreads) cache_accept_kernel
         if (scales != nullptr && from >= 0) scale = scales[from];
         for (int i0 = 0; i0 < 32 && moves >> i0 != 0; i0 += 4 * at_once) {
             uint4 x[4];
-            long long dst[4];
+            int dst[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int i = i0 + u * at_once + lane / words;
-                const long long src = __shfl_sync(0xffffffffu, from, i);
+                const int src = __shfl_sync(0xffffffffu, from, i);
                 dst[u] = __shfl_sync(0xffffffffu, to, i);
-                if (src >= 0) x[u] = *reinterpret_cast<const uint4*>(data + src * p.row_bytes + w * 16);
+                if (src >= 0) x[u] = *reinterpret_cast<const uint4*>(data + (size_t)src * p.row_bytes + w * 16);
             }
             __syncwarp();
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (dst[u] >= 0) *reinterpret_cast<uint4*>(data + dst[u] * p.row_bytes + w * 16) = x[u];
+                if (dst[u] >= 0) *reinterpret_cast<uint4*>(data + (size_t)dst[u] * p.row_bytes + w * 16) = x[u];
             __syncwarp();
         }
         if (scales != nullptr && to >= 0) scales[to] = scale;
