@@ -742,11 +742,12 @@ aflex_status attn_draft_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const v
     p.batch = batch; p.rows = rows; p.max_pages = kv->max_pages_per_seq;
     p.Hq = d->num_q_heads; p.Hkv = d->num_kv_heads; p.G = p.Hq / p.Hkv; p.num_pages = kv->num_pages;
     p.g_shift = p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3;
-    // Lines per tile by the lines of an average sequence: 8, 16, or 256 on the tensor cores, whose step costs the same for any number of lines while
-    // tiles of 16 read the cache again.  Measured (us, tiles of 16 / tensor cores), heads of 128: 20 lines 86 / 92 in int8 and 100 / 86 in bf16, 32 lines
-    // 110 / 93 and 141 / 87; heads of 64: 32 lines 24 / 33, 52 lines 35 / 33, 64 lines of a larger batch 135 / 104.
+    // Lines per tile by the lines of an average sequence: 8, 16, or 256 on the tensor cores, whose step costs the same for any number of lines up to
+    // 128 while tiles of 16 read the cache again.  Measured (us, tiles of 16 / tensor cores), heads of 128: 32 lines 72 / 84 in int8, 66 / 81 in
+    // e4m3, 88 / 83 in bf16, 441 / 478 in a larger batch, 40 lines 86 / 84, 101 / 83 (bf16), 600 / 486; heads of 64: 40 lines 29 / 32 (bf16),
+    // 48 lines 30 / 31 (bf16), 28 / 33 (int8), 107 / 94 and 91 / 97 in a larger batch, 52 lines 34 / 31.
     const long long lines = (long long)rows << p.g_shift;
-    const int narrow = D == 64 ? 48 : 16;
+    const int narrow = D == 64 ? 48 : 32;
     p.rpt_shift = (lines <= 8LL * batch ? 3 : lines <= (long long)narrow * batch ? 4 : 8) - p.g_shift;
     const float scale = d->sm_scale != 0.f ? d->sm_scale : 1.0f / sqrtf((float)D);
     p.scale_log2 = scale * 1.4426950408889634f;

@@ -50,7 +50,8 @@ def test_up_to_64_caches_are_compacted_by_one_launch(host, ctx, caches, launches
 @pytest.mark.parametrize("rows, batch, Hq, Hkv, D, kernel", [
     (4, 4, 8, 1, 64, "attn_draft_kernel"),               # one token per sequence, 8 lines: a tile of 8
     (12, 4, 8, 2, 128, "attn_draft_kernel"),             # 12 lines
-    (17, 1, 8, 8, 128, "attn_draft_wide_kernel"),        # 17 lines of heads of 128
+    (32, 1, 8, 8, 128, "attn_draft_kernel"),             # 32 lines of heads of 128
+    (33, 1, 8, 8, 128, "attn_draft_wide_kernel"),
     (48, 1, 8, 8, 64, "attn_draft_kernel"),              # 48 of 64
     (49, 1, 8, 8, 64, "attn_draft_wide_kernel"),
 ])
