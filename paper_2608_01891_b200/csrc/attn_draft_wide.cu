@@ -42,22 +42,26 @@ template <int D, int F> struct WideForm {
     static constexpr int kHalves = D / 64;
     static constexpr int kHalf = kBN * 128;                           // 128 rows of 128 bytes: 64 channels of a tile of lines or of tokens
     static constexpr int kTile = kHalves * kHalf;                     // Q of a place, K or V of a step
-    static constexpr int kSlots = kWidens ? 3 : 4;                    // ring of K and V: K(0) V(0) K(1) V(1) ..
-    static constexpr int kRaws = kWidens ? 3 : 0;                     // ring of the same in 8 bits
+    // bf16: a ring of K(0) V(0) K(1) V(1) ..  8 bits: two slots for K and one for V, widened in the order K(0) K(1) V(0) K(2) V(1) ..: the products
+    // with K(t + 2) follow those with V(t), whose slot it must not wait for (one ring of three: 486 against 465 us, 64 trees of 5; 261 against 251, 8 of up to 61); V(t + 1) has the
+    // softmax's time
+    static constexpr int kSlots = kWidens ? 3 : 4;
+    static constexpr int kRaws = kWidens ? 3 : 0;                     // ring of the same in 8 bits, in the same order
     static constexpr int kRawTile = kBN * D;
-    static constexpr int kRaw = kRawTile + kBN * 4;                   // and its scales
+    static constexpr int kRaw = kRawTile + 2 * kBN * 4;               // and with K the scales of K and V
     static constexpr int kSmem = 2 * kTile + kSlots * kTile + kRaws * kRaw;
 };
 
 struct __align__(16) WideShared {
-    float4 scale[2][kBN / 2];                      // by step: of two tokens, K's scales and log2 of V's
-    float4 inv[2][kBN / 4];                        // 1 / V's, of four tokens
+    float4 scale[4][kBN / 2];                      // by step: of two tokens, K's scales and log2 of V's
+    float4 inv[4][kBN / 4];                        // 1 / V's, of four tokens
     float2 state[2][kBM];                          // by place: references and sums of a finished piece
     float factor[2][kBM];                          // by place: what a line's products count, in log2 units
     uint32_t bad[4][kBN / 32];                     // by step: tokens whose V holds an infinity or NaN (bf16)
     uint64_t told[kPieceRing], left[kPieceRing];   // a piece's description is there, everybody has read it
     uint64_t raw_full[4], raw_empty[3];            // pages have landed (bf16: in their slot), have been widened
     uint64_t full[4], empty[4];                    // a slot can be read by the products, has been
+    uint64_t scaled[4];                            // by step: the scales are there
     uint64_t q_ready[2], s_ready[2], p_ready[2], pv_done[2], meet;       // meet: the softmax warps
     DraftPiece piece[kPieceRing];
     DraftShare share;
@@ -136,6 +140,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             mbar_init(&sh.raw_full[i], S::kWidens ? 33 : 1);
             mbar_init(&sh.full[i], 4);
             mbar_init(&sh.empty[i], 1);
+            mbar_init(&sh.scaled[i], 4);
         }
         for (int i = 0; i < 3; ++i) mbar_init(&sh.raw_empty[i], 4);
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_ready[i], 8); mbar_init(&sh.s_ready[i], 1); mbar_init(&sh.p_ready[i], 8); mbar_init(&sh.pv_done[i], 1); }
@@ -194,38 +199,55 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     const int i = t / kPageTokens + page;
                     return t >= 0 && i * kPageTokens < sees ? fetch(table + i) : 0;
                 };
-                int id = page_id(t0);
-                for (int t = t0, left = units; left > 0 && ok && t >= 0; t += kBN, --left) {
-                    const int id_next = left > 1 ? page_id(t + kBN) : 0;
-                    const int np = min(kUnitPages, (sees - t + kPageTokens - 1) / kPageTokens);
-                    if (page < np && (id < 0 || id >= p.num_pages)) { if (part == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS); id = 0; }
-                    if (tile_no == 0) pdl_wait();
-                    for (int isv = 0; isv < 2 && ok; ++isv, ++tile_no) {
-                        if (S::kWidens) {
-                            const int r = tile_no % 3;
-                            ok = wait(&sh.raw_empty[r], ((tile_no / 3) & 1) ^ 1);
-                            if (!ok) break;
-                            uint8_t* raw = sraw + r * S::kRaw;
-                            if (lane == 0) mbar_expect_tx(&sh.raw_full[r], (uint32_t)(np * kPageTokens * D));
-                            __syncwarp();
-                            if (lane < np)
-                                bulk_load_1d(raw + lane * (kPageTokens * D), (isv ? v_codes : k_codes) + ((size_t)id * p.Hkv + g) * (kPageTokens * D), kPageTokens * D, &sh.raw_full[r]);
-                            const int from = __shfl_sync(0xffffffffu, id, lane >> 2);        // four lanes bring a page's scales
-                            if ((lane >> 2) < np)
-                                copy16(smem_u32(raw) + (uint32_t)(S::kRawTile + lane * 16), (isv ? p.v_scales : p.k_scales) + ((size_t)from * p.Hkv + g) * kPageTokens + (lane & 3) * 4);
-                            copies_arrive(&sh.raw_full[r]);
-                        } else {
-                            const int s = tile_no % S::kSlots;
-                            ok = wait(&sh.empty[s], ((tile_no / S::kSlots) & 1) ^ 1);
-                            if (!ok) break;
-                            if (lane == 0) mbar_expect_tx(&sh.raw_full[s], (uint32_t)(np * S::kHalves * kPageTokens * 128));
-                            __syncwarp();
-                            if (part < S::kHalves && page < np)
-                                tma_load_2d_hint(skv + s * S::kTile + part * S::kHalf + page * (kPageTokens * 128), isv ? &tmap_v : &tmap_k, part * 64,
-                                                 (id * p.Hkv + g) * kPageTokens, &sh.raw_full[s], policy);
+                auto pages_of = [&](int t) -> int { return min(kUnitPages, (sees - t + kPageTokens - 1) / kPageTokens); };
+                auto checked = [&](int t, int id) -> int {
+                    if (page < pages_of(t) && (id < 0 || id >= p.num_pages)) { if (part == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS); return 0; }
+                    return id;
+                };
+                auto bring = [&](int isv, int t, int id) {                // K or V of the unit with tokens t ..
+                    const int np = pages_of(t);
+                    if (S::kWidens) {
+                        const int r = tile_no % 3;
+                        ok = ok && wait(&sh.raw_empty[r], ((tile_no / 3) & 1) ^ 1);
+                        if (!ok) return;
+                        uint8_t* raw = sraw + r * S::kRaw;
+                        if (lane == 0) mbar_expect_tx(&sh.raw_full[r], (uint32_t)(np * kPageTokens * D));
+                        __syncwarp();
+                        if (lane < np)
+                            bulk_load_1d(raw + lane * (kPageTokens * D), (isv ? v_codes : k_codes) + ((size_t)id * p.Hkv + g) * (kPageTokens * D), kPageTokens * D, &sh.raw_full[r]);
+                        const int from = __shfl_sync(0xffffffffu, id, lane >> 2);            // four lanes bring a page's scales
+                        if (!isv && (lane >> 2) < np) {
+                            const size_t at = ((size_t)from * p.Hkv + g) * kPageTokens + (lane & 3) * 4;
+                            copy16(smem_u32(raw) + (uint32_t)(S::kRawTile + lane * 16), p.k_scales + at);
+                            copy16(smem_u32(raw) + (uint32_t)(S::kRawTile + kBN * 4 + lane * 16), p.v_scales + at);
                         }
+                        copies_arrive(&sh.raw_full[r]);
+                    } else {
+                        const int s = tile_no % S::kSlots;
+                        ok = ok && wait(&sh.empty[s], ((tile_no / S::kSlots) & 1) ^ 1);
+                        if (!ok) return;
+                        if (lane == 0) mbar_expect_tx(&sh.raw_full[s], (uint32_t)(np * S::kHalves * kPageTokens * 128));
+                        __syncwarp();
+                        if (part < S::kHalves && page < np)
+                            tma_load_2d_hint(skv + s * S::kTile + part * S::kHalf + page * (kPageTokens * 128), isv ? &tmap_v : &tmap_k, part * 64,
+                                             (id * p.Hkv + g) * kPageTokens, &sh.raw_full[s], policy);
                     }
-                    id = id_next;
+                    ++tile_no;
+                };
+                if (t0 >= 0) {
+                    int id = page_id(t0), id_next = units > 1 ? page_id(t0 + kBN) : 0;
+                    if (tile_no == 0) pdl_wait();
+                    id = checked(t0, id);
+                    bring(0, t0, id);
+                    for (int t = t0, left = units; left > 0 && ok; t += kBN, --left) {
+                        const int id_then = left > 2 ? page_id(t + 2 * kBN) : 0;
+                        if (left > 1) id_next = checked(t + kBN, id_next);
+                        if (S::kWidens && left > 1) bring(0, t + kBN, id_next);
+                        bring(1, t, id);
+                        if (!S::kWidens && left > 1) bring(0, t + kBN, id_next);
+                        id = id_next;
+                        id_next = id_then;
+                    }
                 }
                 if (ok) w.advance(p, list, places, total);
             }
@@ -243,11 +265,12 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 const uint32_t idesc_pv = wide_idesc<F>(D) | (1u << 16);  // B operand (V) is MN-major
                 const uint32_t q_lo = desc_lo(smem_u32(sq), 16), k_lo = desc_lo(smem_u32(skv), 16), v_lo = desc_lo(smem_u32(skv), S::kHalf);
                 // (everything kept by increments: between a place's weights and its next scores this thread is what all wait for)
-                uint32_t ks = 0, kp = 0, vs = 1, vp = 0;                  // slot and parity of the next K and V; K(t) V(t) take turns
+                uint32_t ks = 0, kp = 0, vs = S::kWidens ? 2 : 1, vp = 0;             // slot and parity of the next K and V
                 uint32_t p0 = 0, p1 = 0;                                  // parities of the places' weights
                 bool ok = true;
                 uint32_t pc = 0, loaded = 0;
-                auto next = [](uint32_t& slot, uint32_t& parity) { slot += 2; if (slot >= S::kSlots) { slot -= S::kSlots; parity ^= 1; } };
+                auto next_k = [&]() { ks ^= S::kWidens ? 1u : 2u; if (ks == 0) kp ^= 1; };
+                auto next_v = [&]() { if (!S::kWidens) vs ^= 2u; if (S::kWidens || vs == 1) vp ^= 1; };
                 auto issue_s = [&](uint32_t i) {                          // scores of place i with the next K
                     const uint32_t to = tmem + i * kBN, a = q_lo + i * kTileLo, bk = k_lo + ks * kTileLo;
 #pragma unroll
@@ -265,7 +288,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     umma_commit(&sh.pv_done[i]);
                 };
                 auto have_k = [&]() { ok = ok && mbar_wait(&sh.full[ks], kp); tc_fence_after(); return ok; };
-                auto done_k = [&]() { umma_commit(&sh.empty[ks]); next(ks, kp); };
+                auto done_k = [&]() { umma_commit(&sh.empty[ks]); next_k(); };
                 for (; ok; ++pc) {
                     ok = mbar_wait(&sh.told[pc % kPieceRing], (pc / kPieceRing) & 1);
                     if (!ok) break;
@@ -297,7 +320,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                             tc_fence_after();
                             issue_pv(1, t == 0);
                             umma_commit(&sh.empty[vs]);
-                            next(vs, vp);
+                            next_v();
                             if (more) { issue_s(1); done_k(); }
                         }
                     } else {
@@ -314,7 +337,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                             tc_fence_after();
                             issue_pv(i, t < 2);
                             umma_commit(&sh.empty[vs]);
-                            next(vs, vp);
+                            next_v();
                             if (t + 2 < units) { if (!have_k()) break; issue_s(i); done_k(); }
                         }
                     }
@@ -335,63 +358,74 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             if (lane == 0) mbar_arrive(&sh.left[pc % kPieceRing]);
             if (units == 0) break;
             if (t0 < 0) continue;
-            for (int t = 0; t < units && ok; ++t, ++step) {
-                const int here = sees - (t0 + t * kBN);                   // tokens of the step that count
-                for (int isv = 0; isv < 2; ++isv, ++tile_no) {
-                    const int s = tile_no % S::kSlots;
+            if constexpr (S::kWidens) {
+                auto widen = [&](int isv, int t) {
+                    const int here = sees - (t0 + t * kBN), at = step + t;                // tokens of the step that count; the step's number
+                    const int s = isv ? 2 : at & 1;
                     uint8_t* to = skv + s * S::kTile;
-                    if (S::kWidens) {
-                        const int r = tile_no % 3;
-                        const uint8_t* raw = sraw + r * S::kRaw;
-                        ok = wait(&sh.raw_full[r], (tile_no / 3) & 1);
-                        ok = ok && wait(&sh.empty[s], ((tile_no / S::kSlots) & 1) ^ 1);
-                        if (!ok) break;
-                        {   // this thread's token's scale (the buffer of the step before last is free: its V's slot was waited for)
-                            const float x = tid < here ? reinterpret_cast<const float*>(raw + S::kRawTile)[tid] : 0.f;
-                            float* pair = reinterpret_cast<float*>(&sh.scale[step & 1][tid >> 1]) + (tid & 1);
-                            if (isv == 0) pair[0] = x;
-                            else {
-                                float lv = tid < here ? __log2f(x) : 0.f;
-                                if (lv < -64.f) lv = -64.f;               // (a scale of 0; NaN stays, and makes the scores of who sees it NaN)
-                                pair[2] = lv;
-                                const float n = fast_exp2(-lv);
-                                reinterpret_cast<float*>(sh.inv[step & 1])[tid] = n == n ? n : 0.f;
-                            }
+                    const int r = tile_no % 3;
+                    const uint8_t* raw = sraw + r * S::kRaw;
+                    ok = ok && wait(&sh.raw_full[r], (tile_no / 3) & 1);
+                    ok = ok && wait(&sh.empty[s], ((isv ? at : at >> 1) & 1) ^ 1);
+                    if (!ok) return;
+                    if (!isv) {                // this thread's token's scales (the buffer is the step's four back; the products of three back have been waited for)
+                        const float* own = reinterpret_cast<const float*>(raw + S::kRawTile) + tid;
+                        const float x = tid < here ? own[0] : 0.f, y = tid < here ? own[kBN] : 1.f;
+                        float* pair = reinterpret_cast<float*>(&sh.scale[at & 3][tid >> 1]) + (tid & 1);
+                        float lv = __log2f(y);
+                        if (lv < -64.f) lv = -64.f;                   // (a scale of 0; NaN stays, and makes the scores of who sees it NaN)
+                        pair[0] = x;
+                        pair[2] = lv;
+                        const float n = fast_exp2(-lv);
+                        reinterpret_cast<float*>(sh.inv[at & 3])[tid] = n == n ? n : 0.f;
+                    }
+                    // Chunks of 16 codes become two of 16 bytes of the tile, in half c / 4.  Four lanes of eight take a chunk's second eight codes first,
+                    // the other four in rows of the other parity: so both the 8-byte loads and the 16-byte stores of a warp meet every
+                    // bank equally often.  Half of the thread's chunks are loaded before the first is widened
+                    constexpr int kPer = D / 16, kRows = 128 / kPer, kTurns = kBN / kRows;      // chunks per token, tokens per turn of the group
+                    const int c = tid % kPer, row = tid / kPer;       // (kRows is a multiple of 8: a token's last three bits are row's)
+                    const uint32_t second = (uint32_t)((c >> 2) ^ row) & 1;
+                    uint8_t* half = to + (c >> 2) * S::kHalf + row * 128;
+                    const uint8_t* from = raw + row * D + c * 16 + second * 8;
+                    const uint32_t at0 = (uint32_t)((((c & 3) * 2 + second) ^ (row & 7)) << 4), at1 = at0 ^ 16;
+                    const int other = 8 - 16 * (int)second;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint2 x[kTurns / 2], y[kTurns / 2];
+#pragma unroll
+                        for (int it = 0; it < kTurns / 2; ++it) {
+                            const uint8_t* src = from + (h * (kTurns / 2) + it) * kRows * D;
+                            x[it] = *reinterpret_cast<const uint2*>(src);
+                            y[it] = *reinterpret_cast<const uint2*>(src + other);
                         }
-                        // Chunks of 16 codes become two of 16 bytes of the tile, in half c / 4.  Four lanes of eight take a chunk's second eight codes first,
-                        // the other four in rows of the other parity: so both the 8-byte loads and the 16-byte stores of a warp meet every
-                        // bank equally often.  Half of the thread's chunks are loaded before the first is widened
-                        constexpr int kPer = D / 16, kRows = 128 / kPer, kTurns = kBN / kRows;      // chunks per token, tokens per turn of the group
-                        const int c = tid % kPer, row = tid / kPer;       // (kRows is a multiple of 8: a token's last three bits are row's)
-                        const uint32_t second = (uint32_t)((c >> 2) ^ row) & 1;
-                        uint8_t* half = to + (c >> 2) * S::kHalf + row * 128;
-                        const uint8_t* from = raw + row * D + c * 16 + second * 8;
-                        const uint32_t at0 = (uint32_t)((((c & 3) * 2 + second) ^ (row & 7)) << 4), at1 = at0 ^ 16;
-                        const int other = 8 - 16 * (int)second;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint2 x[kTurns / 2], y[kTurns / 2];
-#pragma unroll
-                            for (int it = 0; it < kTurns / 2; ++it) {
-                                const uint8_t* at = from + (h * (kTurns / 2) + it) * kRows * D;
-                                x[it] = *reinterpret_cast<const uint2*>(at);
-                                y[it] = *reinterpret_cast<const uint2*>(at + other);
-                            }
-#pragma unroll
-                            for (int it = 0; it < kTurns / 2; ++it) {
-                                const int turn = h * (kTurns / 2) + it;
-                                uint4 a, b;
-                                widen4<F>(x[it].x, a.x, a.y); widen4<F>(x[it].y, a.z, a.w);
-                                widen4<F>(y[it].x, b.x, b.y); widen4<F>(y[it].y, b.z, b.w);
-                                if (isv && turn * kRows + row >= here) a = b = make_uint4(0, 0, 0, 0);      // slots behind the last token may hold anything
-                                *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at0) = a;
-                                *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at1) = b;
-                            }
+                        for (int it = 0; it < kTurns / 2; ++it) {
+                            const int turn = h * (kTurns / 2) + it;
+                            uint4 a, b;
+                            widen4<F>(x[it].x, a.x, a.y); widen4<F>(x[it].y, a.z, a.w);
+                            widen4<F>(y[it].x, b.x, b.y); widen4<F>(y[it].y, b.z, b.w);
+                            if (isv && turn * kRows + row >= here) a = b = make_uint4(0, 0, 0, 0);      // slots behind the last token may hold anything
+                            *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at0) = a;
+                            *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at1) = b;
                         }
-                        fence_proxy_async();
-                        __syncwarp();
-                        if (lane == 0) { mbar_arrive(&sh.full[s]); mbar_arrive(&sh.raw_empty[r]); }
-                    } else {
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) { mbar_arrive(&sh.full[s]); mbar_arrive(&sh.raw_empty[r]); if (!isv) mbar_arrive(&sh.scaled[at & 3]); }
+                    ++tile_no;
+                };
+#pragma unroll 1
+                for (int i = 0; i < 2 * units && ok; ++i) {               // K(0) K(1) V(0) K(2) V(1) .. V(units - 1)
+                    const bool k = i == 0 || ((i & 1) && i != 2 * units - 1);
+                    widen(k ? 0 : 1, k ? (i + 1) / 2 : i == 2 * units - 1 ? units - 1 : i / 2 - 1);
+                }
+                step += units;
+            } else {
+                for (int t = 0; t < units && ok; ++t, ++step) {
+                    const int here = sees - (t0 + t * kBN);                   // tokens of the step that count
+                    for (int isv = 0; isv < 2; ++isv, ++tile_no) {
+                        const int s = tile_no % S::kSlots;
+                        uint8_t* to = skv + s * S::kTile;
                         ok = wait(&sh.raw_full[s], (tile_no / S::kSlots) & 1);
                         if (!ok) break;
                         if (isv && t0 + (t + 1) * kBN > min(ctx, sees)) {
@@ -497,7 +531,8 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 const int step = steps_before + t, jv = 2 * step + 1, sv = jv % S::kSlots;
                 ok = wait(&sh.s_ready[place], done & 1);
                 const bool masked = t0 + (t + 1) * kBN > plain;
-                if (S::kWidens || masked) ok = ok && wait(&sh.full[sv], (jv / S::kSlots) & 1);      // (the scales, and what is known of V)
+                if (S::kWidens) ok = ok && wait(&sh.scaled[step & 3], (step >> 2) & 1);
+                else if (masked) ok = ok && wait(&sh.full[sv], (jv / S::kSlots) & 1);               // (what is known of V)
                 if (!ok) break;
                 if (busy) {
                     tc_fence_after();
@@ -507,7 +542,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                         uint32_t x0[16], x1[16];   // scores of 32 tokens each
                         tmem_ld_16x256b_x4(s_addr + (uint32_t)(half * 64), x0);
                         tmem_ld_16x256b_x4(s_addr + (uint32_t)(half * 64 + 32), x1);
-                        const ulonglong2* scales = reinterpret_cast<const ulonglong2*>(sh.scale[step & 1]) + half * 32 + l4;
+                        const ulonglong2* scales = reinterpret_cast<const ulonglong2*>(sh.scale[step & 3]) + half * 32 + l4;
                         const uint64_t cc[2] = {pack_f32x2(c[0], c[0]), pack_f32x2(c[1], c[1])};
                         tmem_ld_wait();
                         auto scaled = [&](uint32_t (&x)[16], int first) {
@@ -624,7 +659,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                             }
                         }
                         uint32_t hi[16], lo[16];
-                        const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 1]) + half * 32 + l4;
+                        const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 3]) + half * 32 + l4;
                         const uint64_t m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
                         uint64_t sum[2] = {0, 0};
                         auto weights = [&](const uint32_t (&x)[16], int first) {
