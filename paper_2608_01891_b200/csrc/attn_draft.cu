@@ -16,6 +16,10 @@
 //               taken of weight / scale.  A reference moves only when a score outgrows it by 2^7.  Of a bf16 cache the weights are the
 //               sum of two bf16 values.
 //   masks       only pages that hold drafted tokens look at one
+//
+// Bound: the read of the cache; for few or short sequences the chain plan -> page ids -> pages -> join, some 12 us of a single long context's.
+// 256 rows (32 / 8 heads of 128) over up to 8192 int8 tokens 402 us (5.9 TB/s; one page of a warp at a time instead of two: 541), one row over
+// 131072 55 us (5.0 TB/s), 13 chains of 5 (16 / 4 heads of 64) over up to 6000 bf16 tokens 20 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>

@@ -1,5 +1,5 @@
 // Attention of drafted tokens over a paged cache in bf16 or in 8 bits, for sequences with more lines (rows x query heads of a KV head's
-// group) than attn_draft.cu is for: a page's K and V serve up to 256 lines, the products bound it, and they run on the tcgen05 tensor cores.
+// group) than attn_draft.cu is for: a page's K and V serve up to 256 lines, and the products run on the tcgen05 tensor cores.
 //
 //   work        as in attn_draft.cu: equal shares of the list of units, one CTA per SM, pieces joined by the CTA that is last
 //   tiles       two S / P and two O accumulators in TMEM.  An item of more than 128 lines has two tiles of 128, both at every step of 128 cached
@@ -10,12 +10,14 @@
 //               and the warp group only looks at the V of drafted tokens.  K is a K-major operand, V (as stored) an MN-major one
 //   softmax     eight warps per place, sixteen lines each, read from TMEM as fragments (two lines x 32 tokens per thread), so that a token's
 //               scales, which every line needs, are loaded once for two lines and by four lanes at a time (with a line per thread the loads of scales alone
-//               took longer than the products); statistics, references and weights as in attn_draft.cu.  The weights of an 8-bit cache are
-//               stored back over the scores they came from, in fp16; those of a bf16 cache as two bf16 parts, which fill the place of the
-//               scores, and the second product is issued for each part
+//               took longer than the products); 64 tokens at a time, since all 128 did not fit the registers (329 against 267 us); statistics,
+//               references and weights as in attn_draft.cu.  The weights of an 8-bit cache are stored back over the scores they came from, in
+//               fp16; those of a bf16 cache as two bf16 parts, which fill the place of the scores, and the second product is issued for each part
 //
-// Bound: of long trees the exponentials (16 per cycle and SM against 4096 multiply-adds) and the products about equally; of short ones with few lines
-// the widening and the read of the cache.
+// Bound: neither the products (1024 cycles per 128 lines x 128 tokens, 1536 with two parts of weights) nor the exponentials (16 per cycle: 1024)
+// but the chain from a place's scores to its weights and back, some 3400 cycles per 128 x 128 with two places under way, of which TMEM has
+// no room for a third.  8 trees of up to 61 tokens, 64 / 8 heads of 128, over up to 16384 tokens (120 GFLOP): 251 us in int8 (0.48
+// PFLOP/s), 227 in e4m3, 248 in bf16; of 5 tokens each 82 us (2.0 TB/s of int8, 3.9 of bf16).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -33,7 +35,7 @@ constexpr int kBM = 128;                           // lines per tile
 constexpr int kBN = 128;                           // cached tokens per step
 constexpr int kUnitPages = kBN / kPageTokens;
 constexpr int kWideLines = 2 * kBM;
-constexpr int kSoftmaxWarps = 16;                  // [place][half of 32 lines][32 lines]
+constexpr int kSoftmaxWarps = 16;                  // [place][sixteen lines]
 constexpr int kWideThreads = (kSoftmaxWarps + 8) * 32;       // and producer, issuer (and two idle), four that widen: 80 registers a thread
 constexpr int kPieceRing = 4;
 
