@@ -624,6 +624,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                 m[y] = mn;
                                 l[y] *= corr[y];
                             }
+                            tmem_st_wait();        // (in the second half: the first one's weights, and the sums if it moved the references too)
                             if (mine_steps > 0) {
                                 ok = wait(&sh.pv_done[place], (done - 1) & 1);
                                 if (!ok) break;
@@ -640,7 +641,6 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                             }
                             if (half == 1) {       // and the weights of the first half
                                 uint32_t hi[16], lo[16];
-                                tmem_st_wait();
                                 tmem_ld_16x128b_x8(s_addr, hi);
                                 if (!S::kWidens) tmem_ld_16x128b_x8(s_addr + 32, lo);
                                 tmem_ld_wait();
