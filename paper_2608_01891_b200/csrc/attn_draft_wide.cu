@@ -185,6 +185,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     const DraftPiece d = draft_piece(p, list, w, x1);
                     units = d.units; t0 = d.t0; sees = d.sees;
                     if (units == 0) { w.advance(p, list, places, total); continue; }      // (the second place of the CTA's before)
+                    if (pieces == kPieceRing) pdl_wait();      // (the softmax warps, which leave pieces, wait for the preceding kernel without a limit)
                     ok = wait(&sh.left[pieces % kPieceRing], ((pieces / kPieceRing) & 1) ^ 1);
                     if (!ok) break;
                     if (lane == 0) {
@@ -253,6 +254,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 }
                 if (ok) w.advance(p, list, places, total);
             }
+            pdl_wait();            // (pieces without tokens have not come by it)
             if (ok) ok = wait(&sh.left[pieces % kPieceRing], ((pieces / kPieceRing) & 1) ^ 1);
             if (ok && lane == 0) {
                 sh.piece[pieces % kPieceRing].units = 0;
@@ -261,6 +263,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             if (!ok) give_up();
         } else if (warp == kSoftmaxWarps + 1) {
             // -------------------------------------------------------------- issuer of the products (one thread)
+            pdl_wait();            // (the preceding kernel may run for longer than a wait's limit, which begins behind it)
             if (lane == 0) {
                 constexpr uint32_t kTileLo = S::kTile >> 4;
                 const uint32_t idesc_s = wide_idesc<F>(kBN);
@@ -352,6 +355,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         const int tid = threadIdx.x - (kWideThreads - 128);
         int tile_no = 0, step = 0;
         bool ok = true;
+        pdl_wait();                                // (as the issuer)
         for (int pc = 0; ok; ++pc) {
             ok = wait(&sh.told[pc % kPieceRing], (pc / kPieceRing) & 1);
             if (!ok) break;
