@@ -62,7 +62,7 @@ template <int W> struct __align__(8) DraftShared {            // W: compute warp
     float m[2][W][kMaxLines], l[2][W][kMaxLines];              // of pieces in turn
     float3 carry[kMaxLines];       // while pieces are joined: reference and sum so far, and what the sums before are to be multiplied by
     DraftShare share;
-    int merges;                    // items that this CTA has to join at the end
+    int merges, units;             // items that this CTA has to join at the end; units that the producer brought
     DraftPiece merge[2];
     volatile int abort;
 };
@@ -527,7 +527,9 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
                 mbar_arrive(&sh.told[it % kStages]);
                 mbar_arrive_n(&sh.full[it % kStages], F == AFLEX_CACHE_BF16 ? 1 : 33);
             }
+            ++it;
         }
+        if (lane == 0) sh.units = it;
         if (!ok && lane == 0) { sh.abort = 1; atomicExch(p.status, AFLEX_ERR_TIMEOUT); }
     } else if (warp < W) {
         // ------------------------------------------------------------------ compute
@@ -619,7 +621,11 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         }
     }
     __syncthreads();
-    if (sh.abort || sh.merges == 0) return;
+    if (sh.abort) {                                // copies under way are waited for once more, since this memory will be another CTA's
+        for (int i = max(0, sh.units - kStages); i < sh.units; ++i) mbar_wait(&sh.full[i % kStages], (i / kStages) & 1);
+        return;
+    }
+    if (sh.merges == 0) return;
     __threadfence();
     fence_proxy_async_all();
     __syncthreads();
@@ -649,6 +655,7 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
             phase ^= 1;
             if (__syncthreads_or(!ok)) {
                 if (threadIdx.x == 0) atomicExch(p.status, AFLEX_ERR_TIMEOUT);
+                mbar_wait(&sh.pieces, phase ^ 1);
                 return;
             }
             // factors of the pieces' sums, a warp for a line

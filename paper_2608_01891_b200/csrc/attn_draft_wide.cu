@@ -64,11 +64,11 @@ struct __align__(16) WideShared {
     uint64_t raw_full[4], raw_empty[3];            // pages have landed (bf16: in their slot), have been widened
     uint64_t full[4], empty[4];                    // a slot can be read by the products, has been
     uint64_t scaled[4];                            // by step: the scales are there
-    uint64_t q_ready[2], s_ready[2], p_ready[2], pv_done[2], meet;       // meet: the softmax warps
+    uint64_t q_ready[2], s_ready[2], p_ready[2], pv_done[2], meet, spent;       // meet: the softmax warps; spent: after a wait that ran out, the products issued before
     DraftPiece piece[kPieceRing];
     DraftShare share;
     DraftPiece merge[2];
-    int merges;
+    int merges, tiles;             // tiles: K and V tiles that the producer brought
     uint32_t tmem_base;
     volatile int abort;
 };
@@ -147,6 +147,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         for (int i = 0; i < 3; ++i) mbar_init(&sh.raw_empty[i], 4);
         for (int i = 0; i < 2; ++i) { mbar_init(&sh.q_ready[i], 8); mbar_init(&sh.s_ready[i], 1); mbar_init(&sh.p_ready[i], 8); mbar_init(&sh.pv_done[i], 1); }
         mbar_init(&sh.meet, kSoftmaxWarps);
+        mbar_init(&sh.spent, 1);
         sh.abort = 0;
         sh.merges = 0;
         fence_mbar_init();
@@ -260,6 +261,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 sh.piece[pieces % kPieceRing].units = 0;
                 mbar_arrive(&sh.told[pieces % kPieceRing]);
             }
+            if (lane == 0) sh.tiles = tile_no;
             if (!ok) give_up();
         } else if (warp == kSoftmaxWarps + 1) {
             // -------------------------------------------------------------- issuer of the products (one thread)
@@ -347,7 +349,12 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                         }
                     }
                 }
-                if (!ok) { sh.abort = 1; atomicExch(p.status, AFLEX_ERR_TIMEOUT); }
+                if (!ok) {
+                    sh.abort = 1;
+                    atomicExch(p.status, AFLEX_ERR_TIMEOUT);
+                    umma_commit(&sh.spent);
+                    mbar_wait(&sh.spent, 0);
+                }
             }
         }
     } else if (group == 5) {
@@ -838,6 +845,11 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
     }
     tc_fence_before();
     __syncthreads();
+    if (sh.abort) {                                // copies under way are waited for once more, since this memory will be another CTA's
+        constexpr int kRing = S::kWidens ? 3 : S::kSlots;
+        for (int i = max(0, sh.tiles - kRing); i < sh.tiles; ++i) mbar_wait(&sh.raw_full[i % kRing], (i / kRing) & 1);
+        __syncthreads();
+    }
     if (warp == kSoftmaxWarps + 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
 }
 
