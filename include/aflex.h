@@ -634,7 +634,7 @@ AFLEX_API aflex_status aflex_cache_convert(aflex_ctx* ctx, const aflex_attn_desc
  * V enter the second product as the sum of two bf16 values (bf16 cache), or (8 bits) in fp16 with the token's scale multiplied in, each off
  * by at most half a step of fp16 or 2^-33 of the row's largest.
  * A row that sees no token, or whose sequence raises AFLEX_ERR_BOUNDS, gets out 0 and lse -infinity.  A score of -infinity weighs
- * nothing; a score of +infinity or NaN makes its head's out and lse NaN.  A token with infinite or NaN values, or such a scale, makes
+ * nothing; a score of +infinity or NaN makes its head's out and lse NaN.  A token with infinite or NaN values (e4m3 codes of NaN), or such a scale, makes
  * out of the rows that see it infinite or NaN, in the channel at least (their lse may be NaN too), and does not touch the others.
  * A bad page id raises AFLEX_ERR_BOUNDS (page 0 is read instead).  Uses the workspace: aflex_attn_draft_workspace_bytes.
  * The result is the same from run to run.

@@ -247,35 +247,40 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
 #pragma unroll
         for (int g = 0; g < N; ++g) {
             const int first = tp + g * kPageTokens;
-            // slots behind the last token may hold anything; and an infinity or NaN of a drafted token must not enter the product, which
-            // would carry it to the lines that do not see it
+            // slots behind the last token may hold anything; and an infinity or NaN of a drafted token (int8 has neither) must not enter the
+            // product, which would carry it to the lines that do not see it
             uint32_t here = 0;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int t = 2 * l4 + (k & 1) + 8 * (k >> 1);
                 bool odd = first + t >= seen;
-                if (F == AFLEX_CACHE_BF16) {
+                // (the words that this lane is to multiply; of e4m3 not where a single row sees itself and there is nobody to be kept from it)
+                if (F == AFLEX_CACHE_E4M3 && p.mask == nullptr && u.m == 1) {
+                } else if (F == AFLEX_CACHE_E4M3 && D == 64) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(kp + g * kPageBytes + S::kBlock + chunk_at<kRow>(t, hl >> 1) + (hl & 1) * 8);
+                    odd = odd || odd_e4m3(v.x) || odd_e4m3(v.y);
+                } else if (F != AFLEX_CACHE_INT8) {
 #pragma unroll
-                    for (int h = 0; h < D / 64; ++h) {
+                    for (int h = 0; h < (F == AFLEX_CACHE_BF16 ? D / 64 : 1); ++h) {
                         const uint4 v = *reinterpret_cast<const uint4*>(kp + g * kPageBytes + S::kBlock + chunk_at<kRow>(t, 8 * h + hl));
                         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) odd = odd || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+                        for (int i = 0; i < 4; ++i) odd = odd || (F == AFLEX_CACHE_BF16 ? odd_bf16(w[i]) : odd_e4m3(w[i]));
                     }
                 }
                 if (odd) here |= 1u << k;
             }
             uint32_t all = (here & 3u) << (2 * l4) | (here >> 2) << (2 * l4 + 8);         // bit t: token t
-            if (F == AFLEX_CACHE_BF16) {
-#pragma unroll
-                for (int off = 1; off < 32; off <<= 1) all |= __shfl_xor_sync(0xffffffffu, all, off);
+            if (F != AFLEX_CACHE_INT8) {
+                all = __reduce_or_sync(0xffffffffu, all);
                 here = (all >> (2 * l4) & 3u) | (all >> (2 * l4 + 8) & 3u) << 2;
             }
             dead |= here << (4 * g);
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const int t = first + hl + 8 * r;
-                const bool bad = F == AFLEX_CACHE_BF16 ? all >> (hl + 8 * r) & 1u : !(inv[g][r] == inv[g][r]);      // (a scale that is no number)
+                bool bad = F != AFLEX_CACHE_INT8 && (all >> (hl + 8 * r) & 1u);
+                if (F != AFLEX_CACHE_BF16) bad = bad || !(inv[g][r] == inv[g][r]);      // (a scale that is no number)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll

@@ -22,6 +22,8 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "draft.cuh"
 #include "internal.h"
 #include "ptx.cuh"
@@ -70,6 +72,7 @@ struct __align__(16) WideShared {
     DraftPiece merge[2];
     int merges, tiles;             // tiles: K and V tiles that the producer brought
     uint32_t tmem_base;
+    int odd[kPieceRing];           // e4m3: number (from 1) of the last piece there with a NaN in V of a drafted token
     volatile int abort;
 };
 
@@ -118,6 +121,21 @@ __device__ __forceinline__ void tmem_st_16x128b_x8(uint32_t taddr, const uint32_
 #undef I4
 #undef I16
 
+// A drafted token of an e4m3 cache whose V (codes at `raw`) has a NaN becomes zeros in the widened tile, whose row is at `to`: it would spread to
+// lines that do not see it.  Those that do are looked for when the piece is done.  (A thread per token: they share their banks, so each begins at a
+// chunk of its own.  Not inlined: the loop that widens, which all wait for, was slower with this in its middle)
+template <int D> __noinline__ __device__ bool zero_odd_token(const uint8_t* raw, uint8_t* to) {
+    bool odd = false;
+#pragma unroll 1
+    for (int k = 0; k < D / 16; ++k) {
+        const uint4 v = *reinterpret_cast<const uint4*>(raw + ((k + threadIdx.x) & (D / 16 - 1)) * 16);
+        odd = odd || odd_e4m3(v.x) || odd_e4m3(v.y) || odd_e4m3(v.z) || odd_e4m3(v.w);
+    }
+#pragma unroll 1
+    for (int k = 0; odd && k < D / 8; ++k) *reinterpret_cast<uint4*>(to + (k >> 3) * (kBN * 128) + (k & 7) * 16) = make_uint4(0, 0, 0, 0);
+    return odd;
+}
+
 // Floats of a piece's slot in global memory: [line][2] reference and sum, then [run of four channels][line][4] sums.
 constexpr int kWideCarry = 2 * kWideLines;
 template <int D> constexpr int kWideSlot = kWideCarry + kWideLines * D;
@@ -150,6 +168,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         mbar_init(&sh.spent, 1);
         sh.abort = 0;
         sh.merges = 0;
+        for (int i = 0; i < kPieceRing; ++i) sh.odd[i] = 0;
         fence_mbar_init();
         if (!S::kWidens) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); }
     }
@@ -372,7 +391,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             if (units == 0) break;
             if (t0 < 0) continue;
             if constexpr (S::kWidens) {
-                auto widen = [&](int isv, int t) {
+                auto widen = [&](int isv, int t, auto look) {
                     const int here = sees - (t0 + t * kBN), at = step + t;                // tokens of the step that count; the step's number
                     const int s = isv ? 2 : at & 1;
                     uint8_t* to = skv + s * S::kTile;
@@ -422,16 +441,29 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                             *reinterpret_cast<uint4*>(half + turn * kRows * 128 + at1) = b;
                         }
                     }
+                    if (look && isv) {
+                        // (a thread per token, of those that the warp has widened)
+                        __syncwarp();
+                        const int mine = lane / (32 / kPer) * kRows + warp % 4 * (32 / kPer) + lane % (32 / kPer);
+                        if (mine < here && t0 + t * kBN + mine >= ctx && zero_odd_token<D>(raw + mine * D, to + mine * 128)) sh.odd[pc % kPieceRing] = pc + 1;
+                    }
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) { mbar_arrive(&sh.full[s]); mbar_arrive(&sh.raw_empty[r]); if (!isv) mbar_arrive(&sh.scaled[at & 3]); }
                     ++tile_no;
                 };
-#pragma unroll 1
-                for (int i = 0; i < 2 * units && ok; ++i) {               // K(0) K(1) V(0) K(2) V(1) .. V(units - 1)
+                auto tile = [&](int i, auto look) {                       // the i-th of K(0) K(1) V(0) K(2) V(1) .. V(units - 1)
                     const bool k = i == 0 || ((i & 1) && i != 2 * units - 1);
-                    widen(k ? 0 : 1, k ? (i + 1) / 2 : i == 2 * units - 1 ? units - 1 : i / 2 - 1);
-                }
+                    widen(k ? 0 : 1, k ? (i + 1) / 2 : i == 2 * units - 1 ? units - 1 : i / 2 - 1, look);
+                };
+                // e4m3: from the first V with drafted tokens on they are looked at (8 trees of up to 61: 227 us without that, 230 with, 239 if the
+                // first tiles went through the same loop)
+                int i = 0;
+                const int plain = F == AFLEX_CACHE_E4M3 ? min(max((min(ctx, sees) - t0) / kBN, 0), units) : units;       // units without drafted tokens
+#pragma unroll 1
+                for (; i < 2 * plain && ok; ++i) tile(i, std::false_type());
+#pragma unroll 1
+                for (; F == AFLEX_CACHE_E4M3 && i < 2 * units && ok; ++i) tile(i, std::bool_constant<F == AFLEX_CACHE_E4M3>());
                 step += units;
             } else {
                 for (int t = 0; t < units && ok; ++t, ++step) {
@@ -451,7 +483,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                     const uint4 v = *reinterpret_cast<const uint4*>(to + (k >> 3) * S::kHalf + tid * 128 + (k & 7) * 16);
                                     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                                    for (int i = 0; i < 4; ++i) odd = odd || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+                                    for (int i = 0; i < 4; ++i) odd = odd || odd_bf16(w[i]);
                                 }
                             }
                             if (odd || tid >= here) {
@@ -714,6 +746,21 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             // ---- the piece is done: normalised to the output, or its sums to the CTA's slot
             if (mine_steps > 0) ok = wait(&sh.pv_done[place], (done - 1) & 1);
             if (!ok) break;
+            if (F == AFLEX_CACHE_E4M3 && mine_steps > 0 && sh.odd[pc % kPieceRing] == pc + 1) {
+                // some drafted token has a NaN in V: the lines that see it become NaN.  (A search that takes long, for something that seldom is)
+#pragma unroll 1
+                for (int j = max(t0, d.ctx); j < min(d.sees, t0 + units * kBN); ++j) {
+                    const int id = fetch(p.page_table + (size_t)d.b * p.max_pages + j / kPageTokens);
+                    const bool there = id >= 0 && id < p.num_pages;
+                    const uint8_t* v = v_codes + (((size_t)(there ? id : 0) * p.Hkv + d.g) * kPageTokens + j % kPageTokens) * D;
+                    if (!__any_sync(0xffffffffu, lane * 4 < D && odd_e4m3(fetch(reinterpret_cast<const uint32_t*>(v) + lane)))) continue;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int line = line0 + hl + 8 * y, i = line >> p.g_shift;
+                        if (line < d.lines && sees_drafted(p, d.row0 + i, d.i0 + i, j - d.ctx, d.m)) l[y] = __uint_as_float(0x7fc00000u);
+                    }
+                }
+            }
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
                 l[y] += __shfl_xor_sync(0xffffffffu, l[y], 1);

@@ -142,7 +142,7 @@ template <int kTokens, int kFull> struct DraftWalk {
 struct DraftPiece {
     int units, t0, sees, ctx;      // units with tokens, or 1 for an item without (t0 < 0); first token, tokens the tile's rows may see, earlier tokens
     int row0, lines, i0, m, g;     // first row and lines of the tile, number of the first row and of all rows in the sequence, KV head
-    int item, slot, whole;
+    int item, slot, whole, b;      // b: the sequence
     long long first, last;         // positions of the item's first and last unit with tokens
 };
 // The piece that starts at w (not at the empty place of an item that has tokens) and ends with the item or at x1; no units: nothing to do.
@@ -155,7 +155,7 @@ __device__ __forceinline__ DraftPiece draft_piece(const DraftParams& p, const Dr
     d.sees = list.sees(w.s, w.tile); d.ctx = w.s.ctx;
     d.i0 = w.tile << p.rpt_shift; d.row0 = w.s.o0 + d.i0; d.m = w.s.m; d.g = w.g;
     d.lines = min(1 << p.rpt_shift, w.s.m - d.i0) << p.g_shift;
-    d.item = w.id + w.g; d.slot = k0 > 0 ? 0 : 1; d.whole = k0 <= 0 && k1 == all;
+    d.b = w.b; d.item = w.id + w.g; d.slot = k0 > 0 ? 0 : 1; d.whole = k0 <= 0 && k1 == all;
     d.first = w.pos - w.u + 1; d.last = d.first + (long long)wt * (all - 1);
     return d;
 }
@@ -270,6 +270,10 @@ template <int F> __device__ __forceinline__ void widen4(uint32_t w, uint32_t& lo
         asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
     }
 }
+
+// Whether one of four e4m3 codes is a NaN (0x7f or 0xff); of two bf16 values whether one is an infinity or NaN.
+__device__ __forceinline__ bool odd_e4m3(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
+__device__ __forceinline__ bool odd_bf16(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
 // 16 bytes of scales (the L2 cache is told to fetch the neighbouring heads' with them), and one arrival when this thread's copies so far have landed.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {

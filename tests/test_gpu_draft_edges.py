@@ -1,11 +1,12 @@
-"""Attention of drafted tokens and the operators around it where one value decides: references that move twice in a step of the tensor-core kernel."""
+"""Attention of drafted tokens and the operators around it where one value decides: references that move twice in a step of the tensor-core kernel,
+codes that are no numbers."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import draft_oracle as DO
 from paper_2608_01891_b200 import aflex as AF
-from test_gpu_draft import DEV, FORMATS, TYPES, Cache, check_attention, ctx, f64, offsets_of  # noqa: F401 (fixtures)
+from test_gpu_draft import DEV, FORMATS, TYPES, Cache, check_attention, ctx, f64, offsets_of, random_masks  # noqa: F401 (fixtures)
 
 pytestmark = pytest.mark.gpu
 WEIGHT = {"bf16": 2.0 ** -17, "int8": 2.0 ** -12, "e4m3": 2.0 ** -12}     # what a weight of V is off by (test_gpu_draft.py)
@@ -53,3 +54,69 @@ def test_references_move_in_both_halves_of_every_step(ctx, fmt, Hq, Hkv, D, m): 
     offs = offsets_of([m])
     out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
     check_attention(out, lse, q, c, offs, None, m, WEIGHT[fmt])
+
+
+MASKED = [  # Hq, Hkv, D, lens, rows per sequence: tiles of 8 lines, of 16, of 256 in two places, of 256
+    (8, 4, 128, [90, 40, 33], [3, 4, 5]),
+    (8, 4, 64, [90, 40, 33], [3, 4, 5]),
+    (16, 4, 128, [90, 40, 33], [3, 4, 5]),
+    (16, 4, 64, [90, 140, 33], [3, 4, 12]),
+    (8, 4, 128, [90, 40, 33], [20, 40, 17]),
+    (16, 2, 128, [390, 40, 33], [40, 33, 17]),
+    (32, 4, 64, [290, 40, 133], [20, 40, 17]),
+]
+
+
+@pytest.mark.parametrize("scale", ["number", "nan"])
+@pytest.mark.parametrize("Hq,Hkv,D,lens,new", MASKED)
+def test_codes_that_are_no_numbers_do_not_spread(ctx, Hq, Hkv, D, lens, new, scale):  # noqa: F811
+    """e4m3 has two codes of NaN.  In K or V of a drafted token they reach the rows that see it, and leave the others' bits as they are."""
+    offs = offsets_of(new)
+    T = int(offs[-1])
+    ints, mask = random_masks(np.random.default_rng(1), new, "tree")
+    q = torch.randn(T, Hq, D, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    draft = AF.draft_rows(torch.from_numpy(offs).to(DEV), None, mask)
+    bad = {0: 1, 1: 3, 2: 0}                                               # sequence: drafted token
+    clean = Cache(lens, Hkv, D, "e4m3", seed=8)
+    want, want_lse = attend(ctx, clean, q, draft)
+    for at in (0, 1):
+        c = Cache(lens, Hkv, D, "e4m3", seed=8)
+        for b, j in bad.items():
+            t = lens[b] - new[b] + j
+            page, slot = int(c.table[b, t // 16]), t % 16
+            for g in range(Hkv):
+                # both codes, in different parts of the head; one head has a single one, in its last channel
+                where = [(D - 1, 0x7f)] if g == 1 else [(3, 0x7f), (4, 0xff), (D // 2 + 9, 0xff)]
+                for ch, code in where:
+                    c.tensors[at].view(torch.uint8)[page, g, slot, ch] = code
+                if scale == "nan":
+                    c.tensors[at + 2][page, g, slot] = float("nan")
+        c.put()
+        out, lse = attend(ctx, c, q, draft)
+        for r, (b, i, m) in enumerate(DO.rows_of(lens, offs)):
+            if ints[r] >> bad[b] & 1:
+                assert torch.isnan(out[r]).any(1).all(), (at, b, i)
+            else:
+                assert torch.equal(want[r], out[r]) and torch.equal(want_lse[r], lse[r]), (at, b, i)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens,new", MASKED)
+def test_a_code_that_is_no_number_in_an_earlier_token(ctx, Hq, Hkv, D, lens, new):  # noqa: F811
+    """Every row of its sequence sees it, in the channel at least; other sequences and KV heads do not."""
+    offs = offsets_of(new)
+    T = int(offs[-1])
+    q = torch.randn(T, Hq, D, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    draft = AF.draft_rows(torch.from_numpy(offs).to(DEV))
+    got = []
+    for t in (None, 2, lens[0] - new[0] - 1):                              # in the first step; beside the drafted tokens
+        c = Cache(lens, Hkv, D, "e4m3", seed=8)
+        if t is not None:
+            c.tensors[1].view(torch.uint8)[int(c.table[0, t // 16]), 1, t % 16, 7] = 0xff
+            c.put()
+        got.append(attend(ctx, c, q, draft))
+    G = Hq // Hkv
+    mine = torch.zeros(T, Hq, dtype=torch.bool)
+    mine[:new[0], G:2 * G] = True
+    for out, lse in got[1:]:
+        assert torch.isnan(out[:new[0], G:2 * G, 7]).all()
+        assert torch.equal(out[~mine], got[0][0][~mine]) and torch.equal(lse[~mine], got[0][1][~mine])
