@@ -307,10 +307,9 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
             mx[n][e] = fmaxf(x[0][n][0][e], x[0][n][1][e]);
 #pragma unroll
             for (int g = 1; g < N; ++g) mx[n][e] = fmaxf(mx[n][e], fmaxf(x[g][n][0][e], x[g][n][1][e]));
-            grow = grow || mx[n][e] > st.m[n][e] + 15.f;
+            grow = grow || mx[n][e] > st.m[n][e] + (kBelow<F> + 7.f);
         }
-    // weights are 2^(x - m), m the running maximum less 8 (the same for all lanes of a line); they stay below 2^15 until a score is 2^15
-    // times the reference
+    // (m is the same for all lanes of a line)
     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -321,7 +320,7 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-                const float mn = v > st.m[n][e] + 15.f ? v - 8.f : st.m[n][e];          // (a line's bits do not depend on who else's moves)
+                const float mn = v > st.m[n][e] + (kBelow<F> + 7.f) ? v - kBelow<F> : st.m[n][e];          // (a line's bits do not depend on who else's moves)
                 corr[e] = fast_exp2(st.m[n][e] - mn);
                 st.m[n][e] = mn;
                 st.l[n][e] *= corr[e];

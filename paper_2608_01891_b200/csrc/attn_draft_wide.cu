@@ -655,14 +655,14 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                 mx[y] = max3(mx[y], __uint_as_float(x0[4 * i + 2 * y]), __uint_as_float(x0[4 * i + 2 * y + 1]));
                                 mx[y] = max3(mx[y], __uint_as_float(x1[4 * i + 2 * y]), __uint_as_float(x1[4 * i + 2 * y + 1]));
                             }
-                        // weights are 2^(x - m), m the running maximum less 8: below 2^15 until a score outgrows it
-                        if (__any_sync(0xffffffffu, mx[0] > m[0] + 15.f || mx[1] > m[1] + 15.f)) {
+                        constexpr float kRoom = kBelow<F> + 7.f;
+                        if (__any_sync(0xffffffffu, mx[0] > m[0] + kRoom || mx[1] > m[1] + kRoom)) {
                             float corr[2];
 #pragma unroll
                             for (int y = 0; y < 2; ++y) {
                                 mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 1));
                                 mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
-                                const float mn = mx[y] > m[y] + 15.f ? ceilf(mx[y]) - 8.f : m[y];          // (whole: what was rounded is scaled exactly)
+                                const float mn = mx[y] > m[y] + kRoom ? ceilf(mx[y]) - kBelow<F> : m[y];          // (whole: what was rounded is scaled exactly)
                                 corr[y] = fast_exp2(m[y] - mn);
                                 m[y] = mn;
                                 l[y] *= corr[y];

@@ -239,6 +239,11 @@ __device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList
     __syncthreads();
 }
 
+// Weights are 2^(x - m): m is the running maximum less kBelow, and moves when a weight would pass 2^(kBelow + 7).  In fp16 (8-bit caches) weights
+// from 2^8 to 2^15 leave the most room below; bf16 has room enough anywhere, and weights from 2^-8 to 2^-1 keep the sums of weights times values
+// finite where those of a softmax in 32 bits are.
+template <int F> constexpr float kBelow = F == AFLEX_CACHE_BF16 ? -8.f : 8.f;
+
 // Sums of one run of four channels of a line over pieces.
 struct RunSum {
     float M, L;

@@ -1,5 +1,5 @@
 """Attention of drafted tokens and the operators around it where one value decides: references that move twice in a step of the tensor-core kernel,
-codes that are no numbers."""
+codes that are no numbers, values of any size."""
 import numpy as np
 import pytest
 import torch
@@ -120,3 +120,35 @@ def test_a_code_that_is_no_number_in_an_earlier_token(ctx, Hq, Hkv, D, lens, new
     for out, lse in got[1:]:
         assert torch.isnan(out[:new[0], G:2 * G, 7]).all()
         assert torch.equal(out[~mine], got[0][0][~mine]) and torch.equal(lse[~mine], got[0][1][~mine])
+
+
+LINES = [  # Hq, Hkv, D, rows: tiles of 8 lines, of 16, of 256 in two places, of 256
+    (8, 1, 128, 1), (8, 2, 64, 2), (8, 1, 128, 2), (8, 1, 64, 2), (8, 1, 128, 8), (8, 1, 64, 8), (8, 1, 128, 40), (8, 1, 64, 40)]
+
+
+def check_values(ctx, fmt, Hq, Hkv, D, m, large, big):  # noqa: F811
+    """Tokens of zeros (every second one), of numbers near 1, and of up to 4 times `big` (those of `large`)."""
+    n, gen = 700, torch.Generator().manual_seed(31)
+    c = Cache([n], Hkv, D, fmt, seed=30)
+    for g in range(Hkv):
+        v = torch.randn(n, D, generator=gen)
+        v[::2] = 0
+        for t in large:
+            v[t] = big * torch.randn(D, generator=gen)
+        for t in range(n):
+            put_token(c, 0, t, g, v=v[t].to(torch.bfloat16))
+    c.put()
+    q = (2.0 * torch.randn(m, Hq, D, generator=gen)).to(torch.bfloat16).to(DEV)
+    offs = offsets_of([m])
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
+    check_attention(out, lse, q, c, offs, None, m, WEIGHT[fmt])
+
+
+LARGE = {"one": [333], "early": range(0, 60), "late": range(600, 700), "mixed": range(0, 700, 3)}
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,m", LINES)
+@pytest.mark.parametrize("where", list(LARGE))
+def test_very_large_values_of_a_bf16_cache(ctx, Hq, Hkv, D, m, where):  # noqa: F811
+    """Sums of weights times values up to 2^122 stay finite."""
+    check_values(ctx, "bf16", Hq, Hkv, D, m, LARGE[where], 2.0 ** 120)
