@@ -13,7 +13,7 @@
 //               that brings the line's largest entry to [2^14, 2^15).
 //   softmax     online, fp32, base 2, each warp with its own running state.  Of an 8-bit cache the weight of a code is p_j * scale_j, so
 //               the running reference follows s_j + log2 scale_j, the weights enter the product in fp16 below 2^15, and their sum is
-//               taken of weight / scale.  A reference moves only when a score outgrows it by 2^7.  Of a bf16 cache the weights are the
+//               taken of p_j, with the same reference.  A reference moves only when a score outgrows it by 2^7.  Of a bf16 cache the weights are the
 //               sum of two bf16 values.
 //   masks       only pages that hold drafted tokens look at one
 //
@@ -217,18 +217,16 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                 }
         }
     }
-    // ---- scores in log2 units, of the lane's lines: x[g][n][r][e] for token hl + 8 r; inv: 1 / scale of the token's V
-    float x[N][NT][2][2], inv[N][2];
+    // ---- scores in log2 units, of the lane's lines: x[g][n][r][e] for token hl + 8 r, with lv of the token's V (log2_scale)
+    float x[N][NT][2][2], lv[N][2];
 #pragma unroll
     for (int g = 0; g < N; ++g)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            float ks = 1.f, lv = 0.f;
+            float ks = 1.f;
             if (F != AFLEX_CACHE_BF16) {
                 ks = sp[g * kPageScales + hl + 8 * r];
-                lv = __log2f(sp[g * kPageScales + kPageTokens + hl + 8 * r]);
-                if (lv < -64.f) lv = -64.f;        // (a scale of 0; NaN stays)
-                inv[g][r] = fast_exp2(-lv);
+                lv[g][r] = log2_scale(sp[g * kPageScales + kPageTokens + hl + 8 * r]);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -236,7 +234,7 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                 for (int e = 0; e < 2; ++e) {
                     float& v = x[g][n][r][e];
                     v = F == AFLEX_CACHE_INT8 ? fmaf(s[g][n][2 * r + e], st.c[n][e], st.off[n][e]) : s[g][n][2 * r + e] * st.c[n][e];
-                    if (F != AFLEX_CACHE_BF16) v = fmaf(v, ks, lv);
+                    if (F != AFLEX_CACHE_BF16) v = fmaf(v, ks, lv[g][r]);
                 }
         }
     uint32_t dead = 0;                             // bit 4 g + k: nothing of token 2 l4 + (k & 1) + 8 (k >> 1) of V may enter the product
@@ -280,7 +278,7 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
             for (int r = 0; r < 2; ++r) {
                 const int t = first + hl + 8 * r;
                 bool bad = F != AFLEX_CACHE_INT8 && (all >> (hl + 8 * r) & 1u);
-                if (F != AFLEX_CACHE_BF16) bad = bad || !(inv[g][r] == inv[g][r]);      // (a scale that is no number)
+                if (F != AFLEX_CACHE_BF16) bad = bad || !(lv[g][r] == lv[g][r]);      // (a scale that is no number)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -290,7 +288,7 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                         if (see && bad) poison[n][e] = true;
                         if (!see) x[g][n][r][e] = -INFINITY;
                     }
-                if (F != AFLEX_CACHE_BF16 && bad) inv[g][r] = 0.f;      // (0 times the weight, for the lines that do not see it)
+                if (F != AFLEX_CACHE_BF16 && bad) lv[g][r] = 0.f;       // (for the lines that do not see it, whose x is -infinity)
             }
         }
 #pragma unroll
@@ -322,8 +320,8 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
                 const float mn = v > st.m[n][e] + (kBelow<F> + 7.f) ? v - kBelow<F> : st.m[n][e];          // (a line's bits do not depend on who else's moves)
                 corr[e] = fast_exp2(st.m[n][e] - mn);
+                st.l[n][e] = scale_sum(st.l[n][e], st.m[n][e] - mn);
                 st.m[n][e] = mn;
-                st.l[n][e] *= corr[e];
             }
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) { st.o[j][n][0] *= corr[0]; st.o[j][n][1] *= corr[1]; st.o[j][n][2] *= corr[0]; st.o[j][n][3] *= corr[1]; }
@@ -344,8 +342,8 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
                     a[g][n][r] = movmatrix_trans(hi);
                     b[g][n][r] = movmatrix_trans(pack_bf16x2(w0 - __uint_as_float(hi << 16), w1 - __uint_as_float(hi & 0xffff0000u)));
                 } else {
-                    st.l[n][0] = fmaf(w0, inv[g][r], st.l[n][0]);
-                    st.l[n][1] = fmaf(w1, inv[g][r], st.l[n][1]);
+                    st.l[n][0] += fast_exp2(x[g][n][r][0] - st.m[n][0] - lv[g][r]);
+                    st.l[n][1] += fast_exp2(x[g][n][r][1] - st.m[n][1] - lv[g][r]);
                     const __half2 h = __floats2half2_rn(w0, w1);
                     a[g][n][r] = movmatrix_trans(*reinterpret_cast<const uint32_t*>(&h));
                 }
@@ -674,13 +672,13 @@ attn_draft_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 #pragma unroll 1
                 for (int k = lane; k < here; k += 32) {
                     float2* x = weight(k, line);
+                    L += scale_sum(x->y, x->x - M);
                     x->x = fast_exp2(x->x - M);
-                    L = fmaf(x->y, x->x, L);
                 }
 #pragma unroll
                 for (int off = 16; off > 0; off >>= 1) L += __shfl_xor_sync(0xffffffffu, L, off);
                 const float f = fast_exp2(before - M);
-                if (lane == 0) sh.carry[line] = make_float3(M, k0 > 0 ? fmaf(sh.carry[line].y, f, L) : L, f);
+                if (lane == 0) sh.carry[line] = make_float3(M, k0 > 0 ? L + scale_sum(sh.carry[line].y, before - M) : L, f);
             }
             __syncthreads();
 #pragma unroll 1
@@ -766,6 +764,7 @@ aflex_status attn_draft_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const v
     p.rpt_shift = (lines <= 8LL * batch ? 3 : lines <= (long long)narrow * batch ? 4 : 8) - p.g_shift;
     const float scale = d->sm_scale != 0.f ? d->sm_scale : 1.0f / sqrtf((float)D);
     p.scale_log2 = scale * 1.4426950408889634f;
+    p.unit = cache->format == AFLEX_CACHE_BF16 ? 1.f : exp2f(kScaleShift);
     p.out = (__nv_bfloat16*)out; p.lse = lse; p.status = ctx->dev_status;
     p.counters = ctx->counters_attn;
     const size_t need = attn_draft_workspace_bytes(d, ctx->num_sms);

@@ -57,8 +57,8 @@ template <int D, int F> struct WideForm {
 };
 
 struct __align__(16) WideShared {
-    float4 scale[4][kBN / 2];                      // by step: of two tokens, K's scales and log2 of V's
-    float4 inv[4][kBN / 4];                        // 1 / V's, of four tokens
+    float4 scale[4][kBN / 2];                      // by step: of two tokens, K's scales and lv of V's (log2_scale)
+    float4 inv[4][kBN / 4];                        // 2^-lv, of four tokens
     float2 state[2][kBM];                          // by place: references and sums of a finished piece
     float factor[2][kBM];                          // by place: what a line's products count, in log2 units
     uint32_t bad[4][kBN / 32];                     // by step: tokens whose V holds an infinity or NaN (bf16)
@@ -72,6 +72,7 @@ struct __align__(16) WideShared {
     DraftPiece merge[2];
     int merges, tiles;             // tiles: K and V tiles that the producer brought
     uint32_t tmem_base;
+    int far;                       // the first step with a token whose lv is above kNear
     int odd[kPieceRing];           // e4m3: number (from 1) of the last piece there with a NaN in V of a drafted token
     volatile int abort;
 };
@@ -81,6 +82,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
+
+// The largest lv up to which a token's part of the sum of weights may be formed as weight * 2^-lv: a weight that is lost (below 2^-126) is then one of
+// less than 2^(-134 + kNear + 80) of the sum.  Behind a token with a larger one it takes an exponential of its own.
+constexpr float kNear = 10.f;
 
 // Two weights of a line as operand: fp16, or the two bf16 parts.
 template <int F> __device__ __forceinline__ void pack_weights(float w0, float w1, uint32_t& hi, uint32_t& lo) {
@@ -168,6 +173,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
         mbar_init(&sh.spent, 1);
         sh.abort = 0;
         sh.merges = 0;
+        sh.far = 0x7fffffff;
         for (int i = 0; i < kPieceRing; ++i) sh.odd[i] = 0;
         fence_mbar_init();
         if (!S::kWidens) { prefetch_tmap(&tmap_k); prefetch_tmap(&tmap_v); }
@@ -404,12 +410,12 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                         const float* own = reinterpret_cast<const float*>(raw + S::kRawTile) + tid;
                         const float x = tid < here ? own[0] : 0.f, y = tid < here ? own[kBN] : 1.f;
                         float* pair = reinterpret_cast<float*>(&sh.scale[at & 3][tid >> 1]) + (tid & 1);
-                        float lv = __log2f(y);
-                        if (lv < -64.f) lv = -64.f;                   // (a scale of 0; NaN stays, and makes the scores of who sees it NaN)
+                        const float lv = log2_scale(y);               // (NaN makes the scores of who sees it NaN)
                         pair[0] = x;
                         pair[2] = lv;
                         const float n = fast_exp2(-lv);
                         reinterpret_cast<float*>(sh.inv[at & 3])[tid] = n == n ? n : 0.f;
+                        if (lv > kNear && lv < INFINITY) atomicMin(&sh.far, at);
                     }
                     // Chunks of 16 codes become two of 16 bytes of the tile, in half c / 4.  Four lanes of eight take a chunk's second eight codes first,
                     // the other four in rows of the other parity: so both the 8-byte loads and the 16-byte stores of a warp meet every
@@ -580,6 +586,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 else if (masked) ok = ok && wait(&sh.full[sv], (jv / S::kSlots) & 1);               // (what is known of V)
                 if (!ok) break;
                 if (busy) {
+                    const bool far = S::kWidens && step >= sh.far;      // (a later step's number may stand there already, and changes nothing)
                     tc_fence_after();
                     // Half of the tokens at a time, whose weights go where their scores were: both halves' scores would not fit the registers.
 #pragma unroll 1
@@ -664,8 +671,8 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                 mx[y] = fmaxf(mx[y], __shfl_xor_sync(0xffffffffu, mx[y], 2));
                                 const float mn = mx[y] > m[y] + kRoom ? ceilf(mx[y]) - kBelow<F> : m[y];          // (whole: what was rounded is scaled exactly)
                                 corr[y] = fast_exp2(m[y] - mn);
+                                l[y] = scale_sum(l[y], m[y] - mn);
                                 m[y] = mn;
-                                l[y] *= corr[y];
                             }
                             tmem_st_wait();        // (in the second half: the first one's weights, and the sums if it moved the references too)
                             if (mine_steps > 0) {
@@ -703,6 +710,18 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                                 if (!S::kWidens) tmem_st_16x128b_x8(s_addr + 32, lo);
                             }
                         }
+                        if (far) {                 // the sums by exponentials of their own (see kNear)
+                            const float* lvs = reinterpret_cast<const float*>(&sh.scale[step & 3][half * 32 + l4]) + 2;
+                            auto count = [&](const uint32_t (&x)[16], int first) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const float lv = lvs[4 * (first + 4 * (i >> 2)) + (i & 1)];
+                                    l[(i >> 1) & 1] += fast_exp2(__uint_as_float(x[i]) - m[(i >> 1) & 1] - (lv == lv ? lv : 0.f));
+                                }
+                            };
+                            count(x0, 0);
+                            count(x1, 16);
+                        }
                         uint32_t hi[16], lo[16];
                         const float2* invs = reinterpret_cast<const float2*>(sh.inv[step & 3]) + half * 32 + l4;
                         const uint64_t m2[2] = {pack_f32x2(-m[0], -m[0]), pack_f32x2(-m[1], -m[1])};
@@ -731,7 +750,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                         for (int y = 0; y < 2; ++y) {
                             float a, b;
                             unpack_f32x2(sum[y], a, b);
-                            l[y] += a + b;
+                            if (!far) l[y] += a + b;
                         }
                     }
                     if (!ok) break;
@@ -786,7 +805,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     const float M = fmaxf(m[y], other.x);
                     f[y][0] = fast_exp2(m[y] - M);
                     f[y][1] = fast_exp2(other.x - M);
-                    l[y] = l[y] * f[y][0] + other.y * f[y][1];
+                    l[y] = scale_sum(l[y], m[y] - M) + scale_sum(other.y, other.x - M);
                     m[y] = M;
                 }
                 ch0 = place * (D / 2);
@@ -803,7 +822,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                     const int line = line0 + hl + 8 * y;
                     there[y] = line < d.lines;
                     hq[y] = (size_t)(d.row0 + (line >> p.g_shift)) * p.Hq + (size_t)d.g * p.G + (line & (p.G - 1));
-                    inv[y] = l[y] == 0.f ? 0.f : __frcp_rn(l[y]);
+                    inv[y] = l[y] == 0.f ? 0.f : __frcp_rn(l[y]) * p.unit;
                     if (there[y] && ch0 == 0 && l4 == 0) {
                         if (!whole) __stcg(reinterpret_cast<float2*>(slot) + line, make_float2(m[y], l[y]));
                         else if (p.lse != nullptr) p.lse[hq[y]] = l[y] == 0.f ? -INFINITY : (m[y] + __log2f(l[y])) * 0.6931471805599453f;
@@ -866,7 +885,7 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
                 for (int k = 0; k < n; ++k) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(part(k)) + line).x);
                 for (int k = 0; k < n; ++k) {
                     const float2 ml = __ldcg(reinterpret_cast<const float2*>(part(k)) + line);
-                    L = fmaf(ml.y, fast_exp2(ml.x - M), L);
+                    L += scale_sum(ml.y, ml.x - M);
                 }
                 constexpr int kAtOnce = 8;         // runs of four channels
 #pragma unroll 1

@@ -26,7 +26,7 @@ struct DraftParams {
     const uint32_t* mask;          // [rows][mask_words] or null
     int mask_words, batch, rows, max_pages, Hq, Hkv, G, g_shift, rpt_shift;      // G = 2^g_shift; rows per tile: 2^rpt_shift
     long long num_pages;
-    float scale_log2;
+    float scale_log2, unit;        // unit: what the sums of weights times codes count (2^16 of an 8-bit cache)
     __nv_bfloat16* out;
     float* lse;
     float* parts;                  // [CTA][2][slot]: of an item's piece, [lines][2] reference of the weights (log2 units) and their sum, then
@@ -244,6 +244,20 @@ __device__ __forceinline__ void draft_plan(const DraftParams& p, const DraftList
 // finite where those of a softmax in 32 bits are.
 template <int F> constexpr float kBelow = F == AFLEX_CACHE_BF16 ? -8.f : 8.f;
 
+// Of an 8-bit cache x is the score plus lv = log2 of the token's V scale less 16 (at least -80: a scale of 0, or of a value of zeros), so that 2^(x - m) is
+// what its codes count and 2^(x - m - lv) what the token counts in the sum L of all weights: by its score alone, whatever its value's size.  The 16
+// leave L room below where V's scales are near 2^121 (terms of 2^-97) and above where they are the least (2^95); sums of codes are multiplied by 2^16 at the end.
+constexpr float kScaleShift = 16.f, kLeastScale = -64.f - kScaleShift;
+__device__ __forceinline__ float log2_scale(float scale) {
+    const float lv = __log2f(scale) - kScaleShift;
+    return lv < kLeastScale ? kLeastScale : lv;    // (NaN stays)
+}
+// l * 2^d where 2^d alone could be 0 and the product not: of pieces whose V's scales are far apart
+__device__ __forceinline__ float scale_sum(float l, float d) {
+    const float c = fmaxf(d, -100.f);
+    return l * fast_exp2(c) * fast_exp2(d - c);
+}
+
 // Sums of one run of four channels of a line over pieces.
 struct RunSum {
     float M, L;
@@ -251,12 +265,12 @@ struct RunSum {
 };
 __device__ __forceinline__ void add_piece(RunSum& s, float m, float l, const float4& v) {
     const float f = fast_exp2(m - s.M);            // (s.M: the largest m of all pieces)
-    s.L = fmaf(l, f, s.L);
+    s.L += scale_sum(l, m - s.M);
     s.acc.x = fmaf(v.x, f, s.acc.x); s.acc.y = fmaf(v.y, f, s.acc.y); s.acc.z = fmaf(v.z, f, s.acc.z); s.acc.w = fmaf(v.w, f, s.acc.w);
 }
 template <int D>
 __device__ __forceinline__ void store_run(const DraftParams& p, const DraftPiece& u, int line, int c, const RunSum& s) {
-    const float inv = s.L == 0.f ? 0.f : __frcp_rn(s.L);       // a line with nothing to attend to: zeros
+    const float inv = s.L == 0.f ? 0.f : __frcp_rn(s.L) * p.unit;      // a line with nothing to attend to: zeros
     const size_t hq = (size_t)(u.row0 + (line >> p.g_shift)) * p.Hq + (size_t)u.g * p.G + (line & (p.G - 1));
     reinterpret_cast<uint2*>(p.out + hq * D)[c] = make_uint2(pack_bf16x2(s.acc.x * inv, s.acc.y * inv), pack_bf16x2(s.acc.z * inv, s.acc.w * inv));
     if (p.lse != nullptr && c == 0) p.lse[hq] = s.L == 0.f ? -INFINITY : (s.M + __log2f(s.L)) * 0.6931471805599453f;

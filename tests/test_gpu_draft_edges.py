@@ -152,3 +152,29 @@ LARGE = {"one": [333], "early": range(0, 60), "late": range(600, 700), "mixed": 
 def test_very_large_values_of_a_bf16_cache(ctx, Hq, Hkv, D, m, where):  # noqa: F811
     """Sums of weights times values up to 2^122 stay finite."""
     check_values(ctx, "bf16", Hq, Hkv, D, m, LARGE[where], 2.0 ** 120)
+
+
+@pytest.mark.parametrize("big", [2.0 ** 60, 2.0 ** 120])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,D,m", LINES)
+@pytest.mark.parametrize("where", list(LARGE))
+def test_values_of_zero_beside_very_large_ones(ctx, fmt, Hq, Hkv, D, m, where, big):  # noqa: F811
+    """The sum of the weights counts every token by its score alone, whatever its value's size: in the same pages, before and behind one another, in
+    pieces of several CTAs."""
+    check_values(ctx, fmt, Hq, Hkv, D, m, LARGE[where], big)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,D,m", LINES)
+def test_values_that_are_all_zero(ctx, fmt, Hq, Hkv, D, m):  # noqa: F811
+    n = 700
+    c = Cache([n], Hkv, D, fmt, seed=30)
+    for g in range(Hkv):
+        for t in range(n):
+            put_token(c, 0, t, g, v=torch.zeros(D, dtype=torch.bfloat16))
+    c.put()
+    q = (2.0 * torch.randn(m, Hq, D, generator=torch.Generator().manual_seed(3))).to(torch.bfloat16).to(DEV)
+    offs = offsets_of([m])
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
+    assert (out == 0).all()
+    check_attention(out, lse, q, c, offs, None, m, WEIGHT[fmt])
