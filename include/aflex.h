@@ -629,8 +629,8 @@ AFLEX_API aflex_status aflex_cache_convert(aflex_ctx* ctx, const aflex_attn_desc
  * Attention of every row over the tokens that it sees:
  *     s_j = sm_scale * <q, K_j>,  out = sum_j softmax(s)_j V_j -> bf16,  lse = ln sum_j exp(s_j)
  * q, out bf16 [rows][Hq][D]; lse fp32 [rows][Hq] or NULL.  The cache's codes enter the products exactly; of an 8-bit cache a row's
- * queries are scaled by a power of two (entries below 2^-31 of the head's largest lose precision;
- * with int8 those of 2^116 and more count as infinite).  fp32 scores and sums; the weights of
+ * queries are scaled by a power of two (entries below 2^-31 of the head's largest lose precision; K's scale is multiplied in last, so
+ * that entries of 2^112 and more can make a score infinite).  fp32 scores and sums; the weights of
  * V enter the second product as the sum of two bf16 values (bf16 cache), or (8 bits) in fp16 with the token's scale multiplied in, each off
  * by at most half a step of fp16 or 2^-33 of the row's largest.
  * A row that sees no token, or whose sequence raises AFLEX_ERR_BOUNDS, gets out 0 and lse -infinity.  A score of -infinity weighs

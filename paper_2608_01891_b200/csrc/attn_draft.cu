@@ -9,7 +9,7 @@
 //   arithmetic  mma.sync m16n8k16 with the 16 tokens of a page, or 16 channels, as rows and 8 lines as columns, so that single tokens of
 //               groups of 8 waste nothing: S^T = K Q^T, O^T += V^T P^T, P^T from S^T by movmatrix; operands made in registers from 16-byte
 //               reads (the order of channels inside a product is free).  Codes of 8 bits become fp16 exactly: int8 + 128 under the exponent
-//               of 1024, less 1152, or (K) as subnormal numbers; e4m3 by the hardware's conversion.  Queries are bf16, or fp16 after a power of two
+//               of 1024, less 1152; e4m3 by the hardware's conversion.  Queries are bf16, or fp16 after a power of two
 //               that brings the line's largest entry to [2^14, 2^15).
 //   softmax     online, fp32, base 2, each warp with its own running state.  Of an 8-bit cache the weight of a code is p_j * scale_j, so
 //               the running reference follows s_j + log2 scale_j, the weights enter the product in fp16 below 2^15, and their sum is
@@ -74,18 +74,6 @@ template <int kRow> __device__ __forceinline__ uint32_t chunk_at(int t, int ch) 
     return (uint32_t)(t * 64 + ((ch ^ ((t >> 1) & 3)) << 4));
 }
 
-// Four codes of K as two pairs of fp16: of int8 (code + 128) * 2^-24, the subnormal numbers whose bits are the byte's -- what they add, 128
-// times the sum of the line's queries, is taken off the product.
-template <int F> __device__ __forceinline__ void widen4_k(uint32_t w, uint32_t& lo, uint32_t& hi) {
-    if (F == AFLEX_CACHE_INT8) {
-        w ^= 0x80808080u;
-        lo = __byte_perm(w, 0u, 0x4140);
-        hi = __byte_perm(w, 0u, 0x4342);
-    } else {
-        widen4<F>(w, lo, hi);
-    }
-}
-
 // D(16x8, fp32) += A(16x16) * B(16x8).  (Not volatile, like the loads around it: what a page's products wait for may be done in any order.)
 template <int F>
 __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -101,7 +89,7 @@ template <int D, int NT> struct LineState {        // of a warp: a lane's lines 
     float o[D / 16][NT][4];                        // channels of n-tiles' pairs (channel_of 2 j, 2 j + 1) x the two lines
     float m[NT][2], l[NT][2];
     uint32_t q[D / 16][NT][2];                     // operand: line 8 nt + lane / 4
-    float c[NT][2], off[NT][2];                    // what a product counts, in log2 units, and what comes on top (int8)
+    float c[NT][2];                                // what a product counts, in log2 units
     __device__ __forceinline__ void reset() {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -125,7 +113,7 @@ __device__ __forceinline__ void load_queries(LineState<D, NT>& st, const DraftPa
         const int line = hl + 8 * n;
         const bool there = line < u.lines;
         const uint4* src = reinterpret_cast<const uint4*>(p.q + ((size_t)(u.row0 + (there ? line >> p.g_shift : 0)) * p.Hq + (size_t)u.g * p.G + (there ? line & (p.G - 1) : 0)) * D);
-        float c = p.scale_log2, off = 0.f;
+        float c = p.scale_log2;
         if (F == AFLEX_CACHE_BF16) {
 #pragma unroll
             for (int k = 0; k < kRow / 64; ++k) {
@@ -153,26 +141,15 @@ __device__ __forceinline__ void load_queries(LineState<D, NT>& st, const DraftPa
             const int e = max((int)(big >> 7) - 127, -112);
             const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
             c = big >= 0x7f80u ? __uint_as_float(0x7fc00000u) : p.scale_log2 * __uint_as_float((uint32_t)(127 - 14 + e) << 23);
-            float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
                 const __half2 h = __floats2half2_rn(__uint_as_float(v[i] << 16) * up, __uint_as_float(v[i] & 0xffff0000u) * up);
                 st.q[i / 2][n][i & 1] = *reinterpret_cast<const uint32_t*>(&h);
-                sum += __low2float(h) + __high2float(h);
-            }
-            if (F == AFLEX_CACHE_INT8) {           // see widen4_k
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                off = -128.f * sum * c;
-                c *= 16777216.f;
             }
         }
         // from the lanes that loaded a line to those that hold its scores
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            st.c[n][e] = __shfl_sync(0xffffffffu, c, l4 * 8 + 4 * e);
-            st.off[n][e] = __shfl_sync(0xffffffffu, off, l4 * 8 + 4 * e);
-        }
+        for (int e = 0; e < 2; ++e) st.c[n][e] = __shfl_sync(0xffffffffu, c, l4 * 8 + 4 * e);
     }
 }
 
@@ -210,8 +187,8 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
 #pragma unroll
                 for (int g = 0; g < N; ++g) {
                     uint32_t a[4];
-                    widen4_k<F>(reinterpret_cast<const uint32_t*>(&x[g])[k], a[0], a[2]);
-                    widen4_k<F>(reinterpret_cast<const uint32_t*>(&y[g])[k], a[1], a[3]);
+                    widen4<F>(reinterpret_cast<const uint32_t*>(&x[g])[k], a[0], a[2]);
+                    widen4<F>(reinterpret_cast<const uint32_t*>(&y[g])[k], a[1], a[3]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) mma_16816<F>(s[g][n], a, st.q[4 * c + k][n][0], st.q[4 * c + k][n][1]);
                 }
@@ -233,7 +210,7 @@ __device__ __forceinline__ void attend_pages(LineState<D, NT>& st, const DraftPa
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     float& v = x[g][n][r][e];
-                    v = F == AFLEX_CACHE_INT8 ? fmaf(s[g][n][2 * r + e], st.c[n][e], st.off[n][e]) : s[g][n][2 * r + e] * st.c[n][e];
+                    v = s[g][n][2 * r + e] * st.c[n][e];
                     if (F != AFLEX_CACHE_BF16) v = fmaf(v, ks, lv[g][r]);
                 }
         }

@@ -1,5 +1,5 @@
 """Attention of drafted tokens and the operators around it where one value decides: references that move twice in a step of the tensor-core kernel,
-codes that are no numbers, values of any size."""
+codes that are no numbers, values of any size, a channel of large keys."""
 import numpy as np
 import pytest
 import torch
@@ -178,3 +178,26 @@ def test_values_that_are_all_zero(ctx, fmt, Hq, Hkv, D, m):  # noqa: F811
     out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
     assert (out == 0).all()
     check_attention(out, lse, q, c, offs, None, m, WEIGHT[fmt])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,D,m", [(8, 2, 64, 1), (8, 1, 128, 1), (8, 1, 128, 2), (8, 1, 128, 8), (8, 1, 64, 40)])
+def test_scores_beside_a_channel_of_large_keys(ctx, fmt, Hq, Hkv, D, m):  # noqa: F811
+    """One key channel is 127 times the others, whose codes are then of one bit, and the queries' sum is far from zero.  A score is a sum of products
+    that 32 bits hold exactly, so lse is off by roundings of a handful of numbers below 64 (in units of log2) only: 2^-18 each at most."""
+    n, gen = 60, torch.Generator().manual_seed(41)
+    c = Cache([n], Hkv, D, fmt, seed=40)
+    for g in range(Hkv):
+        k = torch.randint(0, 2, (n, D), generator=gen).float() * 2 - 1
+        k[:, 5] = 127
+        for t in range(n):
+            put_token(c, 0, t, g, k=k[t].to(torch.bfloat16))
+    c.put()
+    q = 0.125 + 1.875 * torch.rand(m, Hq, D, generator=gen)                # (8 bits each, steps of 2^-10 and more)
+    q[:, :, 5] = 0
+    q = q.to(torch.bfloat16).to(DEV)
+    offs = offsets_of([m])
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
+    k, v = (np.nan_to_num(x) for x in c.stands_for())
+    _, want, *_ = DO.attend(f64(q), k, v, c.table, c.lens, offs, None)
+    assert np.abs(f64(lse) - want).max() <= 4 * 2.0 ** -18
