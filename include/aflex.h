@@ -648,7 +648,8 @@ AFLEX_API size_t aflex_attn_draft_workspace_bytes(const aflex_attn_desc* desc);
  * `caches` (HOST array [num_caches], of one format: the layers' caches).  base i32 [batch]: tokens before the drafted ones; path i32
  * [batch][path_stride], ascending; path_len i32 [batch], 0 allowed (all DEVICE).  K, V and their scales are moved as they are.  The
  * sequence's new length is base[b] + path_len[b]; what lies behind is left.  A path that does not ascend, or leaves the seq_lens[b]
- * tokens that the caches hold, raises AFLEX_ERR_BOUNDS and moves nothing of that sequence.  No page may belong to two of the sequences
+ * tokens that the caches hold, raises AFLEX_ERR_BOUNDS and moves nothing of that sequence; one with a bad page id moves nothing of it in
+ * that cache.  No page may belong to two of the sequences
  * unless it is full of earlier tokens.
  */
 AFLEX_API aflex_status aflex_cache_accept(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_cache* caches, int num_caches,

@@ -446,7 +446,8 @@ template <int N> struct AcceptParams {             // of up to N caches: a launc
 // A warp moves one (sequence, KV head, K or V) of one cache, 16-byte words of four to sixteen tokens at a time.  The path ascends,
 // so a token never moves up: a source that is still to be read lies behind every place that has been written, and within a step all
 // reads come before the writes.  Bound: the chain of dependent loads (path -> page ids -> tokens); a tree's path is a few KB per head.  64 int8
-// caches of 32 sequences take 12.9 us (2.7 TB/s); with 4, 6 or 8 CTAs per SM 13.5, 13.8 and 14.0 (the last two spill).
+// caches of 32 sequences, 64 of whose 128 path tokens move (17.4 MB read and written), take 13.8 us (1.3 TB/s).  Without the look at every page before
+// the first move it was 12.9, and with 4, 6 or 8 CTAs per SM 13.5, 13.8 and 14.0 (the last two spill).
 template <int N> __global__ void __launch_bounds__(kThreads, 5) cache_accept_kernel(const __grid_constant__ AcceptParams<N> p) {
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -457,20 +458,6 @@ template <int N> __global__ void __launch_bounds__(kThreads, 5) cache_accept_ker
     const int n = fetch(p.count + b), base = fetch(p.base + b), len = fetch(c.lens + b);
     auto from_path = [&](int k) -> int { return k < p.stride ? fetch(path + k) : 0; };
     const int first = from_path(lane);             // (whatever the length: no second trip to memory for most paths)
-    // the whole path is looked at before anything moves: it has to ascend inside the sequence
-    bool bad = n < 0 || n > p.stride || base < 0 || len < 0 || len > c.max_pages * kPageTokens;
-    int before = -1;
-    for (int k0 = 0; k0 < n && !bad; k0 += 32) {
-        const int s = k0 == 0 ? first : from_path(k0 + lane);
-        int last = __shfl_up_sync(0xffffffffu, s, 1);
-        if (lane == 0) last = before;
-        before = __shfl_sync(0xffffffffu, s, 31);
-        bad = __any_sync(0xffffffffu, k0 + lane < n && (s <= last || (long long)base + s >= len));
-    }
-    if (bad) {
-        if (lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
-        return;
-    }
     const int g = head % p.Hkv;
     uint8_t* data = head < p.Hkv ? c.k : c.v;
     float* scales = head < p.Hkv ? c.ks : c.vs;
@@ -480,14 +467,33 @@ template <int N> __global__ void __launch_bounds__(kThreads, 5) cache_accept_ker
         const int page = fetch(table + t / kPageTokens);
         return page >= 0 && page < c.num_pages ? (page * p.Hkv + g) * kPageTokens + t % kPageTokens : -1;
     };
+    // the whole path is looked at before anything moves: it has to ascend inside the sequence, and every page of a move has to be one
+    bool bad = n < 0 || n > p.stride || base < 0 || len < 0 || len > c.max_pages * kPageTokens;
+    int before = -1, first_from = -1, first_to = -1;       // (places of the first 32 moves, which most paths do not exceed)
+    for (int k0 = 0; k0 < n && !bad; k0 += 32) {
+        const int k = k0 + lane, s = k0 == 0 ? first : from_path(k);
+        int last = __shfl_up_sync(0xffffffffu, s, 1);
+        if (lane == 0) last = before;
+        before = __shfl_sync(0xffffffffu, s, 31);
+        bad = __any_sync(0xffffffffu, k < n && (s <= last || (long long)base + s >= len));
+        if (bad) break;
+        int from = -1, to = -1;
+        if (k < n && s != k) { from = place(base + s); to = place(base + k); }
+        bad = __any_sync(0xffffffffu, k < n && s != k && (from < 0 || to < 0));
+        if (k0 == 0) { first_from = from; first_to = to; }
+    }
+    if (bad) {
+        if (lane == 0) atomicExch(p.status, AFLEX_ERR_BOUNDS);
+        return;
+    }
     for (int k0 = 0; k0 < n; k0 += 32) {
         // lane i knows the k0 + i-th move
-        int from = -1, to = -1;
-        const int k = k0 + lane, s = k0 == 0 ? first : from_path(k);
-        if (k < n && s != k) {
-            from = place(base + s);
-            to = place(base + k);
-            if (from < 0 || to < 0) { atomicExch(p.status, AFLEX_ERR_BOUNDS); from = to = -1; }
+        int from = first_from, to = first_to;
+        if (k0 > 0) {
+            const int k = k0 + lane, s = from_path(k);
+            const bool moves = k < n && s != k;
+            from = moves ? place(base + s) : -1;
+            to = moves ? place(base + k) : -1;
         }
         const uint32_t moves = __ballot_sync(0xffffffffu, from >= 0);
         if (moves == 0) continue;

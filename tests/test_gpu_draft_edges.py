@@ -1,5 +1,5 @@
 """Attention of drafted tokens and the operators around it where one value decides: references that move twice in a step of the tensor-core kernel,
-codes that are no numbers, values of any size, a channel of large keys."""
+codes that are no numbers, values of any size, a channel of large keys, paths with bad pages."""
 import numpy as np
 import pytest
 import torch
@@ -201,3 +201,37 @@ def test_scores_beside_a_channel_of_large_keys(ctx, fmt, Hq, Hkv, D, m):  # noqa
     k, v = (np.nan_to_num(x) for x in c.stands_for())
     _, want, *_ = DO.attend(f64(q), k, v, c.table, c.lens, offs, None)
     assert np.abs(f64(lse) - want).max() <= 4 * 2.0 ** -18
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("Hkv,D", [(2, 64), (8, 128)])
+def test_a_path_with_a_bad_page_moves_nothing(ctx, fmt, Hkv, D):  # noqa: F811
+    """A path is moved whole or not at all: a page id that is none, of its first tokens or of its last, as source or as destination, leaves the
+    sequence as it is in that cache; the other sequences and caches are compacted."""
+    lens = [90, 90, 120, 120, 60]
+    base = np.array([10, 10, 8, 8, 3], dtype=np.int32)
+    paths = [[1, 20, 60], [1, 20, 60], list(range(5, 105)), list(range(5, 105)), [0, 2, 40]]
+    spoilt = {0: 1, 1: 4, 2: 6, 3: 0}                                      # sequence: page of its table (of a source, a source, a source, a destination)
+    path = np.zeros((len(lens), 100), dtype=np.int32)
+    for b, p in enumerate(paths):
+        path[b, :len(p)] = p
+    dev = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    n = torch.tensor([len(p) for p in paths], dtype=torch.int32, device=DEV)
+    cs = [Cache(lens, Hkv, D, fmt, seed=s, poison=False) for s in (1, 2)]
+    for b, page in spoilt.items():
+        cs[0].td[b, page] = -1 if b % 2 else cs[0].total
+    ctx.cache_accept(AF.attn_desc(Hkv, Hkv, D), [c.cache for c in cs], len(lens), dev(base), dev(path), n)
+    assert ctx.device_status() == AF.ERR_BOUNDS
+    for c in cs:
+        for t, got in zip(c.tensors, c.dev):
+            if t is None:
+                continue
+            raw = lambda x: x.view(torch.int32 if x.dim() == 3 else torch.uint8)  # noqa: E731
+            want = t.clone()
+            for b, p in enumerate(paths):
+                for k, s in enumerate(p):
+                    if c is cs[0] and b in spoilt:
+                        continue
+                    f, to = int(base[b]) + s, int(base[b]) + k
+                    raw(want)[int(c.table[b, to // 16]), :, to % 16] = raw(t)[int(c.table[b, f // 16]), :, f % 16]
+            assert torch.equal(raw(want), raw(got.cpu()))
