@@ -97,7 +97,7 @@ bool encode_tmap_rows_u8(CUtensorMap* out, const void* base, uint64_t rows, uint
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 static aflex_status validate_attn(aflex_ctx* ctx, const aflex_attn_desc* d, const void* q, const aflex_kv* kv, int batch,
-                                  const void* out) {
+                                  const void* out, int least_len = 1) {
     if (!ctx) return AFLEX_ERR_INVALID_ARG;
     if (!d || !q || !kv || !out) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "attention: null argument");
     if (!kv->k_cache || !kv->v_cache || !kv->page_table || !kv->seq_lens)
@@ -120,9 +120,9 @@ static aflex_status validate_attn(aflex_ctx* ctx, const aflex_attn_desc* d, cons
     if (kv->seq_lens_host) {
         const long long max_len = (long long)kv->max_pages_per_seq * 16;
         for (int b = 0; b < batch; ++b)
-            if (kv->seq_lens_host[b] < 1 || kv->seq_lens_host[b] > max_len)
-                return set_error(ctx, AFLEX_ERR_INVALID_ARG, "attention: seq_lens_host[%d] = %d outside [1, %lld]", b,
-                                 kv->seq_lens_host[b], max_len);
+            if (kv->seq_lens_host[b] < least_len || kv->seq_lens_host[b] > max_len)
+                return set_error(ctx, AFLEX_ERR_INVALID_ARG, "attention: seq_lens_host[%d] = %d outside [%d, %lld]", b,
+                                 kv->seq_lens_host[b], least_len, max_len);
     }
     return AFLEX_OK;
 }
@@ -913,10 +913,10 @@ aflex_status aflex_attn_decode_pages(aflex_ctx* ctx, const aflex_attn_desc* desc
 // ---- caches of 16 or 8 bits, and drafted tokens ------------------------------------------------
 namespace {
 aflex_status validate_cache(aflex_ctx* ctx, const char* what, const aflex_attn_desc* desc, const aflex_cache* cache, int batch,
-                            const void* in, const void* out) {
+                            const void* in, const void* out, int least_len = 1) {
     if (!ctx) return AFLEX_ERR_INVALID_ARG;
     if (!cache) return set_error(ctx, AFLEX_ERR_INVALID_ARG, "%s: null cache", what);
-    aflex_status s = validate_attn(ctx, desc, in, &cache->kv, batch, out);
+    aflex_status s = validate_attn(ctx, desc, in, &cache->kv, batch, out, least_len);
     if (s == AFLEX_OK) s = validate_pages(ctx, what, &cache->kv);
     if (s != AFLEX_OK) return s;
     if (cache->format != AFLEX_CACHE_BF16 && cache->format != AFLEX_CACHE_INT8 && cache->format != AFLEX_CACHE_E4M3)
@@ -954,7 +954,7 @@ aflex_status aflex_cache_append(aflex_ctx* ctx, const aflex_attn_desc* desc, con
 aflex_status aflex_cache_convert(aflex_ctx* ctx, const aflex_attn_desc* desc, const aflex_cache* src, const aflex_cache* dst, int batch,
                                  const int32_t* first_token, void* stream) {
     aflex_status s = ctx && (!src || !dst) ? set_error(ctx, AFLEX_ERR_INVALID_ARG, "cache convert: null cache") : AFLEX_OK;
-    if (s == AFLEX_OK) s = validate_cache(ctx, "cache convert", desc, src, batch, src ? src->kv.k_cache : nullptr, src ? src->kv.v_cache : nullptr);
+    if (s == AFLEX_OK) s = validate_cache(ctx, "cache convert", desc, src, batch, src ? src->kv.k_cache : nullptr, src ? src->kv.v_cache : nullptr, 0);
     if (s != AFLEX_OK) return s;
     aflex_cache to = *dst;                                    // (seq_lens of dst is not read, and may be null)
     to.kv.seq_lens = src->kv.seq_lens;
