@@ -783,7 +783,10 @@ class Context:
     # ---- caches of 16 or 8 bits, and drafted tokens.  draft: None for one row per sequence, else draft_rows(...) (see the header).
     def _draft_args(self, desc: AttnDesc, cache: Cache, rows: int, draft: Optional[Draft], what: str):
         """(batch, draft, tensors to find on the context's device), once they fit the cache and one another."""
-        kept = draft.__dict__.get("_keep", (None, None, None)) if draft is not None else (None, None, None)
+        kept = draft.__dict__.get("_keep") if draft is not None else (None, None, None)
+        if kept is None:
+            assert not draft.q_offsets, "the number of sequences is not known: drafted rows of several are made by draft_rows"
+            kept = (None, None, None)
         batch = rows if kept[0] is None else kept[0].shape[0] - 1
         assert kept[1] is None or kept[1].numel() >= rows, "fewer positions than rows"
         assert kept[2] is None or kept[2].shape[0] >= rows, "a mask of fewer rows than " + what
