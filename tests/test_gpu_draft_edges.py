@@ -1,5 +1,6 @@
 """Attention of drafted tokens and the operators around it where one value decides: references that move twice in a step of the tensor-core kernel,
-codes that are no numbers, values of any size, a channel of large keys, paths with bad pages."""
+codes that are no numbers, values of any size, a channel of large keys, paths with bad pages, scores of any size,
+masks of other widths."""
 import numpy as np
 import pytest
 import torch
@@ -235,3 +236,93 @@ def test_a_path_with_a_bad_page_moves_nothing(ctx, fmt, Hkv, D):  # noqa: F811
                     f, to = int(base[b]) + s, int(base[b]) + k
                     raw(want)[int(c.table[b, to // 16]), :, to % 16] = raw(t)[int(c.table[b, f // 16]), :, f % 16]
             assert torch.equal(raw(want), raw(got.cpu()))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("scale", [0.37, 1e-4, -0.2])
+@pytest.mark.parametrize("Hq,Hkv,D,m", [(8, 1, 128, 1), (8, 1, 64, 2), (8, 1, 128, 8), (8, 1, 64, 40)])
+def test_scores_are_scaled_as_the_descriptor_says(ctx, fmt, Hq, Hkv, D, m, scale):  # noqa: F811
+    c = Cache([300], Hkv, D, fmt, seed=50)
+    q = torch.randn(m, Hq, D, generator=torch.Generator().manual_seed(51)).to(torch.bfloat16).to(DEV)
+    offs = offsets_of([m])
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)), scale)
+    # (check_attention knows the usual scale: as if the queries were longer or shorter)
+    by = float(np.float32(scale)) * D ** 0.5
+    check_attention(out, lse, q.double().cpu() * by, c, offs, None, m, WEIGHT[fmt])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,D,m", [(8, 1, 128, 1), (8, 1, 64, 2), (8, 1, 128, 8), (8, 1, 64, 40)])
+def test_infinite_scores_of_finite_queries(ctx, fmt, Hq, Hkv, D, m):  # noqa: F811
+    """A score of -infinity weighs nothing, one of +infinity makes its head NaN, and neither touches the other heads."""
+    n, far = 300, 7
+    c = Cache([n], Hkv, D, fmt, seed=60)
+    for t in range(n):
+        k = torch.randn(D, generator=torch.Generator().manual_seed(t))
+        k[3], k[4] = 0, 0
+        put_token(c, 0, t, 0, k=k.to(torch.bfloat16))
+    k = torch.zeros(D)
+    k[3] = 2.0 ** 100
+    put_token(c, 0, far, 0, k=k.to(torch.bfloat16))
+    c.put()
+    q = torch.randn(m, Hq, D, generator=torch.Generator().manual_seed(61))
+    q[:, :, 3], q[:, 1], q[:, 2] = 0, 0, 0
+    q[:, 1, 3], q[:, 2, 3] = -2.0 ** 100, 2.0 ** 100
+    q[:, 1, 4] = 2.0 ** 100                                                # (where all keys are 0)
+    q = q.to(torch.bfloat16).to(DEV)
+    offs = offsets_of([m])
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
+    assert torch.isnan(out[:, 2]).any(1).all() and torch.isnan(lse[:, 2]).all()
+    assert torch.isfinite(out[:, [0, 1, 3, 4, 5, 6, 7]]).all()
+    # head 1: all other tokens have the score 0, and the far one is not there
+    v = np.nan_to_num(c.stands_for()[1])
+    flat = v[c.table[0], 0].reshape(-1, D)[:n]
+    for i in range(m):
+        see = [t for t in range(n - m + i + 1) if t != far]
+        want, spread = flat[see].mean(0), np.abs(flat[see]).mean(0)
+        err = np.abs(f64(out)[i, 1] - want)
+        assert (err <= 2.0 ** -8 * np.abs(want) + 2 * (WEIGHT[fmt] + n * 2.0 ** -24 + 2.0 ** -19) * spread + 2.0 ** -32 * np.abs(flat).max()).all()
+        assert abs(float(lse[i, 1]) - np.log(len(see))) <= 2.0 ** -17
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_masks_of_single_rows(ctx, fmt):  # noqa: F811
+    """One row per sequence, with a mask: a row may be told not to see its own token."""
+    Hq, Hkv, D, lens = 8, 2, 64, [1, 1, 40, 40, 130, 129]
+    c = Cache(lens, Hkv, D, fmt, seed=70)
+    q = torch.randn(len(lens), Hq, D, generator=torch.Generator().manual_seed(71)).to(torch.bfloat16).to(DEV)
+    ints = [1, 0, 1, 0, 6, 7]                                              # (bits of tokens that there are not change nothing)
+    out, lse = attend(ctx, c, q, AF.draft_rows(None, None, torch.tensor(ints, dtype=torch.int32, device=DEV).view(-1, 1)))
+    check_attention(out, lse, q, c, None, ints, len(lens), WEIGHT[fmt])
+    assert (out[1] == 0).all() and torch.isneginf(lse[1]).all()
+
+
+@pytest.mark.parametrize("words", [1, 2, 5])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("Hq,Hkv,D,lens,new", [(2, 2, 64, [300, 64, 90, 70], [8, 64, 3, 70]), (8, 1, 128, [300, 64, 90], [80, 64, 3])])
+def test_masks_of_more_or_fewer_words_than_rows(ctx, fmt, Hq, Hkv, D, lens, new, words):  # noqa: F811
+    """Drafted tokens behind the last word are not seen; words behind the last token are not looked at."""
+    offs = offsets_of(new)
+    T = int(offs[-1])
+    rng = np.random.default_rng(72)
+    a = rng.integers(0, 1 << 32, (T, words), dtype=np.uint64).astype(np.uint32)
+    ints = [sum(int(x) << 32 * w for w, x in enumerate(row)) for row in a]
+    c = Cache(lens, Hkv, D, fmt, seed=73)
+    q = torch.randn(T, Hq, D, generator=torch.Generator().manual_seed(74)).to(torch.bfloat16).to(DEV)
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV), None, torch.from_numpy(a.view(np.int32)).to(DEV)))
+    check_attention(out, lse, q, c, offs, ints, T, WEIGHT[fmt])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("others", [3, 40])
+def test_a_chunk_among_single_tokens(ctx, fmt, others):  # noqa: F811
+    """The form of the tiles is chosen for all sequences: single tokens on the tensor-core kernel, and a prompt chunk in tiles of 16 lines."""
+    Hq, Hkv, D = 8, 2, 64
+    new = [1] * others + [150] + [1] * 2
+    lens = [1 + 37 * i % 300 for i in range(others)] + [400, 16, 129]
+    offs = offsets_of(new)
+    T = int(offs[-1])
+    c = Cache(lens, Hkv, D, fmt, seed=75)
+    q = torch.randn(T, Hq, D, generator=torch.Generator().manual_seed(76)).to(torch.bfloat16).to(DEV)
+    out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
+    check_attention(out, lse, q, c, offs, None, T, WEIGHT[fmt])
