@@ -18,8 +18,12 @@
 //   masks       only pages that hold drafted tokens look at one
 //
 // Bound: the read of the cache; for few or short sequences the chain plan -> page ids -> pages -> join, some 12 us of a single long context's.
-// 256 rows (32 / 8 heads of 128) over up to 8192 int8 tokens 402 us (5.9 TB/s; one page of a warp at a time instead of two: 541), one row over
-// 131072 55 us (5.0 TB/s), 13 chains of 5 (16 / 4 heads of 64) over up to 6000 bf16 tokens 20 us.
+// 256 rows (32 / 8 heads of 128) over up to 8192 int8 tokens 402 us (5.9 TB/s) repeated over one cache, 459 over another one at every call; one row
+// over 131072 55 us (5.0 TB/s), 13 chains of up to 5 (16 / 4 heads of 64) over up to 6000 bf16 tokens 21 us.
+//
+// Weights of an 8-bit cache are rounded to fp16 once: off by at most 2^-11 of each, an eighth of what the output's rounding to bf16 may be off, and at
+// random over the tokens; outputs are as far from the definition in 64 bits as those of weights in 32 bits.  A second fp16 part took 2 % more for
+// single tokens, 4 - 10 % for 9 - 32 lines and 10 - 35 % in attn_draft_wide.cu.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -37,7 +41,8 @@ constexpr int kMaxLines = 16;                      // of a tile
 constexpr int kStages = 3;
 
 // F: the cache's format; NT: eights of lines.  Four compute warps, each with one page (bf16) or two (8 bits) of a unit, which are the place of its
-// state at the end.  Two pages are worked on together where 8 lines leave the registers for it: a page alone is a chain of dependent steps.
+// state at the end.  Two pages are worked on together where 8 lines leave the registers for it: one row over 131072 tokens 55.1 us against 55.8 with
+// one at a time; no gain for many rows (256 rows of up to 8192 403 against 400).  Tiles of 16 lines of heads of 128 spill 112 - 120 bytes a thread.
 template <int D, int F, int NT> struct DraftForm {
     static constexpr int kLines = 8 * NT;
     static constexpr int kBytes = F == AFLEX_CACHE_BF16 ? 2 : 1;      // of an element
@@ -733,9 +738,12 @@ aflex_status attn_draft_launch(aflex_ctx* ctx, const aflex_attn_desc* d, const v
     p.Hq = d->num_q_heads; p.Hkv = d->num_kv_heads; p.G = p.Hq / p.Hkv; p.num_pages = kv->num_pages;
     p.g_shift = p.G == 1 ? 0 : p.G == 2 ? 1 : p.G == 4 ? 2 : 3;
     // Lines per tile by the lines of an average sequence: 8, 16, or 256 on the tensor cores, whose step costs the same for any number of lines up to
-    // 128 while tiles of 16 read the cache again.  Measured (us, tiles of 16 / tensor cores), heads of 128: 32 lines 72 / 84 in int8, 66 / 81 in
-    // e4m3, 88 / 83 in bf16, 441 / 478 in a larger batch, 40 lines 86 / 84, 101 / 83 (bf16), 600 / 486; heads of 64: 40 lines 29 / 32 (bf16),
-    // 48 lines 30 / 31 (bf16), 28 / 33 (int8), 107 / 94 and 91 / 97 in a larger batch, 52 lines 34 / 31.
+    // 128 while tiles of 16 read the cache again.  Measured (us, tiles of 16 / tensor cores) with ragged sequences, by their average:
+    //   heads of 128, 8 sequences   25 lines 73 / 83 in int8, 68 / 80 in e4m3, 88 / 83 in bf16;   33 lines 88 / 83, 81 / 81, 101 / 83
+    //   64 sequences, int8          24 lines 449 / 473;   32 lines 620 / 475
+    //   heads of 64, 13 sequences   31 lines 27 / 33 in int8, 29 / 32 in bf16;   37 lines 30 / 33, 31 / 32;   41 lines 35 / 32 in bf16
+    //   64 sequences                36 lines 95 / 96 in int8, 109 / 94 in bf16
+    // One rule for all formats and batches, which costs up to 30 % beside its border; and a batch of single tokens and a long chunk has one form.
     const long long lines = (long long)rows << p.g_shift;
     const int narrow = D == 64 ? 48 : 32;
     p.rpt_shift = (lines <= 8LL * batch ? 3 : lines <= (long long)narrow * batch ? 4 : 8) - p.g_shift;

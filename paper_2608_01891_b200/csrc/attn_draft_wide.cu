@@ -10,14 +10,15 @@
 //               and the warp group only looks at the V of drafted tokens.  K is a K-major operand, V (as stored) an MN-major one
 //   softmax     eight warps per place, sixteen lines each, read from TMEM as fragments (two lines x 32 tokens per thread), so that a token's
 //               scales, which every line needs, are loaded once for two lines and by four lanes at a time (with a line per thread the loads of scales alone
-//               took longer than the products); 64 tokens at a time, since all 128 did not fit the registers (329 against 267 us); statistics,
+//               took longer than the products); 64 tokens at a time, since all 128 did not fit the registers (329 against 267 us when it was made so); statistics,
 //               references and weights as in attn_draft.cu.  The weights of an 8-bit cache are stored back over the scores they came from, in
 //               fp16; those of a bf16 cache as two bf16 parts, which fill the place of the scores, and the second product is issued for each part
 //
 // Bound: neither the products (1024 cycles per 128 lines x 128 tokens, 1536 with two parts of weights) nor the exponentials (16 per cycle: 1024)
-// but the chain from a place's scores to its weights and back, some 3400 cycles per 128 x 128 with two places under way, of which TMEM has
-// no room for a third.  8 trees of up to 61 tokens, 64 / 8 heads of 128, over up to 16384 tokens (120 GFLOP): 251 us in int8 (0.48
-// PFLOP/s), 227 in e4m3, 248 in bf16; of 5 tokens each 82 us (2.0 TB/s of int8, 3.9 of bf16).
+// but the chain from a place's scores to its weights and back, some 3400 cycles per 128 x 128 with two places under way.  (attn_prefill.cu is
+// twice as fast with the same two places: its softmax has a line per thread and 216 registers, where 24 warps here have 80 each and spill 44 - 100 bytes
+// a thread.)  8 trees of up to 61 tokens, 64 / 8 heads of 128, over up to 16384 tokens (120 GFLOP): 256 us in int8 (0.47 PFLOP/s), 237 in e4m3, 249
+// in bf16; of up to 5 tokens 83 us (2.0 TB/s of int8, 3.9 of bf16).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
