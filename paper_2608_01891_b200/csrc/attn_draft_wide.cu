@@ -767,17 +767,29 @@ attn_draft_wide_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_
             if (mine_steps > 0) ok = wait(&sh.pv_done[place], (done - 1) & 1);
             if (!ok) break;
             if (F == AFLEX_CACHE_E4M3 && mine_steps > 0 && sh.odd[pc % kPieceRing] == pc + 1) {
-                // some drafted token has a NaN in V: the lines that see it become NaN.  (A search that takes long, for something that seldom is)
+                // some drafted token has a NaN in V: the lines that see it become NaN.  (A search of all of the piece's, a token per lane, for
+                // something that seldom is; well inside a wait's limit for a million of them)
+                const int end = min(d.sees, t0 + units * kBN);
 #pragma unroll 1
-                for (int j = max(t0, d.ctx); j < min(d.sees, t0 + units * kBN); ++j) {
-                    const int id = fetch(p.page_table + (size_t)d.b * p.max_pages + j / kPageTokens);
-                    const bool there = id >= 0 && id < p.num_pages;
-                    const uint8_t* v = v_codes + (((size_t)(there ? id : 0) * p.Hkv + d.g) * kPageTokens + j % kPageTokens) * D;
-                    if (!__any_sync(0xffffffffu, lane * 4 < D && odd_e4m3(fetch(reinterpret_cast<const uint32_t*>(v) + lane)))) continue;
+                for (int j0 = max(t0, d.ctx); j0 < end; j0 += 32) {
+                    bool odd = false;
+                    if (j0 + lane < end) {
+                        const int j = j0 + lane, id = fetch(p.page_table + (size_t)d.b * p.max_pages + j / kPageTokens);
+                        const uint4* v = reinterpret_cast<const uint4*>(v_codes + (((size_t)(id >= 0 && id < p.num_pages ? id : 0) * p.Hkv + d.g) * kPageTokens + j % kPageTokens) * D);
+#pragma unroll 1
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint4 x = fetch(v + k);
+                            odd = odd || odd_e4m3(x.x) || odd_e4m3(x.y) || odd_e4m3(x.z) || odd_e4m3(x.w);
+                        }
+                    }
+#pragma unroll 1
+                    for (uint32_t left = __ballot_sync(0xffffffffu, odd); left != 0; left &= left - 1) {
+                        const int j = j0 + __ffs(left) - 1 - d.ctx;
 #pragma unroll
-                    for (int y = 0; y < 2; ++y) {
-                        const int line = line0 + hl + 8 * y, i = line >> p.g_shift;
-                        if (line < d.lines && sees_drafted(p, d.row0 + i, d.i0 + i, j - d.ctx, d.m)) l[y] = __uint_as_float(0x7fc00000u);
+                        for (int y = 0; y < 2; ++y) {
+                            const int line = line0 + hl + 8 * y, i = line >> p.g_shift;
+                            if (line < d.lines && l[y] == l[y] && sees_drafted(p, d.row0 + i, d.i0 + i, j, d.m)) l[y] = __uint_as_float(0x7fc00000u);
+                        }
                     }
                 }
             }

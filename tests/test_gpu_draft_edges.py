@@ -326,3 +326,30 @@ def test_a_chunk_among_single_tokens(ctx, fmt, others):  # noqa: F811
     q = torch.randn(T, Hq, D, generator=torch.Generator().manual_seed(76)).to(torch.bfloat16).to(DEV)
     out, lse = attend(ctx, c, q, AF.draft_rows(torch.from_numpy(offs).to(DEV)))
     check_attention(out, lse, q, c, offs, None, T, WEIGHT[fmt])
+
+
+@pytest.mark.parametrize("bad", [[1999], [0], [31, 32, 700, 1500], "all"])
+def test_codes_that_are_no_numbers_in_a_long_chunk(ctx, bad):  # noqa: F811
+    """A prompt chunk over an e4m3 cache: rows from a bad token on are NaN, rows before it are as they are without it."""
+    Hq, Hkv, D, m, before = 8, 1, 128, 2000, 100
+    pages = (m + before + 15) // 16
+    k, v, ks, vs = AF.empty_cache(pages, Hkv, D, torch.float8_e4m3fn, DEV)
+    g = torch.Generator(device=DEV).manual_seed(80)
+    for x in (k, v):
+        x.view(torch.uint8).copy_(torch.randint(0, 126, x.shape, generator=g, device=DEV, dtype=torch.uint8))
+    ks.fill_(1e-3)
+    vs.fill_(1e-2)
+    cache = AF.make_cache(k, v, torch.randperm(pages, generator=g, device=DEV).to(torch.int32).view(1, -1), torch.tensor([m + before], dtype=torch.int32, device=DEV), ks, vs)
+    table = cache._keep[2].cpu()
+    q = torch.randn(m, Hq, D, generator=g, device=DEV).to(torch.bfloat16)
+    draft = AF.draft_rows(torch.tensor([0, m], dtype=torch.int32, device=DEV))
+    outs = []
+    for dirty in (False, True):
+        for j in (range(m) if bad == "all" else bad) if dirty else ():
+            v.view(torch.uint8)[int(table[0, (before + j) // 16]), 0, (before + j) % 16, j % D] = 0xff
+        out = torch.zeros_like(q)
+        ctx.attn_draft(AF.attn_desc(Hq, Hkv, D), q, cache, out, draft=draft)
+        assert ctx.device_status() == AF.OK
+        outs.append(out)
+    first = 0 if bad == "all" else bad[0]
+    assert torch.isnan(outs[1][first:]).any(2).all() and torch.equal(outs[0][:first], outs[1][:first])
