@@ -353,3 +353,41 @@ def test_codes_that_are_no_numbers_in_a_long_chunk(ctx, bad):  # noqa: F811
         outs.append(out)
     first = 0 if bad == "all" else bad[0]
     assert torch.isnan(outs[1][first:]).any(2).all() and torch.equal(outs[0][:first], outs[1][:first])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("rows,batch", [(3, 2), (200, 2), (200, 1)])
+def test_a_call_of_padding_only(ctx, fmt, rows, batch):  # noqa: F811
+    """No sequence has a drafted token: nothing is read, written or reported, whatever the lengths are."""
+    Hq, Hkv, D = 8, 2, 64
+    c = Cache([40, 0][:batch], Hkv, D, fmt, seed=90)
+    before = [None if t is None else t.view(torch.uint8).clone() for t in c.dev]
+    q, qkv = torch.full((rows, Hq, D), float("nan"), dtype=torch.bfloat16, device=DEV), torch.full((rows, (Hq + 2 * Hkv) * D), float("nan"), dtype=torch.bfloat16, device=DEV)
+    out, lse, q_out = torch.full_like(q, 7.5), torch.full((rows, Hq), 7.5, device=DEV), torch.full_like(q, 7.5)
+    draft = AF.draft_rows(torch.zeros(batch + 1, dtype=torch.int32, device=DEV))
+    desc = AF.attn_desc(Hq, Hkv, D)
+    ctx.cache_append(desc, qkv, c.cache, q_out, None, None, 1e-6, 1e4, draft=draft)
+    ctx.attn_draft(desc, q, c.cache, out, lse, draft=draft)
+    assert ctx.device_status() == AF.OK
+    assert (out == 7.5).all() and (lse == 7.5).all() and (q_out == 7.5).all()
+    assert all(a is None or torch.equal(a, b.view(torch.uint8)) for a, b in zip(before, c.dev))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("most", [1, 3, 60])
+def test_thousands_of_sequences(ctx, fmt, most):  # noqa: F811
+    """More sequences than threads plan them, many of them without a row; up to 60 rows put them on the tensor cores."""
+    Hq, Hkv, D, batch = 2, 1, 64, 3000
+    rng = np.random.default_rng(91)
+    new = [1] * batch if most == 1 else (rng.integers(0, most + 1, batch) * (rng.random(batch) < 0.3)).tolist()
+    lens = [max(1, m) + int(x) for m, x in zip(new, rng.integers(0, 40, batch))]
+    if most == 60:                                                         # (few sequences with many rows: an average above the rule's border)
+        new, lens, batch = new[:200], lens[:200], 200
+        new = [60 if m else 25 for m in new]
+        lens = [max(n, m) for n, m in zip(lens, new)]
+    offs = offsets_of(new)
+    T = int(offs[-1])
+    c = Cache(lens, Hkv, D, fmt, seed=92)
+    q = torch.randn(T, Hq, D, generator=torch.Generator().manual_seed(93)).to(torch.bfloat16).to(DEV)
+    out, lse = attend(ctx, c, q, None if most == 1 else AF.draft_rows(torch.from_numpy(offs).to(DEV)))
+    check_attention(out, lse, q, c, None if most == 1 else offs, None, T, WEIGHT[fmt])
